@@ -202,6 +202,7 @@ def _inputs(case, seed, dev):
             s["dlogits"] = _rows(T, V, dt, case["pad"], dev)
         for name in ("logp", "lse", "entropy"):
             s[name] = torch.empty((T,), device=dev)
+        s["stats"] = torch.empty((T, 2), device=dev)
         if case["top"]:
             s["top_idx"] = torch.empty((T, case["top"]), dtype=torch.int32, device=dev)
             s["top_logp"] = torch.empty((T, case["top"]), device=dev)
@@ -476,11 +477,12 @@ def _run_own(s):
             ops.token_logprobs_workspace(c["T"], c["V"], c["top"])))
         ops.detonation_token_logprobs(s["logits"], s["targets"], s["logp"], lse=s["lse"],
                                       entropy=s["entropy"], top_idx=s.get("top_idx"),
-                                      top_logp=s.get("top_logp"), workspace=ws)
+                                      top_logp=s.get("top_logp"),
+                                      stats=s["stats"] if c["train"] else None, workspace=ws)
         names = ["logp", "lse", "entropy"] + (["top_idx", "top_logp"] if c["top"] else [])
         if c["train"]:
             ops.detonation_token_logprobs_backward(
-                s["logits"], s["targets"], s["lse"], s["dlogits"], g_logp=s["g_logp"],
+                s["logits"], s["targets"], s["stats"], s["dlogits"], g_logp=s["g_logp"],
                 entropy=s["entropy"], g_entropy=s["g_entropy"])
             names.append("dlogits")
     elif op == "norm_fwd":
