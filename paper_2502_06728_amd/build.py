@@ -52,6 +52,9 @@ UNITS = [
     "tiled_scheme_narrow_s32.hip", "tiled_scheme_narrow_s64.hip",
     "tiled_topk_s64.hip", "tiled_topk_s32.hip", "tiled_topk_s16.hip",
     "raw_compress.hip",
+    # operators around the library products of a training step (detonation_model.h)
+    "model_norm_backward.hip", "model_norm.hip", "model_act8.hip", "model_weight_grad.hip",
+    "model_logprobs.hip",
     # validation, dispatch, general kernels
     "detonation.hip",
 ]
