@@ -10,6 +10,7 @@ from concurrent.futures import ThreadPoolExecutor
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(_HERE, "csrc")
+CSRC_MODEL = os.path.join(_HERE, "csrc_model")
 OBJ = os.path.join(_HERE, "_build")
 LIB = os.path.join(_HERE, "libdetonation.so")
 # (the interpreter's own suffix: binding.MARSHAL_PATH)
@@ -52,12 +53,12 @@ UNITS = [
     "tiled_scheme_narrow_s32.hip", "tiled_scheme_narrow_s64.hip",
     "tiled_topk_s64.hip", "tiled_topk_s32.hip", "tiled_topk_s16.hip",
     "raw_compress.hip",
-    # operators around the library products of a training step (detonation_model.h)
-    "model_norm_backward.hip", "model_norm.hip", "model_act8.hip", "model_weight_grad.hip",
-    "model_logprobs.hip",
     # validation, dispatch, general kernels
     "detonation.hip",
 ]
+
+# the operators around the library products of a training step (include/detonation_model.h)
+MODEL_UNITS = ["norm_backward.hip", "norm.hip", "act8.hip", "weight_grad.hip", "logprobs.hip"]
 
 
 def _build_marshal(verbose: bool) -> None:
@@ -111,12 +112,14 @@ def build(verbose: bool = False) -> str:
     lib = os.environ.get("DETO_BUILD_OUT", LIB)
     obj_dir = OBJ + ("_" + os.path.basename(lib) if lib != LIB else "")
     os.makedirs(obj_dir, exist_ok=True)
-    objs = [os.path.join(obj_dir, u.replace(".hip", ".o")) for u in UNITS]
-    jobs = [[hipcc, *HIPCC_FLAGS, *extra, "-c", "-o", o, os.path.join(CSRC, u)]
-            for u, o in zip(UNITS, objs)]
+    units = ([os.path.join(CSRC, u) for u in UNITS] + [os.path.join(CSRC_MODEL, u) for u in MODEL_UNITS])
+    # (two folders: a unit of the second is named after both)
+    objs = [os.path.join(obj_dir, ("model_" if os.path.dirname(u) == CSRC_MODEL else "") +
+                         os.path.basename(u).replace(".hip", ".o")) for u in units]
+    jobs = [[hipcc, *HIPCC_FLAGS, *extra, "-c", "-o", o, u] for u, o in zip(units, objs)]
     if os.environ.get("DETO_INCREMENTAL"):
         # developer convenience: keep an object that is newer than everything its unit includes
-        jobs = [j for j, u, o in zip(jobs, UNITS, objs) if _stale(os.path.join(CSRC, u), o)]
+        jobs = [j for j, u, o in zip(jobs, units, objs) if _stale(u, o)]
     with ThreadPoolExecutor(max_workers=max(1, min(len(jobs), 8))) as pool:
         list(pool.map(lambda c: _run(c, verbose), jobs))
     _run([hipcc, "--offload-arch=gfx950", "-shared", "-fPIC", "-o", lib, *objs], verbose)

@@ -4,7 +4,7 @@
 // lanes in a row are a group of 32, so a group's largest magnitude is two moves between neighbouring lanes
 // and no element is read twice.  Items (a lane's eight features) are numbered through the matrix, each row
 // padded to whole groups: one launch whatever the shape, no wavefront half empty because a row is short.
-#include "model_device.hip.h"
+#include "device.hip.h"
 
 namespace deto {
 namespace model {

@@ -11,7 +11,7 @@
 // the list does not hold them (many equal values) is searched K times instead.
 //
 // Backward.  A stream: p = exp(z - m - log s) from the row's saved m and log s.
-#include "model_device.hip.h"
+#include "device.hip.h"
 
 namespace deto {
 namespace model {

@@ -4,7 +4,7 @@
 // Bound by memory: x and f are read once, x_out, y and the codes written once; a row stays in registers
 // between its two norms.  LAYER takes its variance around the row's mean (two sums one after the other), so
 // that a large mean costs no digits.
-#include "model_norm_device.hip.h"
+#include "norm_device.hip.h"
 
 namespace deto {
 namespace model {

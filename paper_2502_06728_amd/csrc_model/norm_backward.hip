@@ -8,7 +8,7 @@
 // team then writes itself).
 //
 // Bound by memory: x_out, f, dy, dx_out are read once, dx and df written once.
-#include "model_norm_device.hip.h"
+#include "norm_device.hip.h"
 
 namespace deto {
 namespace model {

@@ -5,7 +5,7 @@
 // one wavefront, which needs no barrier (four teams a workgroup); wider rows take a workgroup.
 #pragma once
 
-#include "model_device.hip.h"
+#include "device.hip.h"
 
 namespace deto {
 namespace model {

@@ -13,7 +13,7 @@
 //
 // Bound by the matrix cores for large products; few tiles are cut along t and joined by a second launch, always
 // in the same order.
-#include "model_device.hip.h"
+#include "device.hip.h"
 
 namespace deto {
 namespace model {
