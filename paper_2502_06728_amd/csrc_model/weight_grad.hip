@@ -70,25 +70,90 @@ __device__ __forceinline__ float rest(float v) {
 template <int DT> struct UnitA { Raw8<DT> row[4]; };
 struct UnitB { u32x2 codes[4]; uint32_t exps[4]; };
 
-template <int DT>
-__device__ __forceinline__ void load_a(UnitA<DT>& u, const Args& a, int64_t t, int64_t end, int64_t n) {
-    const int64_t left = a.N - n;
-    const int count = left >= 8 ? 8 : left > 0 ? static_cast<int>(left) : 0;
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-        u.row[i] = load8<DT>(a.dy.data, (t + i) * a.dy.ld + n, t + i < end ? count : 0);
+// ---- Loads of a step.  NEAR: through buffer resources that end where the matrix does: rows past its end read as
+// zeros without a comparison, a lane needs one 32-bit offset, and columns past a row's end read whatever comes
+// next (they add to columns of dw that are not written).  Otherwise (rows far apart, or not at multiples of four
+// bytes) element by element where a row ends.
+typedef __amdgpu_buffer_rsrc_t Rsrc;
+
+// (The words that hold the last bytes count whole: a buffer gives no part of a word.  They are aligned.)
+__device__ __forceinline__ Rsrc resource(const void* base, int64_t bytes) {
+    const int n = bytes > 0x7FFFFFF0 ? 0x7FFFFFF0 : bytes > 0 ? (static_cast<int>(bytes) + 3) & ~3 : 0;
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(base), 0, n, 0x00020000);
 }
 
-__device__ __forceinline__ void load_b(UnitB& u, const Args& a, int64_t t, int64_t end, int64_t k) {
-    const int64_t left = a.K - k;
-    const int count = left >= 8 ? 8 : left > 0 ? static_cast<int>(left) : 0;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const bool on = t + i < end && count > 0;
-        u.codes[i] = load_codes(a.x.codes + (t + i) * a.x.ld_codes + k, on ? count : 0);
-        u.exps[i] = on ? a.x.exps[(t + i) * a.x.ld_exps + k / DETO_ACT8_GROUP] : 0u;
-    }
+__device__ __forceinline__ int exps_left(int64_t bytes) {      // bytes, read one by one
+    return bytes > 0x7FFFFFF0 ? 0x7FFFFFF0 : bytes > 0 ? static_cast<int>(bytes) : 0;
 }
+
+template <int DT, class TL, bool NEAR>
+struct Loader {
+    const Args& a;
+    int64_t n0, k0, end;
+    __device__ __forceinline__ Loader(const Args& args, int64_t n, int64_t k, int64_t e)
+        : a(args), n0(n), k0(k), end(e) {}
+
+    __device__ __forceinline__ void load(int64_t t, UnitA<DT> (&ua)[TL::kUnitsA],
+                                         UnitB (&ub)[TL::kUnitsB]) const {
+        if constexpr (NEAR) {
+            constexpr int kElem = kSize<DT>;
+            const int ld = static_cast<int>(a.dy.ld) * kElem, ldc = static_cast<int>(a.x.ld_codes),
+                      lde = static_cast<int>(a.x.ld_exps);
+            const int64_t at_a = (t * a.dy.ld + n0) * kElem, at_c = t * a.x.ld_codes + k0,
+                          at_e = t * a.x.ld_exps + k0 / DETO_ACT8_GROUP;
+            const Rsrc ra = resource(static_cast<const char*>(a.dy.data) + at_a,
+                                     ((end - 1) * a.dy.ld + a.N) * kElem - at_a);
+            const Rsrc rc = resource(a.x.codes + at_c, (end - 1) * a.x.ld_codes + a.K - at_c);
+            const Rsrc re = __builtin_amdgcn_make_buffer_rsrc(
+                a.x.exps + at_e, 0, exps_left((end - 1) * a.x.ld_exps +
+                                              (a.K + DETO_ACT8_GROUP - 1) / DETO_ACT8_GROUP - at_e),
+                0x00020000);
+#pragma unroll
+            for (int i = 0; i < TL::kUnitsA; ++i) {
+                const int u = threadIdx.x + i * TL::kThreads;
+                const int off = u / (TL::BM / 8) * 4 * ld + u % (TL::BM / 8) * 8 * kElem;
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    ua[i].row[r].a = __builtin_amdgcn_raw_buffer_load_b128(ra, off, r * ld, 0);
+                    if constexpr (DT == DETO_F32)
+                        ua[i].row[r].b = __builtin_amdgcn_raw_buffer_load_b128(ra, off + 16, r * ld, 0);
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < TL::kUnitsB; ++i) {
+                const int u = threadIdx.x + i * TL::kThreads;
+                const int t4 = u / (TL::BN / 8) * 4, c8 = u % (TL::BN / 8);
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    ub[i].codes[r] = __builtin_amdgcn_raw_buffer_load_b64(rc, t4 * ldc + c8 * 8, r * ldc, 0);
+                    ub[i].exps[r] = __builtin_amdgcn_raw_buffer_load_b8(re, t4 * lde + c8 / 4, r * lde, 0);
+                }
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < TL::kUnitsA; ++i) {
+                const int u = threadIdx.x + i * TL::kThreads;
+                const int64_t n = n0 + u % (TL::BM / 8) * 8, left = a.N - n, row = t + u / (TL::BM / 8) * 4;
+                const int count = left >= 8 ? 8 : left > 0 ? static_cast<int>(left) : 0;
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+                    ua[i].row[r] = load8<DT>(a.dy.data, (row + r) * a.dy.ld + n, row + r < end ? count : 0);
+            }
+#pragma unroll
+            for (int i = 0; i < TL::kUnitsB; ++i) {
+                const int u = threadIdx.x + i * TL::kThreads;
+                const int64_t k = k0 + u % (TL::BN / 8) * 8, left = a.K - k, row = t + u / (TL::BN / 8) * 4;
+                const int count = left >= 8 ? 8 : left > 0 ? static_cast<int>(left) : 0;
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const bool on = row + r < end && count > 0;
+                    ub[i].codes[r] = load_codes(a.x.codes + (row + r) * a.x.ld_codes + k, on ? count : 0);
+                    ub[i].exps[r] = on ? a.x.exps[(row + r) * a.x.ld_exps + k / DETO_ACT8_GROUP] : 0u;
+                }
+            }
+        }
+    }
+};
 
 // four rows (quarter tq of the step) of column `column`: 8 bytes
 __device__ __forceinline__ void put4(char* lds, int column, int tq, uint32_t first, uint32_t second) {
@@ -146,7 +211,7 @@ __device__ __forceinline__ void write_any(const deto_rows& dw, int64_t n, int64_
     else write_dw<DETO_F16>(dw, n, k, v, accumulate);
 }
 
-template <int DT, class TL>
+template <int DT, class TL, bool NEAR>
 __global__ __launch_bounds__(TL::kThreads) void weight_grad_kernel(Args a) {
     extern __shared__ __align__(16) char lds[];
     constexpr int kTermsA = kTerms<DT>;
@@ -169,18 +234,7 @@ __global__ __launch_bounds__(TL::kThreads) void weight_grad_kernel(Args a) {
 
     UnitA<DT> ua[TL::kUnitsA];
     UnitB ub[TL::kUnitsB];
-    auto load = [&](int64_t t) {
-#pragma unroll
-        for (int i = 0; i < TL::kUnitsA; ++i) {
-            const int u = threadIdx.x + i * TL::kThreads;
-            load_a<DT>(ua[i], a, t + u / (TL::BM / 8) * 4, end, n0 + u % (TL::BM / 8) * 8);
-        }
-#pragma unroll
-        for (int i = 0; i < TL::kUnitsB; ++i) {
-            const int u = threadIdx.x + i * TL::kThreads;
-            load_b(ub[i], a, t + u / (TL::BN / 8) * 4, end, k0 + u % (TL::BN / 8) * 8);
-        }
-    };
+    const Loader<DT, TL, NEAR> loader(a, n0, k0, end);
     auto store = [&](char* at) {
 #pragma unroll
         for (int i = 0; i < TL::kUnitsA; ++i) {
@@ -193,31 +247,38 @@ __global__ __launch_bounds__(TL::kThreads) void weight_grad_kernel(Args a) {
             store_b(ub[i], at + kTermsA * kBytesA, u % (TL::BN / 8) * 8, u / (TL::BN / 8));
         }
     };
+    // Where a lane's operands of 16 rows t are, from the first of a wavefront's 32-column blocks.  (A block further
+    // flips the third bit of column / 8, which is that of rows 32 further.)
+    uint32_t at_a[kDepth / 16], at_b[kDepth / 16];
+#pragma unroll
+    for (int s = 0; s < kDepth / 16; ++s) {
+        at_a[s] = lds_at(wm + lane % 32, 2 * s + lane / 32);
+        at_b[s] = lds_at(wn + lane % 32, 2 * s + lane / 32);
+    }
     int buffer = 0;
     if (t0 < end) {
-        load(t0);
+        loader.load(t0, ua, ub);
         store(lds);
     }
     __syncthreads();
     for (int64_t t = t0; t < end; t += kDepth) {
         const bool more = t + kDepth < end;
-        if (more) load(t + kDepth);
+        if (more) loader.load(t + kDepth, ua, ub);
         const char* la = lds + buffer * kBuffer;
         const char* lb = la + kTermsA * kBytesA;
 #pragma unroll
         for (int s = 0; s < kDepth / 16; ++s) {
-            const int t8 = 2 * s + lane / 32;
             bf16x8 fb[TL::WN / 32];
 #pragma unroll
             for (int j = 0; j < TL::WN / 32; ++j)
-                fb[j] = *reinterpret_cast<const bf16x8*>(lb + lds_at(wn + j * 32 + lane % 32, t8));
+                fb[j] = *reinterpret_cast<const bf16x8*>(lb + at_b[s ^ 2 * (j % 2)] + j * 32 * kRowBytes);
 #pragma unroll
             for (int term = 0; term < kTermsA; ++term) {
                 bf16x8 fa[TL::WM / 32];
 #pragma unroll
                 for (int i = 0; i < TL::WM / 32; ++i)
-                    fa[i] = *reinterpret_cast<const bf16x8*>(la + term * kBytesA +
-                                                             lds_at(wm + i * 32 + lane % 32, t8));
+                    fa[i] = *reinterpret_cast<const bf16x8*>(la + term * kBytesA + at_a[s ^ 2 * (i % 2)] +
+                                                             i * 32 * kRowBytes);
 #pragma unroll
                 for (int i = 0; i < TL::WM / 32; ++i)
 #pragma unroll
@@ -281,10 +342,17 @@ Plan plan_with(int64_t T, int64_t N, int64_t K, bool large) {
     return p;
 }
 
+// Whether a step's rows lie within 2^31 bytes and at multiples of four: the loader's buffers.
+bool reaches(const Args& a) {
+    const int64_t e = type_size(a.dy.dtype), most = (int64_t{1} << 31) / (2 * kDepth);
+    return a.dy.ld * e < most && a.x.ld_codes < most && a.x.ld_exps < most && a.dy.ld * e % 4 == 0 &&
+           a.x.ld_codes % 4 == 0 && is_aligned(a.dy.data, 4) && is_aligned(a.x.codes, 4);
+}
+
 // Large tiles where they fill the chip by themselves, and dy is one term.
-Plan plan_of(int64_t T, int64_t N, int64_t K, int dtype) {
+Plan plan_of(int64_t T, int64_t N, int64_t K, bool may_be_large) {
     const Plan p = plan_with(T, N, K, true);
-    return dtype == DETO_BF16 && p.tiles >= 192 ? p : plan_with(T, N, K, false);
+    return may_be_large && p.tiles >= 192 ? p : plan_with(T, N, K, false);
 }
 
 }  // namespace
@@ -298,8 +366,8 @@ extern "C" {
 int64_t detonation_act8_weight_grad_workspace(int64_t T, int64_t N, int64_t K) {
     if (bad_shape(T, N, K)) return -1;
     int64_t most = 0;
-    for (int dtype : {DETO_BF16, DETO_F32}) {
-        const Plan p = plan_of(T, N, K, dtype);
+    for (bool large : {true, false}) {
+        const Plan p = plan_of(T, N, K, large);
         if (p.splits > 1 && p.splits > most) most = p.splits;
     }
     return most * N * K * static_cast<int64_t>(sizeof(float));
@@ -314,26 +382,35 @@ int detonation_act8_weight_grad(int64_t T, int64_t N, int64_t K, const deto_rows
                                T ? check_act8(x8, T, K) : 0);
     if (rc) return rc;
     const int dtype = T ? dy->dtype : static_cast<int>(DETO_BF16);
-    const Plan p = plan_of(T, N, K, dtype);
+    const deto_rows none = {};
+    const deto_act8 none8 = {};
+    Args a = {T, N, K, T ? *dy : none, *dw, T ? *x8 : none8, accumulate != 0, 0, 0, 0,
+              static_cast<float*>(workspace)};
+    if (T <= 1) {           // (a single row's distance to the next one says nothing)
+        a.dy.ld = (N + 1) / 2 * 2;
+        a.x.ld_codes = (K + 3) / 4 * 4;
+        a.x.ld_exps = (K + DETO_ACT8_GROUP - 1) / DETO_ACT8_GROUP;
+    }
+    const bool near = T > 0 && reaches(a);
+    const Plan p = plan_of(T, N, K, near && dtype == DETO_BF16);
     if (p.splits > 1 && !workspace) return DETO_ERR_NULL;
     if (p.splits > 1 && !is_aligned(workspace, 16)) return DETO_ERR_ALIGN;
     const int64_t blocks = (N * K + 255) / 256;
     if (p.tiles * p.splits > 0x7FFFFFFF || (p.splits > 1 && blocks > 0x7FFFFFFF))
         return DETO_ERR_UNSUPPORTED;
-    const deto_rows none = {};
-    const deto_act8 none8 = {};
-    const Args a = {T, N, K, T ? *dy : none, *dw, T ? *x8 : none8, accumulate != 0,
-                    static_cast<int>(p.tiles_k), static_cast<int>(p.splits), p.span,
-                    static_cast<float*>(workspace)};
+    a.tiles_k = static_cast<int>(p.tiles_k);
+    a.splits = static_cast<int>(p.splits);
+    a.span = p.span;
     const hipStream_t st = static_cast<hipStream_t>(stream);
     const unsigned grid = static_cast<unsigned>(p.tiles * p.splits);
     fresh();
     if (p.large)
-        weight_grad_kernel<DETO_BF16, Large><<<grid, Large::kThreads, Large::lds(1), st>>>(a);
+        weight_grad_kernel<DETO_BF16, Large, true><<<grid, Large::kThreads, Large::lds(1), st>>>(a);
     else
         by_type(dtype, [&](auto dt) {
-            weight_grad_kernel<dt.value, Small>
-                <<<grid, Small::kThreads, Small::lds(kTerms<dt.value>), st>>>(a);
+            constexpr int kLds = Small::lds(kTerms<dt.value>);
+            if (near) weight_grad_kernel<dt.value, Small, true><<<grid, Small::kThreads, kLds, st>>>(a);
+            else weight_grad_kernel<dt.value, Small, false><<<grid, Small::kThreads, kLds, st>>>(a);
             return 0;
         });
     if (p.splits > 1)

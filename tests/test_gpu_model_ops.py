@@ -566,8 +566,41 @@ def test_weight_grad(gpu, dtype, out, T, N, K):
     assert_near(dw, want + start, mag + start.abs(), 3 * T + 41, "dw accumulated")
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("N,K,pad_y,pad_x", [(129, 130, 3, 2), (131, 127, 1, 1), (64, 33, 0, 3), (7, 5, 1, 0)])
+def test_weight_grad_of_rows_apart(gpu, dtype, N, K, pad_y, pad_x):
+    """Widths that are not whole words, at strides that are, and the other way round; what lies between the
+    rows is NaN (and codes under exponents of 255)."""
+    T = 130
+    dy = rows(normal(1, T, N), dtype, pad_y)
+    codes, exps, x = ref.act8(normal(2, T, K))
+    x8 = empty_act8(T, K, pad_x)
+    torch.as_strided(x8.exps, (T, x8.exps.stride(0)), (x8.exps.stride(0), 1)).fill_(255)
+    x8.codes.copy_(codes)
+    x8.exps.copy_(exps)
+    dw = like(N, K, F32, 1)
+    ops.detonation_act8_weight_grad(dy, x8, dw,
+                                    workspace=scratch(ops.act8_weight_grad_workspace(T, N, K)))
+    d = ref.double(dy)
+    assert_near(dw, d.t() @ x, d.abs().t() @ x.abs(), 3 * T + 40, "dw")
+    untouched(dw)
+
+
+def test_weight_grad_of_distant_rows(gpu):
+    """Rows of one matrix 2^25 bytes apart: a step of them passes 2^31 bytes."""
+    T, N, K = 70, 20, 40
+    far = torch.zeros((T, 1 << 24), dtype=BF16, device=DEV)
+    dy = far[:, 100:100 + N]
+    dy.copy_(normal(1, T, N))
+    x8, x = act8_of(normal(2, T, K))
+    dw = like(N, K, F32)
+    ops.detonation_act8_weight_grad(dy, x8, dw, workspace=scratch(ops.act8_weight_grad_workspace(T, N, K)))
+    d = ref.double(dy)
+    assert_near(dw, d.t() @ x, d.abs().t() @ x.abs(), 3 * T + 40, "dw")
+
+
 def test_weight_grad_large_tiles(gpu):
-    T, N, K = 136, 2049, 6100
+    T, N, K = 136, 2050, 6100
     say(T, N, K)
     dy = rows(normal(1, T, N), BF16)
     x8 = empty_act8(T, K)
