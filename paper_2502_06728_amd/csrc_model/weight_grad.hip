@@ -19,6 +19,7 @@ namespace deto {
 namespace model {
 namespace {
 
+constexpr int kBand = 4;                // tiles along n that share their part of x
 constexpr int kDepth = 64;              // rows t of a step
 constexpr int kRowBytes = kDepth * 2;   // of an LDS column
 
@@ -61,6 +62,16 @@ __device__ __forceinline__ uint32_t high_halves(uint32_t first, uint32_t second)
 
 template <int DT> constexpr int kTerms = DT == DETO_BF16 ? 1 : DT == DETO_F16 ? 2 : 3;
 
+template <int DT>
+__device__ __forceinline__ float element(const Raw8<DT>& r, int j) {
+    if constexpr (DT == DETO_F32) return bits_f32(j < 4 ? r.a[j & 3] : r.b[j & 3]);
+    else {
+        const uint32_t word = r.a[j / 2];
+        const f16x2 h = __builtin_bit_cast(f16x2, word);
+        return static_cast<float>(j % 2 ? h.y : h.x);
+    }
+}
+
 // What is left of v above its leading 8 bits.  (An infinity is one term, a NaN stays one.)
 __device__ __forceinline__ float rest(float v) {
     const float r = v - bits_f32(f32_bits(v) & 0xFFFF0000u);
@@ -93,21 +104,13 @@ struct Loader {
     __device__ __forceinline__ Loader(const Args& args, int64_t n, int64_t k, int64_t e)
         : a(args), n0(n), k0(k), end(e) {}
 
-    __device__ __forceinline__ void load(int64_t t, UnitA<DT> (&ua)[TL::kUnitsA],
-                                         UnitB (&ub)[TL::kUnitsB]) const {
+    __device__ __forceinline__ void load_a(int64_t t, UnitA<DT> (&ua)[TL::kUnitsA]) const {
         if constexpr (NEAR) {
             constexpr int kElem = kSize<DT>;
-            const int ld = static_cast<int>(a.dy.ld) * kElem, ldc = static_cast<int>(a.x.ld_codes),
-                      lde = static_cast<int>(a.x.ld_exps);
-            const int64_t at_a = (t * a.dy.ld + n0) * kElem, at_c = t * a.x.ld_codes + k0,
-                          at_e = t * a.x.ld_exps + k0 / DETO_ACT8_GROUP;
+            const int ld = static_cast<int>(a.dy.ld) * kElem;
+            const int64_t at_a = (t * a.dy.ld + n0) * kElem;
             const Rsrc ra = resource(static_cast<const char*>(a.dy.data) + at_a,
                                      ((end - 1) * a.dy.ld + a.N) * kElem - at_a);
-            const Rsrc rc = resource(a.x.codes + at_c, (end - 1) * a.x.ld_codes + a.K - at_c);
-            const Rsrc re = __builtin_amdgcn_make_buffer_rsrc(
-                a.x.exps + at_e, 0, exps_left((end - 1) * a.x.ld_exps +
-                                              (a.K + DETO_ACT8_GROUP - 1) / DETO_ACT8_GROUP - at_e),
-                0x00020000);
 #pragma unroll
             for (int i = 0; i < TL::kUnitsA; ++i) {
                 const int u = threadIdx.x + i * TL::kThreads;
@@ -117,16 +120,6 @@ struct Loader {
                     ua[i].row[r].a = __builtin_amdgcn_raw_buffer_load_b128(ra, off, r * ld, 0);
                     if constexpr (DT == DETO_F32)
                         ua[i].row[r].b = __builtin_amdgcn_raw_buffer_load_b128(ra, off + 16, r * ld, 0);
-                }
-            }
-#pragma unroll
-            for (int i = 0; i < TL::kUnitsB; ++i) {
-                const int u = threadIdx.x + i * TL::kThreads;
-                const int t4 = u / (TL::BN / 8) * 4, c8 = u % (TL::BN / 8);
-#pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    ub[i].codes[r] = __builtin_amdgcn_raw_buffer_load_b64(rc, t4 * ldc + c8 * 8, r * ldc, 0);
-                    ub[i].exps[r] = __builtin_amdgcn_raw_buffer_load_b8(re, t4 * lde + c8 / 4, r * lde, 0);
                 }
             }
         } else {
@@ -139,6 +132,29 @@ struct Loader {
                 for (int r = 0; r < 4; ++r)
                     ua[i].row[r] = load8<DT>(a.dy.data, (row + r) * a.dy.ld + n, row + r < end ? count : 0);
             }
+        }
+    }
+
+    __device__ __forceinline__ void load_b(int64_t t, UnitB (&ub)[TL::kUnitsB]) const {
+        if constexpr (NEAR) {
+            const int ldc = static_cast<int>(a.x.ld_codes), lde = static_cast<int>(a.x.ld_exps);
+            const int64_t at_c = t * a.x.ld_codes + k0, at_e = t * a.x.ld_exps + k0 / DETO_ACT8_GROUP;
+            const Rsrc rc = resource(a.x.codes + at_c, (end - 1) * a.x.ld_codes + a.K - at_c);
+            const Rsrc re = __builtin_amdgcn_make_buffer_rsrc(
+                a.x.exps + at_e, 0, exps_left((end - 1) * a.x.ld_exps +
+                                              (a.K + DETO_ACT8_GROUP - 1) / DETO_ACT8_GROUP - at_e),
+                0x00020000);
+#pragma unroll
+            for (int i = 0; i < TL::kUnitsB; ++i) {
+                const int u = threadIdx.x + i * TL::kThreads;
+                const int t4 = u / (TL::BN / 8) * 4, c8 = u % (TL::BN / 8);
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    ub[i].codes[r] = __builtin_amdgcn_raw_buffer_load_b64(rc, t4 * ldc + c8 * 8, r * ldc, 0);
+                    ub[i].exps[r] = __builtin_amdgcn_raw_buffer_load_b8(re, t4 * lde + c8 / 4, r * lde, 0);
+                }
+            }
+        } else {
 #pragma unroll
             for (int i = 0; i < TL::kUnitsB; ++i) {
                 const int u = threadIdx.x + i * TL::kThreads;
@@ -161,42 +177,57 @@ __device__ __forceinline__ void put4(char* lds, int column, int tq, uint32_t fir
     *reinterpret_cast<u32x2*>(lds + lds_at(column, tq >> 1) + (tq & 1) * 8) = v;
 }
 
-template <int DT, class TL>
+// Quarter Q (two columns) of a unit of dy, in all its terms.
+template <int DT, class TL, int Q>
 __device__ __forceinline__ void store_a(const UnitA<DT>& u, char* lds, int column, int tq) {
     if constexpr (DT == DETO_BF16) {
-#pragma unroll
-        for (int p = 0; p < 4; ++p) {
-            put4(lds, column + 2 * p, tq, low_halves(u.row[0].a[p], u.row[1].a[p]),
-                 low_halves(u.row[2].a[p], u.row[3].a[p]));
-            put4(lds, column + 2 * p + 1, tq, high_halves(u.row[0].a[p], u.row[1].a[p]),
-                 high_halves(u.row[2].a[p], u.row[3].a[p]));
-        }
+        put4(lds, column + 2 * Q, tq, low_halves(u.row[0].a[Q], u.row[1].a[Q]),
+             low_halves(u.row[2].a[Q], u.row[3].a[Q]));
+        put4(lds, column + 2 * Q + 1, tq, high_halves(u.row[0].a[Q], u.row[1].a[Q]),
+             high_halves(u.row[2].a[Q], u.row[3].a[Q]));
     } else {
-        float v[4][8];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) unpack8<DT>(u.row[i], v[i]);
+        for (int j = 2 * Q; j < 2 * Q + 2; ++j) {
+            float v[4];
 #pragma unroll
-        for (int term = 0; term < kTerms<DT>; ++term) {
+            for (int i = 0; i < 4; ++i) v[i] = element<DT>(u.row[i], j);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
+            for (int term = 0; term < kTerms<DT>; ++term) {
                 put4(lds + term * TL::BM * kRowBytes, column + j, tq,
-                     high_halves(f32_bits(v[0][j]), f32_bits(v[1][j])),
-                     high_halves(f32_bits(v[2][j]), f32_bits(v[3][j])));
+                     high_halves(f32_bits(v[0]), f32_bits(v[1])), high_halves(f32_bits(v[2]), f32_bits(v[3])));
 #pragma unroll
-                for (int i = 0; i < 4; ++i) v[i][j] = rest(v[i][j]);
+                for (int i = 0; i < 4; ++i) v[i] = rest(v[i]);
             }
         }
     }
 }
 
-__device__ __forceinline__ void store_b(const UnitB& u, char* lds, int column, int tq) {
-    float v[4][8];
+// Byte J of a word of codes as fp32.
+template <int J>
+__device__ __forceinline__ float code_value(uint32_t word) {
+    float f;
+    if constexpr (J == 0)
+        asm("v_cvt_f32_i32_sdwa %0, sext(%1) dst_sel:DWORD dst_unused:UNUSED_PAD src0_sel:BYTE_0" : "=v"(f) : "v"(word));
+    else if constexpr (J == 1)
+        asm("v_cvt_f32_i32_sdwa %0, sext(%1) dst_sel:DWORD dst_unused:UNUSED_PAD src0_sel:BYTE_1" : "=v"(f) : "v"(word));
+    else if constexpr (J == 2)
+        asm("v_cvt_f32_i32_sdwa %0, sext(%1) dst_sel:DWORD dst_unused:UNUSED_PAD src0_sel:BYTE_2" : "=v"(f) : "v"(word));
+    else
+        asm("v_cvt_f32_i32_sdwa %0, sext(%1) dst_sel:DWORD dst_unused:UNUSED_PAD src0_sel:BYTE_3" : "=v"(f) : "v"(word));
+    return f;
+}
+
+// Column J of a unit of x.  (The lower halves of the values are zeros: bf16 holds them.)
+template <int J>
+__device__ __forceinline__ void store_b(const UnitB& u, const float (&scale)[4], char* lds, int column, int tq) {
+    float v[4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) act8_decode8(u.codes[i], u.exps[i], v[i]);
-#pragma unroll
-    for (int j = 0; j < 8; ++j)         // (the lower halves are zeros: bf16 holds the value)
-        put4(lds, column + j, tq, high_halves(f32_bits(v[0][j]), f32_bits(v[1][j])),
-             high_halves(f32_bits(v[2][j]), f32_bits(v[3][j])));
+    for (int i = 0; i < 4; ++i) {
+        const uint32_t word = u.codes[i][J / 4];
+        v[i] = code_value<J % 4>(word) * scale[i];
+    }
+    put4(lds, column + J, tq, high_halves(f32_bits(v[0]), f32_bits(v[1])),
+         high_halves(f32_bits(v[2]), f32_bits(v[3])));
 }
 
 template <int DT>
@@ -211,14 +242,30 @@ __device__ __forceinline__ void write_any(const deto_rows& dw, int64_t n, int64_
     else write_dw<DETO_F16>(dw, n, k, v, accumulate);
 }
 
+// f(Type<0>) ... f(Type<N - 1>)
+template <int N, class F>
+__device__ __forceinline__ void each_of(F f) {
+    if constexpr (N > 0) {
+        each_of<N - 1>(f);
+        f(Type<N - 1>{});
+    }
+}
+
 template <int DT, class TL, bool NEAR>
 __global__ __launch_bounds__(TL::kThreads) void weight_grad_kernel(Args a) {
     extern __shared__ __align__(16) char lds[];
     constexpr int kTermsA = kTerms<DT>;
     constexpr int kBytesA = TL::BM * kRowBytes, kBuffer = (TL::BM * kTermsA + TL::BN) * kRowBytes;
-    const int tile = blockIdx.x / a.splits, split = blockIdx.x % a.splits;
-    const int64_t n0 = static_cast<int64_t>(tile / a.tiles_k) * TL::BM;
-    const int64_t k0 = static_cast<int64_t>(tile % a.tiles_k) * TL::BN;
+    // Workgroups go to the chip's eight parts in turn: a part takes a run of tiles, four high, whose operands
+    // its own cache then holds for all of them.
+    const unsigned all = gridDim.x, part = blockIdx.x % 8, each = all / 8, more_parts = all % 8;
+    const unsigned id = part * each + (part < more_parts ? part : more_parts) + blockIdx.x / 8;
+    const int tiles = all / a.splits, split = id / tiles;
+    const int tile = id % tiles, tiles_n = tiles / a.tiles_k;
+    const int band = tile / (kBand * a.tiles_k), within = tile % (kBand * a.tiles_k);
+    const int high = tiles_n - band * kBand < kBand ? tiles_n - band * kBand : kBand;
+    const int64_t n0 = static_cast<int64_t>(band * kBand + within % high) * TL::BM;
+    const int64_t k0 = static_cast<int64_t>(within / high) * TL::BN;
     const int64_t t0 = split * a.span;
     const int64_t end = t0 + a.span < a.T ? t0 + a.span : a.T;
     const int lane = threadIdx.x % kLanes, wave = threadIdx.x / kLanes;
@@ -235,17 +282,25 @@ __global__ __launch_bounds__(TL::kThreads) void weight_grad_kernel(Args a) {
     UnitA<DT> ua[TL::kUnitsA];
     UnitB ub[TL::kUnitsB];
     const Loader<DT, TL, NEAR> loader(a, n0, k0, end);
-    auto store = [&](char* at) {
+    // (A's and B's units lie alike over their columns where the tile is square)
+    auto place = [&](int i, int wide) { return (threadIdx.x + i * TL::kThreads) % (wide / 8) * 8; };
+    auto quarter = [&](int i, int wide) { return (threadIdx.x + i * TL::kThreads) / (wide / 8); };
+    auto put_a = [&](char* at, auto q) {
 #pragma unroll
-        for (int i = 0; i < TL::kUnitsA; ++i) {
-            const int u = threadIdx.x + i * TL::kThreads;
-            store_a<DT, TL>(ua[i], at, u % (TL::BM / 8) * 8, u / (TL::BM / 8));
-        }
+        for (int i = 0; i < TL::kUnitsA; ++i)
+            store_a<DT, TL, q.value>(ua[i], at, place(i, TL::BM), quarter(i, TL::BM));
+    };
+    float scale[TL::kUnitsB][4];
+    auto scales = [&] {
 #pragma unroll
-        for (int i = 0; i < TL::kUnitsB; ++i) {
-            const int u = threadIdx.x + i * TL::kThreads;
-            store_b(ub[i], at + kTermsA * kBytesA, u % (TL::BN / 8) * 8, u / (TL::BN / 8));
-        }
+        for (int i = 0; i < TL::kUnitsB; ++i)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) scale[i][r] = act8_scale(ub[i].exps[r]);
+    };
+    auto put_b = [&](char* at, auto j) {
+#pragma unroll
+        for (int i = 0; i < TL::kUnitsB; ++i)
+            store_b<j.value>(ub[i], scale[i], at + kTermsA * kBytesA, place(i, TL::BN), quarter(i, TL::BN));
     };
     // Where a lane's operands of 16 rows t are, from the first of a wavefront's 32-column blocks.  (A block further
     // flips the third bit of column / 8, which is that of rows 32 further.)
@@ -255,39 +310,68 @@ __global__ __launch_bounds__(TL::kThreads) void weight_grad_kernel(Args a) {
         at_a[s] = lds_at(wm + lane % 32, 2 * s + lane / 32);
         at_b[s] = lds_at(wn + lane % 32, 2 * s + lane / 32);
     }
-    int buffer = 0;
-    if (t0 < end) {
-        loader.load(t0, ua, ub);
-        store(lds);
-    }
-    __syncthreads();
-    for (int64_t t = t0; t < end; t += kDepth) {
-        const bool more = t + kDepth < end;
-        if (more) loader.load(t + kDepth, ua, ub);
-        const char* la = lds + buffer * kBuffer;
+    bf16x8 fa[2][kTermsA][TL::WM / 32], fb[2][TL::WN / 32];
+    auto fetch = [&](const char* la, auto s) {
+        constexpr int S = s.value;
         const char* lb = la + kTermsA * kBytesA;
 #pragma unroll
-        for (int s = 0; s < kDepth / 16; ++s) {
-            bf16x8 fb[TL::WN / 32];
+        for (int j = 0; j < TL::WN / 32; ++j)
+            fb[S % 2][j] = *reinterpret_cast<const bf16x8*>(lb + at_b[S ^ 2 * (j % 2)] + j * 32 * kRowBytes);
+#pragma unroll
+        for (int term = 0; term < kTermsA; ++term)
+#pragma unroll
+            for (int i = 0; i < TL::WM / 32; ++i)
+                fa[S % 2][term][i] = *reinterpret_cast<const bf16x8*>(
+                    la + term * kBytesA + at_a[S ^ 2 * (i % 2)] + i * 32 * kRowBytes);
+    };
+    // the products of rows 16 S ... + 15 of the step that use blocks I of n
+    auto multiply = [&](auto s, auto block) {
+        constexpr int S = s.value, I = block.value;
+#pragma unroll
+        for (int term = 0; term < kTermsA; ++term)
 #pragma unroll
             for (int j = 0; j < TL::WN / 32; ++j)
-                fb[j] = *reinterpret_cast<const bf16x8*>(lb + at_b[s ^ 2 * (j % 2)] + j * 32 * kRowBytes);
-#pragma unroll
-            for (int term = 0; term < kTermsA; ++term) {
-                bf16x8 fa[TL::WM / 32];
-#pragma unroll
-                for (int i = 0; i < TL::WM / 32; ++i)
-                    fa[i] = *reinterpret_cast<const bf16x8*>(la + term * kBytesA + at_a[s ^ 2 * (i % 2)] +
-                                                             i * 32 * kRowBytes);
-#pragma unroll
-                for (int i = 0; i < TL::WM / 32; ++i)
-#pragma unroll
-                    for (int j = 0; j < TL::WN / 32; ++j)
-                        acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fa[i], fb[j], acc[i][j], 0, 0, 0);
-            }
-        }
+                acc[I][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fa[S % 2][term][I], fb[S % 2][j], acc[I][j],
+                                                                    0, 0, 0);
+    };
+    if (t0 < end) {
+        loader.load_a(t0, ua);
+        loader.load_b(t0, ub);
+        scales();
+        each_of<4>([&](auto q) { put_a(lds, q); });
+        each_of<8>([&](auto j) { put_b(lds, j); });
+        loader.load_a(t0 + kDepth, ua);
+        loader.load_b(t0 + kDepth, ub);
+    }
+    __syncthreads();
+    int buffer = 0;
+    // While a step's products run from one buffer, the next step's rows, in registers, turn into the other, and
+    // the ones after that are loaded as registers fall free.  (Rows past the end are zeros.)
+    constexpr int kBlocks = TL::WM / 32;
+    for (int64_t t = t0; t < end; t += kDepth) {
+        const char* la = lds + buffer * kBuffer;
         buffer ^= 1;
-        if (more) store(lds + buffer * kBuffer);
+        char* next = lds + buffer * kBuffer;
+        fetch(la, Type<0>{});
+        fetch(la, Type<1>{});
+        each_of<kBlocks>([&](auto i) {
+            multiply(Type<0>{}, i);
+            each_of<4 / kBlocks>([&](auto q) { put_a(next, Type<i.value * (4 / kBlocks) + q.value>{}); });
+        });
+        loader.load_a(t + 2 * kDepth, ua);
+        scales();
+        fetch(la, Type<2>{});
+        each_of<kBlocks>([&](auto i) {
+            multiply(Type<1>{}, i);
+            each_of<4 / kBlocks>([&](auto q) { put_b(next, Type<i.value * (4 / kBlocks) + q.value>{}); });
+        });
+        fetch(la, Type<3>{});
+        each_of<kBlocks>([&](auto i) {
+            multiply(Type<2>{}, i);
+            each_of<4 / kBlocks>([&](auto q) { put_b(next, Type<4 + i.value * (4 / kBlocks) + q.value>{}); });
+        });
+        loader.load_b(t + 2 * kDepth, ub);
+        each_of<kBlocks>([&](auto i) { multiply(Type<3>{}, i); });
         __syncthreads();
     }
     // lane l holds column l % 32, rows 8 (r / 4) + 4 (l / 32) + r % 4 of a 32 x 32 block
