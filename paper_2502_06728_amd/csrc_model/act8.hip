@@ -50,7 +50,7 @@ template <int DT>
 __global__ __launch_bounds__(kThreads) void encode_kernel(Items items, deto_rows x, deto_act8 x8) {
     const auto at = items.at(blockIdx.x * kThreads + threadIdx.x);
     float v[8];
-    unpack8<DT>(load8<DT>(x.data, at.t * x.ld + at.d, at.count), v);
+    unpack8<DT>(load8<DT>(x.data, at.t * x.ld, at.d, at.count), v);
     act8_put(x8, at.t, at.d, v, at.count);
 }
 
@@ -97,9 +97,9 @@ __global__ __launch_bounds__(kThreads) void glu_forward_kernel(Items items, deto
                                                                deto_rows h, deto_act8 a8,
                                                                deto_act8 b8) {
     const auto at = items.at(blockIdx.x * kThreads + threadIdx.x);
-    const Raw8<DT> ra = load8<DT>(a.data, at.t * a.ld + at.d, at.count);
+    const Raw8<DT> ra = load8<DT>(a.data, at.t * a.ld, at.d, at.count);
     Raw8<DT> rb = {};
-    if constexpr (GATED) rb = load8<DT>(b.data, at.t * b.ld + at.d, at.count);
+    if constexpr (GATED) rb = load8<DT>(b.data, at.t * b.ld, at.d, at.count);
     float va[8], vb[8], vh[8];
     unpack8<DT>(ra, va);
     unpack8<DT>(rb, vb);
@@ -116,7 +116,7 @@ __global__ __launch_bounds__(kThreads) void glu_backward_kernel(Items items, det
                                                                 deto_rows da, deto_rows db,
                                                                 deto_act8 h8) {
     const auto at = items.at(blockIdx.x * kThreads + threadIdx.x);
-    const Raw8<DT> rd = load8<DT>(dh.data, at.t * dh.ld + at.d, at.count);
+    const Raw8<DT> rd = load8<DT>(dh.data, at.t * dh.ld, at.d, at.count);
     float va[8], vb[8], vd[8], vh[8];
     act8_get(a8, at.t, at.d, va, at.count);
     if constexpr (GATED) act8_get(b8, at.t, at.d, vb, at.count);

@@ -59,33 +59,61 @@ __device__ __forceinline__ void store1(void* base, int64_t at, float v) {
     else static_cast<_Float16*>(base)[at] = static_cast<_Float16>(v);
 }
 
-// elements at .. at + 7, of which `count` (0 ... 8) are there; the others read as zeros
+// elements d .. d + 7 (d a multiple of 8) of a row that starts at element `row`, of which `count` (0 ... 8) are there;
+// the others read as zeros.  A row's partial last vector is read as the eight elements that end with the row and
+// moved down: one access, where element by element takes seven and a register each.  (Only rows of fewer than
+// eight elements have to be.)
 template <int DT>
-__device__ __forceinline__ Raw8<DT> load8(const void* base, int64_t at, int count) {
+__device__ __forceinline__ Raw8<DT> load8(const void* base, int64_t row, int64_t d, int count) {
     Raw8<DT> r = {};
-    const char* p = static_cast<const char*>(base) + at * kSize<DT>;
-    if (count >= 8) {
+    const bool whole = count >= 8;
+    if (whole || (count > 0 && d > 0)) {
+        const int short_by = whole ? 0 : 8 - count;
+        const char* p = static_cast<const char*>(base) + (row + d - short_by) * kSize<DT>;
         if constexpr (DT == DETO_F32) {
             r.a = *reinterpret_cast<const u32x4_any4*>(p);
             r.b = *reinterpret_cast<const u32x4_any4*>(p + 16);
+            if (!whole) {
+                uint32_t w[8] = {r.a[0], r.a[1], r.a[2], r.a[3], r.b[0], r.b[1], r.b[2], r.b[3]};
+#pragma unroll
+                for (int s = 4; s; s >>= 1) {
+#pragma unroll
+                    for (int j = 0; j < 8; ++j)
+                        if (short_by & s) w[j] = j + s < 8 ? w[j + s < 8 ? j + s : 0] : 0u;
+                }
+                r.a = {w[0], w[1], w[2], w[3]};
+                r.b = {w[4], w[5], w[6], w[7]};
+            }
         } else {
             r.a = *reinterpret_cast<const u32x4_any2*>(p);
+            if (!whole) {
+                uint32_t w[4] = {r.a[0], r.a[1], r.a[2], r.a[3]};
+#pragma unroll
+                for (int s = 2; s; s >>= 1) {
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)
+                        if (short_by & (2 * s)) w[j] = j + s < 4 ? w[j + s < 4 ? j + s : 0] : 0u;
+                }
+                if (short_by & 1) {
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) w[j] = w[j] >> 16 | (j < 3 ? w[j < 3 ? j + 1 : 0] << 16 : 0u);
+                }
+                r.a = {w[0], w[1], w[2], w[3]};
+            }
         }
     } else if (count > 0) {
-        if constexpr (DT == DETO_F32) {
-            const uint32_t* q = reinterpret_cast<const uint32_t*>(p);
+        const char* p = static_cast<const char*>(base) + row * kSize<DT>;
 #pragma unroll
-            for (int j = 0; j < 7; ++j)
-                if (j < count) {
-                    if (j < 4) r.a[j] = q[j];
-                    else r.b[j - 4] = q[j];
+        for (int j = 0; j < 7; ++j)
+            if (j < count) {
+                if constexpr (DT == DETO_F32) {
+                    const uint32_t w = reinterpret_cast<const uint32_t*>(p)[j];
+                    if (j < 4) r.a[j] = w;
+                    else r.b[j - 4] = w;
+                } else {
+                    r.a[j / 2] |= static_cast<uint32_t>(reinterpret_cast<const uint16_t*>(p)[j]) << (16 * (j % 2));
                 }
-        } else {
-            const uint16_t* q = reinterpret_cast<const uint16_t*>(p);
-#pragma unroll
-            for (int j = 0; j < 7; ++j)
-                if (j < count) r.a[j / 2] |= static_cast<uint32_t>(q[j]) << (16 * (j % 2));
-        }
+            }
     }
     return r;
 }
@@ -144,11 +172,11 @@ __device__ __forceinline__ void store8(void* base, int64_t at, const float (&v)[
 }
 
 // parameters of a type known only at run time (the branch is uniform)
-__device__ __forceinline__ void load8_any(const void* base, int dtype, int64_t at, int count,
+__device__ __forceinline__ void load8_any(const void* base, int dtype, int64_t row, int64_t d, int count,
                                           float (&v)[8]) {
-    if (dtype == DETO_F32) unpack8<DETO_F32>(load8<DETO_F32>(base, at, count), v);
-    else if (dtype == DETO_BF16) unpack8<DETO_BF16>(load8<DETO_BF16>(base, at, count), v);
-    else unpack8<DETO_F16>(load8<DETO_F16>(base, at, count), v);
+    if (dtype == DETO_F32) unpack8<DETO_F32>(load8<DETO_F32>(base, row, d, count), v);
+    else if (dtype == DETO_BF16) unpack8<DETO_BF16>(load8<DETO_BF16>(base, row, d, count), v);
+    else unpack8<DETO_F16>(load8<DETO_F16>(base, row, d, count), v);
 }
 
 // ---- The 8-bit form.  Four lanes in a row hold a group of 32 features, eight each.
@@ -206,14 +234,18 @@ __device__ __forceinline__ void act8_decode8(const u32x2& q, uint32_t exponent, 
         v[j] = static_cast<float>(static_cast<int8_t>((q[j / 4] >> (8 * (j % 4))) & 0xFFu)) * s;
 }
 
-__device__ __forceinline__ u32x2 load_codes(const int8_t* p, int count) {
+// codes d ... d + 7 of a row, as load8
+__device__ __forceinline__ u32x2 load_codes(const int8_t* row, int64_t d, int count) {
     u32x2 q = {0u, 0u};
     if (count >= 8) {
-        q = *reinterpret_cast<const u32x2_any1*>(p);
+        q = *reinterpret_cast<const u32x2_any1*>(row + d);
+    } else if (count > 0 && d > 0) {
+        q = *reinterpret_cast<const u32x2_any1*>(row + d - (8 - count));
+        q = __builtin_bit_cast(u32x2, __builtin_bit_cast(uint64_t, q) >> (8 * (8 - count)));
     } else {
 #pragma unroll
         for (int j = 0; j < 7; ++j)
-            if (j < count) q[j / 4] |= static_cast<uint32_t>(static_cast<uint8_t>(p[j])) << (8 * (j % 4));
+            if (j < count) q[j / 4] |= static_cast<uint32_t>(static_cast<uint8_t>(row[j])) << (8 * (j % 4));
     }
     return q;
 }
@@ -243,7 +275,7 @@ __device__ __forceinline__ void act8_put(const deto_act8& m, int64_t t, int64_t 
 __device__ __forceinline__ void act8_get(const deto_act8& m, int64_t t, int64_t d, float (&v)[8],
                                          int count) {
     if (count > 0)
-        act8_decode8(load_codes(m.codes + t * m.ld_codes + d, count),
+        act8_decode8(load_codes(m.codes + t * m.ld_codes, d, count),
                      m.exps[t * m.ld_exps + d / DETO_ACT8_GROUP], v);
     else
 #pragma unroll
@@ -264,11 +296,21 @@ struct FastDiv {
     }
 };
 
-// ---- sums over a wavefront, the same in every lane
+// ---- sums over a wavefront, the same in every lane: within rows of 16 lanes by moves between neighbours (no
+// LDS), then the four rows
+template <int CTRL>
+__device__ __forceinline__ float moved(float v) {
+    return bits_f32(__builtin_amdgcn_update_dpp(0, f32_bits(v), CTRL, 0xF, 0xF, true));
+}
+__device__ __forceinline__ float lane_value(float v, int lane) {
+    return bits_f32(__builtin_amdgcn_readlane(f32_bits(v), lane));
+}
 __device__ __forceinline__ float wave_sum(float v) {
-#pragma unroll
-    for (int m = 32; m; m >>= 1) v += __shfl_xor(v, m);
-    return v;
+    v += moved<0xB1>(v);     // lanes 1 0 3 2
+    v += moved<0x4E>(v);     // lanes 2 3 0 1
+    v += moved<0x141>(v);    // the other half of eight
+    v += moved<0x140>(v);    // the other half of sixteen
+    return (lane_value(v, 0) + lane_value(v, 16)) + (lane_value(v, 32) + lane_value(v, 48));
 }
 
 // ---- host side

@@ -161,7 +161,7 @@ __global__ __launch_bounds__(kThreads) void logprobs_kernel(Forward a) {
     for (int64_t d = first + 8 * threadIdx.x; d < end; d += kThreads * 8) {
         const int count = end - d < 8 ? static_cast<int>(end - d) : 8;
         float v[8];
-        unpack8<DT>(load8<DT>(a.logits, row + d, count), v);
+        unpack8<DT>(load8<DT>(a.logits, row, d, count), v);
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
             if (j >= count) v[j] = -__builtin_inff();
@@ -202,7 +202,7 @@ __global__ __launch_bounds__(kThreads) void logprobs_kernel(Forward a) {
         for (int64_t d = first + 8 * threadIdx.x; d < end; d += kThreads * 8) {
             const int count = end - d < 8 ? static_cast<int>(end - d) : 8;
             float v[8];
-            unpack8<DT>(load8<DT>(a.logits, row + d, count), v);
+            unpack8<DT>(load8<DT>(a.logits, row, d, count), v);
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
                 const uint32_t k = order_key(v[j]);
@@ -233,7 +233,7 @@ __global__ __launch_bounds__(kThreads) void logprobs_kernel(Forward a) {
             for (int64_t d = first + 8 * threadIdx.x; d < end; d += kThreads * 8) {
                 const int count = end - d < 8 ? static_cast<int>(end - d) : 8;
                 float v[8];
-                unpack8<DT>(load8<DT>(a.logits, row + d, count), v);
+                unpack8<DT>(load8<DT>(a.logits, row, d, count), v);
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
                     const uint64_t c = candidate(order_key(v[j]), static_cast<uint32_t>(d + j));
@@ -318,7 +318,7 @@ __global__ __launch_bounds__(kThreads) void logprobs_backward_kernel(Backward a)
     for (int i = 0; i < kBackwardVectors; ++i) {
         const int64_t left = a.V - (first + i * kThreads * 8);
         count[i] = left >= 8 ? 8 : left > 0 ? static_cast<int>(left) : 0;
-        raw[i] = load8<DT>(a.logits, t * a.ld + first + i * kThreads * 8, count[i]);
+        raw[i] = load8<DT>(a.logits, t * a.ld, first + i * kThreads * 8, count[i]);
     }
 #pragma unroll
     for (int i = 0; i < kBackwardVectors; ++i) {

@@ -19,10 +19,14 @@ struct Args {
     deto_act8 y8;
 };
 
-// v <- norm(v) * w + b, of a row of which this lane holds C vectors
+template <int C>
+struct Params {
+    float w_post[C][8], b_post[C][8], w_pre[C][8], b_pre[C][8], gate[C][8];
+};
+
+// v <- norm(v), of a row of which this lane holds C vectors (zeros past the row's end)
 template <class TM, int C>
-__device__ __forceinline__ void normalise(TM& team, float (&v)[C][8], int kind, float eps,
-                                          const void* w, const void* b, int dtype, int D) {
+__device__ __forceinline__ void normalise(TM& team, float (&v)[C][8], int kind, float eps, int D) {
     const float inv_d = 1.f / static_cast<float>(D);
     if (kind == DETO_NORM_LAYER) {
         float s[1] = {0.f};
@@ -47,77 +51,107 @@ __device__ __forceinline__ void normalise(TM& team, float (&v)[C][8], int kind, 
     team.sum(q);
     const float r = 1.f / sqrtf(q[0] * inv_d + eps);
 #pragma unroll
-    for (int c = 0; c < C; ++c) {
-        const int d = TM::feature(c), n = TM::count(c, D);
-        float p[8];
-        if (w) load8_any(w, dtype, d, n, p);
+    for (int c = 0; c < C; ++c)
 #pragma unroll
-        for (int j = 0; j < 8; ++j) v[c][j] = v[c][j] * r * (w ? p[j] : 1.f);
-        if (b) {
-            load8_any(b, dtype, d, n, p);
-#pragma unroll
-            for (int j = 0; j < 8; ++j) v[c][j] += p[j];
-        }
-    }
+        for (int j = 0; j < 8; ++j) v[c][j] *= r;
 }
 
-template <int XT, int FT, int W, int C>
-__global__ __launch_bounds__((Team<W, C>::kThreadsWg)) void norm_residual_kernel(Args a) {
-    using TM = Team<W, C>;
+// LAYER: one of the norms is one, or has a bias.  (Without, its registers are not held.)
+template <int XT, int FT, int W, int C, bool WHOLE, bool LAYER>
+__global__ __launch_bounds__((Team<W, C, WHOLE>::kThreadsWg)) void norm_residual_kernel(Args a) {
+    using TM = Team<W, C, WHOLE>;
     __shared__ float lds[TM::kSlots];
     TM team(lds);
     const int D = a.D;
     const int64_t first = TM::index() * a.rows_per_team;
     const int64_t end = first + a.rows_per_team < a.T ? first + a.rows_per_team : a.T;
-    const bool branch = a.f.data != nullptr;
-    for (int64_t t = first; t < end; ++t) {
-        Raw8<XT> rx[C];
-        Raw8<FT> rf[C];
+    if (first >= end) return;                // (teams of one wavefront only: no barriers)
+    const bool branch = a.f.data != nullptr, post = branch && a.cfg.post != DETO_NORM_NONE,
+               pre = a.cfg.pre != DETO_NORM_NONE;
+    const int pre_kind = LAYER ? a.cfg.pre : DETO_NORM_RMS, post_kind = LAYER ? a.cfg.post : DETO_NORM_RMS;
+    Raw8<XT> rx[C];
+    Raw8<FT> rf[C];
+    auto load = [&](int64_t t) {
 #pragma unroll
         for (int c = 0; c < C; ++c) {
-            const int d = TM::feature(c), n = TM::count(c, D);
-            rx[c] = load8<XT>(a.x.data, t * a.x.ld + d, n);
-            if (branch) rf[c] = load8<FT>(a.f.data, t * a.f.ld + d, n);
+            rx[c] = TM::template load<XT>(a.x.data, t * a.x.ld, c, D);
+            if (branch) rf[c] = TM::template load<FT>(a.f.data, t * a.f.ld, c, D);
         }
-        float v[C][8];
-        if (branch) {
+    };
+    if constexpr (!TM::kLean) load(first);
+    // The parameters stay in registers over the team's rows; the gate (with the branch's scale) as long as its
+    // row is the same.
+    Params<C> p;
+    auto param = [&](float (&v)[C][8], const void* at, int64_t row, float otherwise) {
 #pragma unroll
-            for (int c = 0; c < C; ++c) unpack8<FT>(rf[c], v[c]);
-            if (a.cfg.post != DETO_NORM_NONE)
-                normalise(team, v, a.cfg.post, a.cfg.eps_post, a.cfg.w_post, a.cfg.b_post,
-                          a.cfg.param_dtype, D);
-            const int64_t gate_row = a.cfg.rows_per_gate ? t / a.cfg.rows_per_gate : 0;
+        for (int c = 0; c < C; ++c) {
+            if (at) TM::load_any(at, a.cfg.param_dtype, row, c, D, v[c]);
+            else
+#pragma unroll
+                for (int j = 0; j < 8; ++j) v[c][j] = otherwise;
+        }
+    };
+    auto params_of_norms = [&](bool of_post, bool of_pre) {
+        if (of_post && post) param(p.w_post, a.cfg.w_post, 0, 1.f);
+        if (of_pre && pre) param(p.w_pre, a.cfg.w_pre, 0, 1.f);
+        if constexpr (LAYER) {
+            if (of_post && post) param(p.b_post, a.cfg.b_post, 0, 0.f);
+            if (of_pre && pre) param(p.b_pre, a.cfg.b_pre, 0, 0.f);
+        }
+    };
+    if constexpr (!TM::kLean) params_of_norms(true, true);
+    int64_t gate_row = -1;
+    for (int64_t t = first; t < end; ++t) {
+        float v[C][8], x[C][8];
+        if constexpr (TM::kLean) load(t);
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+            unpack8<XT>(rx[c], x[c]);
+            if (branch) unpack8<FT>(rf[c], v[c]);
+        }
+        if constexpr (!TM::kLean)
+            if (t + 1 < end) load(t + 1);
+        if (branch) {
+            const int64_t g = a.cfg.rows_per_gate ? t / a.cfg.rows_per_gate : 0;
+            if (TM::kLean || g != gate_row) {
+                gate_row = g;
+                param(p.gate, a.cfg.gate, g * a.cfg.ld_gate, 1.f);
+#pragma unroll
+                for (int c = 0; c < C; ++c)
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) p.gate[c][j] *= a.cfg.scale;
+            }
+            if (post) normalise(team, v, post_kind, a.cfg.eps_post, D);
+            if constexpr (TM::kLean) params_of_norms(true, false);
 #pragma unroll
             for (int c = 0; c < C; ++c) {
-                const int d = TM::feature(c), n = TM::count(c, D);
-                float x[8], g[8];
-                unpack8<XT>(rx[c], x);
-                if (a.cfg.gate)
-                    load8_any(a.cfg.gate, a.cfg.param_dtype, gate_row * a.cfg.ld_gate + d, n, g);
+                const int n = TM::count(c, D);
 #pragma unroll
-                for (int j = 0; j < 8; ++j)
-                    v[c][j] = j < n ? x[j] + a.cfg.scale * (a.cfg.gate ? g[j] : 1.f) * v[c][j] : 0.f;
+                for (int j = 0; j < 8; ++j) {
+                    float u = v[c][j];
+                    if (post) u *= p.w_post[c][j];
+                    if constexpr (LAYER)
+                        if (post) u += p.b_post[c][j];
+                    x[c][j] = WHOLE || j < n ? x[c][j] + p.gate[c][j] * u : 0.f;
+                }
             }
-        } else {
 #pragma unroll
-            for (int c = 0; c < C; ++c) unpack8<XT>(rx[c], v[c]);
+            for (int c = 0; c < C; ++c) TM::template store<XT>(a.x_out.data, t * a.x_out.ld, c, D, x[c]);
         }
-        if (a.x_out.data) {
-#pragma unroll
-            for (int c = 0; c < C; ++c)
-                store8<XT>(a.x_out.data, t * a.x_out.ld + TM::feature(c), v[c], TM::count(c, D));
-        }
-        if (a.cfg.pre == DETO_NORM_NONE) continue;
-        normalise(team, v, a.cfg.pre, a.cfg.eps_pre, a.cfg.w_pre, a.cfg.b_pre, a.cfg.param_dtype, D);
+        if (!pre) continue;
+        normalise(team, x, pre_kind, a.cfg.eps_pre, D);
+        if constexpr (TM::kLean) params_of_norms(false, true);
 #pragma unroll
         for (int c = 0; c < C; ++c) {
             const int d = TM::feature(c), n = TM::count(c, D);
-            if (a.y.data) store8<FT>(a.y.data, t * a.y.ld + d, v[c], n);
-            if (a.y8.codes) {
 #pragma unroll
-                for (int j = 0; j < 8; ++j) v[c][j] = j < n ? v[c][j] : 0.f;
-                act8_put(a.y8, t, d, v[c], n);
+            for (int j = 0; j < 8; ++j) {
+                x[c][j] *= p.w_pre[c][j];
+                if constexpr (LAYER) x[c][j] += p.b_pre[c][j];
+                if (!WHOLE && j >= n) x[c][j] = 0.f;
             }
+            if (a.y.data) TM::template store<FT>(a.y.data, t * a.y.ld, c, D, x[c]);
+            if (a.y8.codes) act8_put(a.y8, t, d, x[c], n);
         }
     }
 }
@@ -159,14 +193,19 @@ extern "C" int detonation_norm_residual(const deto_norm_residual* cfg, int64_t T
     Args a = {*cfg, T, static_cast<int>(D), 0, *x, branch ? *f : none, branch ? *x_out : none,
               here(y) ? *y : none, here(y8) ? *y8 : deto_act8{}};
     fresh();
-    by_width(D, [&](auto w, auto c) {
-        using TM = Team<w.value, c.value>;
+    const bool layer = cfg->pre == DETO_NORM_LAYER || cfg->post == DETO_NORM_LAYER || cfg->b_pre || cfg->b_post;
+    by_width(D, [&](auto w, auto c, auto whole) {
+        using TM = Team<w.value, c.value, whole.value>;
         a.rows_per_team = rows_per_team(T, TM::kTeamsWg);
         const int64_t teams = (T + a.rows_per_team - 1) / a.rows_per_team;
         const unsigned grid = static_cast<unsigned>((teams + TM::kTeamsWg - 1) / TM::kTeamsWg);
         by_types(x->dtype, ft, [&](auto xt, auto fty) {
-            norm_residual_kernel<xt.value, fty.value, w.value, c.value>
-                <<<grid, TM::kThreadsWg, 0, static_cast<hipStream_t>(stream)>>>(a);
+            if (layer)
+                norm_residual_kernel<xt.value, fty.value, w.value, c.value, whole.value, true>
+                    <<<grid, TM::kThreadsWg, 0, static_cast<hipStream_t>(stream)>>>(a);
+            else
+                norm_residual_kernel<xt.value, fty.value, w.value, c.value, whole.value, false>
+                    <<<grid, TM::kThreadsWg, 0, static_cast<hipStream_t>(stream)>>>(a);
             return 0;
         });
     });

@@ -15,6 +15,7 @@ namespace model {
 namespace {
 
 enum { kWPre, kBPre, kWPost, kBPost, kGate, kSums };
+enum { kWPostRms = 1, kGateRms, kSumsRms };      // where they are without biases
 
 // How rows are dealt to teams: `gates` gate rows of `rows` rows each (one of all rows without
 // rows_per_gate); every gate row is cut into `cuts` runs, or a team takes `group` whole ones.
@@ -33,55 +34,6 @@ struct Args {
     int slots;
 };
 
-// mean and factor of a row; v becomes what the factor multiplies
-template <class TM, int C>
-__device__ __forceinline__ float centre(TM& team, float (&v)[C][8], int kind, float eps, int D) {
-    const float inv_d = 1.f / static_cast<float>(D);
-    if (kind == DETO_NORM_LAYER) {
-        float s[1] = {0.f};
-#pragma unroll
-        for (int c = 0; c < C; ++c)
-#pragma unroll
-            for (int j = 0; j < 8; ++j) s[0] += v[c][j];
-        team.sum(s);
-        const float mean = s[0] * inv_d;
-#pragma unroll
-        for (int c = 0; c < C; ++c) {
-            const int n = TM::count(c, D);
-#pragma unroll
-            for (int j = 0; j < 8; ++j) v[c][j] = j < n ? v[c][j] - mean : 0.f;
-        }
-    }
-    float q[1] = {0.f};
-#pragma unroll
-    for (int c = 0; c < C; ++c)
-#pragma unroll
-        for (int j = 0; j < 8; ++j) q[0] += v[c][j] * v[c][j];
-    team.sum(q);
-    return 1.f / sqrtf(q[0] * inv_d + eps);
-}
-
-// v: the normalised row, a: the gradient of the norm's output times its weight; a <- gradient of the input
-template <class TM, int C>
-__device__ __forceinline__ void back(TM& team, const float (&v)[C][8], float (&a)[C][8], float r,
-                                     int kind, int D) {
-    const float inv_d = 1.f / static_cast<float>(D);
-    float s[2] = {0.f, 0.f};
-#pragma unroll
-    for (int c = 0; c < C; ++c)
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            s[0] += a[c][j] * v[c][j];
-            s[1] += a[c][j];
-        }
-    team.sum(s);
-    const float m0 = s[0] * inv_d, m1 = kind == DETO_NORM_LAYER ? s[1] * inv_d : 0.f;
-#pragma unroll
-    for (int c = 0; c < C; ++c)
-#pragma unroll
-        for (int j = 0; j < 8; ++j) a[c][j] = r * (a[c][j] - v[c][j] * m0 - m1);
-}
-
 template <int C>
 __device__ __forceinline__ void clear(float (&v)[C][8]) {
 #pragma unroll
@@ -90,12 +42,15 @@ __device__ __forceinline__ void clear(float (&v)[C][8]) {
         for (int j = 0; j < 8; ++j) v[c][j] = 0.f;
 }
 
-template <int XT, int FT, int W, int C>
-__global__ __launch_bounds__((Team<W, C>::kThreadsWg)) void norm_backward_kernel(Args a) {
-    using TM = Team<W, C>;
+// LAYER: one of the norms is one, or has a bias, or a bias's gradient is wanted.  (Without, the registers of the
+// biases' sums are not held.)
+template <int XT, int FT, int W, int C, bool WHOLE, bool LAYER>
+__global__ __launch_bounds__((Team<W, C, WHOLE>::kThreadsWg)) void norm_backward_kernel(Args a) {
+    using TM = Team<W, C, WHOLE>;
     __shared__ float lds[TM::kSlots];
     TM team(lds);
     const int D = a.D;
+    const float inv_d = 1.f / static_cast<float>(D);
     const Deal& deal = a.deal;
     const int64_t me = TM::index();
     if (me >= deal.teams) return;            // (teams of one wavefront only: no barriers)
@@ -112,102 +67,180 @@ __global__ __launch_bounds__((Team<W, C>::kThreadsWg)) void norm_backward_kernel
     }
     if (end > deal.T) end = deal.T;
     const bool branch = a.f.data != nullptr, pre = a.cfg.pre != DETO_NORM_NONE,
-               post = a.cfg.post != DETO_NORM_NONE;
-    float sums[kSums][C][8];
-#pragma unroll
-    for (int i = 0; i < kSums; ++i) clear(sums[i]);
-    for (int64_t t = first; t < end; ++t) {
-        float v[C][8], G[C][8], o[C][8];
+               post = branch && a.cfg.post != DETO_NORM_NONE, through = a.dxo.data != nullptr;
+    const bool pre_layer = LAYER && a.cfg.pre == DETO_NORM_LAYER, post_layer = LAYER && a.cfg.post == DETO_NORM_LAYER;
+
+    Raw8<XT> rx[C], ro[C];
+    Raw8<FT> rf[C], ry[C];
+    auto load = [&](int64_t t) {
 #pragma unroll
         for (int c = 0; c < C; ++c) {
-            const int d = TM::feature(c), n = TM::count(c, D);
-            unpack8<XT>(load8<XT>(a.x.data, t * a.x.ld + d, n), v[c]);
-            if (pre) unpack8<FT>(load8<FT>(a.dy.data, t * a.dy.ld + d, n), G[c]);
-            if (a.dxo.data) unpack8<XT>(load8<XT>(a.dxo.data, t * a.dxo.ld + d, n), o[c]);
+            if (pre) {
+                rx[c] = TM::template load<XT>(a.x.data, t * a.x.ld, c, D);
+                ry[c] = TM::template load<FT>(a.dy.data, t * a.dy.ld, c, D);
+            }
+            if (through) ro[c] = TM::template load<XT>(a.dxo.data, t * a.dxo.ld, c, D);
+            if (branch) rf[c] = TM::template load<FT>(a.f.data, t * a.f.ld, c, D);
         }
-        if (!a.dxo.data) clear(o);
-        if (pre) {
-            const float r = centre(team, v, a.cfg.pre, a.cfg.eps_pre, D);
+    };
 #pragma unroll
-            for (int c = 0; c < C; ++c) {
-                const int d = TM::feature(c), n = TM::count(c, D);
-                float w[8];
-                if (a.cfg.w_pre) load8_any(a.cfg.w_pre, a.cfg.param_dtype, d, n, w);
+    for (int c = 0; c < C; ++c) {
+        rx[c] = ro[c] = {};
+        rf[c] = ry[c] = {};
+    }
+    if (!TM::kLean && first < end) load(first);
+    float w_pre[C][8], w_post[C][8], b_post[C][8], gate[C][8];
+    auto param = [&](float (&v)[C][8], const void* at, int64_t row, float otherwise) {
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+            if (at) TM::load_any(at, a.cfg.param_dtype, row, c, D, v[c]);
+            else
+#pragma unroll
+                for (int j = 0; j < 8; ++j) v[c][j] = otherwise;
+        }
+    };
+    auto params_of_pre = [&] { param(w_pre, pre ? a.cfg.w_pre : nullptr, 0, 1.f); };
+    auto params_of_post = [&] {
+        param(w_post, post ? a.cfg.w_post : nullptr, 0, 1.f);
+        if constexpr (LAYER) param(b_post, post ? a.cfg.b_post : nullptr, 0, 0.f);
+    };
+    if constexpr (!TM::kLean) {
+        params_of_pre();
+        params_of_post();
+    }
+    float sums[LAYER ? kSums : kSumsRms][C][8];
+    constexpr int kAtGate = LAYER ? kGate : kGateRms, kAtPost = LAYER ? kWPost : kWPostRms;
+#pragma unroll
+    for (int i = 0; i < (LAYER ? kSums : kSumsRms); ++i) clear(sums[i]);
+    int64_t gate_row = -1;
+    for (int64_t t = first; t < end; ++t) {
+        float x[C][8], f[C][8], G[C][8], o[C][8];
+        if constexpr (TM::kLean) load(t);
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+            unpack8<XT>(rx[c], x[c]);
+            unpack8<XT>(ro[c], o[c]);
+            unpack8<FT>(ry[c], G[c]);
+            unpack8<FT>(rf[c], f[c]);
+        }
+        if constexpr (TM::kLean) params_of_pre();
+        else if (t + 1 < end) load(t + 1);
+        if (pre_layer || post_layer) {
+            float s[2] = {0.f, 0.f};
+#pragma unroll
+            for (int c = 0; c < C; ++c)
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
-                    v[c][j] *= r;
-                    sums[kWPre][c][j] += G[c][j] * v[c][j];
-                    sums[kBPre][c][j] += G[c][j];
-                    if (a.cfg.w_pre) G[c][j] *= w[j];
+                    s[0] += x[c][j];
+                    s[1] += f[c][j];
+                }
+            team.sum(s);
+            const float mx = pre_layer ? s[0] * inv_d : 0.f, mf = post_layer ? s[1] * inv_d : 0.f;
+#pragma unroll
+            for (int c = 0; c < C; ++c) {
+                const int n = TM::count(c, D);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    x[c][j] = j < n ? x[c][j] - mx : 0.f;
+                    f[c][j] = j < n ? f[c][j] - mf : 0.f;
                 }
             }
-            back(team, v, G, r, a.cfg.pre, D);
-#pragma unroll
-            for (int c = 0; c < C; ++c)
-#pragma unroll
-                for (int j = 0; j < 8; ++j) G[c][j] += o[c][j];
-        } else {
-#pragma unroll
-            for (int c = 0; c < C; ++c)
-#pragma unroll
-                for (int j = 0; j < 8; ++j) G[c][j] = o[c][j];
         }
+        // x and f are centred; a = dy (.) w:  sum x^2, sum a x, sum f^2, sum a
+        float s[LAYER ? 4 : 3];
+#pragma unroll
+        for (int i = 0; i < (LAYER ? 4 : 3); ++i) s[i] = 0.f;
 #pragma unroll
         for (int c = 0; c < C; ++c)
-            store8<XT>(a.dx.data, t * a.dx.ld + TM::feature(c), G[c], TM::count(c, D));
-        if (!branch) continue;
-#pragma unroll
-        for (int c = 0; c < C; ++c)
-            unpack8<FT>(load8<FT>(a.f.data, t * a.f.ld + TM::feature(c), TM::count(c, D)), v[c]);
-        float r = 1.f;
-        if (post) r = centre(team, v, a.cfg.post, a.cfg.eps_post, D);
-        const int64_t gate_row = a.cfg.rows_per_gate ? t / a.cfg.rows_per_gate : 0;
-#pragma unroll
-        for (int c = 0; c < C; ++c) {
-            const int d = TM::feature(c), n = TM::count(c, D);
-            float w[8], b[8], g[8];
-            const bool has_w = post && a.cfg.w_post, has_b = post && a.cfg.b_post;
-            if (has_w) load8_any(a.cfg.w_post, a.cfg.param_dtype, d, n, w);
-            if (has_b) load8_any(a.cfg.b_post, a.cfg.param_dtype, d, n, b);
-            if (a.cfg.gate)
-                load8_any(a.cfg.gate, a.cfg.param_dtype, gate_row * a.cfg.ld_gate + d, n, g);
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                v[c][j] *= r;
-                const float u = v[c][j] * (has_w ? w[j] : 1.f) + (has_b ? b[j] : 0.f);
-                float s = a.cfg.scale * G[c][j];
-                sums[kGate][c][j] += s * u;
-                if (a.cfg.gate) s *= g[j];
-                sums[kWPost][c][j] += s * v[c][j];
-                sums[kBPost][c][j] += s;
-                G[c][j] = has_w ? s * w[j] : s;
+                const float dyw = G[c][j] * w_pre[c][j];
+                s[0] += x[c][j] * x[c][j];
+                s[1] += dyw * x[c][j];
+                s[2] += f[c][j] * f[c][j];
+                if constexpr (LAYER) s[3] += dyw;
+            }
+        team.sum(s);
+        const float r = pre ? 1.f / sqrtf(s[0] * inv_d + a.cfg.eps_pre) : 0.f;
+        const float m0 = r * r * (s[1] * inv_d);
+        float m1 = 0.f;
+        if constexpr (LAYER) m1 = pre_layer ? s[3] * inv_d : 0.f;
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                sums[kWPre][c][j] += G[c][j] * (x[c][j] * r);
+                if constexpr (LAYER) sums[kBPre][c][j] += G[c][j];
+                G[c][j] = r * (G[c][j] * w_pre[c][j] - x[c][j] * m0 - m1) + o[c][j];
+            }
+            TM::template store<XT>(a.dx.data, t * a.dx.ld, c, D, G[c]);
+        }
+        if (!branch) continue;
+        const int64_t row = a.cfg.rows_per_gate ? t / a.cfg.rows_per_gate : 0;
+        if constexpr (TM::kLean) params_of_post();
+        if (TM::kLean || row != gate_row) {
+            gate_row = row;
+            param(gate, a.cfg.gate, row * a.cfg.ld_gate, 1.f);
+        }
+        const float rf_ = post ? 1.f / sqrtf(s[2] * inv_d + a.cfg.eps_post) : 1.f;
+        float q[2] = {0.f, 0.f};
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+            const int n = TM::count(c, D);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const float v = f[c][j] * rf_;
+                float u = v * w_post[c][j];
+                if constexpr (LAYER) u += b_post[c][j];
+                const float g = WHOLE || j < n ? a.cfg.scale * G[c][j] : 0.f;
+                sums[kAtGate][c][j] += g * u;
+                const float h = g * gate[c][j];
+                sums[kAtPost][c][j] += h * v;
+                if constexpr (LAYER) sums[kBPost][c][j] += h;
+                G[c][j] = h * w_post[c][j];
+                q[0] += G[c][j] * f[c][j];
+                q[1] += G[c][j];
             }
         }
-        if (post) back(team, v, G, r, a.cfg.post, D);
+        if (post) {
+            if constexpr (LAYER) team.sum(q);
+            else team.sum(reinterpret_cast<float (&)[1]>(q));
+            const float n0 = rf_ * rf_ * (q[0] * inv_d), n1 = post_layer ? q[1] * inv_d : 0.f;
 #pragma unroll
-        for (int c = 0; c < C; ++c)
-            store8<FT>(a.df.data, t * a.df.ld + TM::feature(c), G[c], TM::count(c, D));
+            for (int c = 0; c < C; ++c)
+#pragma unroll
+                for (int j = 0; j < 8; ++j) G[c][j] = rf_ * (G[c][j] - f[c][j] * n0 - n1);
+        }
+#pragma unroll
+        for (int c = 0; c < C; ++c) TM::template store<FT>(a.df.data, t * a.df.ld, c, D, G[c]);
         // a gate row of this team's own ends
         if (deal.group && a.grads.gate && ((t + 1) % deal.rows == 0 || t + 1 == deal.T)) {
 #pragma unroll
             for (int c = 0; c < C; ++c)
-                store8<DETO_F32>(a.grads.gate, t / deal.rows * D + TM::feature(c), sums[kGate][c],
-                                 TM::count(c, D));
-            clear(sums[kGate]);
+                TM::template store<DETO_F32>(a.grads.gate, t / deal.rows * D, c, D, sums[kAtGate][c]);
+            clear(sums[kAtGate]);
         }
     }
+    auto leave = [&](int which, const float (&v)[C][8]) {
+        if (a.slot[which] < 0) return;
 #pragma unroll
-    for (int i = 0; i < kSums; ++i)
-        if (a.slot[i] >= 0) {
-#pragma unroll
-            for (int c = 0; c < C; ++c)
-                store8<DETO_F32>(a.parts, (me * a.slots + a.slot[i]) * D + TM::feature(c), sums[i][c],
-                                 TM::count(c, D));
-        }
+        for (int c = 0; c < C; ++c)
+            TM::template store<DETO_F32>(a.parts, (me * a.slots + a.slot[which]) * D, c, D, v[c]);
+    };
+    leave(kWPre, sums[kWPre]);
+    leave(kWPost, sums[kAtPost]);
+    leave(kGate, sums[kAtGate]);
+    if constexpr (LAYER) {
+        leave(kBPre, sums[kBPre]);
+        leave(kBPost, sums[kBPost]);
+    }
 }
 
-// Adds the teams' sums of 64 columns: four wavefronts take the teams in turn.  blockIdx.y is the output row:
-// the weights' and biases' sums over all teams, then the gate's rows, each over the teams of its own.
+// Adds the teams' sums of 16 columns: 64 lanes in turn for each, their loads side by side (24 MB of 1,024 teams'
+// sums of 2,048 columns: 75 us with four lanes to a column, whose loads follow each other).  blockIdx.y is the output
+// row: the weights' and biases' sums over all teams, then the gate's rows, each over the teams of its own.
+constexpr int kJoinColumns = 16, kJoinThreads = 1024, kJoinLanes = kJoinThreads / kJoinColumns;
+
 struct JoinArgs {
     const float* parts;
     int D, slots;
@@ -218,24 +251,36 @@ struct JoinArgs {
     int64_t gate_teams;   // teams of a gate row
 };
 
-__global__ __launch_bounds__(256) void norm_join_kernel(JoinArgs a, int64_t y0) {
-    __shared__ float lds[4][kLanes];
-    const int col = blockIdx.x * kLanes + threadIdx.x % kLanes, wave = threadIdx.x / kLanes;
+__global__ __launch_bounds__(kJoinThreads) void norm_join_kernel(JoinArgs a, int64_t y0) {
+    __shared__ float lds[kJoinLanes][kJoinColumns + 1];
+    const int c = threadIdx.x % kJoinColumns, lane = threadIdx.x / kJoinColumns;
+    const int col = blockIdx.x * kJoinColumns + c;
     const int64_t y = y0 + blockIdx.y;
     const bool gate = y >= a.outs;
     const int i = gate ? kGate : static_cast<int>(y);
     const int64_t first = gate ? (y - a.outs) * a.gate_teams : 0;
     const int64_t end = gate ? first + a.gate_teams : a.teams;
     float s = 0.f;
-    if (col < a.D)
-        for (int64_t t = first + wave; t < end; t += 4)
-            s += a.parts[(t * a.slots + a.slot[i]) * a.D + col];
-    lds[wave][threadIdx.x % kLanes] = s;
-    __syncthreads();
-    if (wave == 0 && col < a.D) {
-        const int l = threadIdx.x;
-        a.out[i][(gate ? (y - a.outs) * a.D : 0) + col] = (lds[0][l] + lds[1][l]) + (lds[2][l] + lds[3][l]);
+    if (col < a.D) {
+        const float* at = a.parts + static_cast<int64_t>(a.slot[i]) * a.D + col;
+        const int64_t step = static_cast<int64_t>(a.slots) * a.D;
+        int64_t t = first + lane;
+        for (; t + 7 * kJoinLanes < end; t += 8 * kJoinLanes) {
+            float v[8];
+#pragma unroll
+            for (int k = 0; k < 8; ++k) v[k] = at[(t + k * kJoinLanes) * step];
+#pragma unroll
+            for (int k = 0; k < 8; ++k) s += v[k];
+        }
+        for (; t < end; t += kJoinLanes) s += at[t * step];
     }
+    lds[lane][c] = s;
+    __syncthreads();
+    for (int half = kJoinLanes / 2; half; half >>= 1) {
+        if (lane < half) lds[lane][c] += lds[lane + half][c];
+        __syncthreads();
+    }
+    if (lane == 0 && col < a.D) a.out[i][(gate ? (y - a.outs) * a.D : 0) + col] = lds[0][c];
 }
 
 // Teams that are wanted: a wavefront's worth of rows each, as many as fill the chip.
@@ -339,12 +384,18 @@ int detonation_norm_residual_backward(const deto_norm_residual* cfg, int64_t T, 
         a.df = branch ? *df : none;
         a.dy = pre ? *dy : none;
         a.dxo = here(dx_out) ? *dx_out : none;
-        by_width(D, [&](auto w, auto c) {
-            using TM = Team<w.value, c.value>;
+        const bool layer = cfg->pre == DETO_NORM_LAYER || cfg->post == DETO_NORM_LAYER || cfg->b_post || g.b_pre ||
+                           g.b_post;
+        by_width(D, [&](auto w, auto c, auto whole) {
+            using TM = Team<w.value, c.value, whole.value>;
             const unsigned grid = static_cast<unsigned>((a.deal.teams + TM::kTeamsWg - 1) / TM::kTeamsWg);
             by_types(a.x.dtype, branch ? a.f.dtype : a.dy.dtype, [&](auto xt, auto ft) {
-                norm_backward_kernel<xt.value, ft.value, w.value, c.value>
-                    <<<grid, TM::kThreadsWg, 0, st>>>(a);
+                if (layer)
+                    norm_backward_kernel<xt.value, ft.value, w.value, c.value, whole.value, true>
+                        <<<grid, TM::kThreadsWg, 0, st>>>(a);
+                else
+                    norm_backward_kernel<xt.value, ft.value, w.value, c.value, whole.value, false>
+                        <<<grid, TM::kThreadsWg, 0, st>>>(a);
                 return 0;
             });
         });
@@ -360,8 +411,8 @@ int detonation_norm_residual_backward(const deto_norm_residual* cfg, int64_t T, 
         const int64_t all = j.outs + gates;
         for (int64_t y0 = 0; y0 < all; y0 += 65535) {
             const unsigned rows = static_cast<unsigned>(all - y0 < 65535 ? all - y0 : 65535);
-            norm_join_kernel<<<dim3(static_cast<unsigned>((D + kLanes - 1) / kLanes), rows), 256, 0, st>>>(
-                j, y0);
+            const unsigned columns = static_cast<unsigned>((D + kJoinColumns - 1) / kJoinColumns);
+            norm_join_kernel<<<dim3(columns, rows), kJoinThreads, 0, st>>>(j, y0);
         }
     }
     return enqueued();

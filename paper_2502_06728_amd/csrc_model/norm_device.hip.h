@@ -1,9 +1,11 @@
 // What the forward and the backward kernels of norm, gate and residual share: how rows are laid over a
 // workgroup, sums over a row, the launch by width.
 //
-// A row is taken by a team of W wavefronts, a lane C vectors of eight features.  Up to 1,024 features a team is
+// A row is taken by a team of W wavefronts, a lane C vectors of eight features.  Up to 512 features a team is
 // one wavefront, which needs no barrier (four teams a workgroup); wider rows take a workgroup.
 #pragma once
+
+#include <type_traits>
 
 #include "device.hip.h"
 
@@ -12,11 +14,14 @@ namespace model {
 
 constexpr int64_t kMaxNormWidth = 16384;
 
-template <int W, int C>
+// WHOLE: rows of a multiple of eight features, a lane's vectors are whole or empty.
+template <int W, int C, bool WHOLE>
 struct Team {
     static constexpr int kWavesWg = W == 1 ? 4 : W;
     static constexpr int kThreadsWg = kWavesWg * kLanes;
     static constexpr int kTeamsWg = kWavesWg / W;
+    // A lane of a workgroup of 1,024 has 128 registers: not enough to hold the parameters and the next row too.
+    static constexpr bool kLean = W >= 16;
     static constexpr int kSlots = 2 * kWavesWg * 4;    // floats of LDS for sums
 
     float* lds;
@@ -33,7 +38,26 @@ struct Team {
     }
     static __device__ __forceinline__ int count(int c, int D) {
         const int left = D - feature(c);
+        if constexpr (WHOLE) return left > 0 ? 8 : 0;
         return left >= 8 ? 8 : left > 0 ? left : 0;
+    }
+    template <int DT>
+    static __device__ __forceinline__ Raw8<DT> load(const void* base, int64_t row, int c, int D) {
+        if constexpr (!WHOLE) return load8<DT>(base, row, feature(c), count(c, D));
+        Raw8<DT> r = {};
+        if (feature(c) < D) r = load8<DT>(base, row, feature(c), 8);
+        return r;
+    }
+    static __device__ __forceinline__ void load_any(const void* base, int dtype, int64_t row, int c, int D,
+                                                    float (&v)[8]) {
+        if (dtype == DETO_F32) unpack8<DETO_F32>(load<DETO_F32>(base, row, c, D), v);
+        else if (dtype == DETO_BF16) unpack8<DETO_BF16>(load<DETO_BF16>(base, row, c, D), v);
+        else unpack8<DETO_F16>(load<DETO_F16>(base, row, c, D), v);
+    }
+    template <int DT>
+    static __device__ __forceinline__ void store(void* base, int64_t row, int c, int D, const float (&v)[8]) {
+        if constexpr (!WHOLE) store8<DT>(base, row + feature(c), v, count(c, D));
+        else if (feature(c) < D) store8<DT>(base, row + feature(c), v, 8);
     }
     // N sums over the row, in every lane.  Two sets of slots in turn: one barrier a sum, since a wavefront that
     // writes a set again has passed the barrier of the set between, which all reach after reading this one.
@@ -63,12 +87,16 @@ struct Team {
 // Teams by width, for a generic lambda that takes Team's arguments as types.
 template <class F>
 inline void by_width(int64_t D, F f) {
-    if (D <= 512) f(Type<1>{}, Type<1>{});
-    else if (D <= 1024) f(Type<1>{}, Type<2>{});
-    else if (D <= 2048) f(Type<4>{}, Type<1>{});
-    else if (D <= 4096) f(Type<8>{}, Type<1>{});
-    else if (D <= 8192) f(Type<16>{}, Type<1>{});
-    else f(Type<16>{}, Type<2>{});
+    auto g = [&](auto w, auto c) {
+        if (D % 8 == 0) f(w, c, std::true_type{});
+        else f(w, c, std::false_type{});
+    };
+    if (D <= 512) g(Type<1>{}, Type<1>{});
+    else if (D <= 1024) g(Type<2>{}, Type<1>{});
+    else if (D <= 2048) g(Type<4>{}, Type<1>{});
+    else if (D <= 4096) g(Type<8>{}, Type<1>{});
+    else if (D <= 8192) g(Type<16>{}, Type<1>{});
+    else g(Type<16>{}, Type<2>{});
 }
 
 inline bool valid_kind(int k) { return k >= DETO_NORM_NONE && k <= DETO_NORM_LAYER; }

@@ -130,7 +130,7 @@ struct Loader {
                 const int count = left >= 8 ? 8 : left > 0 ? static_cast<int>(left) : 0;
 #pragma unroll
                 for (int r = 0; r < 4; ++r)
-                    ua[i].row[r] = load8<DT>(a.dy.data, (row + r) * a.dy.ld + n, row + r < end ? count : 0);
+                    ua[i].row[r] = load8<DT>(a.dy.data, (row + r) * a.dy.ld, n, row + r < end ? count : 0);
             }
         }
     }
@@ -163,7 +163,7 @@ struct Loader {
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
                     const bool on = row + r < end && count > 0;
-                    ub[i].codes[r] = load_codes(a.x.codes + (row + r) * a.x.ld_codes + k, on ? count : 0);
+                    ub[i].codes[r] = load_codes(a.x.codes + (row + r) * a.x.ld_codes, k, on ? count : 0);
                     ub[i].exps[r] = on ? a.x.exps[(row + r) * a.x.ld_exps + k / DETO_ACT8_GROUP] : 0u;
                 }
             }
