@@ -59,6 +59,47 @@ __device__ __forceinline__ void store1(void* base, int64_t at, float v) {
     else static_cast<_Float16*>(base)[at] = static_cast<_Float16>(v);
 }
 
+template <int DT>
+__device__ __forceinline__ Raw8<DT> load8_whole(const char* p) {
+    Raw8<DT> r;
+    if constexpr (DT == DETO_F32) {
+        r.a = *reinterpret_cast<const u32x4_any4*>(p);
+        r.b = *reinterpret_cast<const u32x4_any4*>(p + 16);
+    } else {
+        r.a = *reinterpret_cast<const u32x4_any2*>(p);
+    }
+    return r;
+}
+
+// element j <- element j + by (0 ... 7), zeros from above
+template <int DT>
+__device__ __forceinline__ void move_down(Raw8<DT>& r, int by) {
+    if constexpr (DT == DETO_F32) {
+        uint32_t w[8] = {r.a[0], r.a[1], r.a[2], r.a[3], r.b[0], r.b[1], r.b[2], r.b[3]};
+#pragma unroll
+        for (int s = 4; s; s >>= 1) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                if (by & s) w[j] = j + s < 8 ? w[j + s < 8 ? j + s : 0] : 0u;
+        }
+        r.a = {w[0], w[1], w[2], w[3]};
+        r.b = {w[4], w[5], w[6], w[7]};
+    } else {
+        uint32_t w[4] = {r.a[0], r.a[1], r.a[2], r.a[3]};
+#pragma unroll
+        for (int s = 2; s; s >>= 1) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                if (by & (2 * s)) w[j] = j + s < 4 ? w[j + s < 4 ? j + s : 0] : 0u;
+        }
+        if (by & 1) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) w[j] = w[j] >> 16 | (j < 3 ? w[j < 3 ? j + 1 : 0] << 16 : 0u);
+        }
+        r.a = {w[0], w[1], w[2], w[3]};
+    }
+}
+
 // elements d .. d + 7 (d a multiple of 8) of a row that starts at element `row`, of which `count` (0 ... 8) are there;
 // the others read as zeros.  A row's partial last vector is read as the eight elements that end with the row and
 // moved down: one access, where element by element takes seven and a register each.  (Only rows of fewer than
@@ -70,50 +111,20 @@ __device__ __forceinline__ Raw8<DT> load8(const void* base, int64_t row, int64_t
     if (whole || (count > 0 && d > 0)) {
         const int short_by = whole ? 0 : 8 - count;
         const char* p = static_cast<const char*>(base) + (row + d - short_by) * kSize<DT>;
-        if constexpr (DT == DETO_F32) {
-            r.a = *reinterpret_cast<const u32x4_any4*>(p);
-            r.b = *reinterpret_cast<const u32x4_any4*>(p + 16);
-            if (!whole) {
-                uint32_t w[8] = {r.a[0], r.a[1], r.a[2], r.a[3], r.b[0], r.b[1], r.b[2], r.b[3]};
-#pragma unroll
-                for (int s = 4; s; s >>= 1) {
-#pragma unroll
-                    for (int j = 0; j < 8; ++j)
-                        if (short_by & s) w[j] = j + s < 8 ? w[j + s < 8 ? j + s : 0] : 0u;
-                }
-                r.a = {w[0], w[1], w[2], w[3]};
-                r.b = {w[4], w[5], w[6], w[7]};
-            }
-        } else {
-            r.a = *reinterpret_cast<const u32x4_any2*>(p);
-            if (!whole) {
-                uint32_t w[4] = {r.a[0], r.a[1], r.a[2], r.a[3]};
-#pragma unroll
-                for (int s = 2; s; s >>= 1) {
-#pragma unroll
-                    for (int j = 0; j < 4; ++j)
-                        if (short_by & (2 * s)) w[j] = j + s < 4 ? w[j + s < 4 ? j + s : 0] : 0u;
-                }
-                if (short_by & 1) {
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) w[j] = w[j] >> 16 | (j < 3 ? w[j < 3 ? j + 1 : 0] << 16 : 0u);
-                }
-                r.a = {w[0], w[1], w[2], w[3]};
-            }
-        }
+        r = load8_whole<DT>(p);
+        if (!whole) move_down<DT>(r, short_by);
     } else if (count > 0) {
         const char* p = static_cast<const char*>(base) + row * kSize<DT>;
-#pragma unroll
-        for (int j = 0; j < 7; ++j)
-            if (j < count) {
-                if constexpr (DT == DETO_F32) {
-                    const uint32_t w = reinterpret_cast<const uint32_t*>(p)[j];
-                    if (j < 4) r.a[j] = w;
-                    else r.b[j - 4] = w;
-                } else {
-                    r.a[j / 2] |= static_cast<uint32_t>(reinterpret_cast<const uint16_t*>(p)[j]) << (16 * (j % 2));
-                }
+#pragma unroll 1
+        for (int j = count - 1; j >= 0; --j) {      // each in front of what is there
+            if constexpr (DT == DETO_F32) {
+                r.b = {r.a[3], r.b[0], r.b[1], r.b[2]};
+                r.a = {reinterpret_cast<const uint32_t*>(p)[j], r.a[0], r.a[1], r.a[2]};
+            } else {
+                r.a = {r.a[0] << 16 | reinterpret_cast<const uint16_t*>(p)[j], r.a[1] << 16 | r.a[0] >> 16,
+                       r.a[2] << 16 | r.a[1] >> 16, r.a[3] << 16 | r.a[2] >> 16};
             }
+        }
     }
     return r;
 }
@@ -164,7 +175,7 @@ __device__ __forceinline__ void store8(void* base, int64_t at, const float (&v)[
                                        : pack_f16(v[2 * j], v[2 * j + 1]);
             *reinterpret_cast<u32x4_any2*>(p) = a;
         }
-    } else {
+    } else if (count > 0) {
 #pragma unroll
         for (int j = 0; j < 7; ++j)
             if (j < count) store1<DT>(p, j, v[j]);
@@ -243,9 +254,10 @@ __device__ __forceinline__ u32x2 load_codes(const int8_t* row, int64_t d, int co
         q = *reinterpret_cast<const u32x2_any1*>(row + d - (8 - count));
         q = __builtin_bit_cast(u32x2, __builtin_bit_cast(uint64_t, q) >> (8 * (8 - count)));
     } else {
-#pragma unroll
-        for (int j = 0; j < 7; ++j)
-            if (j < count) q[j / 4] |= static_cast<uint32_t>(static_cast<uint8_t>(row[j])) << (8 * (j % 4));
+        uint64_t bits = 0;
+#pragma unroll 1
+        for (int j = count - 1; j >= 0; --j) bits = bits << 8 | static_cast<uint8_t>(row[j]);
+        q = __builtin_bit_cast(u32x2, bits);
     }
     return q;
 }

@@ -283,10 +283,21 @@ __global__ __launch_bounds__(kJoinThreads) void norm_join_kernel(JoinArgs a, int
     if (lane == 0 && col < a.D) a.out[i][(gate ? (y - a.outs) * a.D : 0) + col] = lds[0][c];
 }
 
-// Teams that are wanted: a wavefront's worth of rows each, as many as fill the chip.
-constexpr int64_t kTeams = 1024;
+// Teams that are wanted: as many as run side by side, three wavefronts a SIMD, two of the kernels with biases or
+// partial vectors (a workgroup of sixteen: four).  A second round of teams, shorter than the first, costs more than it
+// adds (16,384 x 2,048: 1,024 teams 144 us, 768 127 us).
+int64_t wanted_teams(int64_t D, bool lean) {
+    int64_t teams = 0;
+    by_width(D, [&](auto w, auto, auto whole) {
+        teams = w.value >= 16 ? 256 : (lean && whole.value ? 3072 : 2048) / w.value;
+    });
+    return teams;
+}
 
-Deal deal_rows(const deto_norm_residual* cfg, int64_t T) {
+// lean: no biases.  A team takes two rows at least (1,379 x 771: one row 28 us, two 21, four 23).
+Deal deal_rows(const deto_norm_residual* cfg, int64_t T, int64_t D, bool lean) {
+    int64_t most = wanted_teams(D, lean);
+    if (most > T / 2) most = T / 2 > 0 ? T / 2 : 1;
     Deal d = {};
     d.T = T;
     d.rows = cfg->rows_per_gate ? cfg->rows_per_gate : T;
@@ -296,12 +307,12 @@ Deal deal_rows(const deto_norm_residual* cfg, int64_t T) {
         return d;
     }
     d.gates = (T + d.rows - 1) / d.rows;
-    if (d.gates > kTeams) {
-        d.group = (d.gates + kTeams - 1) / kTeams;
+    if (d.gates > most) {
+        d.group = (d.gates + most - 1) / most;
         d.teams = (d.gates + d.group - 1) / d.group;
         return d;
     }
-    d.cuts = kTeams / d.gates;
+    d.cuts = most / d.gates;
     if (d.cuts > d.rows) d.cuts = d.rows;
     d.run = (d.rows + d.cuts - 1) / d.cuts;
     d.cuts = (d.rows + d.run - 1) / d.run;
@@ -319,7 +330,7 @@ extern "C" {
 
 int64_t detonation_norm_residual_workspace(const deto_norm_residual* cfg, int64_t T, int64_t D) {
     if (check_norm(cfg, T, D)) return -1;
-    return deal_rows(cfg, T).teams * kSums * D * static_cast<int64_t>(sizeof(float));
+    return deal_rows(cfg, T, D, true).teams * kSums * D * static_cast<int64_t>(sizeof(float));
 }
 
 int detonation_norm_residual_backward(const deto_norm_residual* cfg, int64_t T, int64_t D,
@@ -356,7 +367,9 @@ int detonation_norm_residual_backward(const deto_norm_residual* cfg, int64_t T, 
     }
     a.cfg = *cfg;
     a.D = static_cast<int>(D);
-    a.deal = deal_rows(cfg, T);
+    const bool layer = cfg->pre == DETO_NORM_LAYER || cfg->post == DETO_NORM_LAYER || cfg->b_post || g.b_pre ||
+                       g.b_post;
+    a.deal = deal_rows(cfg, T, D, !layer);
     a.grads = g;
     float* const outs[kSums] = {g.w_pre, g.b_pre, g.w_post, g.b_post, g.gate};
     JoinArgs j = {};
@@ -384,8 +397,6 @@ int detonation_norm_residual_backward(const deto_norm_residual* cfg, int64_t T, 
         a.df = branch ? *df : none;
         a.dy = pre ? *dy : none;
         a.dxo = here(dx_out) ? *dx_out : none;
-        const bool layer = cfg->pre == DETO_NORM_LAYER || cfg->post == DETO_NORM_LAYER || cfg->b_post || g.b_pre ||
-                           g.b_post;
         by_width(D, [&](auto w, auto c, auto whole) {
             using TM = Team<w.value, c.value, whole.value>;
             const unsigned grid = static_cast<unsigned>((a.deal.teams + TM::kTeamsWg - 1) / TM::kTeamsWg);

@@ -84,7 +84,8 @@ struct UnitB { u32x2 codes[4]; uint32_t exps[4]; };
 // ---- Loads of a step.  NEAR: through buffer resources that end where the matrix does: rows past its end read as
 // zeros without a comparison, a lane needs one 32-bit offset, and columns past a row's end read whatever comes
 // next (they add to columns of dw that are not written).  Otherwise (rows far apart, or not at multiples of four
-// bytes) element by element where a row ends.
+// bytes) rows past the end are the last row and columns past the end the last eight, put right when they are used:
+// the loads themselves are without a branch, which would make each wait for the one before.
 typedef __amdgpu_buffer_rsrc_t Rsrc;
 
 // (The words that hold the last bytes count whole: a buffer gives no part of a word.  They are aligned.)
@@ -126,11 +127,31 @@ struct Loader {
 #pragma unroll
             for (int i = 0; i < TL::kUnitsA; ++i) {
                 const int u = threadIdx.x + i * TL::kThreads;
-                const int64_t n = n0 + u % (TL::BM / 8) * 8, left = a.N - n, row = t + u / (TL::BM / 8) * 4;
-                const int count = left >= 8 ? 8 : left > 0 ? static_cast<int>(left) : 0;
+                const int64_t n = n0 + u % (TL::BM / 8) * 8, row = t + u / (TL::BM / 8) * 4;
 #pragma unroll
-                for (int r = 0; r < 4; ++r)
-                    ua[i].row[r] = load8<DT>(a.dy.data, (row + r) * a.dy.ld, n, row + r < end ? count : 0);
+                for (int r = 0; r < 4; ++r) {
+                    const int64_t at = row + r < end ? row + r : end - 1;
+                    if (a.N >= 8)
+                        ua[i].row[r] = load8_whole<DT>(static_cast<const char*>(a.dy.data) +
+                                                       (at * a.dy.ld + (n < a.N - 8 ? n : a.N - 8)) * kSize<DT>);
+                    else ua[i].row[r] = load8<DT>(a.dy.data, at * a.dy.ld, n, n < a.N ? static_cast<int>(a.N - n) : 0);
+                }
+            }
+        }
+    }
+
+    // Makes what a unit of rows t ... holds what was asked for: nothing to do for NEAR.
+    __device__ __forceinline__ void settle_a(int64_t t, UnitA<DT> (&ua)[TL::kUnitsA]) const {
+        if constexpr (!NEAR) {
+#pragma unroll
+            for (int i = 0; i < TL::kUnitsA; ++i) {
+                const int u = threadIdx.x + i * TL::kThreads;
+                const int64_t by = n0 + u % (TL::BM / 8) * 8 - (a.N - 8), row = t + u / (TL::BM / 8) * 4;
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    if (a.N >= 8 && by > 0 && by < 8) move_down<DT>(ua[i].row[r], static_cast<int>(by));
+                    if (row + r >= end) ua[i].row[r] = {};
+                }
             }
         }
     }
@@ -158,13 +179,33 @@ struct Loader {
 #pragma unroll
             for (int i = 0; i < TL::kUnitsB; ++i) {
                 const int u = threadIdx.x + i * TL::kThreads;
-                const int64_t k = k0 + u % (TL::BN / 8) * 8, left = a.K - k, row = t + u / (TL::BN / 8) * 4;
-                const int count = left >= 8 ? 8 : left > 0 ? static_cast<int>(left) : 0;
+                const int64_t k = k0 + u % (TL::BN / 8) * 8, row = t + u / (TL::BN / 8) * 4;
+                const int64_t last = (a.K - 1) / DETO_ACT8_GROUP, group = k / DETO_ACT8_GROUP;
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
-                    const bool on = row + r < end && count > 0;
-                    ub[i].codes[r] = load_codes(a.x.codes + (row + r) * a.x.ld_codes, k, on ? count : 0);
-                    ub[i].exps[r] = on ? a.x.exps[(row + r) * a.x.ld_exps + k / DETO_ACT8_GROUP] : 0u;
+                    const int64_t at = row + r < end ? row + r : end - 1;
+                    const int8_t* codes = a.x.codes + at * a.x.ld_codes;
+                    if (a.K >= 8)
+                        ub[i].codes[r] = *reinterpret_cast<const u32x2_any1*>(codes + (k < a.K - 8 ? k : a.K - 8));
+                    else ub[i].codes[r] = load_codes(codes, k, k < a.K ? static_cast<int>(a.K - k) : 0);
+                    ub[i].exps[r] = a.x.exps[at * a.x.ld_exps + (group < last ? group : last)];
+                }
+            }
+        }
+    }
+
+    __device__ __forceinline__ void settle_b(int64_t t, UnitB (&ub)[TL::kUnitsB]) const {
+        if constexpr (!NEAR) {
+#pragma unroll
+            for (int i = 0; i < TL::kUnitsB; ++i) {
+                const int u = threadIdx.x + i * TL::kThreads;
+                const int64_t by = k0 + u % (TL::BN / 8) * 8 - (a.K - 8), row = t + u / (TL::BN / 8) * 4;
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    if (a.K >= 8 && by > 0 && by < 8)
+                        ub[i].codes[r] = __builtin_bit_cast(
+                            u32x2, __builtin_bit_cast(uint64_t, ub[i].codes[r]) >> (8 * by));
+                    if (row + r >= end) ub[i].exps[r] = 0u;
                 }
             }
         }
@@ -228,18 +269,6 @@ __device__ __forceinline__ void store_b(const UnitB& u, const float (&scale)[4],
     }
     put4(lds, column + J, tq, high_halves(f32_bits(v[0]), f32_bits(v[1])),
          high_halves(f32_bits(v[2]), f32_bits(v[3])));
-}
-
-template <int DT>
-__device__ __forceinline__ void write_dw(const deto_rows& dw, int64_t n, int64_t k, float v, int accumulate) {
-    const int64_t at = n * dw.ld + k;
-    if (accumulate) v += load1<DT>(dw.data, at);
-    store1<DT>(dw.data, at, v);
-}
-__device__ __forceinline__ void write_any(const deto_rows& dw, int64_t n, int64_t k, float v, int accumulate) {
-    if (dw.dtype == DETO_F32) write_dw<DETO_F32>(dw, n, k, v, accumulate);
-    else if (dw.dtype == DETO_BF16) write_dw<DETO_BF16>(dw, n, k, v, accumulate);
-    else write_dw<DETO_F16>(dw, n, k, v, accumulate);
 }
 
 // f(Type<0>) ... f(Type<N - 1>)
@@ -337,6 +366,8 @@ __global__ __launch_bounds__(TL::kThreads) void weight_grad_kernel(Args a) {
     if (t0 < end) {
         loader.load_a(t0, ua);
         loader.load_b(t0, ub);
+        loader.settle_a(t0, ua);
+        loader.settle_b(t0, ub);
         scales();
         each_of<4>([&](auto q) { put_a(lds, q); });
         each_of<8>([&](auto j) { put_b(lds, j); });
@@ -354,11 +385,13 @@ __global__ __launch_bounds__(TL::kThreads) void weight_grad_kernel(Args a) {
         char* next = lds + buffer * kBuffer;
         fetch(la, Type<0>{});
         fetch(la, Type<1>{});
+        loader.settle_a(t + kDepth, ua);
         each_of<kBlocks>([&](auto i) {
             multiply(Type<0>{}, i);
             each_of<4 / kBlocks>([&](auto q) { put_a(next, Type<i.value * (4 / kBlocks) + q.value>{}); });
         });
         loader.load_a(t + 2 * kDepth, ua);
+        loader.settle_b(t + kDepth, ub);
         scales();
         fetch(la, Type<2>{});
         each_of<kBlocks>([&](auto i) {
@@ -374,29 +407,76 @@ __global__ __launch_bounds__(TL::kThreads) void weight_grad_kernel(Args a) {
         each_of<kBlocks>([&](auto i) { multiply(Type<3>{}, i); });
         __syncthreads();
     }
-    // lane l holds column l % 32, rows 8 (r / 4) + 4 (l / 32) + r % 4 of a 32 x 32 block
+    // Lane l holds column l % 32, rows 8 (r / 4) + 4 (l / 32) + r % 4 of a 32 x 32 block.
+    const deto_rows partial = {a.parts + split * a.N * a.K, a.K, DETO_F32, 0};
+    const deto_rows& out = a.splits > 1 ? partial : a.dw;
+    const bool add = a.accumulate && a.splits == 1;
+    const int64_t n = n0 + wm + 4 * (lane / 32), k = k0 + wn + lane % 32;
+    const int rows_left = static_cast<int>(a.N - n < TL::WM ? a.N - n : TL::WM);
+    auto write = [&](auto type) {
+        constexpr int OUT = decltype(type)::value;
+        char* const at = static_cast<char*>(out.data) + (n * out.ld + k) * kSize<OUT>;
 #pragma unroll
-    for (int i = 0; i < TL::WM / 32; ++i)
-#pragma unroll
-        for (int j = 0; j < TL::WN / 32; ++j)
+        for (int i = 0; i < TL::WM / 32; ++i)
 #pragma unroll
             for (int r = 0; r < 16; ++r) {
-                const int64_t n = n0 + wm + i * 32 + 8 * (r / 4) + 4 * (lane / 32) + r % 4;
-                const int64_t k = k0 + wn + j * 32 + lane % 32;
-                if (n < a.N && k < a.K) {
-                    if (a.splits > 1) a.parts[(split * a.N + n) * a.K + k] = acc[i][j][r];
-                    else write_any(a.dw, n, k, acc[i][j][r], a.accumulate);
+                const int down = i * 32 + 8 * (r / 4) + r % 4;
+                char* const row = at + down * out.ld * kSize<OUT>;
+                if (down < rows_left) {
+#pragma unroll
+                    for (int j = 0; j < TL::WN / 32; ++j)
+                        if (k + j * 32 < a.K) {
+                            float v = acc[i][j][r];
+                            if (add) v += load1<OUT>(row, j * 32);
+                            store1<OUT>(row, j * 32, v);
+                        }
                 }
             }
+    };
+    if (out.dtype == DETO_F32) write(Type<DETO_F32>{});
+    else if (out.dtype == DETO_BF16) write(Type<DETO_BF16>{});
+    else write(Type<DETO_F16>{});
 }
 
-__global__ __launch_bounds__(256) void weight_grad_join_kernel(Args a) {
-    const int64_t all = a.N * a.K;
-    const int64_t at = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
-    if (at >= all) return;
-    float s = 0.f;
-    for (int i = 0; i < a.splits; ++i) s += a.parts[i * all + at];
-    write_any(a.dw, at / a.K, at % a.K, s, a.accumulate);
+// Adds the splits' sums: a wavefront takes 256 columns of a row, a lane four, the loads of eight splits side by side.
+constexpr int kJoinRows = 4;         // rows of a workgroup
+
+template <int OUT>
+__global__ __launch_bounds__(kJoinRows* kLanes) void weight_grad_join_kernel(Args a) {
+    const int64_t k = (static_cast<int64_t>(blockIdx.x) * kLanes + threadIdx.x % kLanes) * 4;
+    const int count = a.K - k >= 4 ? 4 : a.K - k > 0 ? static_cast<int>(a.K - k) : 0;
+    if (count == 0) return;
+    for (int64_t n = static_cast<int64_t>(blockIdx.y) * kJoinRows + threadIdx.x / kLanes; n < a.N;
+         n += static_cast<int64_t>(gridDim.y) * kJoinRows) {
+        float s[4] = {0.f, 0.f, 0.f, 0.f};
+        const int64_t step = a.N * a.K;
+        const float* at = a.parts + n * a.K + k;
+        if (count == 4) {
+            typedef float f32x4_any4 __attribute__((ext_vector_type(4), aligned(4)));
+            for (int i = 0; i < a.splits; i += 8) {
+                f32x4_any4 v[8];
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
+                    if (i + j < a.splits) v[j] = *reinterpret_cast<const f32x4_any4*>(at + (i + j) * step);
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
+                    if (i + j < a.splits)
+#pragma unroll
+                        for (int c = 0; c < 4; ++c) s[c] += v[j][c];
+            }
+        } else {
+            for (int i = 0; i < a.splits; ++i)
+#pragma unroll
+                for (int c = 0; c < 3; ++c)
+                    if (c < count) s[c] += at[i * step + c];
+        }
+#pragma unroll
+        for (int c = 0; c < 4; ++c)
+            if (c < count) {
+                if (a.accumulate) s[c] += load1<OUT>(a.dw.data, n * a.dw.ld + k + c);
+                store1<OUT>(a.dw.data, n * a.dw.ld + k + c, s[c]);
+            }
+    }
 }
 
 bool bad_shape(int64_t T, int64_t N, int64_t K) {
@@ -407,23 +487,29 @@ bool bad_shape(int64_t T, int64_t N, int64_t K) {
 struct Plan {
     bool large;
     int64_t tiles, tiles_k, splits, span;
+    double us;
 };
 
-Plan plan_with(int64_t T, int64_t N, int64_t K, bool large) {
+// The splits of T that take least time by what was measured (us): a step of 64 rows 0.8 in a workgroup of small tiles
+// that has a CU to itself and 1.25 in one of two (fp32 and fp16 dy, whose terms leave room for one: 1.1), 1.95 in one
+// of large tiles; 5 to start and to write the tile; 3 for the second launch, which the splits' sums go to and come from
+// at 3.5 TB/s.
+Plan plan_with(int64_t T, int64_t N, int64_t K, bool large, bool one_term) {
     const int64_t b = large ? Large::BM : Small::BM;
-    Plan p = {};
-    p.large = large;
-    p.tiles_k = (K + b - 1) / b;
-    p.tiles = (N + b - 1) / b * p.tiles_k;
+    Plan best = {};
+    const int64_t tiles_k = (K + b - 1) / b, tiles = (N + b - 1) / b * tiles_k;
     const int64_t steps = T ? (T + kDepth - 1) / kDepth : 1;
-    const int64_t slots = large ? 256 : 512;      // workgroups that run side by side
-    int64_t splits = slots / p.tiles;
-    if (splits > steps / 4) splits = steps / 4;   // four steps at least
-    if (splits > 32) splits = 32;
-    if (splits < 1) splits = 1;
-    p.span = (steps + splits - 1) / splits * kDepth;
-    p.splits = T ? (T + p.span - 1) / p.span : 1;
-    return p;
+    for (int64_t splits = 1; splits <= 32 && splits <= steps; ++splits) {
+        const int64_t each = (steps + splits - 1) / splits;
+        if (splits > 1 && each * (splits - 1) >= steps) continue;      // an empty split
+        const int64_t slots = large || !one_term ? 256 : 512;
+        const double step = large ? 1.95 : !one_term ? 1.1 : tiles * splits > 256 ? 1.25 : 0.8;
+        double us = static_cast<double>((tiles * splits + slots - 1) / slots) * (step * static_cast<double>(each) + 5.0);
+        if (splits > 1)
+            us += 3.0 + 8.0 * static_cast<double>(splits) * static_cast<double>(N) * static_cast<double>(K) / 3.5e6;
+        if (splits == 1 || us < best.us) best = {large, tiles, tiles_k, splits, each * kDepth, us};
+    }
+    return best;
 }
 
 // Whether a step's rows lie within 2^31 bytes and at multiples of four: the loader's buffers.
@@ -433,10 +519,12 @@ bool reaches(const Args& a) {
            a.x.ld_codes % 4 == 0 && is_aligned(a.dy.data, 4) && is_aligned(a.x.codes, 4);
 }
 
-// Large tiles where they fill the chip by themselves, and dy is one term.
-Plan plan_of(int64_t T, int64_t N, int64_t K, bool may_be_large) {
-    const Plan p = plan_with(T, N, K, true);
-    return may_be_large && p.tiles >= 192 ? p : plan_with(T, N, K, false);
+// One term (bf16 dy) through buffers may take large tiles.
+Plan plan_of(int64_t T, int64_t N, int64_t K, bool near, bool one_term) {
+    const Plan small = plan_with(T, N, K, false, one_term);
+    if (!near || !one_term) return small;
+    const Plan large = plan_with(T, N, K, true, true);
+    return large.us < small.us ? large : small;
 }
 
 }  // namespace
@@ -450,10 +538,11 @@ extern "C" {
 int64_t detonation_act8_weight_grad_workspace(int64_t T, int64_t N, int64_t K) {
     if (bad_shape(T, N, K)) return -1;
     int64_t most = 0;
-    for (bool large : {true, false}) {
-        const Plan p = plan_of(T, N, K, large);
-        if (p.splits > 1 && p.splits > most) most = p.splits;
-    }
+    for (bool near : {true, false})
+        for (bool one_term : {true, false}) {
+            const Plan p = plan_of(T, N, K, near, one_term);
+            if (p.splits > 1 && p.splits > most) most = p.splits;
+        }
     return most * N * K * static_cast<int64_t>(sizeof(float));
 }
 
@@ -476,12 +565,10 @@ int detonation_act8_weight_grad(int64_t T, int64_t N, int64_t K, const deto_rows
         a.x.ld_exps = (K + DETO_ACT8_GROUP - 1) / DETO_ACT8_GROUP;
     }
     const bool near = T > 0 && reaches(a);
-    const Plan p = plan_of(T, N, K, near && dtype == DETO_BF16);
+    const Plan p = plan_of(T, N, K, near, dtype == DETO_BF16);
     if (p.splits > 1 && !workspace) return DETO_ERR_NULL;
     if (p.splits > 1 && !is_aligned(workspace, 16)) return DETO_ERR_ALIGN;
-    const int64_t blocks = (N * K + 255) / 256;
-    if (p.tiles * p.splits > 0x7FFFFFFF || (p.splits > 1 && blocks > 0x7FFFFFFF))
-        return DETO_ERR_UNSUPPORTED;
+    if (p.tiles > 0x7FFFFFFF / p.splits) return DETO_ERR_UNSUPPORTED;
     a.tiles_k = static_cast<int>(p.tiles_k);
     a.splits = static_cast<int>(p.splits);
     a.span = p.span;
@@ -497,8 +584,15 @@ int detonation_act8_weight_grad(int64_t T, int64_t N, int64_t K, const deto_rows
             else weight_grad_kernel<dt.value, Small, false><<<grid, Small::kThreads, kLds, st>>>(a);
             return 0;
         });
-    if (p.splits > 1)
-        weight_grad_join_kernel<<<static_cast<unsigned>(blocks), 256, 0, st>>>(a);
+    if (p.splits > 1) {
+        const int64_t rows = (N + kJoinRows - 1) / kJoinRows;
+        const dim3 join(static_cast<unsigned>((K + 4 * kLanes - 1) / (4 * kLanes)),
+                        static_cast<unsigned>(rows < 65535 ? rows : 65535));
+        by_type(dw->dtype, [&](auto dt) {
+            weight_grad_join_kernel<dt.value><<<join, kJoinRows * kLanes, 0, st>>>(a);
+            return 0;
+        });
+    }
     return enqueued();
 }
 
