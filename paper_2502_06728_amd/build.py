@@ -15,6 +15,7 @@ OBJ = os.path.join(_HERE, "_build")
 LIB = os.path.join(_HERE, "libdetonation.so")
 # (the interpreter's own suffix: binding.MARSHAL_PATH)
 MARSHAL = os.path.join(_HERE, "_marshal" + (sysconfig.get_config_var("EXT_SUFFIX") or ".so"))
+MODEL_MARSHAL = os.path.join(_HERE, "_model_marshal" + (sysconfig.get_config_var("EXT_SUFFIX") or ".so"))
 MEMBENCH = os.path.join(_HERE, "membench")
 
 HIPCC_FLAGS = [
@@ -62,16 +63,18 @@ MODEL_UNITS = ["norm_backward.hip", "norm.hip", "act8.hip", "weight_grad.hip", "
 
 
 def _build_marshal(verbose: bool) -> None:
-    """The binding's argument marshalling (host code, CPython's C API).  Without a C compiler or
-    Python.h the binding does all of it in Python, so that is no error."""
-    if os.path.exists(MARSHAL):
-        os.remove(MARSHAL)
-    try:
-        _run([*shlex.split(os.environ.get("CC", "cc")), "-O2", "-Wall", "-shared", "-fPIC",
-              "-I" + sysconfig.get_paths()["include"], "-o", MARSHAL,
-              os.path.join(CSRC, "marshal.c")], verbose)
-    except (OSError, RuntimeError) as e:
-        print(f"marshal.c is not compiled, the binding goes without it: {e}", file=sys.stderr)
+    """The bindings' argument marshalling (host code, CPython's C API).  Without a C compiler or
+    Python.h the bindings do all of it in Python, so that is no error."""
+    for out, src in ((MARSHAL, os.path.join(CSRC, "marshal.c")),
+                     (MODEL_MARSHAL, os.path.join(CSRC_MODEL, "marshal.c"))):
+        if os.path.exists(out):
+            os.remove(out)
+        try:
+            _run([*shlex.split(os.environ.get("CC", "cc")), "-O2", "-Wall", "-shared", "-fPIC",
+                  "-I" + sysconfig.get_paths()["include"], "-o", out, src], verbose)
+        except (OSError, RuntimeError) as e:
+            print(f"{os.path.relpath(src, _HERE)} is not compiled, the binding goes without it: {e}",
+                  file=sys.stderr)
 
 
 def _run(cmd: list[str], verbose: bool) -> None:

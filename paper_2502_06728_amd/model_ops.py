@@ -4,21 +4,28 @@ library products, next to the optimizer step of binding.py (same library).
 Argument checks and marshalling only: device tensors in, raw pointers out; every tensor is given by the
 caller, outputs too, and is written by the kernels on `stream` (the current stream if it is None).
 Matrices are 2-D tensors whose rows may lie any distance apart; their elements are consecutive.  There
-is no CPU fallback.
+is no CPU fallback.  Calls hand their arguments to csrc_model/marshal.c first, which checks and converts
+what a program usually passes; what it does not take goes through the checks below, which name what is
+wrong, and so does every call where it cannot be used.
 """
 from __future__ import annotations
 
 import ctypes
+import os
+import sysconfig
 from dataclasses import dataclass
 
 from . import binding
-from .binding import BF16, F16, F32, DetonationError
+from .binding import BF16, F16, F32, DetonationError, _handle
 
 NORM_NONE, NORM_RMS, NORM_LAYER = 0, 1, 2
 ACT_SILU, ACT_GELU, ACT_GELU_TANH, ACT_RELU = 0, 1, 2, 3
 ACT8_GROUP = 32
 MAX_TOP = 32
 MAX_NORM_WIDTH = 16384
+
+MARSHAL_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)),
+                            "_model_marshal" + (sysconfig.get_config_var("EXT_SUFFIX") or ".so"))
 
 EXPORTS = ("detonation_token_logprobs", "detonation_token_logprobs_backward",
            "detonation_token_logprobs_workspace", "detonation_norm_residual",
@@ -108,6 +115,64 @@ def _load():
         _codes = {torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16}
         _lib = lib
     return _lib
+
+
+class _NoMarshal:
+    """Leaves every call to the checks of this module."""
+
+    @staticmethod
+    def logprobs(*args) -> int:
+        return -1
+
+    logprobs_backward = norm = norm_backward = encode = decode = logprobs
+    glu_forward = glu_backward = weight_grad = logprobs
+
+
+_marshal = None        # csrc_model/marshal.c, or _NoMarshal; set by the first call
+
+
+def _marshalling():
+    global _marshal
+    lib = _load()
+    if _marshal is None:
+        try:
+            _marshal = _load_marshal(lib)
+        except (ImportError, OSError, AttributeError):
+            _marshal = _NoMarshal
+    return _marshal
+
+
+# in the order of csrc_model/marshal.c
+_MARSHALLED = ("token_logprobs", "token_logprobs_backward", "token_logprobs_workspace", "norm_residual",
+               "norm_residual_backward", "norm_residual_workspace", "act8_encode", "act8_decode",
+               "glu_forward", "glu_backward", "act8_weight_grad", "act8_weight_grad_workspace")
+
+
+def _marshal_types():
+    import torch
+    return (torch.float32, torch.bfloat16, torch.float16, torch.int32, torch.int64, torch.int8, torch.uint8)
+
+
+def _load_marshal(lib):
+    import importlib.machinery
+    import importlib.util
+
+    import torch
+    loader = importlib.machinery.ExtensionFileLoader("_model_marshal", MARSHAL_PATH)
+    spec = importlib.util.spec_from_file_location("_model_marshal", MARSHAL_PATH, loader=loader)
+    m = importlib.util.module_from_spec(spec)
+    loader.exec_module(m)
+    m.setup(tuple(ctypes.cast(getattr(lib, "detonation_" + n), ctypes.c_void_p).value for n in _MARSHALLED),
+            _marshal_types(), torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream,
+            torch.cuda.device_count())
+    return m
+
+
+def _taken(rc: int) -> bool:
+    """Whether the marshalled call ran; it raises for one that the HIP runtime refused."""
+    if rc > 0:
+        raise DetonationError(rc)
+    return rc == 0
 
 
 def _status(rc: int) -> None:
@@ -243,6 +308,9 @@ def detonation_token_logprobs(logits, targets, logp, *, lse=None, entropy=None, 
     """Per row of logits [T, V]: the log probability of targets[t] (int32 or int64; 0 where that is
     outside [0, V)), and where tensors are given for them log sum exp, the entropy, the best tokens
     (top_idx int32 and top_logp float32, both [T, K]), and the [T, 2] `stats` of the backward pass."""
+    if _taken((_marshal or _marshalling()).logprobs(logits, targets, logp, lse, entropy, top_idx, top_logp,
+                                                    stats, logit_scale, workspace, _handle(stream))):
+        return
     import torch
     lib, c = _load(), _Call()
     T, V = logits.shape
@@ -271,6 +339,9 @@ def detonation_token_logprobs_backward(logits, targets, stats, dlogits, *, g_log
                                        stream=None) -> None:
     """dlogits [T, V] (may be the logits themselves): the gradient of sum(g_logp * logp) +
     sum(g_entropy * entropy); stats and entropy as detonation_token_logprobs wrote them."""
+    if _taken((_marshal or _marshalling()).logprobs_backward(logits, targets, stats, dlogits, g_logp, entropy,
+                                                             g_entropy, logit_scale, _handle(stream))):
+        return
     import torch
     lib, c = _load(), _Call()
     T, V = logits.shape
@@ -331,6 +402,9 @@ def detonation_norm_residual(cfg: NormResidual, x, f, x_out, y, *, y8: Act8 | No
     """x_out = x + scale * gate (.) post(f), y = pre(x_out), y8 = y in 8 bits; x_out may be x.  f and
     x_out are None for a norm alone, y (and y8) under cfg.pre = NORM_NONE.  gate: [D], or a row for
     every cfg.rows_per_gate rows.  Weights, biases and gate are of one type."""
+    if _taken((_marshal or _marshalling()).norm(cfg, x, f, x_out, y, y8, gate, w_post, b_post, w_pre, b_pre,
+                                                _handle(stream))):
+        return
     lib, c = _load(), _Call()
     T, D = x.shape
     s = _norm_struct(c, cfg, T, D, gate, w_post, b_post, w_pre, b_pre)
@@ -350,6 +424,10 @@ def detonation_norm_residual_backward(cfg: NormResidual, x_out, f, dy, dx_out, d
     """Gradients of detonation_norm_residual, given those of y (dy; None under NORM_NONE) and of x_out
     (dx_out; None: zeros): dx (may be dx_out), df, and the sums over rows that float32 tensors are
     given for."""
+    if _taken((_marshal or _marshalling()).norm_backward(
+            cfg, x_out, f, dy, dx_out, dx, df, workspace, gate, w_post, b_post, w_pre, dgate, dw_post,
+            db_post, dw_pre, db_pre, _handle(stream))):
+        return
     import torch
     lib, c = _load(), _Call()
     T, D = x_out.shape
@@ -378,6 +456,8 @@ def detonation_norm_residual_backward(cfg: NormResidual, x_out, f, dy, dx_out, d
 
 def detonation_act8_encode(x, x8: Act8, stream=None) -> None:
     """x [T, D] into 8 bits."""
+    if _taken((_marshal or _marshalling()).encode(x, x8, _handle(stream))):
+        return
     lib, c = _load(), _Call()
     T, D = x.shape
     xs, q = c.rows(x, "x", T, D), c.act8(x8, "x8", T, D)
@@ -386,6 +466,8 @@ def detonation_act8_encode(x, x8: Act8, stream=None) -> None:
 
 def detonation_act8_decode(x8: Act8, x, stream=None) -> None:
     """The values of x8, rounded to x's type."""
+    if _taken((_marshal or _marshalling()).decode(x8, x, _handle(stream))):
+        return
     lib, c = _load(), _Call()
     T, D = x.shape
     xs, q = c.rows(x, "x", T, D), c.act8(x8, "x8", T, D)
@@ -396,6 +478,8 @@ def detonation_glu_forward(act: int, a, b, h, *, a8: Act8 | None = None, b8: Act
                            stream=None) -> None:
     """h = act(a) (.) b (b None: act(a)), with a and b left in 8 bits for the backward pass; h may be a
     or b."""
+    if _taken((_marshal or _marshalling()).glu_forward(act, a, b, h, a8, b8, _handle(stream))):
+        return
     lib, c = _load(), _Call()
     T, D = a.shape
     sa, sb = c.rows(a, "a", T, D), c.rows(b, "b", T, D, a.dtype)
@@ -410,6 +494,8 @@ def detonation_glu_backward(act: int, dh, a8: Act8, b8: Act8 | None, da, db=None
                             h8: Act8 | None = None, stream=None) -> None:
     """da and db (None without b8) from dh and the saved a and b; h8 receives act(a) (.) b of the saved
     values.  da or db may be dh."""
+    if _taken((_marshal or _marshalling()).glu_backward(act, dh, a8, b8, da, db, h8, _handle(stream))):
+        return
     lib, c = _load(), _Call()
     T, D = dh.shape
     sd, sa = c.rows(dh, "dh", T, D), c.rows(da, "da", T, D, dh.dtype)
@@ -430,6 +516,8 @@ def act8_weight_grad_workspace(T: int, N: int, K: int) -> int:
 def detonation_act8_weight_grad(dy, x8: Act8, dw, *, accumulate: bool = False, workspace=None,
                                 stream=None) -> None:
     """dw [N, K] = [dw +] dy^T x with dy [T, N] and x [T, K] in 8 bits."""
+    if _taken((_marshal or _marshalling()).weight_grad(dy, x8, dw, accumulate, workspace, _handle(stream))):
+        return
     lib, c = _load(), _Call()
     T, N = dy.shape
     K = dw.shape[1]
