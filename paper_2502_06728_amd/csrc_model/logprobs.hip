@@ -1,9 +1,13 @@
 // Log probabilities of given tokens: log sum exp, entropy and the best tokens of every row of the logits, and
 // the gradient of the logits.
 //
-// Forward.  A workgroup takes a piece of a row: one pass with the running maximum m, s = sum exp(z - m) and
+// Forward.  A workgroup takes a piece of a row in one pass with the running maximum m, s = sum exp(z - m) and
 // w = sum (z - m) exp(z - m), in fp32 and in units of log 2:
 //     lse = m + log s        entropy = log s - w / s
+// A lane's 32 values raise the maximum once, and their exponents are one fused multiply-add each, d = z / log 2 - c
+// with c the product of the maximum as rounded: sums relative to c are exact in that respect, and are brought to
+// the maximum itself at the end.  (Where the product leaves fp32's range, at a type's lowest value say, the lane
+// takes its values once more and subtracts first.)
 // Rows are cut into pieces where there are too few of them to fill the chip (a sampled token is one row); a
 // second launch joins a row's pieces.  The best tokens: the K-th largest of the threads' maxima is a value
 // that at least K elements reach, and seldom many more do; a second look at the piece lists those, and the
@@ -22,11 +26,12 @@ constexpr int kWaves = kThreads / kLanes;
 constexpr int kMaxTop = 32;
 constexpr int kList = 1024;                    // listed candidates of a piece
 constexpr int kMaxPieces = kList / kMaxTop;    // the join ranks kMaxTop of every piece in one list
+static_assert(kMaxPieces <= kLanes, "a lane for each piece");
 constexpr int64_t kPieceElems = kThreads * 8;  // least length of a piece: eight elements a lane
 constexpr int64_t kFillWorkgroups = 1024;      // workgroups that fill the chip
 
-// What a piece, or a part of one, has seen: m over the raw logits; s, w scaled (w in units of log 2).  m is
-// -infinity before the first value above that.
+// What a piece, or a part of one, has seen: m over the raw logits, a NaN if one was; s, w scaled (w in units of
+// log 2).  m is -infinity before the first value above that.
 struct Seen {
     float m, s, w;
 };
@@ -58,18 +63,39 @@ struct Forward {
 
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
 
-// a and b as one.  (m = -infinity stands for nothing above it: no difference is taken from it.)
-__device__ __forceinline__ Seen join(const Seen& a, const Seen& b, float unit) {
-    const float m = fmaxf(a.m, b.m);
+// the larger, a NaN if either is one
+__device__ __forceinline__ float larger(float a, float b) { return __builtin_elementwise_maximum(a, b); }
+
+__device__ __forceinline__ float wave_larger(float v) {
+    v = larger(v, moved<0xB1>(v));
+    v = larger(v, moved<0x4E>(v));
+    v = larger(v, moved<0x141>(v));
+    v = larger(v, moved<0x140>(v));
+    return larger(larger(lane_value(v, 0), lane_value(v, 16)), larger(lane_value(v, 32), lane_value(v, 48)));
+}
+
+// d 2^d is 0 where 2^d is
+constexpr float kFarBelow = -16384.f;
+// products of the maximum that sums may be relative to
+constexpr float kInRange = 1e30f;
+
+// The same relative to m, which is not below r.m.  (m = -infinity stands for nothing above it: no difference is
+// taken from it.)
+__device__ __forceinline__ Seen relative_to(const Seen& r, float m, float unit) {
     const float ref = m == -__builtin_inff() ? 0.f : m;
-    const float da = fmaxf((a.m - ref) * unit, -16384.f), db = fmaxf((b.m - ref) * unit, -16384.f);
-    const float ea = exp2_fast(da), eb = exp2_fast(db);
-    return {m, a.s * ea + b.s * eb, (a.w + a.s * da) * ea + (b.w + b.s * db) * eb};
+    const float d = fmaxf((r.m - ref) * unit, kFarBelow), e = exp2_fast(d);
+    return {m, r.s * e, (r.w + r.s * d) * e};
+}
+
+// All lanes of a wavefront as one, in every lane.
+__device__ __forceinline__ Seen join_wave(Seen r, float unit) {
+    r = relative_to(r, wave_larger(r.m), unit);
+    return {r.m, wave_sum(r.s), wave_sum(r.w)};
 }
 
 // An order of all values, NaNs above everything, -0 and +0 the same: larger means earlier.  0 is no value, and
 // no candidate is all ones.
-constexpr uint32_t kNanKey = 0xFFFFFFFEu;
+constexpr uint32_t kNanKey = 0xFFFFFFFEu, kLowestKey = 0x007FFFFFu;      // of a NaN, of -infinity
 __device__ __forceinline__ uint32_t order_key(float v) {
     const uint32_t b = f32_bits(v + 0.f);      // (-0 + 0 = +0)
     if (v != v) return kNanKey;
@@ -88,19 +114,26 @@ __device__ __forceinline__ int64_t target_of(const void* targets, int bytes, int
     return bytes == 8 ? static_cast<const int64_t*>(targets)[t] : static_cast<const int32_t*>(targets)[t];
 }
 
+// A row's target and its logit (loaded early: two loads, one after the other)
+struct Target {
+    int64_t y;
+    float z;
+    bool scored;
+};
 template <int DT>
-__device__ __forceinline__ void write_row(const Forward& a, int64_t t, const Seen& r) {
-    const float log_s = logf(r.s);
-    const bool none = r.m == -__builtin_inff() && r.s == 0.f;       // -infinities throughout
-    const float top = r.m * a.scale;
+__device__ __forceinline__ Target load_target(const Forward& a, int64_t t) {
     const int64_t y = target_of(a.targets, a.target_bytes, t);
+    const bool scored = y >= 0 && y < a.V;
+    return {y, scored ? load1<DT>(a.logits, t * a.ld + y) : 0.f, scored};
+}
+
+__device__ __forceinline__ void write_row(const Forward& a, int64_t t, const Seen& r, const Target& y) {
+    const float log_s = logf(r.s);
+    const bool none = r.m == -__builtin_inff();       // -infinities throughout
     float logp = 0.f;
-    if (y >= 0 && y < a.V) {
-        const float z = load1<DT>(a.logits, t * a.ld + y);
-        logp = none ? -__builtin_inff() : (z - r.m) * a.scale - log_s;
-    }
+    if (y.scored) logp = none ? -__builtin_inff() : (y.z - r.m) * a.scale - log_s;
     a.logp[t] = logp;
-    if (a.lse) a.lse[t] = none ? -__builtin_inff() : top + log_s;
+    if (a.lse) a.lse[t] = none ? -__builtin_inff() : r.m * a.scale + log_s;
     if (a.entropy) a.entropy[t] = none ? 0.f : log_s - 0.69314718055994531f * (r.w / r.s);
     if (a.stats) {
         a.stats[2 * t] = r.m;
@@ -117,35 +150,112 @@ __device__ __forceinline__ void write_best(const Forward& a, int64_t t, int rank
         v == -__builtin_inff() && log_s == log_s ? v : (v - m) * a.scale - log_s;
 }
 
-// (a NaN row's s is NaN: a NaN, or +infinity - +infinity)
+// Vectors of eight that a lane takes at a time: 64 bytes.
+template <int DT> constexpr int kVectors = DT == DETO_F32 ? 2 : 4;
+
+template <int DT>
+struct Taken {
+    float v[kVectors<DT>][8];        // -infinity past the end
+};
+
+template <int DT>
+struct Piece {
+    const void* logits;
+    int64_t row, first, end;
+    __device__ __forceinline__ int64_t at(int64_t d, int i) const { return d + i * kThreads * 8; }
+    __device__ __forceinline__ int count(int64_t d, int i) const {
+        const int64_t left = end - at(d, i);
+        return left >= 8 ? 8 : left > 0 ? static_cast<int>(left) : 0;
+    }
+    __device__ __forceinline__ void load(int64_t d, Raw8<DT> (&raw)[kVectors<DT>]) const {
+#pragma unroll
+        for (int i = 0; i < kVectors<DT>; ++i) raw[i] = load8<DT>(logits, row, at(d, i), count(d, i));
+    }
+    __device__ __forceinline__ void unpack(int64_t d, const Raw8<DT> (&raw)[kVectors<DT>], Taken<DT>& x) const {
+#pragma unroll
+        for (int i = 0; i < kVectors<DT>; ++i) {
+            unpack8<DT>(raw[i], x.v[i]);
+            const int n = count(d, i);
+            if (n < 8) {
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
+                    if (j >= n) x.v[i][j] = -__builtin_inff();
+            }
+        }
+    }
+};
+
+// r.s and r.w are relative to the product of r.m and unit as rounded.
 template <int DT, bool ENTROPY>
-__device__ __forceinline__ void see8(Seen& r, const float (&v)[8], float unit) {
+__device__ __forceinline__ void see(Seen& r, const Taken<DT>& x, float unit) {
     float m = r.m;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) m = fmaxf(m, v[j]);
-    const float ref = m == -__builtin_inff() ? 0.f : m;
-    const float d0 = fmaxf((r.m - ref) * unit, -16384.f), e0 = exp2_fast(d0);
+    for (int i = 0; i < kVectors<DT>; ++i)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) m = larger(m, x.v[i][j]);
+    const float c = fabsf(m * unit) <= kInRange ? m * unit : 0.f;     // (else the lane starts again at the end)
+    const float d0 = fmaxf(r.m * unit - c, kFarBelow), e0 = exp2_fast(d0);
     float s = r.s * e0, w = (r.w + r.s * d0) * e0;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-        const float d = (v[j] - ref) * unit, e = exp2_fast(d);
-        s += e;
-        if constexpr (ENTROPY) w += fmaxf(d, -16384.f) * e;
-    }
+    for (int i = 0; i < kVectors<DT>; ++i)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            float d = __builtin_fmaf(x.v[i][j], unit, -c);
+            if constexpr (ENTROPY) d = fmaxf(d, kFarBelow);
+            const float e = exp2_fast(d);
+            s += e;
+            if constexpr (ENTROPY) w = __builtin_fmaf(d, e, w);
+        }
     r = {m, s, w};
 }
 
-// The same over all threads of the workgroup, in every thread.
+// The whole workgroup's, in every thread.
 __device__ __forceinline__ Seen join_workgroup(Seen r, float unit, Seen* lds) {
-#pragma unroll
-    for (int step = 1; step < kLanes; step <<= 1)
-        r = join(r, {__shfl_xor(r.m, step), __shfl_xor(r.s, step), __shfl_xor(r.w, step)}, unit);
+    r = join_wave(r, unit);
     if (threadIdx.x % kLanes == 0) lds[threadIdx.x / kLanes] = r;
     __syncthreads();
-    r = lds[0];
+    float m = lds[0].m;
 #pragma unroll
-    for (int i = 1; i < kWaves; ++i) r = join(r, lds[i], unit);
-    return r;
+    for (int i = 1; i < kWaves; ++i) m = larger(m, lds[i].m);
+    Seen all = {m, 0.f, 0.f};
+#pragma unroll
+    for (int i = 0; i < kWaves; ++i) {
+        const Seen p = relative_to(lds[i], m, unit);
+        all.s += p.s;
+        all.w += p.w;
+    }
+    return all;
+}
+
+// The K-th largest of the workgroup's keys, down to its upper 16 bits, by bisection: counts of keys in each wavefront
+// alone, which holds all of them.
+__device__ __forceinline__ uint32_t kth_key(const uint32_t* lds_keys, int K) {
+    uint32_t k[kWaves];
+#pragma unroll
+    for (int i = 0; i < kWaves; ++i) k[i] = lds_keys[i * kLanes + threadIdx.x % kLanes];
+    uint32_t found = 0;
+#pragma unroll
+    for (int bit = 31; bit >= 16; --bit) {
+        const uint32_t t = found | 1u << bit;
+        int n = 0;
+#pragma unroll
+        for (int i = 0; i < kWaves; ++i) n += __popcll(__ballot(k[i] >= t));
+        if (n >= K) found = t;
+    }
+    return found;
+}
+
+// How many of the list's n candidates rank before c.  (The list is filled up with zeros to a multiple of 8.)
+__device__ __forceinline__ int rank_of(const uint64_t* list, int n, uint64_t c) {
+    int rank = 0;
+    for (int j = 0; j < n; j += 8) {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) rank += list[j + k] > c;
+    }
+    return rank;
+}
+__device__ __forceinline__ void fill_up(uint64_t* list, int n) {
+    if (threadIdx.x < 8 && n + static_cast<int>(threadIdx.x) < (n + 7) / 8 * 8) list[n + threadIdx.x] = 0;
 }
 
 template <int DT, bool ENTROPY, bool TOP>
@@ -153,35 +263,52 @@ __global__ __launch_bounds__(kThreads) void logprobs_kernel(Forward a) {
     __shared__ Seen lds_seen[kWaves];
     const int64_t t = blockIdx.x / a.parts.pieces;
     const int piece = blockIdx.x % a.parts.pieces;
-    const int64_t first = piece * a.piece;
-    const int64_t end = first + a.piece < a.V ? first + a.piece : a.V;
-    const int64_t row = t * a.ld;
+    const int64_t begin = piece * a.piece;
+    const Piece<DT> p = {a.logits, t * a.ld, begin, begin + a.piece < a.V ? begin + a.piece : a.V};
+    const bool whole = a.parts.pieces == 1;
+    Target y = {};
+    if (whole) y = load_target<DT>(a, t);
+    constexpr int64_t kStep = kThreads * 8 * kVectors<DT>;
+    const int64_t mine = p.first + 8 * threadIdx.x;
     Seen r = {-__builtin_inff(), 0.f, 0.f};
-    uint32_t key = 0;                       // the thread's largest
-    for (int64_t d = first + 8 * threadIdx.x; d < end; d += kThreads * 8) {
-        const int count = end - d < 8 ? static_cast<int>(end - d) : 8;
-        float v[8];
-        unpack8<DT>(load8<DT>(a.logits, row, d, count), v);
+    Raw8<DT> raw[kVectors<DT>];
+    Taken<DT> x;
+    for (int64_t d = mine; d < p.end; d += kStep) {
+        p.load(d, raw);
+        p.unpack(d, raw, x);
+        see<DT, ENTROPY>(r, x, a.unit);
+    }
+    {
+        // from the rounded product to the maximum itself
+        const float c = r.m * a.unit, off = __builtin_fmaf(r.m, a.unit, -c), e = exp2_fast(-off);
+        if (fabsf(c) <= kInRange) {
+            r = {r.m, r.s * e, (r.w - off * r.s) * e};
+        } else if (r.m == r.m && r.m != -__builtin_inff()) {
+            r.s = r.w = 0.f;
+            for (int64_t d = mine; d < p.end; d += kStep) {
+                p.load(d, raw);
+                p.unpack(d, raw, x);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            if (j >= count) v[j] = -__builtin_inff();
-            else if constexpr (TOP) {
-                const uint32_t k = order_key(v[j]);
-                key = k > key ? k : key;
+                for (int i = 0; i < kVectors<DT>; ++i)
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) {
+                        const float l = (x.v[i][j] - r.m) * a.unit, e1 = exp2_fast(l);
+                        r.s += e1;
+                        r.w += fmaxf(l, kFarBelow) * e1;
+                    }
             }
         }
-        see8<DT, ENTROPY>(r, v, a.unit);
     }
+    const uint32_t key = mine < p.end ? order_key(r.m) : 0u;
     r = join_workgroup(r, a.unit, lds_seen);
-    const bool whole = a.parts.pieces == 1;
     if (threadIdx.x == 0) {
-        if (whole) write_row<DT>(a, t, r);
+        if (whole) write_row(a, t, r, y);
         else a.parts.seen[blockIdx.x] = r;
     }
     if constexpr (TOP) {
         __shared__ uint32_t lds_keys[kThreads];
-        __shared__ uint64_t list[kList];
-        __shared__ uint32_t threshold, listed;
+        __shared__ uint64_t list[kList + 8];
+        __shared__ uint32_t listed;
         const float log_s = logf(r.s);
         uint64_t* part = a.parts.best + static_cast<int64_t>(blockIdx.x) * a.top;
         auto give = [&](int rank, uint64_t c) {
@@ -191,34 +318,39 @@ __global__ __launch_bounds__(kThreads) void logprobs_kernel(Forward a) {
         lds_keys[threadIdx.x] = key;
         if (threadIdx.x == 0) listed = 0;
         __syncthreads();
-        int above = 0;                      // of the threads' keys, before this one's
-        for (int i = 0; i < kThreads; ++i) {
-            const uint32_t k = lds_keys[i];
-            above += k > key || (k == key && i < static_cast<int>(threadIdx.x));
-        }
-        if (above == a.top - 1) threshold = key;
-        __syncthreads();
-        const uint32_t least = threshold ? threshold : 1u;   // 0: fewer than `top` threads saw a value
-        for (int64_t d = first + 8 * threadIdx.x; d < end; d += kThreads * 8) {
-            const int count = end - d < 8 ? static_cast<int>(end - d) : 8;
-            float v[8];
-            unpack8<DT>(load8<DT>(a.logits, row, d, count), v);
+        const uint32_t least = kth_key(lds_keys, a.top);
+        // (0: fewer than `top` threads saw a value, all of them are listed; a NaN is not below anything)
+        const float least_value = least > kLowestKey ? key_value(least) : -__builtin_inff();
+        for (int64_t d = mine; d < p.end; d += kStep) {
+            if (p.end - p.first > kStep) {       // (else the registers still hold the piece)
+                p.load(d, raw);
+                p.unpack(d, raw, x);
+            }
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const uint32_t k = order_key(v[j]);
-                if (j < count && k >= least) {
-                    const uint32_t at = atomicAdd(&listed, 1u);
-                    if (at < kList) list[at] = candidate(k, static_cast<uint32_t>(d + j));
+            for (int i = 0; i < kVectors<DT>; ++i) {
+                float m = x.v[i][0];
+#pragma unroll
+                for (int j = 1; j < 8; ++j) m = larger(m, x.v[i][j]);
+                if (m < least_value) continue;
+                const int n = p.count(d, i);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    if (j < n && !(x.v[i][j] < least_value)) {
+                        const uint32_t at = atomicAdd(&listed, 1u);
+                        if (at < kList)
+                            list[at] = candidate(order_key(x.v[i][j]), static_cast<uint32_t>(p.at(d, i) + j));
+                    }
                 }
             }
         }
         __syncthreads();
         const int n = listed;
         if (n <= kList) {
+            fill_up(list, n);
+            __syncthreads();
             for (int i = threadIdx.x; i < n; i += kThreads) {
                 const uint64_t c = list[i];
-                int rank = 0;
-                for (int j = 0; j < n; ++j) rank += list[j] > c;
+                const int rank = rank_of(list, n, c);
                 if (rank < a.top) give(rank, c);
             }
             // a piece of fewer than `top` elements: the rest of its part is empty
@@ -230,14 +362,17 @@ __global__ __launch_bounds__(kThreads) void logprobs_kernel(Forward a) {
         uint64_t before = ~uint64_t{0};
         for (int rank = 0; rank < a.top; ++rank) {
             uint64_t best = 0;
-            for (int64_t d = first + 8 * threadIdx.x; d < end; d += kThreads * 8) {
-                const int count = end - d < 8 ? static_cast<int>(end - d) : 8;
-                float v[8];
-                unpack8<DT>(load8<DT>(a.logits, row, d, count), v);
+            for (int64_t d = mine; d < p.end; d += kStep) {
+                p.load(d, raw);
+                p.unpack(d, raw, x);
 #pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    const uint64_t c = candidate(order_key(v[j]), static_cast<uint32_t>(d + j));
-                    if (j < count && c < before && c > best) best = c;
+                for (int i = 0; i < kVectors<DT>; ++i) {
+                    const int n_there = p.count(d, i);
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) {
+                        const uint64_t c = candidate(order_key(x.v[i][j]), static_cast<uint32_t>(p.at(d, i) + j));
+                        if (j < n_there && c < before && c > best) best = c;
+                    }
                 }
             }
 #pragma unroll
@@ -256,28 +391,27 @@ __global__ __launch_bounds__(kThreads) void logprobs_kernel(Forward a) {
     }
 }
 
-// A workgroup per row: its pieces as one.
+// A workgroup per row: its pieces as one.  (Every wavefront joins the sums for itself: no barrier for those.)
 template <int DT>
 __global__ __launch_bounds__(kThreads) void logprobs_join_kernel(Forward a) {
-    __shared__ Seen lds_seen[kWaves];
-    __shared__ uint64_t list[kList];
+    __shared__ uint64_t list[kList + 8];
     const int64_t t = blockIdx.x;
-    const int pieces = a.parts.pieces;
+    const int pieces = a.parts.pieces, lane = threadIdx.x % kLanes;
+    const Target y = load_target<DT>(a, t);
     Seen r = {-__builtin_inff(), 0.f, 0.f};
-    for (int i = threadIdx.x; i < pieces; i += kThreads)
-        r = join(r, a.parts.seen[t * pieces + i], a.unit);
-    r = join_workgroup(r, a.unit, lds_seen);
-    if (threadIdx.x == 0) write_row<DT>(a, t, r);
-    if (a.top == 0) return;
+    if (lane < pieces) r = a.parts.seen[t * pieces + lane];
     const int n = pieces * a.top;           // at most kList
     const uint64_t* part = a.parts.best + t * n;
     for (int i = threadIdx.x; i < n; i += kThreads) list[i] = part[i];
+    fill_up(list, n);
+    r = join_wave(r, a.unit);
+    if (threadIdx.x == 0) write_row(a, t, r, y);
+    if (a.top == 0) return;
     __syncthreads();
     const float log_s = logf(r.s);
     for (int i = threadIdx.x; i < n; i += kThreads) {
         const uint64_t c = list[i];
-        int rank = 0;
-        for (int j = 0; j < n; ++j) rank += list[j] > c;
+        const int rank = rank_of(list, n, c);
         if (rank < a.top && c) write_best(a, t, rank, c, r.m, log_s);
     }
 }
