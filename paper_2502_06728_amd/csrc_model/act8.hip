@@ -46,20 +46,20 @@ int check_shape(int64_t T, int64_t D) {
     return T < 0 || D < 1 || D > (int64_t{1} << 30) ? DETO_ERR_BAD_CONFIG : DETO_OK;
 }
 
-template <int DT>
+template <int DT, bool ONCE>
 __global__ __launch_bounds__(kThreads) void encode_kernel(Items items, deto_rows x, deto_act8 x8) {
     const auto at = items.at(blockIdx.x * kThreads + threadIdx.x);
     float v[8];
-    unpack8<DT>(load8<DT>(x.data, at.t * x.ld, at.d, at.count), v);
-    act8_put(x8, at.t, at.d, v, at.count);
+    unpack8<DT>(load8<DT, ONCE>(x.data, at.t * x.ld, at.d, at.count), v);
+    act8_put<ONCE>(x8, at.t, at.d, v, at.count);
 }
 
-template <int DT>
+template <int DT, bool ONCE>
 __global__ __launch_bounds__(kThreads) void decode_kernel(Items items, deto_act8 x8, deto_rows x) {
     const auto at = items.at(blockIdx.x * kThreads + threadIdx.x);
     float v[8];
-    act8_get(x8, at.t, at.d, v, at.count);
-    store8<DT>(x.data, at.t * x.ld + at.d, v, at.count);
+    act8_get<ONCE>(x8, at.t, at.d, v, at.count);
+    store8<DT, ONCE>(x.data, at.t * x.ld + at.d, v, at.count);
 }
 
 // act(x), and its slope where that is asked for
@@ -92,34 +92,34 @@ __device__ __forceinline__ void act_both(float x, float& value, float& slope) {
     }
 }
 
-template <int DT, int ACT, bool GATED>
+template <int DT, int ACT, bool GATED, bool ONCE>
 __global__ __launch_bounds__(kThreads) void glu_forward_kernel(Items items, deto_rows a, deto_rows b,
                                                                deto_rows h, deto_act8 a8,
                                                                deto_act8 b8) {
     const auto at = items.at(blockIdx.x * kThreads + threadIdx.x);
-    const Raw8<DT> ra = load8<DT>(a.data, at.t * a.ld, at.d, at.count);
+    const Raw8<DT> ra = load8<DT, ONCE>(a.data, at.t * a.ld, at.d, at.count);
     Raw8<DT> rb = {};
-    if constexpr (GATED) rb = load8<DT>(b.data, at.t * b.ld, at.d, at.count);
+    if constexpr (GATED) rb = load8<DT, ONCE>(b.data, at.t * b.ld, at.d, at.count);
     float va[8], vb[8], vh[8];
     unpack8<DT>(ra, va);
     unpack8<DT>(rb, vb);
 #pragma unroll
     for (int j = 0; j < 8; ++j) vh[j] = act_value<ACT>(va[j]) * (GATED ? vb[j] : 1.f);
-    if (a8.codes) act8_put(a8, at.t, at.d, va, at.count);
-    if (GATED && b8.codes) act8_put(b8, at.t, at.d, vb, at.count);
-    store8<DT>(h.data, at.t * h.ld + at.d, vh, at.count);
+    if (a8.codes) act8_put<ONCE>(a8, at.t, at.d, va, at.count);
+    if (GATED && b8.codes) act8_put<ONCE>(b8, at.t, at.d, vb, at.count);
+    store8<DT, ONCE>(h.data, at.t * h.ld + at.d, vh, at.count);
 }
 
-template <int DT, int ACT, bool GATED>
+template <int DT, int ACT, bool GATED, bool ONCE>
 __global__ __launch_bounds__(kThreads) void glu_backward_kernel(Items items, deto_rows dh,
                                                                 deto_act8 a8, deto_act8 b8,
                                                                 deto_rows da, deto_rows db,
                                                                 deto_act8 h8) {
     const auto at = items.at(blockIdx.x * kThreads + threadIdx.x);
-    const Raw8<DT> rd = load8<DT>(dh.data, at.t * dh.ld, at.d, at.count);
+    const Raw8<DT> rd = load8<DT, ONCE>(dh.data, at.t * dh.ld, at.d, at.count);
     float va[8], vb[8], vd[8], vh[8];
-    act8_get(a8, at.t, at.d, va, at.count);
-    if constexpr (GATED) act8_get(b8, at.t, at.d, vb, at.count);
+    act8_get<ONCE>(a8, at.t, at.d, va, at.count);
+    if constexpr (GATED) act8_get<ONCE>(b8, at.t, at.d, vb, at.count);
     unpack8<DT>(rd, vd);
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
@@ -129,9 +129,15 @@ __global__ __launch_bounds__(kThreads) void glu_backward_kernel(Items items, det
         vh[j] = GATED ? value * vb[j] : value;
         if constexpr (GATED) vb[j] = vd[j] * value;
     }
-    if (h8.codes) act8_put(h8, at.t, at.d, vh, at.count);
-    store8<DT>(da.data, at.t * da.ld + at.d, va, at.count);
-    if constexpr (GATED) store8<DT>(db.data, at.t * db.ld + at.d, vb, at.count);
+    if (h8.codes) act8_put<ONCE>(h8, at.t, at.d, vh, at.count);
+    store8<DT, ONCE>(da.data, at.t * da.ld + at.d, va, at.count);
+    if constexpr (GATED) store8<DT, ONCE>(db.data, at.t * db.ld + at.d, vb, at.count);
+}
+
+// Matrices that the caches do not hold until the next kernel takes them are loaded and stored without a trace there.
+template <class F>
+int by_size(int64_t T, int64_t D, int dtype, F f) {
+    return T * D * type_size(dtype) >= kCacheBytes / 4 ? f(std::true_type{}) : f(std::false_type{});
 }
 
 template <class F>
@@ -162,8 +168,11 @@ int detonation_act8_encode(int64_t T, int64_t D, const deto_rows* x, const deto_
     if (rc) return rc;
     return for_items(T, D, [&](const Items& it, unsigned grid) {
         by_type(x->dtype, [&](auto dt) {
-            encode_kernel<dt.value><<<grid, kThreads, 0, static_cast<hipStream_t>(stream)>>>(it, *x, *x8);
-            return 0;
+            return by_size(T, D, x->dtype, [&](auto once) {
+                encode_kernel<dt.value, once.value>
+                    <<<grid, kThreads, 0, static_cast<hipStream_t>(stream)>>>(it, *x, *x8);
+                return 0;
+            });
         });
     });
 }
@@ -177,8 +186,11 @@ int detonation_act8_decode(int64_t T, int64_t D, const deto_act8* x8, const deto
     if (rc) return rc;
     return for_items(T, D, [&](const Items& it, unsigned grid) {
         by_type(x->dtype, [&](auto dt) {
-            decode_kernel<dt.value><<<grid, kThreads, 0, static_cast<hipStream_t>(stream)>>>(it, *x8, *x);
-            return 0;
+            return by_size(T, D, x->dtype, [&](auto once) {
+                decode_kernel<dt.value, once.value>
+                    <<<grid, kThreads, 0, static_cast<hipStream_t>(stream)>>>(it, *x8, *x);
+                return 0;
+            });
         });
     });
 }
@@ -202,10 +214,12 @@ int detonation_glu_forward(int act, int64_t T, int64_t D, const deto_rows* a, co
     return for_items(T, D, [&](const Items& it, unsigned grid) {
         by_type(a->dtype, [&](auto dt) {
             return by_act(act, gated, [&](auto k, auto g) {
-                glu_forward_kernel<dt.value, k.value, g.value>
-                    <<<grid, kThreads, 0, static_cast<hipStream_t>(stream)>>>(
-                        it, *a, gated ? *b : none, *h, here(a8) ? *a8 : none8, here(b8) ? *b8 : none8);
-                return 0;
+                return by_size(T, D, a->dtype, [&](auto once) {
+                    glu_forward_kernel<dt.value, k.value, g.value, once.value>
+                        <<<grid, kThreads, 0, static_cast<hipStream_t>(stream)>>>(
+                            it, *a, gated ? *b : none, *h, here(a8) ? *a8 : none8, here(b8) ? *b8 : none8);
+                    return 0;
+                });
             });
         });
     });
@@ -231,11 +245,13 @@ int detonation_glu_backward(int act, int64_t T, int64_t D, const deto_rows* dh, 
     return for_items(T, D, [&](const Items& it, unsigned grid) {
         by_type(dh->dtype, [&](auto dt) {
             return by_act(act, gated, [&](auto k, auto g) {
-                glu_backward_kernel<dt.value, k.value, g.value>
-                    <<<grid, kThreads, 0, static_cast<hipStream_t>(stream)>>>(
-                        it, *dh, *a8, gated ? *b8 : none8, *da, gated ? *db : none,
-                        here(h8) ? *h8 : none8);
-                return 0;
+                return by_size(T, D, dh->dtype, [&](auto once) {
+                    glu_backward_kernel<dt.value, k.value, g.value, once.value>
+                        <<<grid, kThreads, 0, static_cast<hipStream_t>(stream)>>>(
+                            it, *dh, *a8, gated ? *b8 : none8, *da, gated ? *db : none,
+                            here(h8) ? *h8 : none8);
+                    return 0;
+                });
             });
         });
     });

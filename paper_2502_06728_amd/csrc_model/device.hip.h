@@ -6,12 +6,15 @@
 #include <math.h>
 #include <stdint.h>
 
+#include <type_traits>
+
 #include "../../include/detonation_model.h"
 
 namespace deto {
 namespace model {
 
 constexpr int kLanes = 64;
+constexpr int64_t kCacheBytes = int64_t{1} << 28;     // the cache that all of the chip shares
 
 // ---- Eight consecutive elements of a row.  Rows start at any multiple of the element's size: the
 // vectors below say so, and the compiler still makes 16-byte accesses of them (global memory on gfx950
@@ -59,14 +62,17 @@ __device__ __forceinline__ void store1(void* base, int64_t at, float v) {
     else static_cast<_Float16*>(base)[at] = static_cast<_Float16>(v);
 }
 
-template <int DT>
+// ONCE: data that nothing reads again soon (large streams): it need not stay in the caches
+template <int DT, bool ONCE = false>
 __device__ __forceinline__ Raw8<DT> load8_whole(const char* p) {
+    using Vec = std::conditional_t<DT == DETO_F32, u32x4_any4, u32x4_any2>;
+    const Vec* v = reinterpret_cast<const Vec*>(p);
     Raw8<DT> r;
+    if constexpr (ONCE) r.a = __builtin_nontemporal_load(v);
+    else r.a = *v;
     if constexpr (DT == DETO_F32) {
-        r.a = *reinterpret_cast<const u32x4_any4*>(p);
-        r.b = *reinterpret_cast<const u32x4_any4*>(p + 16);
-    } else {
-        r.a = *reinterpret_cast<const u32x4_any2*>(p);
+        if constexpr (ONCE) r.b = __builtin_nontemporal_load(v + 1);
+        else r.b = v[1];
     }
     return r;
 }
@@ -104,14 +110,14 @@ __device__ __forceinline__ void move_down(Raw8<DT>& r, int by) {
 // the others read as zeros.  A row's partial last vector is read as the eight elements that end with the row and
 // moved down: one access, where element by element takes seven and a register each.  (Only rows of fewer than
 // eight elements have to be.)
-template <int DT>
+template <int DT, bool ONCE = false>
 __device__ __forceinline__ Raw8<DT> load8(const void* base, int64_t row, int64_t d, int count) {
     Raw8<DT> r = {};
     const bool whole = count >= 8;
     if (whole || (count > 0 && d > 0)) {
         const int short_by = whole ? 0 : 8 - count;
         const char* p = static_cast<const char*>(base) + (row + d - short_by) * kSize<DT>;
-        r = load8_whole<DT>(p);
+        r = load8_whole<DT, ONCE>(p);
         if (!whole) move_down<DT>(r, short_by);
     } else if (count > 0) {
         const char* p = static_cast<const char*>(base) + row * kSize<DT>;
@@ -154,7 +160,7 @@ __device__ __forceinline__ void unpack8(const Raw8<DT>& r, float (&v)[8]) {
     }
 }
 
-template <int DT>
+template <int DT, bool ONCE = false>
 __device__ __forceinline__ void store8(void* base, int64_t at, const float (&v)[8], int count) {
     char* p = static_cast<char*>(base) + at * kSize<DT>;
     if (count >= 8) {
@@ -165,15 +171,23 @@ __device__ __forceinline__ void store8(void* base, int64_t at, const float (&v)[
                 a[j] = f32_bits(v[j]);
                 b[j] = f32_bits(v[j + 4]);
             }
-            *reinterpret_cast<u32x4_any4*>(p) = a;
-            *reinterpret_cast<u32x4_any4*>(p + 16) = b;
+            u32x4_any4* at = reinterpret_cast<u32x4_any4*>(p);
+            if constexpr (ONCE) {
+                __builtin_nontemporal_store(u32x4_any4(a), at);
+                __builtin_nontemporal_store(u32x4_any4(b), at + 1);
+            } else {
+                at[0] = a;
+                at[1] = b;
+            }
         } else {
             u32x4 a;
 #pragma unroll
             for (int j = 0; j < 4; ++j)
                 a[j] = DT == DETO_BF16 ? pack_bf16(v[2 * j], v[2 * j + 1])
                                        : pack_f16(v[2 * j], v[2 * j + 1]);
-            *reinterpret_cast<u32x4_any2*>(p) = a;
+            u32x4_any2* at = reinterpret_cast<u32x4_any2*>(p);
+            if constexpr (ONCE) __builtin_nontemporal_store(u32x4_any2(a), at);
+            else *at = a;
         }
     } else if (count > 0) {
 #pragma unroll
@@ -246,10 +260,13 @@ __device__ __forceinline__ void act8_decode8(const u32x2& q, uint32_t exponent, 
 }
 
 // codes d ... d + 7 of a row, as load8
+template <bool ONCE = false>
 __device__ __forceinline__ u32x2 load_codes(const int8_t* row, int64_t d, int count) {
     u32x2 q = {0u, 0u};
     if (count >= 8) {
-        q = *reinterpret_cast<const u32x2_any1*>(row + d);
+        const u32x2_any1* at = reinterpret_cast<const u32x2_any1*>(row + d);
+        if constexpr (ONCE) q = __builtin_nontemporal_load(at);
+        else q = *at;
     } else if (count > 0 && d > 0) {
         q = *reinterpret_cast<const u32x2_any1*>(row + d - (8 - count));
         q = __builtin_bit_cast(u32x2, __builtin_bit_cast(uint64_t, q) >> (8 * (8 - count)));
@@ -262,9 +279,12 @@ __device__ __forceinline__ u32x2 load_codes(const int8_t* row, int64_t d, int co
     return q;
 }
 
+template <bool ONCE = false>
 __device__ __forceinline__ void store_codes(int8_t* p, const u32x2& q, int count) {
     if (count >= 8) {
-        *reinterpret_cast<u32x2_any1*>(p) = q;
+        u32x2_any1* at = reinterpret_cast<u32x2_any1*>(p);
+        if constexpr (ONCE) __builtin_nontemporal_store(u32x2_any1(q), at);
+        else *at = q;
     } else {
 #pragma unroll
         for (int j = 0; j < 7; ++j)
@@ -274,20 +294,22 @@ __device__ __forceinline__ void store_codes(int8_t* p, const u32x2& q, int count
 
 // Eight values at feature d (a multiple of 8) of row t: codes, and the exponent from the group's first lane.
 // Every lane of a group of four takes part, whatever its count.
+template <bool ONCE = false>
 __device__ __forceinline__ void act8_put(const deto_act8& m, int64_t t, int64_t d, const float (&v)[8],
                                          int count) {
     uint32_t e;
     const u32x2 q = act8_encode8(v, e);
     if (count > 0) {
-        store_codes(m.codes + t * m.ld_codes + d, q, count);
+        store_codes<ONCE>(m.codes + t * m.ld_codes + d, q, count);
         if (d % DETO_ACT8_GROUP == 0) m.exps[t * m.ld_exps + d / DETO_ACT8_GROUP] = static_cast<uint8_t>(e);
     }
 }
 
+template <bool ONCE = false>
 __device__ __forceinline__ void act8_get(const deto_act8& m, int64_t t, int64_t d, float (&v)[8],
                                          int count) {
     if (count > 0)
-        act8_decode8(load_codes(m.codes + t * m.ld_codes, d, count),
+        act8_decode8(load_codes<ONCE>(m.codes + t * m.ld_codes, d, count),
                      m.exps[t * m.ld_exps + d / DETO_ACT8_GROUP], v);
     else
 #pragma unroll

@@ -21,14 +21,14 @@ namespace deto {
 namespace model {
 namespace {
 
-constexpr int kThreads = 256;
-constexpr int kWaves = kThreads / kLanes;
+constexpr int kThreads = 256;                  // of the join and of the backward pass
 constexpr int kMaxTop = 32;
+constexpr int kKeys = 256;                     // maxima of parts of a piece that the threshold is taken of
 constexpr int kList = 1024;                    // listed candidates of a piece
 constexpr int kMaxPieces = kList / kMaxTop;    // the join ranks kMaxTop of every piece in one list
 static_assert(kMaxPieces <= kLanes, "a lane for each piece");
-constexpr int64_t kPieceElems = kThreads * 8;  // least length of a piece: eight elements a lane
-constexpr int64_t kFillWorkgroups = 1024;      // workgroups that fill the chip
+constexpr int64_t kPieceElems = 1 << 16;       // above a piece's length, if there are no more of them than
+constexpr int64_t kFillWorkgroups = 512;       // fill the chip
 
 // What a piece, or a part of one, has seen: m over the raw logits, a NaN if one was; s, w scaled (w in units of
 // log 2).  m is -infinity before the first value above that.
@@ -158,18 +158,18 @@ struct Taken {
     float v[kVectors<DT>][8];        // -infinity past the end
 };
 
-template <int DT>
+template <int DT, int THREADS, bool ONCE>
 struct Piece {
     const void* logits;
     int64_t row, first, end;
-    __device__ __forceinline__ int64_t at(int64_t d, int i) const { return d + i * kThreads * 8; }
+    __device__ __forceinline__ int64_t at(int64_t d, int i) const { return d + i * THREADS * 8; }
     __device__ __forceinline__ int count(int64_t d, int i) const {
         const int64_t left = end - at(d, i);
         return left >= 8 ? 8 : left > 0 ? static_cast<int>(left) : 0;
     }
     __device__ __forceinline__ void load(int64_t d, Raw8<DT> (&raw)[kVectors<DT>]) const {
 #pragma unroll
-        for (int i = 0; i < kVectors<DT>; ++i) raw[i] = load8<DT>(logits, row, at(d, i), count(d, i));
+        for (int i = 0; i < kVectors<DT>; ++i) raw[i] = load8<DT, ONCE>(logits, row, at(d, i), count(d, i));
     }
     __device__ __forceinline__ void unpack(int64_t d, const Raw8<DT> (&raw)[kVectors<DT>], Taken<DT>& x) const {
 #pragma unroll
@@ -210,36 +210,29 @@ __device__ __forceinline__ void see(Seen& r, const Taken<DT>& x, float unit) {
 }
 
 // The whole workgroup's, in every thread.
+template <int WAVES>
 __device__ __forceinline__ Seen join_workgroup(Seen r, float unit, Seen* lds) {
     r = join_wave(r, unit);
-    if (threadIdx.x % kLanes == 0) lds[threadIdx.x / kLanes] = r;
+    const int lane = threadIdx.x % kLanes;
+    if (lane == 0) lds[threadIdx.x / kLanes] = r;
     __syncthreads();
-    float m = lds[0].m;
-#pragma unroll
-    for (int i = 1; i < kWaves; ++i) m = larger(m, lds[i].m);
-    Seen all = {m, 0.f, 0.f};
-#pragma unroll
-    for (int i = 0; i < kWaves; ++i) {
-        const Seen p = relative_to(lds[i], m, unit);
-        all.s += p.s;
-        all.w += p.w;
-    }
-    return all;
+    r = {-__builtin_inff(), 0.f, 0.f};
+    if (lane < WAVES) r = lds[lane];
+    return join_wave(r, unit);
 }
 
-// The K-th largest of the workgroup's keys, down to its upper 16 bits, by bisection: counts of keys in each wavefront
-// alone, which holds all of them.
+// The K-th largest of kKeys keys, down to its upper 16 bits, by bisection: counts in one wavefront, which holds all.
 __device__ __forceinline__ uint32_t kth_key(const uint32_t* lds_keys, int K) {
-    uint32_t k[kWaves];
+    uint32_t k[kKeys / kLanes];
 #pragma unroll
-    for (int i = 0; i < kWaves; ++i) k[i] = lds_keys[i * kLanes + threadIdx.x % kLanes];
+    for (int i = 0; i < kKeys / kLanes; ++i) k[i] = lds_keys[i * kLanes + threadIdx.x % kLanes];
     uint32_t found = 0;
 #pragma unroll
     for (int bit = 31; bit >= 16; --bit) {
         const uint32_t t = found | 1u << bit;
         int n = 0;
 #pragma unroll
-        for (int i = 0; i < kWaves; ++i) n += __popcll(__ballot(k[i] >= t));
+        for (int i = 0; i < kKeys / kLanes; ++i) n += __popcll(__ballot(k[i] >= t));
         if (n >= K) found = t;
     }
     return found;
@@ -258,25 +251,52 @@ __device__ __forceinline__ void fill_up(uint64_t* list, int n) {
     if (threadIdx.x < 8 && n + static_cast<int>(threadIdx.x) < (n + 7) / 8 * 8) list[n + threadIdx.x] = 0;
 }
 
-template <int DT, bool ENTROPY, bool TOP>
-__global__ __launch_bounds__(kThreads) void logprobs_kernel(Forward a) {
+// Elements of a lane that stay in registers between the two looks at a piece: a second look at memory is what they
+// save.
+constexpr int kKept = 64;
+
+template <int DT, bool ENTROPY, bool TOP, int THREADS, bool ONCE>
+__global__ __launch_bounds__(THREADS) void logprobs_kernel(Forward a) {
+    constexpr int kWaves = THREADS / kLanes, V8 = kVectors<DT>, kKeep = TOP && THREADS > 256 ? kKept / (8 * V8) : 1;
     __shared__ Seen lds_seen[kWaves];
     const int64_t t = blockIdx.x / a.parts.pieces;
     const int piece = blockIdx.x % a.parts.pieces;
     const int64_t begin = piece * a.piece;
-    const Piece<DT> p = {a.logits, t * a.ld, begin, begin + a.piece < a.V ? begin + a.piece : a.V};
+    const Piece<DT, THREADS, ONCE> p = {a.logits, t * a.ld, begin, begin + a.piece < a.V ? begin + a.piece : a.V};
     const bool whole = a.parts.pieces == 1;
     Target y = {};
     if (whole) y = load_target<DT>(a, t);
-    constexpr int64_t kStep = kThreads * 8 * kVectors<DT>;
+    constexpr int64_t kStep = THREADS * 8 * V8;
     const int64_t mine = p.first + 8 * threadIdx.x;
     Seen r = {-__builtin_inff(), 0.f, 0.f};
-    Raw8<DT> raw[kVectors<DT>];
+    Raw8<DT> raw[kKeep][V8];
     Taken<DT> x;
-    for (int64_t d = mine; d < p.end; d += kStep) {
-        p.load(d, raw);
-        p.unpack(d, raw, x);
-        see<DT, ENTROPY>(r, x, a.unit);
+    const bool kept = p.end - p.first <= kKeep * kStep;
+    if constexpr (kKeep > 1) {
+        // The first kKeep steps' loads go out together.
+#pragma unroll
+        for (int k = 0; k < kKeep; ++k)
+            if (mine + k * kStep < p.end) p.load(mine + k * kStep, raw[k]);
+#pragma unroll
+        for (int k = 0; k < kKeep; ++k)
+            if (mine + k * kStep < p.end) {
+                p.unpack(mine + k * kStep, raw[k], x);
+                see<DT, ENTROPY>(r, x, a.unit);
+            }
+        for (int64_t d = mine + kKeep * kStep; d < p.end; d += kStep) {
+            Raw8<DT> more[V8];
+            p.load(d, more);
+            p.unpack(d, more, x);
+            see<DT, ENTROPY>(r, x, a.unit);
+        }
+    } else {
+        // A step's loads go out before the one before is summed.
+        if (mine < p.end) p.load(mine, raw[0]);
+        for (int64_t d = mine; d < p.end; d += kStep) {
+            p.unpack(d, raw[0], x);
+            if (d + kStep < p.end) p.load(d + kStep, raw[0]);
+            see<DT, ENTROPY>(r, x, a.unit);
+        }
     }
     {
         // from the rounded product to the maximum itself
@@ -285,62 +305,87 @@ __global__ __launch_bounds__(kThreads) void logprobs_kernel(Forward a) {
             r = {r.m, r.s * e, (r.w - off * r.s) * e};
         } else if (r.m == r.m && r.m != -__builtin_inff()) {
             r.s = r.w = 0.f;
-            for (int64_t d = mine; d < p.end; d += kStep) {
-                p.load(d, raw);
-                p.unpack(d, raw, x);
+            for (int64_t d = mine; d < p.end; d += THREADS * 8) {
+                const int n = p.count(d, 0);
+                float v[8];
+                unpack8<DT>(load8<DT>(a.logits, p.row, d, n), v);
 #pragma unroll
-                for (int i = 0; i < kVectors<DT>; ++i)
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) {
-                        const float l = (x.v[i][j] - r.m) * a.unit, e1 = exp2_fast(l);
+                for (int j = 0; j < 8; ++j) {
+                    const float l = (v[j] - r.m) * a.unit, e1 = exp2_fast(l);
+                    if (j < n) {
                         r.s += e1;
                         r.w += fmaxf(l, kFarBelow) * e1;
                     }
+                }
             }
         }
     }
-    const uint32_t key = mine < p.end ? order_key(r.m) : 0u;
-    r = join_workgroup(r, a.unit, lds_seen);
+    uint32_t key = mine < p.end ? order_key(r.m) : 0u;
+    r = join_workgroup<kWaves>(r, a.unit, lds_seen);
     if (threadIdx.x == 0) {
         if (whole) write_row(a, t, r, y);
         else a.parts.seen[blockIdx.x] = r;
     }
     if constexpr (TOP) {
-        __shared__ uint32_t lds_keys[kThreads];
+        __shared__ uint32_t lds_keys[kKeys];
         __shared__ uint64_t list[kList + 8];
-        __shared__ uint32_t listed;
+        __shared__ uint32_t listed, threshold;
         const float log_s = logf(r.s);
         uint64_t* part = a.parts.best + static_cast<int64_t>(blockIdx.x) * a.top;
         auto give = [&](int rank, uint64_t c) {
             if (whole) write_best(a, t, rank, c, r.m, log_s);
             else part[rank] = c;
         };
-        lds_keys[threadIdx.x] = key;
+        // a key for each kShare neighbours
+        constexpr int kShare = THREADS / kKeys;
+#pragma unroll
+        for (int step = 1; step < kShare; step <<= 1) {
+            const uint32_t o = __shfl_xor(key, step);
+            key = o > key ? o : key;
+        }
+        if (threadIdx.x % kShare == 0) lds_keys[threadIdx.x / kShare] = key;
         if (threadIdx.x == 0) listed = 0;
         __syncthreads();
-        const uint32_t least = kth_key(lds_keys, a.top);
+        if (threadIdx.x < kLanes) {
+            const uint32_t found = kth_key(lds_keys, a.top);
+            if (threadIdx.x == 0) threshold = found;
+        }
+        __syncthreads();
+        const uint32_t least = threshold;
         // (0: fewer than `top` threads saw a value, all of them are listed; a NaN is not below anything)
         const float least_value = least > kLowestKey ? key_value(least) : -__builtin_inff();
-        for (int64_t d = mine; d < p.end; d += kStep) {
-            if (p.end - p.first > kStep) {       // (else the registers still hold the piece)
-                p.load(d, raw);
-                p.unpack(d, raw, x);
-            }
+        auto look = [&](int64_t d) {
 #pragma unroll
-            for (int i = 0; i < kVectors<DT>; ++i) {
-                float m = x.v[i][0];
+            for (int i = 0; i < V8; ++i) {
+                const float(&v)[8] = x.v[i];
+                float m = v[0];
 #pragma unroll
-                for (int j = 1; j < 8; ++j) m = larger(m, x.v[i][j]);
+                for (int j = 1; j < 8; ++j) m = larger(m, v[j]);
                 if (m < least_value) continue;
                 const int n = p.count(d, i);
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
-                    if (j < n && !(x.v[i][j] < least_value)) {
+                    if (j < n && !(v[j] < least_value)) {
                         const uint32_t at = atomicAdd(&listed, 1u);
                         if (at < kList)
-                            list[at] = candidate(order_key(x.v[i][j]), static_cast<uint32_t>(p.at(d, i) + j));
+                            list[at] = candidate(order_key(v[j]), static_cast<uint32_t>(p.at(d, i) + j));
                     }
                 }
+            }
+        };
+        if (kKeep > 1 && kept) {
+#pragma unroll
+            for (int k = 0; k < kKeep; ++k)
+                if (mine + k * kStep < p.end) {
+                    p.unpack(mine + k * kStep, raw[k], x);
+                    look(mine + k * kStep);
+                }
+        } else {
+            if (mine < p.end) p.load(mine, raw[0]);
+            for (int64_t d = mine; d < p.end; d += kStep) {
+                p.unpack(d, raw[0], x);
+                if (d + kStep < p.end) p.load(d + kStep, raw[0]);
+                look(d);
             }
         }
         __syncthreads();
@@ -348,13 +393,13 @@ __global__ __launch_bounds__(kThreads) void logprobs_kernel(Forward a) {
         if (n <= kList) {
             fill_up(list, n);
             __syncthreads();
-            for (int i = threadIdx.x; i < n; i += kThreads) {
+            for (int i = threadIdx.x; i < n; i += THREADS) {
                 const uint64_t c = list[i];
                 const int rank = rank_of(list, n, c);
                 if (rank < a.top) give(rank, c);
             }
             // a piece of fewer than `top` elements: the rest of its part is empty
-            for (int i = n + threadIdx.x; i < a.top; i += kThreads) give(i, 0);
+            for (int i = n + threadIdx.x; i < a.top; i += THREADS) give(i, 0);
             return;
         }
         // Too many reach the threshold: one search for each place, each for the largest candidate below the
@@ -362,17 +407,14 @@ __global__ __launch_bounds__(kThreads) void logprobs_kernel(Forward a) {
         uint64_t before = ~uint64_t{0};
         for (int rank = 0; rank < a.top; ++rank) {
             uint64_t best = 0;
-            for (int64_t d = mine; d < p.end; d += kStep) {
-                p.load(d, raw);
-                p.unpack(d, raw, x);
+            for (int64_t d = mine; d < p.end; d += THREADS * 8) {
+                const int n_there = p.count(d, 0);
+                float v[8];
+                unpack8<DT>(load8<DT>(a.logits, p.row, d, n_there), v);
 #pragma unroll
-                for (int i = 0; i < kVectors<DT>; ++i) {
-                    const int n_there = p.count(d, i);
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) {
-                        const uint64_t c = candidate(order_key(x.v[i][j]), static_cast<uint32_t>(p.at(d, i) + j));
-                        if (j < n_there && c < before && c > best) best = c;
-                    }
+                for (int j = 0; j < 8; ++j) {
+                    const uint64_t c = candidate(order_key(v[j]), static_cast<uint32_t>(d + j));
+                    if (j < n_there && c < before && c > best) best = c;
                 }
             }
 #pragma unroll
@@ -433,7 +475,7 @@ struct Backward {
 constexpr int kBackwardVectors = 4;      // of eight elements, a lane
 constexpr int64_t kBackwardElems = kThreads * 8 * kBackwardVectors;
 
-template <int DT, bool ENTROPY>
+template <int DT, bool ENTROPY, bool ONCE>
 __global__ __launch_bounds__(kThreads) void logprobs_backward_kernel(Backward a) {
     const int64_t t = blockIdx.x / a.pieces;
     const int64_t first = (blockIdx.x % a.pieces) * kBackwardElems + 8 * threadIdx.x;
@@ -452,7 +494,7 @@ __global__ __launch_bounds__(kThreads) void logprobs_backward_kernel(Backward a)
     for (int i = 0; i < kBackwardVectors; ++i) {
         const int64_t left = a.V - (first + i * kThreads * 8);
         count[i] = left >= 8 ? 8 : left > 0 ? static_cast<int>(left) : 0;
-        raw[i] = load8<DT>(a.logits, t * a.ld, first + i * kThreads * 8, count[i]);
+        raw[i] = load8<DT, ONCE>(a.logits, t * a.ld, first + i * kThreads * 8, count[i]);
     }
 #pragma unroll
     for (int i = 0; i < kBackwardVectors; ++i) {
@@ -468,7 +510,7 @@ __global__ __launch_bounds__(kThreads) void logprobs_backward_kernel(Backward a)
             if (d + j == y) o += g;
             v[j] = none ? 0.f : o;
         }
-        store8<DT>(a.dlogits, t * a.ld_out + d, v, count[i]);
+        store8<DT, ONCE>(a.dlogits, t * a.ld_out + d, v, count[i]);
     }
 }
 
@@ -476,14 +518,22 @@ bool bad_shape(int64_t T, int64_t V, int top) {
     return T < 0 || V < 1 || V > 0x7FFFFFFF || top < 0 || top > kMaxTop || top > V;
 }
 
-// Pieces of a row: as many as fill the chip, each of kPieceElems elements at least.
+// Few rows take a workgroup of 1,024 threads each (one row of 50,304 bf16 logits with its eight best: 25 pieces and
+// their join 13 us, 1,024 threads @@ us).  Rows that are long even for those are cut in pieces.
+constexpr int64_t kFewRows = 512;
+constexpr int kThreadsFew = 1024, kThreadsMany = 256;
+
 int pieces_of(int64_t T, int64_t V) {
-    const int64_t most = (V + kPieceElems - 1) / kPieceElems;
-    int64_t want = T > 0 ? kFillWorkgroups / T : 1;
-    if (want > most) want = most;
+    if (T >= kFewRows) return 1;
+    int64_t want = V / kPieceElems + 1;
+    if (T * want > kFillWorkgroups) want = kFillWorkgroups / T;
     if (want > kMaxPieces) want = kMaxPieces;
     return want < 1 ? 1 : static_cast<int>(want);
 }
+
+// Logits that the caches do not hold until the backward pass, nor their gradient until whoever takes that: loads and
+// stores that leave no trace there are faster (8,192 x 50,304 bf16, forward and backward, us: 467, without 430).
+bool streams(int64_t T, int64_t V, int dtype) { return T * V * type_size(dtype) > kCacheBytes / 2; }
 
 // Rows whose workgroups a launch can count (31 bits).
 constexpr int64_t kMaxGrid = 0x7FFFFFFF;
@@ -533,17 +583,23 @@ int detonation_token_logprobs(int64_t T, int64_t V, const deto_rows* logits, flo
     const hipStream_t st = static_cast<hipStream_t>(stream);
     const unsigned grid = static_cast<unsigned>(T * pieces);
     fresh();
-    by_type(logits->dtype, [&](auto dt) {
-        constexpr int DT = dt.value;
-        if (top) {
-            if (entropy) logprobs_kernel<DT, true, true><<<grid, kThreads, 0, st>>>(a);
-            else logprobs_kernel<DT, false, true><<<grid, kThreads, 0, st>>>(a);
+    const auto run = [&](auto dt, auto threads, auto once) {
+        constexpr int DT = decltype(dt)::value, THREADS = decltype(threads)::value;
+        constexpr bool ONCE = decltype(once)::value;
+        if (top) {      // (looks at the logits twice)
+            if (entropy) logprobs_kernel<DT, true, true, THREADS, false><<<grid, THREADS, 0, st>>>(a);
+            else logprobs_kernel<DT, false, true, THREADS, false><<<grid, THREADS, 0, st>>>(a);
         } else {
-            if (entropy) logprobs_kernel<DT, true, false><<<grid, kThreads, 0, st>>>(a);
-            else logprobs_kernel<DT, false, false><<<grid, kThreads, 0, st>>>(a);
+            if (entropy) logprobs_kernel<DT, true, false, THREADS, ONCE><<<grid, THREADS, 0, st>>>(a);
+            else logprobs_kernel<DT, false, false, THREADS, ONCE><<<grid, THREADS, 0, st>>>(a);
         }
+    };
+    by_type(logits->dtype, [&](auto dt) {
+        if (T < kFewRows) run(dt, Type<kThreadsFew>{}, std::false_type{});
+        else if (streams(T, V, logits->dtype)) run(dt, Type<kThreadsMany>{}, std::true_type{});
+        else run(dt, Type<kThreadsMany>{}, std::false_type{});
         if (pieces > 1)
-            logprobs_join_kernel<DT><<<static_cast<unsigned>(T), kThreads, 0, st>>>(a);
+            logprobs_join_kernel<dt.value><<<static_cast<unsigned>(T), kThreads, 0, st>>>(a);
         return 0;
     });
     return enqueued();
@@ -577,8 +633,13 @@ int detonation_token_logprobs_backward(int64_t T, int64_t V, const deto_rows* lo
     fresh();
     by_type(logits->dtype, [&](auto dt) {
         constexpr int DT = dt.value;
-        if (g_entropy) logprobs_backward_kernel<DT, true><<<grid, kThreads, 0, st>>>(a);
-        else logprobs_backward_kernel<DT, false><<<grid, kThreads, 0, st>>>(a);
+        const auto run = [&](auto once) {
+            constexpr bool ONCE = decltype(once)::value;
+            if (g_entropy) logprobs_backward_kernel<DT, true, ONCE><<<grid, kThreads, 0, st>>>(a);
+            else logprobs_backward_kernel<DT, false, ONCE><<<grid, kThreads, 0, st>>>(a);
+        };
+        if (streams(T, V, logits->dtype)) run(std::true_type{});
+        else run(std::false_type{});
         return 0;
     });
     return enqueued();

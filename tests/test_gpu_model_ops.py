@@ -161,6 +161,25 @@ def test_logprobs_of_unusual_rows(gpu, dtype, V):
 
 
 @pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("T,V", [(3, 40000), (2, 65535), (3, 70001), (1, 200003), (530, 9001), (520, 70001)])
+def test_logprobs_of_long_rows(gpu, dtype, T, V):
+    """Rows that take a workgroup several steps or several workgroups; a lane sees masked values (the type's
+    lowest, -infinity) for its first steps and others later, and the other way round."""
+    say(dtype, T, V)
+    x = normal(V + T, T, V, scale=2.0).float()
+    x[0, :V // 2] = torch.finfo(dtype).min
+    x[T - 1, V // 2:] = -INF if T > 1 else torch.finfo(dtype).min
+    x[T // 2, ::3] = torch.finfo(dtype).min
+    d = rows(x, dtype)
+    y = torch.randint(0, V, (T,), generator=torch.Generator().manual_seed(1)).to(DEV)
+    y[0] = V - 1
+    out = run_logprobs(d, y, 6, 2.0)
+    keep = torch.arange(0, T, max(1, T // 16))
+    part = {n: v[keep] for n, v in out.items()}
+    check_logprobs(d[keep], y[keep], part, 2.0, 6)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("T,V,pad,offset,scale", [
     (1, 1, 0, 0, 1.0), (3, 9, 2, 1, 1.0), (2, 8192, 0, 0, 1.0), (5, 8193, 1, 3, 0.5), (700, 515, 0, 0, 2.0)])
 def test_logprobs_gradient(gpu, dtype, T, V, pad, offset, scale):
@@ -185,6 +204,27 @@ def test_logprobs_gradient(gpu, dtype, T, V, pad, offset, scale):
     ops.detonation_token_logprobs_backward(twin_rows, y, out["stats"], twin_rows, g_logp=g, g_entropy=ge,
                                            entropy=out["entropy"], logit_scale=scale)
     assert torch.equal(twin_rows, got)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_logprobs_of_large_matrices(gpu, dtype):
+    """More logits than the caches hold: the kernels that stream them."""
+    T, V = (1400, 50001) if dtype != F32 else (700, 50001)
+    say(dtype, T, V)
+    g = torch.Generator(device=DEV).manual_seed(1)
+    x = (torch.randn((T, V), generator=g, device=DEV) * 2).to(dtype)
+    y = torch.randint(0, V, (T,), generator=g, device=DEV)
+    out = run_logprobs(x, y)
+    gl, ge = torch.randn(T, generator=g, device=DEV), torch.randn(T, generator=g, device=DEV)
+    keep = torch.tensor([0, 1, T // 2, T - 1])
+    before = x[keep].clone()
+    check_logprobs(before, y[keep], {n: v[keep] for n, v in out.items()})
+    ops.detonation_token_logprobs_backward(x, y, out["stats"], x, g_logp=gl, entropy=out["entropy"], g_entropy=ge)
+    want = ref.logprobs_grad(before, y[keep], gl[keep], ge[keep])
+    size = (gl.abs().max() + ge.abs().max()).item() * (2 + math.log(V))
+    mag = size * torch.exp(ref.double(before) - out["lse"][keep].cpu().double()[:, None]).clamp(min=1e-30)
+    mag[torch.arange(4), y[keep].cpu()] += size
+    assert_near(x[keep], want, mag * (1 + ref.double(before).abs()), V / 128 + 320, "dlogits")
 
 
 def test_logprobs_gradient_by_differences(gpu):
