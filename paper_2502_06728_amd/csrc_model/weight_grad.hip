@@ -81,132 +81,149 @@ __device__ __forceinline__ float rest(float v) {
 template <int DT> struct UnitA { Raw8<DT> row[4]; };
 struct UnitB { u32x2 codes[4]; uint32_t exps[4]; };
 
-// ---- Loads of a step.  NEAR: through buffer resources that end where the matrix does: rows past its end read as
-// zeros without a comparison, a lane needs one 32-bit offset, and columns past a row's end read whatever comes
-// next (they add to columns of dw that are not written).  Otherwise (rows far apart, or not at multiples of four
-// bytes) rows past the end are the last row and columns past the end the last eight, put right when they are used:
-// the loads themselves are without a branch, which would make each wait for the one before.
+// ---- Loads of a step, without a branch, which would make each wait for the one before.
+// NEAR: through buffers that end where the matrix does: rows past its end read as zeros without a comparison, a lane
+// needs one offset, and columns past a row's end read whatever comes next (they add to columns of dw that are not
+// written).  A buffer gives whole words at multiples of four bytes: rows have to start at those.
+// REACH: rows past the end are the last row and columns past the end the last eight, put right when they are used.
+// (4,096 x 2,048 x 2,048 bf16: NEAR 66 us, REACH 91.)
+// FAR: the same with 64-bit places, for steps of more than 2^32 bytes, and for rows of fewer than eight columns.
+enum Mode { kNear, kReach, kFar };
 typedef __amdgpu_buffer_rsrc_t Rsrc;
 
-// (The words that hold the last bytes count whole: a buffer gives no part of a word.  They are aligned.)
-__device__ __forceinline__ Rsrc resource(const void* base, int64_t bytes) {
-    const int n = bytes > 0x7FFFFFF0 ? 0x7FFFFFF0 : bytes > 0 ? (static_cast<int>(bytes) + 3) & ~3 : 0;
-    return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(base), 0, n, 0x00020000);
+// (The word that holds the last byte counts whole.  It is aligned: no access leaves the memory's last word.)
+__device__ __forceinline__ Rsrc resource(const void* base, int64_t bytes, bool words = true) {
+    const int n = bytes > 0x7FFFFFF0 ? 0x7FFFFFF0 : bytes > 0 ? static_cast<int>(bytes) : 0;
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(base), 0, words ? (n + 3) & ~3 : n, 0x00020000);
 }
 
-__device__ __forceinline__ int exps_left(int64_t bytes) {      // bytes, read one by one
-    return bytes > 0x7FFFFFF0 ? 0x7FFFFFF0 : bytes > 0 ? static_cast<int>(bytes) : 0;
-}
-
-template <int DT, class TL, bool NEAR>
+template <int DT, class TL, int MODE>
 struct Loader {
+    static constexpr bool REACH = MODE == kReach;
     const Args& a;
     int64_t n0, k0, end;
     __device__ __forceinline__ Loader(const Args& args, int64_t n, int64_t k, int64_t e)
         : a(args), n0(n), k0(k), end(e) {}
 
+    // Units of eight columns and four rows: rows 4 (u / units a row) of the step.
+    static __device__ __forceinline__ int unit(int i) { return threadIdx.x + i * TL::kThreads; }
+    // the step's first row, and how many it has
+    __device__ __forceinline__ int64_t from(int64_t t) const { return t < end ? t : end - 1; }
+    __device__ __forceinline__ int rows(int64_t t) const {
+        return end - t >= kDepth ? kDepth : end - t > 0 ? static_cast<int>(end - t) : 0;
+    }
+    static __device__ __forceinline__ int within(int row, int rows) { return row < rows ? row : rows > 0 ? rows - 1 : 0; }
+
     __device__ __forceinline__ void load_a(int64_t t, UnitA<DT> (&ua)[TL::kUnitsA]) const {
-        if constexpr (NEAR) {
+        if constexpr (MODE == kNear) {
             constexpr int kElem = kSize<DT>;
             const int ld = static_cast<int>(a.dy.ld) * kElem;
-            const int64_t at_a = (t * a.dy.ld + n0) * kElem;
-            const Rsrc ra = resource(static_cast<const char*>(a.dy.data) + at_a,
-                                     ((end - 1) * a.dy.ld + a.N) * kElem - at_a);
+            const int64_t at = (t * a.dy.ld + n0) * kElem;
+            const Rsrc rsrc = resource(static_cast<const char*>(a.dy.data) + at,
+                                       ((end - 1) * a.dy.ld + a.N) * kElem - at);
 #pragma unroll
             for (int i = 0; i < TL::kUnitsA; ++i) {
-                const int u = threadIdx.x + i * TL::kThreads;
-                const int off = u / (TL::BM / 8) * 4 * ld + u % (TL::BM / 8) * 8 * kElem;
+                const int off = unit(i) / (TL::BM / 8) * 4 * ld + unit(i) % (TL::BM / 8) * 8 * kElem;
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
-                    ua[i].row[r].a = __builtin_amdgcn_raw_buffer_load_b128(ra, off, r * ld, 0);
+                    ua[i].row[r].a = __builtin_amdgcn_raw_buffer_load_b128(rsrc, off, r * ld, 0);
                     if constexpr (DT == DETO_F32)
-                        ua[i].row[r].b = __builtin_amdgcn_raw_buffer_load_b128(ra, off + 16, r * ld, 0);
+                        ua[i].row[r].b = __builtin_amdgcn_raw_buffer_load_b128(rsrc, off + 16, r * ld, 0);
                 }
             }
-        } else {
+            return;
+        }
+        const int have = rows(t);
+        const char* const base = static_cast<const char*>(a.dy.data) + from(t) * a.dy.ld * kSize<DT>;
 #pragma unroll
-            for (int i = 0; i < TL::kUnitsA; ++i) {
-                const int u = threadIdx.x + i * TL::kThreads;
-                const int64_t n = n0 + u % (TL::BM / 8) * 8, row = t + u / (TL::BM / 8) * 4;
+        for (int i = 0; i < TL::kUnitsA; ++i) {
+            const int64_t n = n0 + unit(i) % (TL::BM / 8) * 8;
+            const int row = unit(i) / (TL::BM / 8) * 4;
 #pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    const int64_t at = row + r < end ? row + r : end - 1;
-                    if (a.N >= 8)
-                        ua[i].row[r] = load8_whole<DT>(static_cast<const char*>(a.dy.data) +
-                                                       (at * a.dy.ld + (n < a.N - 8 ? n : a.N - 8)) * kSize<DT>);
-                    else ua[i].row[r] = load8<DT>(a.dy.data, at * a.dy.ld, n, n < a.N ? static_cast<int>(a.N - n) : 0);
+            for (int r = 0; r < 4; ++r) {
+                const int at = within(row + r, have);
+                if constexpr (REACH) {
+                    const uint32_t column = static_cast<uint32_t>(n < a.N - 8 ? n : a.N - 8);
+                    const uint32_t off = (static_cast<uint32_t>(at) * static_cast<uint32_t>(a.dy.ld) + column) * kSize<DT>;
+                    ua[i].row[r] = load8_whole<DT>(base + off);
+                } else {
+                    ua[i].row[r] = load8<DT>(base, at * a.dy.ld, n, n >= a.N ? 0 : a.N - n < 8 ? static_cast<int>(a.N - n) : 8);
                 }
             }
         }
     }
 
-    // Makes what a unit of rows t ... holds what was asked for: nothing to do for NEAR.
+    // Makes what units of rows t ... hold what was asked for.
     __device__ __forceinline__ void settle_a(int64_t t, UnitA<DT> (&ua)[TL::kUnitsA]) const {
-        if constexpr (!NEAR) {
+        if constexpr (MODE == kNear) return;
+        const int have = rows(t);
+        if (have == kDepth && (!REACH || n0 + TL::BM <= a.N)) return;
 #pragma unroll
-            for (int i = 0; i < TL::kUnitsA; ++i) {
-                const int u = threadIdx.x + i * TL::kThreads;
-                const int64_t by = n0 + u % (TL::BM / 8) * 8 - (a.N - 8), row = t + u / (TL::BM / 8) * 4;
+        for (int i = 0; i < TL::kUnitsA; ++i) {
+            const int64_t by = n0 + unit(i) % (TL::BM / 8) * 8 - (a.N - 8);
 #pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    if (a.N >= 8 && by > 0 && by < 8) move_down<DT>(ua[i].row[r], static_cast<int>(by));
-                    if (row + r >= end) ua[i].row[r] = {};
-                }
+            for (int r = 0; r < 4; ++r) {
+                if (REACH && by > 0 && by < 8) move_down<DT>(ua[i].row[r], static_cast<int>(by));
+                if (unit(i) / (TL::BM / 8) * 4 + r >= have) ua[i].row[r] = {};
             }
         }
     }
 
     __device__ __forceinline__ void load_b(int64_t t, UnitB (&ub)[TL::kUnitsB]) const {
-        if constexpr (NEAR) {
+        if constexpr (MODE == kNear) {
             const int ldc = static_cast<int>(a.x.ld_codes), lde = static_cast<int>(a.x.ld_exps);
             const int64_t at_c = t * a.x.ld_codes + k0, at_e = t * a.x.ld_exps + k0 / DETO_ACT8_GROUP;
+            const int64_t groups = (a.K + DETO_ACT8_GROUP - 1) / DETO_ACT8_GROUP;
             const Rsrc rc = resource(a.x.codes + at_c, (end - 1) * a.x.ld_codes + a.K - at_c);
-            const Rsrc re = __builtin_amdgcn_make_buffer_rsrc(
-                a.x.exps + at_e, 0, exps_left((end - 1) * a.x.ld_exps +
-                                              (a.K + DETO_ACT8_GROUP - 1) / DETO_ACT8_GROUP - at_e),
-                0x00020000);
+            const Rsrc re = resource(a.x.exps + at_e, (end - 1) * a.x.ld_exps + groups - at_e, false);    // bytes
 #pragma unroll
             for (int i = 0; i < TL::kUnitsB; ++i) {
-                const int u = threadIdx.x + i * TL::kThreads;
-                const int t4 = u / (TL::BN / 8) * 4, c8 = u % (TL::BN / 8);
+                const int t4 = unit(i) / (TL::BN / 8) * 4, c8 = unit(i) % (TL::BN / 8);
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
                     ub[i].codes[r] = __builtin_amdgcn_raw_buffer_load_b64(rc, t4 * ldc + c8 * 8, r * ldc, 0);
                     ub[i].exps[r] = __builtin_amdgcn_raw_buffer_load_b8(re, t4 * lde + c8 / 4, r * lde, 0);
                 }
             }
-        } else {
+            return;
+        }
+        const int have = rows(t);
+        const int8_t* const codes = a.x.codes + from(t) * a.x.ld_codes;
+        const uint8_t* const exps = a.x.exps + from(t) * a.x.ld_exps;
+        const int last = static_cast<int>((a.K - 1) / DETO_ACT8_GROUP);
 #pragma unroll
-            for (int i = 0; i < TL::kUnitsB; ++i) {
-                const int u = threadIdx.x + i * TL::kThreads;
-                const int64_t k = k0 + u % (TL::BN / 8) * 8, row = t + u / (TL::BN / 8) * 4;
-                const int64_t last = (a.K - 1) / DETO_ACT8_GROUP, group = k / DETO_ACT8_GROUP;
+        for (int i = 0; i < TL::kUnitsB; ++i) {
+            const int64_t k = k0 + unit(i) % (TL::BN / 8) * 8;
+            const int row = unit(i) / (TL::BN / 8) * 4;
+            const int group = k / DETO_ACT8_GROUP < last ? static_cast<int>(k / DETO_ACT8_GROUP) : last;
 #pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    const int64_t at = row + r < end ? row + r : end - 1;
-                    const int8_t* codes = a.x.codes + at * a.x.ld_codes;
-                    if (a.K >= 8)
-                        ub[i].codes[r] = *reinterpret_cast<const u32x2_any1*>(codes + (k < a.K - 8 ? k : a.K - 8));
-                    else ub[i].codes[r] = load_codes(codes, k, k < a.K ? static_cast<int>(a.K - k) : 0);
-                    ub[i].exps[r] = a.x.exps[at * a.x.ld_exps + (group < last ? group : last)];
+            for (int r = 0; r < 4; ++r) {
+                const int at = within(row + r, have);
+                if constexpr (REACH) {
+                    const uint32_t column = static_cast<uint32_t>(k < a.K - 8 ? k : a.K - 8);
+                    ub[i].codes[r] = *reinterpret_cast<const u32x2_any1*>(
+                        codes + (static_cast<uint32_t>(at) * static_cast<uint32_t>(a.x.ld_codes) + column));
+                    ub[i].exps[r] = exps[static_cast<uint32_t>(at) * static_cast<uint32_t>(a.x.ld_exps) + static_cast<uint32_t>(group)];
+                } else {
+                    ub[i].codes[r] = load_codes(codes + at * a.x.ld_codes, k, k >= a.K ? 0 : a.K - k < 8 ? static_cast<int>(a.K - k) : 8);
+                    ub[i].exps[r] = exps[at * a.x.ld_exps + group];
                 }
             }
         }
     }
 
     __device__ __forceinline__ void settle_b(int64_t t, UnitB (&ub)[TL::kUnitsB]) const {
-        if constexpr (!NEAR) {
+        if constexpr (MODE == kNear) return;
+        const int have = rows(t);
+        if (have == kDepth && (!REACH || k0 + TL::BN <= a.K)) return;
 #pragma unroll
-            for (int i = 0; i < TL::kUnitsB; ++i) {
-                const int u = threadIdx.x + i * TL::kThreads;
-                const int64_t by = k0 + u % (TL::BN / 8) * 8 - (a.K - 8), row = t + u / (TL::BN / 8) * 4;
+        for (int i = 0; i < TL::kUnitsB; ++i) {
+            const int64_t by = k0 + unit(i) % (TL::BN / 8) * 8 - (a.K - 8);
 #pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    if (a.K >= 8 && by > 0 && by < 8)
-                        ub[i].codes[r] = __builtin_bit_cast(
-                            u32x2, __builtin_bit_cast(uint64_t, ub[i].codes[r]) >> (8 * by));
-                    if (row + r >= end) ub[i].exps[r] = 0u;
-                }
+            for (int r = 0; r < 4; ++r) {
+                if (REACH && by > 0 && by < 8)
+                    ub[i].codes[r] = __builtin_bit_cast(u32x2, __builtin_bit_cast(uint64_t, ub[i].codes[r]) >> (8 * by));
+                if (unit(i) / (TL::BN / 8) * 4 + r >= have) ub[i].exps[r] = 0u;
             }
         }
     }
@@ -280,7 +297,7 @@ __device__ __forceinline__ void each_of(F f) {
     }
 }
 
-template <int DT, class TL, bool NEAR>
+template <int DT, class TL, int MODE>
 __global__ __launch_bounds__(TL::kThreads) void weight_grad_kernel(Args a) {
     extern __shared__ __align__(16) char lds[];
     constexpr int kTermsA = kTerms<DT>;
@@ -310,7 +327,7 @@ __global__ __launch_bounds__(TL::kThreads) void weight_grad_kernel(Args a) {
 
     UnitA<DT> ua[TL::kUnitsA];
     UnitB ub[TL::kUnitsB];
-    const Loader<DT, TL, NEAR> loader(a, n0, k0, end);
+    const Loader<DT, TL, MODE> loader(a, n0, k0, end);
     // (A's and B's units lie alike over their columns where the tile is square)
     auto place = [&](int i, int wide) { return (threadIdx.x + i * TL::kThreads) % (wide / 8) * 8; };
     auto quarter = [&](int i, int wide) { return (threadIdx.x + i * TL::kThreads) / (wide / 8); };
@@ -379,6 +396,8 @@ __global__ __launch_bounds__(TL::kThreads) void weight_grad_kernel(Args a) {
     // While a step's products run from one buffer, the next step's rows, in registers, turn into the other, and
     // the ones after that are loaded as registers fall free.  (Rows past the end are zeros.)
     constexpr int kBlocks = TL::WM / 32;
+    // (The quarters stay apart: scheduled over the whole step, products wait for operands.  4,096 x 2,048 x 2,048: 75 us.)
+    auto fence = [] { __builtin_amdgcn_sched_barrier(0); };
     for (int64_t t = t0; t < end; t += kDepth) {
         const char* la = lds + buffer * kBuffer;
         buffer ^= 1;
@@ -390,6 +409,7 @@ __global__ __launch_bounds__(TL::kThreads) void weight_grad_kernel(Args a) {
             multiply(Type<0>{}, i);
             each_of<4 / kBlocks>([&](auto q) { put_a(next, Type<i.value * (4 / kBlocks) + q.value>{}); });
         });
+        fence();
         loader.load_a(t + 2 * kDepth, ua);
         loader.settle_b(t + kDepth, ub);
         scales();
@@ -398,11 +418,13 @@ __global__ __launch_bounds__(TL::kThreads) void weight_grad_kernel(Args a) {
             multiply(Type<1>{}, i);
             each_of<4 / kBlocks>([&](auto q) { put_b(next, Type<i.value * (4 / kBlocks) + q.value>{}); });
         });
+        fence();
         fetch(la, Type<3>{});
         each_of<kBlocks>([&](auto i) {
             multiply(Type<2>{}, i);
             each_of<4 / kBlocks>([&](auto q) { put_b(next, Type<4 + i.value * (4 / kBlocks) + q.value>{}); });
         });
+        fence();
         loader.load_b(t + 2 * kDepth, ub);
         each_of<kBlocks>([&](auto i) { multiply(Type<3>{}, i); });
         __syncthreads();
@@ -490,11 +512,11 @@ struct Plan {
     double us;
 };
 
-// The splits of T that take least time by what was measured (us): a step of 64 rows 0.8 in a workgroup of small tiles
-// that has a CU to itself and 1.25 in one of two (fp32 and fp16 dy, whose terms leave room for one: 1.1), 1.95 in one
-// of large tiles; 5 to start and to write the tile; 3 for the second launch, which the splits' sums go to and come from
-// at 3.5 TB/s.
-Plan plan_with(int64_t T, int64_t N, int64_t K, bool large, bool one_term) {
+// The splits of T that take least time by what was measured (us): a step of 64 rows 0.95 in a workgroup of small tiles
+// that has a CU to itself and 1.25 in one of two; 1.4 and 2.0 with two and three terms, which leave room for one; 1.9 in
+// one of large tiles; 5 to start and to write the tile; 3 for the second launch, which the splits' sums go to and come
+// from at 3.5 TB/s.
+Plan plan_with(int64_t T, int64_t N, int64_t K, bool large, int terms) {
     const int64_t b = large ? Large::BM : Small::BM;
     Plan best = {};
     const int64_t tiles_k = (K + b - 1) / b, tiles = (N + b - 1) / b * tiles_k;
@@ -502,8 +524,8 @@ Plan plan_with(int64_t T, int64_t N, int64_t K, bool large, bool one_term) {
     for (int64_t splits = 1; splits <= 32 && splits <= steps; ++splits) {
         const int64_t each = (steps + splits - 1) / splits;
         if (splits > 1 && each * (splits - 1) >= steps) continue;      // an empty split
-        const int64_t slots = large || !one_term ? 256 : 512;
-        const double step = large ? 1.95 : !one_term ? 1.1 : tiles * splits > 256 ? 1.25 : 0.8;
+        const int64_t slots = large || terms > 1 ? 256 : 512;
+        const double step = large ? 1.9 : terms == 2 ? 1.4 : terms == 3 ? 2.0 : tiles * splits > 256 ? 1.25 : 0.95;
         double us = static_cast<double>((tiles * splits + slots - 1) / slots) * (step * static_cast<double>(each) + 5.0);
         if (splits > 1)
             us += 3.0 + 8.0 * static_cast<double>(splits) * static_cast<double>(N) * static_cast<double>(K) / 3.5e6;
@@ -512,18 +534,19 @@ Plan plan_with(int64_t T, int64_t N, int64_t K, bool large, bool one_term) {
     return best;
 }
 
-// Whether a step's rows lie within 2^31 bytes and at multiples of four: the loader's buffers.
-bool reaches(const Args& a) {
-    const int64_t e = type_size(a.dy.dtype), most = (int64_t{1} << 31) / (2 * kDepth);
-    return a.dy.ld * e < most && a.x.ld_codes < most && a.x.ld_exps < most && a.dy.ld * e % 4 == 0 &&
-           a.x.ld_codes % 4 == 0 && is_aligned(a.dy.data, 4) && is_aligned(a.x.codes, 4);
+int mode_of(const Args& a) {
+    const int64_t e = type_size(a.dy.dtype), row = a.dy.ld * e, least = int64_t{1} << 24, most = int64_t{1} << 25;
+    if (row < least && a.x.ld_codes < least && a.x.ld_exps < least && row % 4 == 0 && a.x.ld_codes % 4 == 0 &&
+        is_aligned(a.dy.data, 4) && is_aligned(a.x.codes, 4))
+        return kNear;
+    return row < most && a.x.ld_codes < most && a.x.ld_exps < most && a.N >= 8 && a.K >= 8 ? kReach : kFar;
 }
 
-// One term (bf16 dy) through buffers may take large tiles.
-Plan plan_of(int64_t T, int64_t N, int64_t K, bool near, bool one_term) {
-    const Plan small = plan_with(T, N, K, false, one_term);
-    if (!near || !one_term) return small;
-    const Plan large = plan_with(T, N, K, true, true);
+// One term (bf16 dy) may take large tiles.
+Plan plan_of(int64_t T, int64_t N, int64_t K, bool may_be_large, int terms) {
+    const Plan small = plan_with(T, N, K, false, terms);
+    if (!may_be_large || terms > 1) return small;
+    const Plan large = plan_with(T, N, K, true, 1);
     return large.us < small.us ? large : small;
 }
 
@@ -538,9 +561,9 @@ extern "C" {
 int64_t detonation_act8_weight_grad_workspace(int64_t T, int64_t N, int64_t K) {
     if (bad_shape(T, N, K)) return -1;
     int64_t most = 0;
-    for (bool near : {true, false})
-        for (bool one_term : {true, false}) {
-            const Plan p = plan_of(T, N, K, near, one_term);
+    for (bool may_be_large : {true, false})
+        for (int terms : {1, 2, 3}) {
+            const Plan p = plan_of(T, N, K, may_be_large, terms);
             if (p.splits > 1 && p.splits > most) most = p.splits;
         }
     return most * N * K * static_cast<int64_t>(sizeof(float));
@@ -564,8 +587,8 @@ int detonation_act8_weight_grad(int64_t T, int64_t N, int64_t K, const deto_rows
         a.x.ld_codes = (K + 3) / 4 * 4;
         a.x.ld_exps = (K + DETO_ACT8_GROUP - 1) / DETO_ACT8_GROUP;
     }
-    const bool near = T > 0 && reaches(a);
-    const Plan p = plan_of(T, N, K, near, dtype == DETO_BF16);
+    const int mode = T > 0 ? mode_of(a) : static_cast<int>(kNear);
+    const Plan p = plan_of(T, N, K, mode != kFar, dtype == DETO_BF16 ? 1 : dtype == DETO_F16 ? 2 : 3);
     if (p.splits > 1 && !workspace) return DETO_ERR_NULL;
     if (p.splits > 1 && !is_aligned(workspace, 16)) return DETO_ERR_ALIGN;
     if (p.tiles > 0x7FFFFFFF / p.splits) return DETO_ERR_UNSUPPORTED;
@@ -575,15 +598,21 @@ int detonation_act8_weight_grad(int64_t T, int64_t N, int64_t K, const deto_rows
     const hipStream_t st = static_cast<hipStream_t>(stream);
     const unsigned grid = static_cast<unsigned>(p.tiles * p.splits);
     fresh();
-    if (p.large)
-        weight_grad_kernel<DETO_BF16, Large, true><<<grid, Large::kThreads, Large::lds(1), st>>>(a);
-    else
+    if (p.large) {
+        if (mode == kNear)
+            weight_grad_kernel<DETO_BF16, Large, kNear><<<grid, Large::kThreads, Large::lds(1), st>>>(a);
+        else
+            weight_grad_kernel<DETO_BF16, Large, kReach><<<grid, Large::kThreads, Large::lds(1), st>>>(a);
+    } else {
         by_type(dtype, [&](auto dt) {
             constexpr int kLds = Small::lds(kTerms<dt.value>);
-            if (near) weight_grad_kernel<dt.value, Small, true><<<grid, Small::kThreads, kLds, st>>>(a);
-            else weight_grad_kernel<dt.value, Small, false><<<grid, Small::kThreads, kLds, st>>>(a);
+            if (mode == kNear) weight_grad_kernel<dt.value, Small, kNear><<<grid, Small::kThreads, kLds, st>>>(a);
+            else if (mode == kReach)
+                weight_grad_kernel<dt.value, Small, kReach><<<grid, Small::kThreads, kLds, st>>>(a);
+            else weight_grad_kernel<dt.value, Small, kFar><<<grid, Small::kThreads, kLds, st>>>(a);
             return 0;
         });
+    }
     if (p.splits > 1) {
         const int64_t rows = (N + kJoinRows - 1) / kJoinRows;
         const dim3 join(static_cast<unsigned>((K + 4 * kLanes - 1) / (4 * kLanes)),
