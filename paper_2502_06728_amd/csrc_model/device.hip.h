@@ -346,6 +346,17 @@ __device__ __forceinline__ float wave_sum(float v) {
     v += moved<0x140>(v);    // the other half of sixteen
     return (lane_value(v, 0) + lane_value(v, 16)) + (lane_value(v, 32) + lane_value(v, 48));
 }
+// sums over each L lanes in a row (16, 32 or all), the same in all of them
+template <int L>
+__device__ __forceinline__ float lanes_sum(float v) {
+    if constexpr (L == kLanes) return wave_sum(v);
+    v += moved<0xB1>(v);
+    v += moved<0x4E>(v);
+    v += moved<0x141>(v);
+    v += moved<0x140>(v);
+    if constexpr (L == 32) v += __shfl_xor(v, 16);
+    return v;
+}
 
 // ---- host side
 inline bool valid_type(int d) { return d == DETO_F32 || d == DETO_BF16 || d == DETO_F16; }

@@ -29,6 +29,7 @@ struct Args {
     Deal deal;
     deto_rows x, f, dy, dxo, dx, df;
     deto_norm_grads grads;
+    bool once;           // dx and df are stored past the caches
     float* parts;        // [team][slot][D]
     int slot[kSums];     // of a sum in `parts`, -1: not wanted, or written by the team itself
     int slots;
@@ -44,9 +45,9 @@ __device__ __forceinline__ void clear(float (&v)[C][8]) {
 
 // LAYER: one of the norms is one, or has a bias, or a bias's gradient is wanted.  (Without, the registers of the
 // biases' sums are not held.)
-template <int XT, int FT, int W, int C, bool WHOLE, bool LAYER>
-__global__ __launch_bounds__((Team<W, C, WHOLE>::kThreadsWg)) void norm_backward_kernel(Args a) {
-    using TM = Team<W, C, WHOLE>;
+template <int XT, int FT, int W, int C, int L, bool WHOLE, bool LAYER>
+__global__ __launch_bounds__((Team<W, C, L, WHOLE>::kThreadsWg)) void norm_backward_kernel(Args a) {
+    using TM = Team<W, C, L, WHOLE>;
     __shared__ float lds[TM::kSlots];
     TM team(lds);
     const int D = a.D;
@@ -173,7 +174,7 @@ __global__ __launch_bounds__((Team<W, C, WHOLE>::kThreadsWg)) void norm_backward
                 if constexpr (LAYER) sums[kBPre][c][j] += G[c][j];
                 G[c][j] = r * (G[c][j] * w_pre[c][j] - x[c][j] * m0 - m1) + o[c][j];
             }
-            TM::template store<XT>(a.dx.data, t * a.dx.ld, c, D, G[c]);
+            TM::template store<XT>(a.dx.data, t * a.dx.ld, c, D, G[c], a.once);
         }
         if (!branch) continue;
         const int64_t row = a.cfg.rows_per_gate ? t / a.cfg.rows_per_gate : 0;
@@ -212,7 +213,7 @@ __global__ __launch_bounds__((Team<W, C, WHOLE>::kThreadsWg)) void norm_backward
                 for (int j = 0; j < 8; ++j) G[c][j] = rf_ * (G[c][j] - f[c][j] * n0 - n1);
         }
 #pragma unroll
-        for (int c = 0; c < C; ++c) TM::template store<FT>(a.df.data, t * a.df.ld, c, D, G[c]);
+        for (int c = 0; c < C; ++c) TM::template store<FT>(a.df.data, t * a.df.ld, c, D, G[c], a.once);
         // a gate row of this team's own ends
         if (deal.group && a.grads.gate && ((t + 1) % deal.rows == 0 || t + 1 == deal.T)) {
 #pragma unroll
@@ -288,8 +289,8 @@ __global__ __launch_bounds__(kJoinThreads) void norm_join_kernel(JoinArgs a, int
 // adds (16,384 x 2,048: 1,024 teams 144 us, 768 127 us).
 int64_t wanted_teams(int64_t D, bool lean) {
     int64_t teams = 0;
-    by_width(D, [&](auto w, auto, auto whole) {
-        teams = w.value >= 16 ? 256 : (lean && whole.value ? 3072 : 2048) / w.value;
+    by_width(D, [&](auto w, auto, auto l, auto whole) {
+        teams = w.value >= 16 ? 256 : (lean && whole.value ? 3072 : 2048) * (kLanes / l.value) / w.value;
     });
     return teams;
 }
@@ -366,6 +367,9 @@ int detonation_norm_residual_backward(const deto_norm_residual* cfg, int64_t T, 
             return DETO_ERR_BAD_CONFIG;
     }
     a.cfg = *cfg;
+    // (16,384 x 2,048, us: all bf16 95, past the caches 79; with an fp32 residual stream, of which a lane's 16 bytes are
+    // half of what lies together, 135 and 137)
+    a.once = T > 0 && x_out->dtype != DETO_F32 && T * D * 2 >= kCacheBytes / 4;
     a.D = static_cast<int>(D);
     const bool layer = cfg->pre == DETO_NORM_LAYER || cfg->post == DETO_NORM_LAYER || cfg->b_post || g.b_pre ||
                        g.b_post;
@@ -397,15 +401,15 @@ int detonation_norm_residual_backward(const deto_norm_residual* cfg, int64_t T, 
         a.df = branch ? *df : none;
         a.dy = pre ? *dy : none;
         a.dxo = here(dx_out) ? *dx_out : none;
-        by_width(D, [&](auto w, auto c, auto whole) {
-            using TM = Team<w.value, c.value, whole.value>;
+        by_width(D, [&](auto w, auto c, auto l, auto whole) {
+            using TM = Team<w.value, c.value, l.value, whole.value>;
             const unsigned grid = static_cast<unsigned>((a.deal.teams + TM::kTeamsWg - 1) / TM::kTeamsWg);
             by_types(a.x.dtype, branch ? a.f.dtype : a.dy.dtype, [&](auto xt, auto ft) {
                 if (layer)
-                    norm_backward_kernel<xt.value, ft.value, w.value, c.value, whole.value, true>
+                    norm_backward_kernel<xt.value, ft.value, w.value, c.value, l.value, whole.value, true>
                         <<<grid, TM::kThreadsWg, 0, st>>>(a);
                 else
-                    norm_backward_kernel<xt.value, ft.value, w.value, c.value, whole.value, false>
+                    norm_backward_kernel<xt.value, ft.value, w.value, c.value, l.value, whole.value, false>
                         <<<grid, TM::kThreadsWg, 0, st>>>(a);
                 return 0;
             });

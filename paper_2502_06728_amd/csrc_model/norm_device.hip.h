@@ -2,7 +2,8 @@
 // workgroup, sums over a row, the launch by width.
 //
 // A row is taken by a team of W wavefronts, a lane C vectors of eight features.  Up to 512 features a team is
-// one wavefront, which needs no barrier (four teams a workgroup); wider rows take a workgroup.
+// one wavefront or a part of L lanes of one, which needs no barrier (several teams a workgroup); wider rows take a
+// workgroup.
 #pragma once
 
 #include <type_traits>
@@ -15,11 +16,12 @@ namespace model {
 constexpr int64_t kMaxNormWidth = 16384;
 
 // WHOLE: rows of a multiple of eight features, a lane's vectors are whole or empty.
-template <int W, int C, bool WHOLE>
+template <int W, int C, int L, bool WHOLE>
 struct Team {
+    static_assert(W == 1 || L == kLanes, "a part of a wavefront is a team by itself");
     static constexpr int kWavesWg = W == 1 ? 4 : W;
     static constexpr int kThreadsWg = kWavesWg * kLanes;
-    static constexpr int kTeamsWg = kWavesWg / W;
+    static constexpr int kTeamsWg = kThreadsWg / (W * L);
     // A lane of a workgroup of 1,024 has 128 registers: not enough to hold the parameters and the next row too.
     static constexpr bool kLean = W >= 16;
     static constexpr int kSlots = 2 * kWavesWg * 4;    // floats of LDS for sums
@@ -30,11 +32,11 @@ struct Team {
     __device__ __forceinline__ explicit Team(float* l) : lds(l) {}
     static __device__ __forceinline__ int wave() { return threadIdx.x / kLanes % W; }
     static __device__ __forceinline__ int64_t index() {     // of the team in the launch
-        return static_cast<int64_t>(blockIdx.x) * kTeamsWg + threadIdx.x / kLanes / W;
+        return static_cast<int64_t>(blockIdx.x) * kTeamsWg + threadIdx.x / (W * L);
     }
     // first feature of vector c: lanes of a wavefront side by side
     static __device__ __forceinline__ int feature(int c) {
-        return 8 * ((c * W + wave()) * kLanes + static_cast<int>(threadIdx.x % kLanes));
+        return 8 * ((c * W + wave()) * L + static_cast<int>(threadIdx.x % L));
     }
     static __device__ __forceinline__ int count(int c, int D) {
         const int left = D - feature(c);
@@ -54,10 +56,20 @@ struct Team {
         else if (dtype == DETO_BF16) unpack8<DETO_BF16>(load<DETO_BF16>(base, row, c, D), v);
         else unpack8<DETO_F16>(load<DETO_F16>(base, row, c, D), v);
     }
+    // (once: past the caches)
     template <int DT>
-    static __device__ __forceinline__ void store(void* base, int64_t row, int c, int D, const float (&v)[8]) {
+    static __device__ __forceinline__ void store(void* base, int64_t row, int c, int D, const float (&v)[8],
+                                                 bool once = false) {
         if constexpr (!WHOLE) store8<DT>(base, row + feature(c), v, count(c, D));
-        else if (feature(c) < D) store8<DT>(base, row + feature(c), v, 8);
+        else if (feature(c) < D) {
+            if (once) {
+                asm volatile("");        // (or the two stores become one, without the hint)
+                store8<DT, true>(base, row + feature(c), v, 8);
+                asm volatile("");
+            } else {
+                store8<DT>(base, row + feature(c), v, 8);
+            }
+        }
     }
     // N sums over the row, in every lane.  Two sets of slots in turn: one barrier a sum, since a wavefront that
     // writes a set again has passed the barrier of the set between, which all reach after reading this one.
@@ -65,7 +77,7 @@ struct Team {
     __device__ __forceinline__ void sum(float (&v)[N]) {
         static_assert(N <= 4, "slots");
 #pragma unroll
-        for (int i = 0; i < N; ++i) v[i] = wave_sum(v[i]);
+        for (int i = 0; i < N; ++i) v[i] = lanes_sum<L>(v[i]);
         if constexpr (W > 1) {
             float* at = lds + parity * kWavesWg * 4;
             if (threadIdx.x % kLanes == 0) {
@@ -87,16 +99,18 @@ struct Team {
 // Teams by width, for a generic lambda that takes Team's arguments as types.
 template <class F>
 inline void by_width(int64_t D, F f) {
-    auto g = [&](auto w, auto c) {
-        if (D % 8 == 0) f(w, c, std::true_type{});
-        else f(w, c, std::false_type{});
+    auto g = [&](auto w, auto c, auto l) {
+        if (D % 8 == 0) f(w, c, l, std::true_type{});
+        else f(w, c, l, std::false_type{});
     };
-    if (D <= 512) g(Type<1>{}, Type<1>{});
-    else if (D <= 1024) g(Type<2>{}, Type<1>{});
-    else if (D <= 2048) g(Type<4>{}, Type<1>{});
-    else if (D <= 4096) g(Type<8>{}, Type<1>{});
-    else if (D <= 8192) g(Type<16>{}, Type<1>{});
-    else g(Type<16>{}, Type<2>{});
+    if (D <= 128) g(Type<1>{}, Type<1>{}, Type<16>{});
+    else if (D <= 256) g(Type<1>{}, Type<1>{}, Type<32>{});
+    else if (D <= 512) g(Type<1>{}, Type<1>{}, Type<64>{});
+    else if (D <= 1024) g(Type<2>{}, Type<1>{}, Type<64>{});
+    else if (D <= 2048) g(Type<4>{}, Type<1>{}, Type<64>{});
+    else if (D <= 4096) g(Type<8>{}, Type<1>{}, Type<64>{});
+    else if (D <= 8192) g(Type<16>{}, Type<1>{}, Type<64>{});
+    else g(Type<16>{}, Type<2>{}, Type<64>{});
 }
 
 inline bool valid_kind(int k) { return k >= DETO_NORM_NONE && k <= DETO_NORM_LAYER; }
