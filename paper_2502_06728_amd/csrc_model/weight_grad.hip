@@ -26,17 +26,25 @@ constexpr int kRowBytes = kDepth * 2;   // of an LDS column
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 
-template <int BM_, int BN_, int WM_, int WN_>
+// BM, BN: of a workgroup's tile; WM, WN: of a wavefront's part of it; GROUPS of wavefronts that take the tile's rows t
+// in turns of their own and add up their sums at the end.
+template <int BM_, int BN_, int WM_, int WN_, int GROUPS_ = 1>
 struct Tile {
-    static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_;   // of a workgroup, of a wavefront: n, k
-    static constexpr int kThreads = (BM / WM) * (BN / WN) * kLanes;
-    static_assert((kDepth / 4) * (BM / 8) % kThreads == 0 && (kDepth / 4) * (BN / 8) % kThreads == 0, "");
-    static constexpr int kUnitsA = (kDepth / 4) * (BM / 8) / kThreads;
-    static constexpr int kUnitsB = (kDepth / 4) * (BN / 8) / kThreads;
-    static constexpr int lds(int terms) { return 2 * (BM * terms + BN) * kRowBytes; }
+    static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, GROUPS = GROUPS_;
+    static constexpr int kGroup = (BM / WM) * (BN / WN) * kLanes, kThreads = kGroup * GROUPS;
+    static_assert((kDepth / 4) * (BM / 8) % kGroup == 0 && (kDepth / 4) * (BN / 8) % kGroup == 0, "");
+    static constexpr int kUnitsA = (kDepth / 4) * (BM / 8) / kGroup;
+    static constexpr int kUnitsB = (kDepth / 4) * (BN / 8) / kGroup;
+    static constexpr int step_lds(int terms) { return (BM * terms + BN) * kRowBytes; }
+    // two buffers of a step; groups have one each, and their sums in the end
+    static constexpr int lds(int terms) {
+        const int steps = (GROUPS > 1 ? GROUPS : 2) * step_lds(terms), sums = GROUPS > 1 ? GROUPS * BM * BN * 4 : 0;
+        return steps > sums ? steps : sums;
+    }
 };
 using Large = Tile<256, 256, 128, 64>;
 using Small = Tile<128, 128, 64, 64>;
+using Grouped = Tile<64, 64, 64, 64, 4>;
 
 struct Args {
     int64_t T, N, K;
@@ -106,7 +114,7 @@ struct Loader {
         : a(args), n0(n), k0(k), end(e) {}
 
     // Units of eight columns and four rows: rows 4 (u / units a row) of the step.
-    static __device__ __forceinline__ int unit(int i) { return threadIdx.x + i * TL::kThreads; }
+    static __device__ __forceinline__ int unit(int i) { return threadIdx.x % TL::kGroup + i * TL::kGroup; }
     // the step's first row, and how many it has
     __device__ __forceinline__ int64_t from(int64_t t) const { return t < end ? t : end - 1; }
     __device__ __forceinline__ int rows(int64_t t) const {
@@ -297,11 +305,12 @@ __device__ __forceinline__ void each_of(F f) {
     }
 }
 
-template <int DT, class TL, int MODE>
-__global__ __launch_bounds__(TL::kThreads) void weight_grad_kernel(Args a) {
-    extern __shared__ __align__(16) char lds[];
-    constexpr int kTermsA = kTerms<DT>;
-    constexpr int kBytesA = TL::BM * kRowBytes, kBuffer = (TL::BM * kTermsA + TL::BN) * kRowBytes;
+// a workgroup's tile and split
+struct Place {
+    int64_t n0, k0, split;
+};
+template <class TL>
+__device__ __forceinline__ Place place_of(const Args& a) {
     // Workgroups go to the chip's eight parts in turn: a part takes a run of tiles, four high, whose operands
     // its own cache then holds for all of them.
     const unsigned all = gridDim.x, part = blockIdx.x % 8, each = all / 8, more_parts = all % 8;
@@ -310,8 +319,58 @@ __global__ __launch_bounds__(TL::kThreads) void weight_grad_kernel(Args a) {
     const int tile = id % tiles, tiles_n = tiles / a.tiles_k;
     const int band = tile / (kBand * a.tiles_k), within = tile % (kBand * a.tiles_k);
     const int high = tiles_n - band * kBand < kBand ? tiles_n - band * kBand : kBand;
-    const int64_t n0 = static_cast<int64_t>(band * kBand + within % high) * TL::BM;
-    const int64_t k0 = static_cast<int64_t>(within / high) * TL::BN;
+    return {static_cast<int64_t>(band * kBand + within % high) * TL::BM, static_cast<int64_t>(within / high) * TL::BN,
+            split};
+}
+
+// where a split's sums go: to its part of the workspace, if there are several
+__device__ __forceinline__ deto_rows output_of(const Args& a, int64_t split) {
+    const deto_rows partial = {a.parts + split * a.N * a.K, a.K, DETO_F32, 0};
+    return a.splits > 1 ? partial : a.dw;
+}
+template <class F>
+__device__ __forceinline__ void by_output(const deto_rows& out, F f) {
+    if (out.dtype == DETO_F32) f(Type<DETO_F32>{});
+    else if (out.dtype == DETO_BF16) f(Type<DETO_BF16>{});
+    else f(Type<DETO_F16>{});
+}
+
+// The 32 x 32 block at (n, k): lane l holds column l % 32, rows 8 (r / 4) + 4 (l / 32) + r % 4.
+template <int OUT>
+__device__ __forceinline__ void write_block(const Args& a, const deto_rows& out, bool add, int64_t n, int64_t k,
+                                            const f32x16& v) {
+    const int lane = threadIdx.x % kLanes;
+    n += 4 * (lane / 32);
+    k += lane % 32;
+    if (k >= a.K) return;
+    const int rows_left = a.N - n < 32 ? static_cast<int>(a.N - n) : 32;
+    char* const at = static_cast<char*>(out.data) + (n * out.ld + k) * kSize<OUT>;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+        const int down = 8 * (r / 4) + r % 4;
+        if (down < rows_left) {
+            char* const row = at + down * out.ld * kSize<OUT>;
+            float s = v[r];
+            if (add) s += load1<OUT>(row, 0);
+            store1<OUT>(row, 0, s);
+        }
+    }
+}
+
+// What this wavefront wrote to LDS is there for its reads, and what it read is read: the compiler keeps the order, and
+// LDS keeps that of one wavefront.
+__device__ __forceinline__ void ordered() {
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+}
+
+template <int DT, class TL, int MODE>
+__global__ __launch_bounds__(TL::kThreads) void weight_grad_kernel(Args a) {
+    extern __shared__ __align__(16) char lds[];
+    constexpr int kTermsA = kTerms<DT>;
+    constexpr int kBytesA = TL::BM * kRowBytes, kBuffer = (TL::BM * kTermsA + TL::BN) * kRowBytes;
+    const Place at = place_of<TL>(a);
+    const int64_t n0 = at.n0, k0 = at.k0, split = at.split;
     const int64_t t0 = split * a.span;
     const int64_t end = t0 + a.span < a.T ? t0 + a.span : a.T;
     const int lane = threadIdx.x % kLanes, wave = threadIdx.x / kLanes;
@@ -329,8 +388,8 @@ __global__ __launch_bounds__(TL::kThreads) void weight_grad_kernel(Args a) {
     UnitB ub[TL::kUnitsB];
     const Loader<DT, TL, MODE> loader(a, n0, k0, end);
     // (A's and B's units lie alike over their columns where the tile is square)
-    auto place = [&](int i, int wide) { return (threadIdx.x + i * TL::kThreads) % (wide / 8) * 8; };
-    auto quarter = [&](int i, int wide) { return (threadIdx.x + i * TL::kThreads) / (wide / 8); };
+    auto place = [&](int i, int wide) { return loader.unit(i) % (wide / 8) * 8; };
+    auto quarter = [&](int i, int wide) { return loader.unit(i) / (wide / 8); };
     auto put_a = [&](char* at, auto q) {
 #pragma unroll
         for (int i = 0; i < TL::kUnitsA; ++i)
@@ -429,35 +488,110 @@ __global__ __launch_bounds__(TL::kThreads) void weight_grad_kernel(Args a) {
         each_of<kBlocks>([&](auto i) { multiply(Type<3>{}, i); });
         __syncthreads();
     }
-    // Lane l holds column l % 32, rows 8 (r / 4) + 4 (l / 32) + r % 4 of a 32 x 32 block.
-    const deto_rows partial = {a.parts + split * a.N * a.K, a.K, DETO_F32, 0};
-    const deto_rows& out = a.splits > 1 ? partial : a.dw;
+    const deto_rows out = output_of(a, split);
     const bool add = a.accumulate && a.splits == 1;
-    const int64_t n = n0 + wm + 4 * (lane / 32), k = k0 + wn + lane % 32;
-    const int rows_left = static_cast<int>(a.N - n < TL::WM ? a.N - n : TL::WM);
     auto write = [&](auto type) {
-        constexpr int OUT = decltype(type)::value;
-        char* const at = static_cast<char*>(out.data) + (n * out.ld + k) * kSize<OUT>;
 #pragma unroll
         for (int i = 0; i < TL::WM / 32; ++i)
 #pragma unroll
-            for (int r = 0; r < 16; ++r) {
-                const int down = i * 32 + 8 * (r / 4) + r % 4;
-                char* const row = at + down * out.ld * kSize<OUT>;
-                if (down < rows_left) {
-#pragma unroll
-                    for (int j = 0; j < TL::WN / 32; ++j)
-                        if (k + j * 32 < a.K) {
-                            float v = acc[i][j][r];
-                            if (add) v += load1<OUT>(row, j * 32);
-                            store1<OUT>(row, j * 32, v);
-                        }
-                }
-            }
+            for (int j = 0; j < TL::WN / 32; ++j)
+                write_block<decltype(type)::value>(a, out, add, n0 + wm + i * 32, k0 + wn + j * 32, acc[i][j]);
     };
-    if (out.dtype == DETO_F32) write(Type<DETO_F32>{});
-    else if (out.dtype == DETO_BF16) write(Type<DETO_BF16>{});
-    else write(Type<DETO_F16>{});
+    by_output(out, write);
+}
+
+// The same for products of few tiles: a wavefront takes a 64 x 64 tile by itself, four of them a quarter of the rows t
+// each, and their sums meet in LDS.  (1,021 x 770 x 519 bf16, us: tiles of 128 split in workgroups and joined by a
+// second launch 20, this 12.)  Wavefronts share nothing until then: what one writes to LDS only it reads, in order.
+template <int DT, class TL, int MODE>
+__global__ __launch_bounds__(TL::kThreads) void weight_grad_groups_kernel(Args a) {
+    static_assert(TL::kGroup == kLanes && TL::GROUPS == 4 && TL::WM == 64 && TL::WN == 64, "a wavefront is a group");
+    extern __shared__ __align__(16) char lds[];
+    constexpr int kTermsA = kTerms<DT>, kBytesA = TL::BM * kRowBytes;
+    const Place at = place_of<TL>(a);
+    const int lane = threadIdx.x % kLanes, wave = threadIdx.x / kLanes;
+    const int64_t t0 = at.split * a.span;
+    const int64_t end = t0 + a.span < a.T ? t0 + a.span : a.T;
+    const int64_t steps = (end - t0 + kDepth - 1) / kDepth, each = (steps + TL::GROUPS - 1) / TL::GROUPS;
+    const int64_t first = t0 + wave * each * kDepth;
+    const int64_t last = first + each * kDepth < end ? first + each * kDepth : end;
+    f32x16 acc[2][2];
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) acc[i / 2][i % 2][r] = 0.f;
+    if (first < last) {
+        UnitA<DT> ua[TL::kUnitsA];
+        UnitB ub[TL::kUnitsB];
+        const Loader<DT, TL, MODE> loader(a, at.n0, at.k0, last);
+        char* const mine = lds + wave * TL::step_lds(kTermsA);
+        loader.load_a(first, ua);
+        loader.load_b(first, ub);
+        for (int64_t t = first; t < last; t += kDepth) {
+            loader.settle_a(t, ua);
+            loader.settle_b(t, ub);
+            ordered();                       // the step before is read
+            each_of<4>([&](auto q) {
+#pragma unroll
+                for (int i = 0; i < TL::kUnitsA; ++i)
+                    store_a<DT, TL, q.value>(ua[i], mine, loader.unit(i) % 8 * 8, loader.unit(i) / 8);
+            });
+#pragma unroll
+            for (int i = 0; i < TL::kUnitsB; ++i) {
+                float scale[4];
+#pragma unroll
+                for (int r = 0; r < 4; ++r) scale[r] = act8_scale(ub[i].exps[r]);
+                each_of<8>([&](auto j) {
+                    store_b<j.value>(ub[i], scale, mine + kTermsA * kBytesA, loader.unit(i) % 8 * 8,
+                                     loader.unit(i) / 8);
+                });
+            }
+            ordered();
+            if (t + kDepth < last) {
+                loader.load_a(t + kDepth, ua);
+                loader.load_b(t + kDepth, ub);
+            }
+#pragma unroll
+            for (int s = 0; s < kDepth / 16; ++s) {
+                const int t8 = 2 * s + lane / 32;
+                bf16x8 fa[kTermsA][2], fb[2];
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    fb[i] = *reinterpret_cast<const bf16x8*>(mine + kTermsA * kBytesA + lds_at(i * 32 + lane % 32, t8));
+#pragma unroll
+                    for (int term = 0; term < kTermsA; ++term)
+                        fa[term][i] = *reinterpret_cast<const bf16x8*>(mine + term * kBytesA +
+                                                                       lds_at(i * 32 + lane % 32, t8));
+                }
+#pragma unroll
+                for (int term = 0; term < kTermsA; ++term)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        acc[i / 2][i % 2] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fa[term][i / 2], fb[i % 2],
+                                                                                    acc[i / 2][i % 2], 0, 0, 0);
+            }
+        }
+    }
+    __syncthreads();                         // the steps' LDS is free
+    float* const sums = reinterpret_cast<float*>(lds);
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) sums[((wave * 4 + i) * 16 + r) * kLanes + lane] = acc[i / 2][i % 2][r];
+    __syncthreads();
+    f32x16 all;                              // a 32 x 32 block of the tile for each wavefront
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+        float v[4];
+#pragma unroll
+        for (int g = 0; g < 4; ++g) v[g] = sums[((g * 4 + wave) * 16 + r) * kLanes + lane];
+        all[r] = (v[0] + v[1]) + (v[2] + v[3]);
+    }
+    const deto_rows out = output_of(a, at.split);
+    const bool add = a.accumulate && a.splits == 1;
+    by_output(out, [&](auto type) {
+        write_block<decltype(type)::value>(a, out, add, at.n0 + wave / 2 * 32, at.k0 + wave % 2 * 32, all);
+    });
 }
 
 // Adds the splits' sums: a wavefront takes 256 columns of a row, a lane four, the loads of eight splits side by side.
@@ -506,30 +640,35 @@ bool bad_shape(int64_t T, int64_t N, int64_t K) {
     return T < 0 || T > kMost || N < 1 || N > kMost || K < 1 || K > kMost;
 }
 
+enum Kind { kLarge, kSmall, kGrouped };
+
 struct Plan {
-    bool large;
+    int kind;
     int64_t tiles, tiles_k, splits, span;
     double us;
 };
 
 // The splits of T that take least time by what was measured (us): a step of 64 rows 0.95 in a workgroup of small tiles
 // that has a CU to itself and 1.25 in one of two; 1.4 and 2.0 with two and three terms, which leave room for one; 1.9 in
-// one of large tiles; 5 to start and to write the tile; 3 for the second launch, which the splits' sums go to and come
-// from at 3.5 TB/s.
-Plan plan_with(int64_t T, int64_t N, int64_t K, bool large, int terms) {
-    const int64_t b = large ? Large::BM : Small::BM;
+// one of large tiles; 1.95 (2.7 in one workgroup of two), 2.8 and 4.0 in a wavefront of grouped ones, which share the
+// steps between four; 5 to start and to write the tile; 3 for the second launch, which the splits' sums go to and come from at 3.5 TB/s.
+Plan plan_with(int64_t T, int64_t N, int64_t K, int kind, int terms) {
+    const int64_t b = kind == kLarge ? Large::BM : kind == kSmall ? Small::BM : Grouped::BM;
     Plan best = {};
     const int64_t tiles_k = (K + b - 1) / b, tiles = (N + b - 1) / b * tiles_k;
     const int64_t steps = T ? (T + kDepth - 1) / kDepth : 1;
     for (int64_t splits = 1; splits <= 32 && splits <= steps; ++splits) {
         const int64_t each = (steps + splits - 1) / splits;
         if (splits > 1 && each * (splits - 1) >= steps) continue;      // an empty split
-        const int64_t slots = large || terms > 1 ? 256 : 512;
-        const double step = large ? 1.9 : terms == 2 ? 1.4 : terms == 3 ? 2.0 : tiles * splits > 256 ? 1.25 : 0.95;
-        double us = static_cast<double>((tiles * splits + slots - 1) / slots) * (step * static_cast<double>(each) + 5.0);
+        const int64_t slots = kind == kLarge || terms > 1 ? 256 : 512;
+        const double step = kind == kLarge ? 1.9
+                            : kind == kGrouped ? (terms == 2 ? 2.8 : terms == 3 ? 4.0 : tiles * splits > 256 ? 2.7 : 1.95)
+                            : terms == 2 ? 1.4 : terms == 3 ? 2.0 : tiles * splits > 256 ? 1.25 : 0.95;
+        const int64_t turns = kind == kGrouped ? (each + Grouped::GROUPS - 1) / Grouped::GROUPS : each;
+        double us = static_cast<double>((tiles * splits + slots - 1) / slots) * (step * static_cast<double>(turns) + 5.0);
         if (splits > 1)
             us += 3.0 + 8.0 * static_cast<double>(splits) * static_cast<double>(N) * static_cast<double>(K) / 3.5e6;
-        if (splits == 1 || us < best.us) best = {large, tiles, tiles_k, splits, each * kDepth, us};
+        if (splits == 1 || us < best.us) best = {kind, tiles, tiles_k, splits, each * kDepth, us};
     }
     return best;
 }
@@ -542,12 +681,15 @@ int mode_of(const Args& a) {
     return row < most && a.x.ld_codes < most && a.x.ld_exps < most && a.N >= 8 && a.K >= 8 ? kReach : kFar;
 }
 
-// One term (bf16 dy) may take large tiles.
-Plan plan_of(int64_t T, int64_t N, int64_t K, bool may_be_large, int terms) {
-    const Plan small = plan_with(T, N, K, false, terms);
-    if (!may_be_large || terms > 1) return small;
-    const Plan large = plan_with(T, N, K, true, 1);
-    return large.us < small.us ? large : small;
+// One term (bf16 dy) may take large tiles; far rows take small ones.
+Plan plan_of(int64_t T, int64_t N, int64_t K, bool far, int terms) {
+    Plan best = plan_with(T, N, K, kSmall, terms);
+    if (far) return best;
+    const Plan grouped = plan_with(T, N, K, kGrouped, terms);
+    if (grouped.us < best.us) best = grouped;
+    if (terms > 1) return best;
+    const Plan large = plan_with(T, N, K, kLarge, 1);
+    return large.us < best.us ? large : best;
 }
 
 }  // namespace
@@ -561,9 +703,9 @@ extern "C" {
 int64_t detonation_act8_weight_grad_workspace(int64_t T, int64_t N, int64_t K) {
     if (bad_shape(T, N, K)) return -1;
     int64_t most = 0;
-    for (bool may_be_large : {true, false})
+    for (bool far : {true, false})
         for (int terms : {1, 2, 3}) {
-            const Plan p = plan_of(T, N, K, may_be_large, terms);
+            const Plan p = plan_of(T, N, K, far, terms);
             if (p.splits > 1 && p.splits > most) most = p.splits;
         }
     return most * N * K * static_cast<int64_t>(sizeof(float));
@@ -588,7 +730,7 @@ int detonation_act8_weight_grad(int64_t T, int64_t N, int64_t K, const deto_rows
         a.x.ld_exps = (K + DETO_ACT8_GROUP - 1) / DETO_ACT8_GROUP;
     }
     const int mode = T > 0 ? mode_of(a) : static_cast<int>(kNear);
-    const Plan p = plan_of(T, N, K, mode != kFar, dtype == DETO_BF16 ? 1 : dtype == DETO_F16 ? 2 : 3);
+    const Plan p = plan_of(T, N, K, mode == kFar, dtype == DETO_BF16 ? 1 : dtype == DETO_F16 ? 2 : 3);
     if (p.splits > 1 && !workspace) return DETO_ERR_NULL;
     if (p.splits > 1 && !is_aligned(workspace, 16)) return DETO_ERR_ALIGN;
     if (p.tiles > 0x7FFFFFFF / p.splits) return DETO_ERR_UNSUPPORTED;
@@ -598,18 +740,26 @@ int detonation_act8_weight_grad(int64_t T, int64_t N, int64_t K, const deto_rows
     const hipStream_t st = static_cast<hipStream_t>(stream);
     const unsigned grid = static_cast<unsigned>(p.tiles * p.splits);
     fresh();
-    if (p.large) {
+    if (p.kind == kLarge) {
         if (mode == kNear)
             weight_grad_kernel<DETO_BF16, Large, kNear><<<grid, Large::kThreads, Large::lds(1), st>>>(a);
         else
             weight_grad_kernel<DETO_BF16, Large, kReach><<<grid, Large::kThreads, Large::lds(1), st>>>(a);
     } else {
         by_type(dtype, [&](auto dt) {
-            constexpr int kLds = Small::lds(kTerms<dt.value>);
-            if (mode == kNear) weight_grad_kernel<dt.value, Small, kNear><<<grid, Small::kThreads, kLds, st>>>(a);
-            else if (mode == kReach)
-                weight_grad_kernel<dt.value, Small, kReach><<<grid, Small::kThreads, kLds, st>>>(a);
-            else weight_grad_kernel<dt.value, Small, kFar><<<grid, Small::kThreads, kLds, st>>>(a);
+            constexpr int DT = dt.value, kLds = Small::lds(kTerms<DT>), kLdsGrouped = Grouped::lds(kTerms<DT>);
+            if (p.kind == kGrouped) {
+                if (mode == kNear)
+                    weight_grad_groups_kernel<DT, Grouped, kNear><<<grid, Grouped::kThreads, kLdsGrouped, st>>>(a);
+                else
+                    weight_grad_groups_kernel<DT, Grouped, kReach><<<grid, Grouped::kThreads, kLdsGrouped, st>>>(a);
+            } else if (mode == kNear) {
+                weight_grad_kernel<DT, Small, kNear><<<grid, Small::kThreads, kLds, st>>>(a);
+            } else if (mode == kReach) {
+                weight_grad_kernel<DT, Small, kReach><<<grid, Small::kThreads, kLds, st>>>(a);
+            } else {
+                weight_grad_kernel<DT, Small, kFar><<<grid, Small::kThreads, kLds, st>>>(a);
+            }
             return 0;
         });
     }

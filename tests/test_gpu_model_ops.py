@@ -639,6 +639,22 @@ def test_weight_grad_of_distant_rows(gpu):
     assert_near(dw, d.t() @ x, d.abs().t() @ x.abs(), 3 * T + 40, "dw")
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("T,N,K", [(500, 1800, 1900), (500, 1801, 1901), (4100, 768, 776), (4100, 769, 777)])
+def test_weight_grad_of_many_tiles(gpu, dtype, T, N, K):
+    """Sizes at which workgroups share tiles of 128, in one split of T and in several."""
+    say(dtype, T, N, K)
+    g = torch.Generator(device=DEV).manual_seed(1)
+    dy = torch.randn((T, N), generator=g, device=DEV).to(dtype)
+    x8 = empty_act8(T, K)
+    ops.detonation_act8_encode(torch.randn((T, K), generator=g, device=DEV), x8)
+    d, v = ref.double(dy), ref.act8_values(x8.codes, x8.exps)
+    for out in (F32, BF16):
+        dw = like(N, K, out)
+        ops.detonation_act8_weight_grad(dy, x8, dw, workspace=scratch(ops.act8_weight_grad_workspace(T, N, K)))
+        assert_near(dw, d.t() @ v, d.abs().t() @ v.abs(), 3 * T + 40, "dw")
+
+
 def test_weight_grad_large_tiles(gpu):
     T, N, K = 136, 2050, 6100
     say(T, N, K)
