@@ -24,6 +24,8 @@ typedef u32x4 u32x4_any2 __attribute__((aligned(2)));
 typedef u32x4 u32x4_any4 __attribute__((aligned(4)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef u32x2 u32x2_any1 __attribute__((aligned(1)));
+typedef u32x2 u32x2_any2 __attribute__((aligned(2)));
+typedef uint32_t u32_any1 __attribute__((aligned(1)));
 typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef float f32x2 __attribute__((ext_vector_type(2)));
@@ -246,6 +248,29 @@ __device__ __forceinline__ u32x2 act8_encode8(const float (&v)[8], uint32_t& exp
         q[w] = word;
     }
     return q;
+}
+
+// The same for four values of each of eight lanes in a row.
+__device__ __forceinline__ uint32_t act8_encode4(const float (&v)[4], uint32_t& exponent) {
+    float top = 0.f;
+    bool odd = false;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        top = fmaxf(top, fabsf(v[j]));
+        odd |= v[j] != v[j];
+    }
+    top = quad_max(odd ? __builtin_inff() : top);
+    top = fmaxf(top, bits_f32(__builtin_amdgcn_mov_dpp(f32_bits(top), 0x141, 0xF, 0xF, true)));  // the other four
+    const bool finite = top < __builtin_inff();
+    exponent = finite ? act8_exponent(top) : 255u;
+    const float inv = finite ? bits_f32((254u - exponent) << 23) : 0.f;
+    uint32_t word = 0;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const float x = finite ? rintf(v[j] * inv) : 0.f;
+        word |= (static_cast<uint32_t>(static_cast<int>(x)) & 0xFFu) << (8 * j);
+    }
+    return word;
 }
 
 __device__ __forceinline__ float act8_scale(uint32_t exponent) {

@@ -38,11 +38,9 @@ __device__ __forceinline__ void normalise(TM& team, float (&v)[C][8], int kind, 
         team.sum(s);
         const float mean = s[0] * inv_d;
 #pragma unroll
-        for (int c = 0; c < C; ++c) {
-            const int n = TM::count(c, D);
+        for (int c = 0; c < C; ++c)
 #pragma unroll
-            for (int j = 0; j < 8; ++j) v[c][j] = j < n ? v[c][j] - mean : 0.f;
-        }
+            for (int j = 0; j < 8; ++j) v[c][j] = TM::has(c, j, D) ? v[c][j] - mean : 0.f;
     }
     float q[1] = {0.f};
 #pragma unroll
@@ -59,8 +57,8 @@ __device__ __forceinline__ void normalise(TM& team, float (&v)[C][8], int kind, 
 
 // LAYER: one of the norms is one, or has a bias.  (Without, its registers are not held.)
 template <int XT, int FT, int W, int C, int L, bool WHOLE, bool LAYER>
-__global__ __launch_bounds__((Team<W, C, L, WHOLE>::kThreadsWg)) void norm_residual_kernel(Args a) {
-    using TM = Team<W, C, L, WHOLE>;
+__global__ __launch_bounds__((Team<W, C, L, WHOLE, WHOLE && XT == DETO_F32>::kThreadsWg)) void norm_residual_kernel(Args a) {
+    using TM = Team<W, C, L, WHOLE, WHOLE && XT == DETO_F32>;
     __shared__ float lds[TM::kSlots];
     TM team(lds);
     const int D = a.D;
@@ -126,14 +124,13 @@ __global__ __launch_bounds__((Team<W, C, L, WHOLE>::kThreadsWg)) void norm_resid
             if constexpr (TM::kLean) params_of_norms(true, false);
 #pragma unroll
             for (int c = 0; c < C; ++c) {
-                const int n = TM::count(c, D);
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
                     float u = v[c][j];
                     if (post) u *= p.w_post[c][j];
                     if constexpr (LAYER)
                         if (post) u += p.b_post[c][j];
-                    x[c][j] = WHOLE || j < n ? x[c][j] + p.gate[c][j] * u : 0.f;
+                    x[c][j] = TM::has(c, j, D) ? x[c][j] + p.gate[c][j] * u : 0.f;
                 }
             }
 #pragma unroll
@@ -144,15 +141,14 @@ __global__ __launch_bounds__((Team<W, C, L, WHOLE>::kThreadsWg)) void norm_resid
         if constexpr (TM::kLean) params_of_norms(false, true);
 #pragma unroll
         for (int c = 0; c < C; ++c) {
-            const int d = TM::feature(c), n = TM::count(c, D);
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
                 x[c][j] *= p.w_pre[c][j];
                 if constexpr (LAYER) x[c][j] += p.b_pre[c][j];
-                if (!WHOLE && j >= n) x[c][j] = 0.f;
+                if (!TM::has(c, j, D)) x[c][j] = 0.f;
             }
             if (a.y.data) TM::template store<FT>(a.y.data, t * a.y.ld, c, D, x[c], a.once);
-            if (a.y8.codes) act8_put(a.y8, t, d, x[c], n);
+            if (a.y8.codes) TM::put8(a.y8, t, c, D, x[c]);
         }
     }
 }
