@@ -284,20 +284,18 @@ __global__ __launch_bounds__(kJoinThreads) void norm_join_kernel(JoinArgs a, int
     if (lane == 0 && col < a.D) a.out[i][(gate ? (y - a.outs) * a.D : 0) + col] = lds[0][c];
 }
 
-// Teams that are wanted: as many as run side by side, three wavefronts a SIMD, two of the kernels with biases or
-// partial vectors (a workgroup of sixteen: four).  A second round of teams, shorter than the first, costs more than it
-// adds (16,384 x 2,048: 1,024 teams 144 us, 768 127 us).
-int64_t wanted_teams(int64_t D, bool lean) {
+// Teams that are wanted: two wavefronts a SIMD (a workgroup of sixteen: four).  What more of them would hide of memory's
+// latency, their sums' way to the workspace and back costs again (16,384 x 2,048, fp32 and bf16, us: 1,024 teams 152, 768
+// 128, 512 123; 8,192 x 4,096: 384 teams 142, 256 127).
+int64_t wanted_teams(int64_t D) {
     int64_t teams = 0;
-    by_width(D, [&](auto w, auto, auto l, auto whole) {
-        teams = w.value >= 16 ? 256 : (lean && whole.value ? 3072 : 2048) * (kLanes / l.value) / w.value;
-    });
+    by_width(D, [&](auto w, auto, auto l, auto) { teams = w.value >= 16 ? 256 : 2048 * (kLanes / l.value) / w.value; });
     return teams;
 }
 
-// lean: no biases.  A team takes two rows at least (1,379 x 771: one row 28 us, two 21, four 23).
-Deal deal_rows(const deto_norm_residual* cfg, int64_t T, int64_t D, bool lean) {
-    int64_t most = wanted_teams(D, lean);
+// A team takes two rows at least (1,379 x 771: one row 28 us, two 21, four 23).
+Deal deal_rows(const deto_norm_residual* cfg, int64_t T, int64_t D) {
+    int64_t most = wanted_teams(D);
     if (most > T / 2) most = T / 2 > 0 ? T / 2 : 1;
     Deal d = {};
     d.T = T;
@@ -331,7 +329,7 @@ extern "C" {
 
 int64_t detonation_norm_residual_workspace(const deto_norm_residual* cfg, int64_t T, int64_t D) {
     if (check_norm(cfg, T, D)) return -1;
-    return deal_rows(cfg, T, D, true).teams * kSums * D * static_cast<int64_t>(sizeof(float));
+    return deal_rows(cfg, T, D).teams * kSums * D * static_cast<int64_t>(sizeof(float));
 }
 
 int detonation_norm_residual_backward(const deto_norm_residual* cfg, int64_t T, int64_t D,
@@ -373,7 +371,7 @@ int detonation_norm_residual_backward(const deto_norm_residual* cfg, int64_t T, 
     a.D = static_cast<int>(D);
     const bool layer = cfg->pre == DETO_NORM_LAYER || cfg->post == DETO_NORM_LAYER || cfg->b_post || g.b_pre ||
                        g.b_post;
-    a.deal = deal_rows(cfg, T, D, !layer);
+    a.deal = deal_rows(cfg, T, D);
     a.grads = g;
     float* const outs[kSums] = {g.w_pre, g.b_pre, g.w_post, g.b_post, g.gate};
     JoinArgs j = {};
