@@ -15,6 +15,10 @@
 // the list does not hold them (many equal values) is searched K times instead.
 //
 // Backward.  A stream: p = exp(z - m - log s) from the row's saved m and log s.
+//
+// Measured (8,192 rows of 50,304 bf16): forward 149 us = 5.5 TB/s, about ten vector instructions a value behind the loads;
+// backward 270 us = 6.1 TB/s, memory.  1,021 rows of 32,101 fp16 with the 20 best: 27 us, of which memory is 11: one round
+// of workgroups, each a chain of first look, threshold, second look and ranking.
 #include "device.hip.h"
 
 namespace deto {
@@ -519,7 +523,7 @@ bool bad_shape(int64_t T, int64_t V, int top) {
 }
 
 // Few rows take a workgroup of 1,024 threads each (one row of 50,304 bf16 logits with its eight best: 25 pieces and
-// their join 13 us, 1,024 threads @@ us).  Rows that are long even for those are cut in pieces.
+// their join 13 us, 1,024 threads 10 us: 3 of them the exponentials of one CU, the rest a chain of latencies).  Rows that are long even for those are cut in pieces.
 constexpr int64_t kFewRows = 512;
 constexpr int kThreadsFew = 1024, kThreadsMany = 256;
 
