@@ -62,19 +62,25 @@ UNITS = [
 MODEL_UNITS = ["norm_backward.hip", "norm.hip", "act8.hip", "weight_grad.hip", "logprobs.hip"]
 
 
+def _build_host(out: str, src: str, verbose: bool) -> None:
+    """A binding's argument marshalling (host code, CPython's C API).  Without a C compiler or
+    Python.h the binding does all of it in Python, so that is no error."""
+    if os.path.exists(out):
+        os.remove(out)
+    try:
+        _run([*shlex.split(os.environ.get("CC", "cc")), "-O2", "-Wall", "-shared", "-fPIC",
+              "-I" + sysconfig.get_paths()["include"], "-o", out, src], verbose)
+    except (OSError, RuntimeError) as e:
+        print(f"{os.path.relpath(src, _HERE)} is not compiled, the binding goes without it: {e}",
+              file=sys.stderr)
+
+
 def _build_marshal(verbose: bool) -> None:
-    """The bindings' argument marshalling (host code, CPython's C API).  Without a C compiler or
-    Python.h the bindings do all of it in Python, so that is no error."""
-    for out, src in ((MARSHAL, os.path.join(CSRC, "marshal.c")),
-                     (MODEL_MARSHAL, os.path.join(CSRC_MODEL, "marshal.c"))):
-        if os.path.exists(out):
-            os.remove(out)
-        try:
-            _run([*shlex.split(os.environ.get("CC", "cc")), "-O2", "-Wall", "-shared", "-fPIC",
-                  "-I" + sysconfig.get_paths()["include"], "-o", out, src], verbose)
-        except (OSError, RuntimeError) as e:
-            print(f"{os.path.relpath(src, _HERE)} is not compiled, the binding goes without it: {e}",
-                  file=sys.stderr)
+    _build_host(MARSHAL, os.path.join(CSRC, "marshal.c"), verbose)
+
+
+def _build_model_marshal(verbose: bool) -> None:
+    _build_host(MODEL_MARSHAL, os.path.join(CSRC_MODEL, "marshal.c"), verbose)
 
 
 def _run(cmd: list[str], verbose: bool) -> None:
@@ -127,6 +133,7 @@ def build(verbose: bool = False) -> str:
         list(pool.map(lambda c: _run(c, verbose), jobs))
     _run([hipcc, "--offload-arch=gfx950", "-shared", "-fPIC", "-o", lib, *objs], verbose)
     _build_marshal(verbose)
+    _build_model_marshal(verbose)
     # the streaming micro-benchmark (HBM ceiling, counter calibration)
     if lib == LIB:
         _run([hipcc, *HIPCC_FLAGS, "-Wno-unused-result", "-o", MEMBENCH, os.path.join(CSRC, "membench.hip")],
