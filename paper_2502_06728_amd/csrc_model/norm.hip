@@ -106,8 +106,8 @@ __global__ __launch_bounds__((Team<W, C, L, WHOLE, WHOLE && XT == DETO_F32>::kTh
         if constexpr (TM::kLean) load(t);
 #pragma unroll
         for (int c = 0; c < C; ++c) {
-            unpack8<XT>(rx[c], x[c]);
-            if (branch) unpack8<FT>(rf[c], v[c]);
+            TM::template unpack<XT>(rx[c], c, D, x[c]);
+            if (branch) TM::template unpack<FT>(rf[c], c, D, v[c]);
         }
         if constexpr (!TM::kLean)
             if (t + 1 < end) load(t + 1);

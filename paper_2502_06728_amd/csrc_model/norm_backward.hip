@@ -122,10 +122,10 @@ __global__ __launch_bounds__((Team<W, C, L, WHOLE>::kThreadsWg)) void norm_backw
         if constexpr (TM::kLean) load(t);
 #pragma unroll
         for (int c = 0; c < C; ++c) {
-            unpack8<XT>(rx[c], x[c]);
-            unpack8<XT>(ro[c], o[c]);
-            unpack8<FT>(ry[c], G[c]);
-            unpack8<FT>(rf[c], f[c]);
+            TM::template unpack<XT>(rx[c], c, D, x[c]);
+            TM::template unpack<XT>(ro[c], c, D, o[c]);
+            TM::template unpack<FT>(ry[c], c, D, G[c]);
+            TM::template unpack<FT>(rf[c], c, D, f[c]);
         }
         if constexpr (TM::kLean) params_of_pre();
         else if (t + 1 < end) load(t + 1);
