@@ -203,6 +203,7 @@ int detonation_glu_backward(int act, int64_t T, int64_t D, const deto_rows* dh, 
  * dw = [dw +] dy^T x :  dw[n][k] = sum_t dy[t][n] * x[t][k],  x decoded from x8 (exactly).
  *   dy   [T, N];  x8  [T, K];  dw  [N, K] of any of the three types
  *   accumulate  0: dw is written; 1: the product is added to what dw holds
+ * T, N and K are at most 2^30, N * K at most 2^40.
  * Products are exact (fp32 and fp16 dy enter as sums of three or two bf16 numbers), sums are fp32.
  */
 int detonation_act8_weight_grad(int64_t T, int64_t N, int64_t K, const deto_rows* dy,

@@ -638,7 +638,7 @@ __global__ __launch_bounds__(kJoinRows* kLanes) void weight_grad_join_kernel(Arg
 
 bool bad_shape(int64_t T, int64_t N, int64_t K) {
     constexpr int64_t kMost = int64_t{1} << 30;
-    return T < 0 || T > kMost || N < 1 || N > kMost || K < 1 || K > kMost;
+    return T < 0 || T > kMost || N < 1 || N > kMost || K < 1 || K > kMost || N > (int64_t{1} << 40) / K;
 }
 
 enum Kind { kLarge, kSmall, kGrouped };

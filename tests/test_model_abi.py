@@ -175,6 +175,13 @@ def test_weight_grad_refusals(lib):
     assert lib.detonation_act8_weight_grad_workspace(4096, 64, 64) > 0
 
 
+def test_weight_grad_sizes_whose_sums_would_not_be_counted(lib):
+    ws, big = lib.detonation_act8_weight_grad_workspace, 1 << 30
+    assert ws(64, big, big) == -1 and ws(64, 1 << 20, (1 << 20) + 1) == -1 and ws(big + 1, 8, 8) == -1
+    assert lib.detonation_act8_weight_grad(4, big, big, rows(ld=big), act8(ld=big, ld_exps=big), rows(ld=big), 0,
+                                           None, None) == BAD
+
+
 def test_binding_refuses_host_tensors():
     x, y = torch.zeros(4, 64), torch.zeros(4, dtype=torch.int64)
     with pytest.raises(ValueError, match="device"):
