@@ -190,13 +190,15 @@ __global__ __launch_bounds__((Team<W, C, L, WHOLE>::kThreadsWg)) void norm_backw
         float q[2] = {0.f, 0.f};
 #pragma unroll
         for (int c = 0; c < C; ++c) {
+            // (Past the row's end G is -r m1, and absent parameters are ones: it would reach the sums.  Without m1 it is
+            // zero where a lane's vectors are whole or empty.)
             const int n = TM::count(c, D);
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
                 const float v = f[c][j] * rf_;
                 float u = v * w_post[c][j];
                 if constexpr (LAYER) u += b_post[c][j];
-                const float g = WHOLE || j < n ? a.cfg.scale * G[c][j] : 0.f;
+                const float g = (WHOLE && !LAYER) || j < n ? a.cfg.scale * G[c][j] : 0.f;
                 sums[kAtGate][c][j] += g * u;
                 const float h = g * gate[c][j];
                 sums[kAtPost][c][j] += h * v;
