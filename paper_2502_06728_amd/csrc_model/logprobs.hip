@@ -189,9 +189,12 @@ struct Piece {
     }
 };
 
-// r.s and r.w are relative to the product of r.m and unit as rounded.
+// r.s and r.w are relative to the product of r.m and unit as rounded.  (Products are rounded where they stand: fused with the
+// difference, d0 would be the rounding's error instead of 0 for as long as the maximum stays, and the sums off by as
+// many of those as a row has steps.)
 template <int DT, bool ENTROPY>
 __device__ __forceinline__ void see(Seen& r, const Taken<DT>& x, float unit) {
+#pragma clang fp contract(off)
     float m = r.m;
 #pragma unroll
     for (int i = 0; i < kVectors<DT>; ++i)

@@ -9,7 +9,7 @@ from paper_2502_06728_amd import model_ops as ops
 from tests import model_reference as ref
 from tests import test_gpu_model_ops as base
 from tests.model_reference import BF16, F16, F32, assert_near
-from tests.test_gpu_model_ops import ACT, DEV, INF, NAN, TYPES, act8_of, empty_act8, like, normal, rows, say, scratch
+from tests.test_gpu_model_ops import DEV, INF, NAN, TYPES, like, normal, rows, say, scratch
 
 pytestmark = pytest.mark.gpu
 
@@ -45,3 +45,63 @@ def test_norm_gradient_at_widths_that_leave_lanes_empty(gpu, D, pre, post, weigh
     assert_near(df, g[1], 32.0, base.NORM_STEPS, "df")
     for (name, got), want in zip(grads.items(), g[2:]):
         assert_near(got, want, 32.0, base.NORM_STEPS, name)
+
+
+# ------------------------------------------------------------------ log probabilities
+
+def check_sums(x, y, out, scale=1.0):
+    """logp, log s and the entropy by what they are made of, whatever the logits' common offset.
+
+    A thread adds at most V / 256 exponentials one after the other, 64 more roundings are joins, the exponential's own
+    (two units) and those of the maximum's; an exponent d is rounded four times, which a sum weighted by the
+    probabilities counts at most log V + 1 of.  logp rounds its difference of logits four times; the entropy's second sum is of
+    terms d p, each as far off, and d itself adds up to log V + 1."""
+    T, V = x.shape
+    z = ref.double(x)
+    unit, log_v = 2.0 ** -24, math.log(V) + 1
+    m = z.max(1).values
+    d = (z - m[:, None]) * scale
+    log_s = torch.log(torch.exp(d).sum(1))
+    sums = unit * (V / 256 + 64 + 4 * log_v + 2 * log_s)
+    assert torch.equal(out["stats"][:, 0].cpu().double(), m)
+    off = (out["stats"][:, 1].cpu().double() - log_s).abs()
+    assert bool((off <= sums).all()), ("log s", off / unit, sums / unit)
+    scored = (y >= 0) & (y < V)
+    gap = d[torch.arange(T), torch.where(scored, y, 0).cpu()]
+    want = torch.where(scored.cpu(), gap - log_s, torch.zeros_like(gap))
+    got = out["logp"].cpu().double()
+    far = want == -INF
+    assert torch.equal(got[far], want[far])
+    off = (got - want)[~far].abs()
+    assert bool((off <= (sums + unit * (4 * gap.abs() + 2 * want.abs()))[~far]).all()), ("logp", off / unit)
+    p = torch.exp(d - log_s[:, None])
+    H = -torch.where(p > 0, p * (d - log_s[:, None]), torch.zeros_like(p)).sum(1)
+    off = (out["entropy"].cpu().double() - H).abs()
+    assert bool((off <= sums * (2 + 2 * log_v)).all()), ("entropy", off / unit)
+
+
+def run_and_check_sums(x, y, scale=1.0, keep=None):
+    keep = torch.arange(x.shape[0]) if keep is None else keep
+    for top in (0, 8):
+        out = base.run_logprobs(x, y, min(top, x.shape[1]), scale)
+        check_sums(x[keep], y[keep], {n: v[keep] for n, v in out.items()}, scale)
+    # without the entropy the sums are others
+    got = {"logp": torch.full((x.shape[0],), NAN, device=DEV), "stats": torch.full((x.shape[0], 2), NAN, device=DEV)}
+    ops.detonation_token_logprobs(x, y, logit_scale=scale, **got,
+                                  workspace=scratch(ops.token_logprobs_workspace(*x.shape, 0)))
+    check_sums(x[keep], y[keep], {n: v[keep] for n, v in got.items()} | {"entropy": out["entropy"][keep]}, scale)
+    return out
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("offset", [0.0, 1e3, -1e3, 1e4, -1e5])
+@pytest.mark.parametrize("T,V", [(3, 70001), (3, 200003), (520, 50001)])
+def test_sums_of_logits_with_a_common_offset(gpu, dtype, offset, T, V):
+    """Rows of many steps a lane, whose maxima a lane has seen long before the row's end."""
+    if dtype == F16:
+        offset = max(offset, -5e4)               # within its range
+    say(dtype, offset, T, V)
+    g = torch.Generator(device=DEV).manual_seed(V)
+    x = (torch.randn((T, V), generator=g, device=DEV) * 2 + offset).to(dtype)
+    y = torch.randint(-1, V, (T,), generator=g, device=DEV)
+    run_and_check_sums(x, y, 1.0, torch.arange(0, T, max(1, T // 16)))
