@@ -5,9 +5,9 @@
 // w = sum (z - m) exp(z - m), in fp32 and in units of log 2:
 //     lse = m + log s        entropy = log s - w / s
 // A lane's 32 values raise the maximum once, and their exponents are one fused multiply-add each, d = z / log 2 - c
-// with c the product of the maximum as rounded: sums relative to c are exact in that respect, and are brought to
-// the maximum itself at the end.  (Where the product leaves fp32's range, at a type's lowest value say, the lane
-// takes its values once more and subtracts first.)
+// with c the product of the maximum as rounded: sums relative to c are exact in that respect, and the 32 values' are brought
+// to the maximum itself.  (Where the product is large, so that its rounding is, the values are subtracted first: masks
+// of -1e10 or a type's lowest value.)
 // Rows are cut into pieces where there are too few of them to fill the chip (a sampled token is one row); a
 // second launch joins a row's pieces.  The best tokens: the K-th largest of the threads' maxima is a value
 // that at least K elements reach, and seldom many more do; a second look at the piece lists those, and the
@@ -80,8 +80,8 @@ __device__ __forceinline__ float wave_larger(float v) {
 
 // d 2^d is 0 where 2^d is
 constexpr float kFarBelow = -16384.f;
-// products of the maximum that sums may be relative to
-constexpr float kInRange = 1e30f;
+// Products of the maximum that values are fused with: up to here their rounding is 2^-4 at most.
+constexpr float kInRange = 1 << 20;
 
 // The same relative to m, which is not below r.m.  (m = -infinity stands for nothing above it: no difference is
 // taken from it.)
@@ -189,31 +189,43 @@ struct Piece {
     }
 };
 
-// r.s and r.w are relative to the product of r.m and unit as rounded.  (Products are rounded where they stand: fused with the
-// difference, d0 would be the rounding's error instead of 0 for as long as the maximum stays, and the sums off by as
-// many of those as a row has steps.)
+// r and the lane's next values, relative to the larger maximum.
 template <int DT, bool ENTROPY>
 __device__ __forceinline__ void see(Seen& r, const Taken<DT>& x, float unit) {
-#pragma clang fp contract(off)
     float m = r.m;
 #pragma unroll
     for (int i = 0; i < kVectors<DT>; ++i)
 #pragma unroll
         for (int j = 0; j < 8; ++j) m = larger(m, x.v[i][j]);
-    const float c = fabsf(m * unit) <= kInRange ? m * unit : 0.f;     // (else the lane starts again at the end)
-    const float d0 = fmaxf(r.m * unit - c, kFarBelow), e0 = exp2_fast(d0);
-    float s = r.s * e0, w = (r.w + r.s * d0) * e0;
+    const Seen before = relative_to(r, m, unit);
+    const float ref = m == -__builtin_inff() ? 0.f : m, c = ref * unit;
+    float s = 0.f, w = 0.f;
+    if (fabsf(c) <= kInRange) {
 #pragma unroll
-    for (int i = 0; i < kVectors<DT>; ++i)
+        for (int i = 0; i < kVectors<DT>; ++i)
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            float d = __builtin_fmaf(x.v[i][j], unit, -c);
-            if constexpr (ENTROPY) d = fmaxf(d, kFarBelow);
-            const float e = exp2_fast(d);
-            s += e;
-            if constexpr (ENTROPY) w = __builtin_fmaf(d, e, w);
-        }
-    r = {m, s, w};
+            for (int j = 0; j < 8; ++j) {
+                float d = __builtin_fmaf(x.v[i][j], unit, -c);
+                if constexpr (ENTROPY) d = fmaxf(d, kFarBelow);
+                const float e = exp2_fast(d);
+                s += e;
+                if constexpr (ENTROPY) w = __builtin_fmaf(d, e, w);
+            }
+        // from the rounded product to the maximum itself
+        const float off = __builtin_fmaf(ref, unit, -c), e = exp2_fast(-off);
+        w = (w - off * s) * e;
+        s *= e;
+    } else {           // (an infinity or a NaN as well: its sums are NaNs)
+#pragma unroll
+        for (int i = 0; i < kVectors<DT>; ++i)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const float d = (x.v[i][j] - ref) * unit, e = exp2_fast(d);
+                s += e;
+                if constexpr (ENTROPY) w = __builtin_fmaf(fmaxf(d, kFarBelow), e, w);
+            }
+    }
+    r = {m, before.s + s, before.w + w};
 }
 
 // The whole workgroup's, in every thread.
@@ -303,28 +315,6 @@ __global__ __launch_bounds__(THREADS) void logprobs_kernel(Forward a) {
             p.unpack(d, raw[0], x);
             if (d + kStep < p.end) p.load(d + kStep, raw[0]);
             see<DT, ENTROPY>(r, x, a.unit);
-        }
-    }
-    {
-        // from the rounded product to the maximum itself
-        const float c = r.m * a.unit, off = __builtin_fmaf(r.m, a.unit, -c), e = exp2_fast(-off);
-        if (fabsf(c) <= kInRange) {
-            r = {r.m, r.s * e, (r.w - off * r.s) * e};
-        } else if (r.m == r.m && r.m != -__builtin_inff()) {
-            r.s = r.w = 0.f;
-            for (int64_t d = mine; d < p.end; d += THREADS * 8) {
-                const int n = p.count(d, 0);
-                float v[8];
-                unpack8<DT>(load8<DT>(a.logits, p.row, d, n), v);
-#pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    const float l = (v[j] - r.m) * a.unit, e1 = exp2_fast(l);
-                    if (j < n) {
-                        r.s += e1;
-                        r.w += fmaxf(l, kFarBelow) * e1;
-                    }
-                }
-            }
         }
     }
     uint32_t key = mine < p.end ? order_key(r.m) : 0u;

@@ -105,3 +105,75 @@ def test_sums_of_logits_with_a_common_offset(gpu, dtype, offset, T, V):
     x = (torch.randn((T, V), generator=g, device=DEV) * 2 + offset).to(dtype)
     y = torch.randint(-1, V, (T,), generator=g, device=DEV)
     run_and_check_sums(x, y, 1.0, torch.arange(0, T, max(1, T // 16)))
+
+
+@pytest.mark.parametrize("dtype,far", [(F16, 3e4)] + [
+    (dtype, far) for dtype in (F32, BF16) for far in (3e4, 1e5, 7e5, 1e6, 1e9, 1e10, 1e12, 1e20, 1e29, 1e31)])
+@pytest.mark.parametrize("V", [2500, 20000, 50001])
+@pytest.mark.parametrize("T", [12, 516])
+def test_sums_of_rows_with_large_finite_values(gpu, dtype, far, V, T):
+    """Masks that are neither a type's lowest value nor an infinity, as a lane sees them first, last, always or
+    never, and rows whose largest values are of that size."""
+    say(dtype, far, V, T)
+    x = normal(V, 12, V, scale=2.0)
+    at = torch.arange(V)
+    x[0, :V // 2] = -far
+    x[1, V // 2:] = -far
+    x[2, at // 8 % 256 < 128] = -far                 # whole lanes
+    x[3, at // 8 % 2 == 0] = -far
+    x[4] = -far                                      # nothing else
+    x[5, 1:] = -far
+    x[6, [3, V // 2, V - 1]] = far                   # three share the row
+    x[7] = far
+    x[8, :V // 2], x[8, V // 2:] = -far, -far / 2
+    x[9, :V // 3], x[9, V // 3:] = far / 2, far
+    x[10] = -far * (1 + torch.rand(V, generator=torch.Generator().manual_seed(1)) * 0.25)
+    x[11] += far / 16
+    x = rows(x.repeat(-(-T // 12), 1)[:T], dtype)
+    y = torch.randint(0, V, (T,), generator=torch.Generator().manual_seed(V)).to(DEV)
+    y[6], y[5] = 3, 0
+    keep = torch.arange(12)
+    out = run_and_check_sums(x, y, 1.0, keep)
+    for name in ("lse", "top_logp"):
+        assert bool(torch.isfinite(out[name]).all())
+    gl, ge = normal(1, T).float().to(DEV), normal(2, T).float().to(DEV)
+    got = like(T, V, dtype)
+    ops.detonation_token_logprobs_backward(x, y, out["stats"], got, g_logp=gl, entropy=out["entropy"], g_entropy=ge)
+    want = ref.logprobs_grad(x[keep], y[keep], gl[keep], ge[keep])
+    # probabilities of rows whose log s is known to V / 256 + 64 roundings of log V
+    assert_near(got[keep], want, 4 * (2 + math.log(V)), V / 256 + 256, "dlogits")
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_sums_at_the_border_of_the_products_range(gpu, dtype):
+    """Values on both sides of powers of two, a few units apart, in the order in which each lane's maximum
+    rises."""
+    V, T = 40000, 40
+    x = torch.zeros((T, V), dtype=torch.float64)
+    step = 2.0 ** (-23 if dtype == F32 else -7)
+    for t in range(T):
+        big = -2.0 ** (t // 2 + 10) if t % 2 else 2.0 ** (t // 2 + 10)
+        x[t] = big * (1 + step * 3 * (torch.arange(V).double() / V - 0.5) * (-1 if t % 2 else 1)).float().double()
+    x = rows(x, dtype)
+    y = torch.randint(0, V, (T,), generator=torch.Generator().manual_seed(3)).to(DEV)
+    run_and_check_sums(x, y)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("odd", [NAN, INF])
+@pytest.mark.parametrize("T,V", [(6, 300), (6, 70001), (600, 300)])
+def test_best_tokens_of_a_row_with_a_nan(gpu, dtype, odd, T, V):
+    """logit - lse is NaN for every token of such a row, -infinite ones too."""
+    x = normal(1, T, V)
+    x[0, 2:] = -INF
+    x[0, 1] = odd
+    x[1, V - 1] = odd
+    x[2, 1:] = -INF
+    d = rows(x, dtype)
+    y = torch.zeros(T, dtype=torch.int64, device=DEV)
+    out = base.run_logprobs(d, y, 5)
+    assert out["top_idx"][0].tolist() == [1, 0, 2, 3, 4] and out["top_idx"][2].tolist() == [0, 1, 2, 3, 4]
+    assert bool(torch.isnan(out["top_logp"][:2]).all())
+    assert out["top_logp"][2].tolist() == [0.0] + [-INF] * 4
+    for name in ("logp", "lse", "entropy"):
+        assert bool(torch.isnan(out[name][:2]).all()) and bool(torch.isfinite(out[name][2:]).all())
