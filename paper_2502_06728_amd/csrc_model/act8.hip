@@ -90,8 +90,9 @@ __device__ __forceinline__ void act_both(float x, float& value, float& slope) {
     } else {
         const float t = tanhf(0.79788456080286536f * (x + 0.044715f * x * x * x));
         value = 0.5f * x * (1.f + t);
+        const float square = fminf(x * x, 256.f);       // (from there on 1 - t t is 0, and has to meet a number)
         slope = 0.5f * (1.f + t) +
-                0.5f * x * (1.f - t * t) * 0.79788456080286536f * (1.f + 3.f * 0.044715f * x * x);
+                0.5f * x * (1.f - t * t) * 0.79788456080286536f * (1.f + 3.f * 0.044715f * square);
     }
 }
 

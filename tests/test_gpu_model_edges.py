@@ -9,7 +9,7 @@ from paper_2502_06728_amd import model_ops as ops
 from tests import model_reference as ref
 from tests import test_gpu_model_ops as base
 from tests.model_reference import BF16, F16, F32, assert_near
-from tests.test_gpu_model_ops import DEV, INF, NAN, TYPES, like, normal, rows, say, scratch
+from tests.test_gpu_model_ops import ACT, DEV, INF, NAN, TYPES, empty_act8, like, normal, rows, say, scratch
 
 pytestmark = pytest.mark.gpu
 
@@ -177,3 +177,28 @@ def test_best_tokens_of_a_row_with_a_nan(gpu, dtype, odd, T, V):
     assert out["top_logp"][2].tolist() == [0.0] + [-INF] * 4
     for name in ("logp", "lse", "entropy"):
         assert bool(torch.isnan(out[name][:2]).all()) and bool(torch.isfinite(out[name][2:]).all())
+
+
+# ------------------------------------------------------------------ gated activations
+
+@pytest.mark.parametrize("act", list(ACT))
+def test_slopes_over_the_range_of_the_8_bit_form(gpu, act):
+    """Every exponent of it: values up to fp32's largest, and down to its smallest."""
+    exps = torch.arange(1, 249, dtype=torch.uint8)[:, None]
+    codes = torch.zeros((248, 32), dtype=torch.int8)
+    codes[:, :7] = torch.tensor([1, -1, 5, -5, 127, -127, 64], dtype=torch.int8)
+    x = ref.act8_values(codes, exps)
+    a8 = ops.Act8(codes.to(DEV), exps.to(DEV))
+    dh, da = rows(torch.ones(248, 32), F32), like(248, 32, F32)
+    ops.detonation_glu_backward(ACT[act], dh, a8, None, da)
+    # beyond 100 every slope is 0 or 1; below, 64 roundings of a value of the argument's size
+    assert_near(da, ref.act_slope(x.clamp(-100, 100), act), 1 + x.abs().clamp(max=100), 64, act)
+    b8, db = empty_act8(248, 32), like(248, 32, F32)
+    b8.codes.fill_(1)
+    b8.exps.fill_(127)
+    ops.detonation_glu_backward(ACT[act], dh, a8, b8, da, db)
+    assert_near(da, ref.act_slope(x.clamp(-100, 100), act), 1 + x.abs().clamp(max=100), 64, act)
+    h = like(248, 32, F32)
+    ops.detonation_glu_forward(ACT[act], rows(x, F32), None, h)
+    for got in (h, db):
+        assert_near(got, ref.act(x, act), x.abs(), 64, act)
