@@ -202,3 +202,21 @@ def test_slopes_over_the_range_of_the_8_bit_form(gpu, act):
     ops.detonation_glu_forward(ACT[act], rows(x, F32), None, h)
     for got in (h, db):
         assert_near(got, ref.act(x, act), x.abs(), 64, act)
+
+
+def test_silu_keeps_its_bits(gpu):
+    """silu(x) of a negative x is x e^x / (1 + e^x): its bits are those of the exponential."""
+    x = torch.linspace(-85, 85, 170 * 64 + 1, dtype=torch.float64)[:-1].float().double().view(-1, 64)
+    h = like(*x.shape, F32)
+    ops.detonation_glu_forward(ops.ACT_SILU, rows(x, F32), None, h)
+    want = x * torch.sigmoid(x)
+    # an exponential (two units in the last place), a sum, a quotient (two)
+    assert bool(((ref.double(h) - want).abs() <= 8 * 2.0 ** -24 * want.abs()).all())
+    codes = torch.arange(-127, 128, dtype=torch.int8).view(-1, 1).repeat(1, 32)
+    a8 = ops.Act8(codes.to(DEV), torch.full((255, 1), 126, dtype=torch.uint8, device=DEV))
+    v = ref.act8_values(a8.codes, a8.exps)
+    dh, da = rows(torch.ones(255, 32), F32), like(255, 32, F32)
+    ops.detonation_glu_backward(ops.ACT_SILU, dh, a8, None, da)
+    # g (1 + x (1 - g)): the bracket is rounded at its terms' size
+    g = torch.sigmoid(v)
+    assert bool(((ref.double(da) - ref.act_slope(v, "silu")).abs() <= 16 * 2.0 ** -24 * g * (1 + v.abs())).all())
