@@ -48,7 +48,7 @@ struct Parts {
 };
 
 struct Forward {
-    int64_t V, ld;
+    int64_t V, ld, row0;     // row0: of this launch
     const void* logits;
     float scale;         // of the logits
     float unit;          // scale / log 2
@@ -278,7 +278,7 @@ template <int DT, bool ENTROPY, bool TOP, int THREADS, bool ONCE>
 __global__ __launch_bounds__(THREADS) void logprobs_kernel(Forward a) {
     constexpr int kWaves = THREADS / kLanes, V8 = kVectors<DT>, kKeep = TOP && THREADS > 256 ? kKept / (8 * V8) : 1;
     __shared__ Seen lds_seen[kWaves];
-    const int64_t t = blockIdx.x / a.parts.pieces;
+    const int64_t t = a.row0 + blockIdx.x / a.parts.pieces;
     const int piece = blockIdx.x % a.parts.pieces;
     const int64_t begin = piece * a.piece;
     const Piece<DT, THREADS, ONCE> p = {a.logits, t * a.ld, begin, begin + a.piece < a.V ? begin + a.piece : a.V};
@@ -456,7 +456,7 @@ __global__ __launch_bounds__(kThreads) void logprobs_join_kernel(Forward a) {
 }
 
 struct Backward {
-    int64_t V, ld, ld_out;
+    int64_t V, ld, ld_out, row0;
     const void* logits;
     void* dlogits;
     float scale, unit;
@@ -474,7 +474,7 @@ constexpr int64_t kBackwardElems = kThreads * 8 * kBackwardVectors;
 
 template <int DT, bool ENTROPY, bool ONCE>
 __global__ __launch_bounds__(kThreads) void logprobs_backward_kernel(Backward a) {
-    const int64_t t = blockIdx.x / a.pieces;
+    const int64_t t = a.row0 + blockIdx.x / a.pieces;
     const int64_t first = (blockIdx.x % a.pieces) * kBackwardElems + 8 * threadIdx.x;
     const float m = a.stats[2 * t], log_s = a.stats[2 * t + 1] * 1.4426950408889634f;
     const int64_t y = target_of(a.targets, a.target_bytes, t);
@@ -532,8 +532,16 @@ int pieces_of(int64_t T, int64_t V) {
 // stores that leave no trace there are faster (8,192 x 50,304 bf16, forward and backward, us: 467, without 430).
 bool streams(int64_t T, int64_t V, int dtype) { return T * V * type_size(dtype) > kCacheBytes / 2; }
 
-// Rows whose workgroups a launch can count (31 bits).
+// Workgroups that a call counts in 31 bits.
 constexpr int64_t kMaxGrid = 0x7FFFFFFF;
+
+// One launch for each run of rows, of `pieces` workgroups each, whose threads are fewer than the 2^32 that a launch may have:
+// launch(first row, workgroups).
+template <class F>
+void for_rows(int64_t T, int64_t pieces, int threads, F launch) {
+    const int64_t most = 0xFFFFFFFF / threads / pieces;
+    for (int64_t t = 0; t < T; t += most) launch(t, static_cast<unsigned>((T - t < most ? T - t : most) * pieces));
+}
 
 }  // namespace
 }  // namespace model
@@ -572,24 +580,26 @@ int detonation_token_logprobs(int64_t T, int64_t V, const deto_rows* logits, flo
     char* ws = static_cast<char*>(workspace);
     const int64_t seen_bytes = (T * pieces * static_cast<int64_t>(sizeof(Seen)) + 15) / 16 * 16;
     const int64_t piece = ((V + pieces - 1) / pieces + 7) / 8 * 8;
-    const Forward a = {V, logits->ld, logits->data, logit_scale, logit_scale * 1.4426950408889634f,
+    Forward a = {V, logits->ld, 0, logits->data, logit_scale, logit_scale * 1.4426950408889634f,
                        targets, target_bytes, logp, lse, entropy, top, top_idx, top_logp, stats,
                        {reinterpret_cast<Seen*>(ws),
                         pieces > 1 ? reinterpret_cast<uint64_t*>(ws + seen_bytes) : nullptr, pieces},
                        piece};
     const hipStream_t st = static_cast<hipStream_t>(stream);
-    const unsigned grid = static_cast<unsigned>(T * pieces);
     fresh();
     const auto run = [&](auto dt, auto threads, auto once) {
         constexpr int DT = decltype(dt)::value, THREADS = decltype(threads)::value;
         constexpr bool ONCE = decltype(once)::value;
-        if (top) {      // (looks at the logits twice)
-            if (entropy) logprobs_kernel<DT, true, true, THREADS, false><<<grid, THREADS, 0, st>>>(a);
-            else logprobs_kernel<DT, false, true, THREADS, false><<<grid, THREADS, 0, st>>>(a);
-        } else {
-            if (entropy) logprobs_kernel<DT, true, false, THREADS, ONCE><<<grid, THREADS, 0, st>>>(a);
-            else logprobs_kernel<DT, false, false, THREADS, ONCE><<<grid, THREADS, 0, st>>>(a);
-        }
+        for_rows(T, pieces, THREADS, [&](int64_t row0, unsigned grid) {      // (of several pieces: T is below kFewRows)
+            a.row0 = row0;
+            if (top) {      // (looks at the logits twice)
+                if (entropy) logprobs_kernel<DT, true, true, THREADS, false><<<grid, THREADS, 0, st>>>(a);
+                else logprobs_kernel<DT, false, true, THREADS, false><<<grid, THREADS, 0, st>>>(a);
+            } else {
+                if (entropy) logprobs_kernel<DT, true, false, THREADS, ONCE><<<grid, THREADS, 0, st>>>(a);
+                else logprobs_kernel<DT, false, false, THREADS, ONCE><<<grid, THREADS, 0, st>>>(a);
+            }
+        });
     };
     by_type(logits->dtype, [&](auto dt) {
         if (T < kFewRows) run(dt, Type<kThreadsFew>{}, std::false_type{});
@@ -622,18 +632,20 @@ int detonation_token_logprobs_backward(int64_t T, int64_t V, const deto_rows* lo
         return DETO_ERR_ALIGN;
     const int64_t pieces = (V + kBackwardElems - 1) / kBackwardElems;
     if (T > kMaxGrid / pieces) return DETO_ERR_UNSUPPORTED;
-    const Backward a = {V, logits->ld, dlogits->ld, logits->data, dlogits->data, logit_scale,
+    Backward a = {V, logits->ld, dlogits->ld, 0, logits->data, dlogits->data, logit_scale,
                         logit_scale * 1.4426950408889634f, targets, target_bytes, stats, entropy,
                         g_logp, g_entropy, static_cast<uint32_t>(pieces)};
     const hipStream_t st = static_cast<hipStream_t>(stream);
-    const unsigned grid = static_cast<unsigned>(T * pieces);
     fresh();
     by_type(logits->dtype, [&](auto dt) {
         constexpr int DT = dt.value;
         const auto run = [&](auto once) {
             constexpr bool ONCE = decltype(once)::value;
-            if (g_entropy) logprobs_backward_kernel<DT, true, ONCE><<<grid, kThreads, 0, st>>>(a);
-            else logprobs_backward_kernel<DT, false, ONCE><<<grid, kThreads, 0, st>>>(a);
+            for_rows(T, pieces, kThreads, [&](int64_t row0, unsigned grid) {
+                a.row0 = row0;
+                if (g_entropy) logprobs_backward_kernel<DT, true, ONCE><<<grid, kThreads, 0, st>>>(a);
+                else logprobs_backward_kernel<DT, false, ONCE><<<grid, kThreads, 0, st>>>(a);
+            });
         };
         if (streams(T, V, logits->dtype)) run(std::true_type{});
         else run(std::false_type{});

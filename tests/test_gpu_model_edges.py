@@ -179,6 +179,27 @@ def test_best_tokens_of_a_row_with_a_nan(gpu, dtype, odd, T, V):
         assert bool(torch.isnan(out[name][:2]).all()) and bool(torch.isfinite(out[name][2:]).all())
 
 
+def test_logprobs_of_more_rows_than_a_launch_counts(gpu):
+    """2^24 workgroups of 256 threads are one launch too many."""
+    T, V = (1 << 24) + 5, 3
+    g = torch.Generator(device=DEV).manual_seed(1)
+    x = torch.randn((T, V), generator=g, device=DEV).to(BF16)
+    y = torch.randint(-1, V, (T,), generator=g, device=DEV, dtype=torch.int32)
+    out = {n: torch.full((T,), NAN, device=DEV) for n in ("logp", "entropy")}
+    out["stats"] = torch.full((T, 2), NAN, device=DEV)
+    best = torch.full((T, 1), -7, dtype=torch.int32, device=DEV)
+    ops.detonation_token_logprobs(x, y, top_idx=best, **out)
+    gl = torch.randn(T, generator=g, device=DEV)
+    dx = torch.full((T, V), NAN, dtype=BF16, device=DEV)
+    ops.detonation_token_logprobs_backward(x, y, out["stats"], dx, g_logp=gl, entropy=out["entropy"], g_entropy=gl)
+    for n in (*out, "dlogits"):
+        assert bool(torch.isfinite(dx if n == "dlogits" else out[n]).all()), n
+    keep = torch.tensor([0, 1, (1 << 24) - 258, (1 << 24) - 257, (1 << 24) - 1, 1 << 24, T - 1], device=DEV)
+    check_sums(x[keep], y[keep], {n: v[keep] for n, v in out.items()})
+    assert torch.equal(best[keep, 0].cpu().long(), ref.logprobs(x[keep], y[keep], 1.0, 1)[3][:, 0])
+    assert_near(dx[keep], ref.logprobs_grad(x[keep], y[keep], gl[keep], gl[keep]), 16.0, 256, "dlogits")
+
+
 # ------------------------------------------------------------------ gated activations
 
 @pytest.mark.parametrize("act", list(ACT))
