@@ -220,14 +220,36 @@ static int scratch_of(const struct call* c, PyObject* t, int64_t bytes, void** o
            n * dt_size[dt] >= bytes;
 }
 
+/* rows of memory, in bytes */
+struct span {
+    const char* at;
+    int64_t rows, step, wide;
+};
+
+static struct span span_of(const deto_rows* m, long long T, long long D) {
+    const struct span s = {m->data, T, m->ld * dt_size[m->dtype], D * dt_size[m->dtype]};
+    return s;
+}
+
+/* whether two of them share memory (columns of one matrix lie side by side; rows a different step apart are taken to
+ * meet where the memory from the first one to the last does) */
+static int meet(const struct span* a, const struct span* b) {
+    if (!a->at || !b->at || a->rows < 1 || b->rows < 1) return 0;
+    if (a->at + (a->rows - 1) * a->step + a->wide <= b->at || b->at + (b->rows - 1) * b->step + b->wide <= a->at)
+        return 0;
+    if ((a->rows == 1 && b->rows == 1) || (a->rows > 1 && b->rows > 1 && a->step != b->step)) return 1;
+    const int64_t step = a->rows > 1 ? a->step : b->step;
+    int64_t d = (b->at - a->at) % step;
+    if (d < 0) d += step;
+    return d < a->wide || d + b->wide > step;
+}
+
 /* the output lies apart from the other matrix, or is the same rows */
 static int apart(const deto_rows* out, const deto_rows* other, long long T, long long D) {
     if (!out->data || !other->data || T == 0) return 1;
     if (out->data == other->data && out->ld == other->ld && out->dtype == other->dtype) return 1;
-    const char *a = (const char*)out->data, *b = (const char*)other->data;
-    const int64_t na = ((T - 1) * out->ld + D) * dt_size[out->dtype],
-                  nb = ((T - 1) * other->ld + D) * dt_size[other->dtype];
-    return a + na <= b || b + nb <= a;
+    const struct span a = span_of(out, T, D), b = span_of(other, T, D);
+    return !meet(&a, &b);
 }
 
 static PyObject* unusual(void) {

@@ -275,18 +275,30 @@ def _apart(out, *others):
     for name, t in others:
         if t is None or out is None:
             continue
-        a0, b0 = out.data_ptr(), t.data_ptr()
-        if a0 == b0 and out.dtype == t.dtype and out.stride() == t.stride():
+        if out.data_ptr() == t.data_ptr() and out.dtype == t.dtype and out.stride() == t.stride():
             continue
-        a1, b1 = a0 + _extent(out), b0 + _extent(t)
-        if a0 < b1 and b0 < a1:
+        if _meet(_span(out), _span(t)):
             raise ValueError(f"an output overlaps {name} without being the same rows")
 
 
-def _extent(t):
-    if t.numel() == 0:
-        return 0
-    return ((t.shape[0] - 1) * t.stride(0) + t.shape[1]) * t.element_size()
+def _span(t):
+    """Rows of memory: address, number, distance and width in bytes."""
+    e = t.element_size()
+    return t.data_ptr(), t.shape[0], t.stride(0) * e, t.shape[1] * e
+
+
+def _meet(a, b) -> bool:
+    """Whether two of them share memory (columns of one matrix lie side by side; rows a different step
+    apart are taken to meet where the memory from the first one to the last does)."""
+    (at, rows, step, wide), (at_b, rows_b, step_b, wide_b) = a, b
+    if not rows or not rows_b:
+        return False
+    if at + (rows - 1) * step + wide <= at_b or at_b + (rows_b - 1) * step_b + wide_b <= at:
+        return False
+    if (rows == 1 and rows_b == 1) or (rows > 1 and rows_b > 1 and step != step_b):
+        return True
+    d = (at_b - at) % (step if rows > 1 else step_b)
+    return d < wide or d + wide_b > (step if rows > 1 else step_b)
 
 
 # ------------------------------------------------------------------ log probabilities
