@@ -244,12 +244,55 @@ static int meet(const struct span* a, const struct span* b) {
     return d < a->wide || d + b->wide > step;
 }
 
-/* the output lies apart from the other matrix, or is the same rows */
-static int apart(const deto_rows* out, const deto_rows* other, long long T, long long D) {
-    if (!out->data || !other->data || T == 0) return 1;
-    if (out->data == other->data && out->ld == other->ld && out->dtype == other->dtype) return 1;
-    const struct span a = span_of(out, T, D), b = span_of(other, T, D);
-    return !meet(&a, &b);
+/* What a call writes, its workspace included, and the matrices that it reads.  `twin`: outputs that may be the very
+ * rows of an input. */
+struct memory {
+    struct span outs[8], ins[12];
+    int twin_out[8], twin_in[12], n_outs, n_ins;
+};
+
+static void writes(struct memory* m, struct span s, int twin) {
+    m->outs[m->n_outs] = s;
+    m->twin_out[m->n_outs++] = twin;
+}
+static void reads(struct memory* m, struct span s, int twin) {
+    m->ins[m->n_ins] = s;
+    m->twin_in[m->n_ins++] = twin;
+}
+static struct span bytes_of(const void* at, int64_t n) {
+    const struct span s = {at, 1, 0, n};
+    return s;
+}
+static struct span codes_of(const deto_act8* q, long long T, long long D) {
+    const struct span s = {(const char*)q->codes, T, q->ld_codes, D};
+    return s;
+}
+static struct span exps_of(const deto_act8* q, long long T, long long D) {
+    const struct span s = {(const char*)q->exps, T, q->ld_exps, (D + DETO_ACT8_GROUP - 1) / DETO_ACT8_GROUP};
+    return s;
+}
+static void writes8(struct memory* m, const deto_act8* q, long long T, long long D) {
+    writes(m, codes_of(q, T, D), 0);
+    writes(m, exps_of(q, T, D), 0);
+}
+static void reads8(struct memory* m, const deto_act8* q, long long T, long long D) {
+    reads(m, codes_of(q, T, D), 0);
+    reads(m, exps_of(q, T, D), 0);
+}
+
+/* no output meets another one, or an input, except as its twin */
+static int apart(const struct memory* m) {
+    for (int i = 0; i < m->n_outs; ++i) {
+        const struct span* o = &m->outs[i];
+        for (int j = i + 1; j < m->n_outs; ++j)
+            if (meet(o, &m->outs[j])) return 0;
+        for (int j = 0; j < m->n_ins; ++j) {
+            const struct span* in = &m->ins[j];
+            const int same = o->at == in->at && o->step == in->step && o->wide == in->wide;
+            if (!(same && m->twin_out[i] && m->twin_in[j]) && meet(o, in)) return 0;
+        }
+    }
+    return 1;
 }
 
 static PyObject* unusual(void) {
@@ -305,8 +348,14 @@ static PyObject* py_logprobs(PyObject* self, PyObject* const* a, Py_ssize_t coun
     }
     const double scale = PyFloat_AsDouble(a[8]);
     if (!vector_of(&c, a[6], x.T * top, DT_F32, &top_logp) || !vector_of(&c, a[7], 2 * x.T, DT_F32, &stats) ||
-        PyErr_Occurred() || top > 32 || !scratch_of(&c, a[9], f_logprobs_workspace(x.T, x.D, (int32_t)top), &ws))
+        PyErr_Occurred() || top > 32)
         return unusual();
+    const int64_t need = f_logprobs_workspace(x.T, x.D, (int32_t)top);
+    if (!scratch_of(&c, a[9], need, &ws)) return unusual();
+    struct memory mem = {.n_outs = 0};
+    writes(&mem, bytes_of(ws, need), 0);
+    reads(&mem, span_of(&x.m, x.T, x.D), 0);
+    if (!apart(&mem)) return unusual();
     RUN(f_logprobs(x.T, x.D, &x.m, (float)scale, y, yb, logp, lse, entropy, (int32_t)top, top_idx, top_logp, stats,
                    ws, c.stream));
 }
@@ -315,6 +364,7 @@ static PyObject* py_logprobs(PyObject* self, PyObject* const* a, Py_ssize_t coun
 static PyObject* py_logprobs_backward(PyObject* self, PyObject* const* a, Py_ssize_t count) {
     (void)self;
     struct call c;
+    struct memory mem = {.n_outs = 0};
     struct matrix x;
     deto_rows dx;
     void* y;
@@ -322,18 +372,20 @@ static PyObject* py_logprobs_backward(PyObject* self, PyObject* const* a, Py_ssi
     int yb;
     if (count != 9 || !begin(&c, a[8]) || !matrix_of(&c, a[0], &x) || x.dt > DT_F16 ||
         !targets_of(&c, a[1], x.T, &y, &yb) || a[2] == Py_None || !vector_of(&c, a[2], 2 * x.T, DT_F32, &stats) ||
-        !rows_of(&c, a[3], x.T, x.D, x.dt, 0, &dx) || !apart(&dx, &x.m, x.T, x.D) ||
+        !rows_of(&c, a[3], x.T, x.D, x.dt, 0, &dx) ||
         !vector_of(&c, a[4], x.T, DT_F32, &g) || !vector_of(&c, a[5], x.T, DT_F32, &entropy) ||
         !vector_of(&c, a[6], x.T, DT_F32, &ge))
         return unusual();
     const double scale = PyFloat_AsDouble(a[7]);
-    if (PyErr_Occurred()) return unusual();
+    writes(&mem, span_of(&dx, x.T, x.D), 1);
+    reads(&mem, span_of(&x.m, x.T, x.D), 1);
+    if (PyErr_Occurred() || !apart(&mem)) return unusual();
     RUN(f_logprobs_backward(x.T, x.D, &x.m, (float)scale, y, yb, stats, entropy, g, ge, &dx, c.stream));
 }
 
 /* cfg, and gate, w_post, b_post, w_pre, b_pre in a[0 .. 4] (vectors and the gate of one type) */
 static int norm_of(const struct call* c, PyObject* cfg, PyObject* const* a, long long T, long long D,
-                   deto_norm_residual* s, long long* gates) {
+                   deto_norm_residual* s, long long* gates, struct memory* mem) {
     long long pre, post, per;
     if (!long_of(cfg, s_pre, &pre) || !long_of(cfg, s_post, &post) || !float_of(cfg, s_eps_pre, &s->eps_pre) ||
         !float_of(cfg, s_eps_post, &s->eps_post) || !float_of(cfg, s_scale, &s->scale) ||
@@ -359,6 +411,7 @@ static int norm_of(const struct call* c, PyObject* cfg, PyObject* const* a, long
             return 0;
         *at[i] = p;
         dtype = dt;
+        reads(mem, bytes_of(p, n * dt_size[dt]), 0);
     }
     if (dtype >= 0) s->param_dtype = dtype;
     return 1;
@@ -372,13 +425,19 @@ static PyObject* py_norm(PyObject* self, PyObject* const* a, Py_ssize_t count) {
     deto_rows f, x_out, y;
     deto_act8 y8;
     deto_norm_residual s;
+    struct memory mem = {.n_outs = 0};
     long long gates;
     if (count != 12 || !begin(&c, a[11]) || !matrix_of(&c, a[1], &x) || x.dt > DT_F16 ||
-        !norm_of(&c, a[0], a + 6, x.T, x.D, &s, &gates) || !rows_of(&c, a[2], x.T, x.D, -1, 1, &f) ||
+        !norm_of(&c, a[0], a + 6, x.T, x.D, &s, &gates, &mem) || !rows_of(&c, a[2], x.T, x.D, -1, 1, &f) ||
         !rows_of(&c, a[3], x.T, x.D, x.dt, 1, &x_out) ||
-        !rows_of(&c, a[4], x.T, x.D, f.data ? f.dtype : -1, 1, &y) || !act8_of(&c, a[5], x.T, x.D, &y8) ||
-        !apart(&x_out, &x.m, x.T, x.D))
+        !rows_of(&c, a[4], x.T, x.D, f.data ? f.dtype : -1, 1, &y) || !act8_of(&c, a[5], x.T, x.D, &y8))
         return unusual();
+    if (x_out.data) writes(&mem, span_of(&x_out, x.T, x.D), 1);
+    if (y.data) writes(&mem, span_of(&y, x.T, x.D), 0);
+    if (y8.codes) writes8(&mem, &y8, x.T, x.D);
+    reads(&mem, span_of(&x.m, x.T, x.D), 1);
+    if (f.data) reads(&mem, span_of(&f, x.T, x.D), 0);
+    if (!apart(&mem)) return unusual();
     RUN(f_norm(&s, x.T, x.D, &x.m, OPTIONAL(f), OPTIONAL(x_out), OPTIONAL(y), OPTIONAL8(y8), c.stream));
 }
 
@@ -391,23 +450,32 @@ static PyObject* py_norm_backward(PyObject* self, PyObject* const* a, Py_ssize_t
     deto_rows f, dy, dxo, dx, df;
     deto_norm_residual s;
     deto_norm_grads g;
+    struct memory mem = {.n_outs = 0};
     long long gates;
     void* ws = NULL;
     if (count != 18) return unusual();
     PyObject* const params[5] = {a[8], a[9], a[10], a[11], Py_None};
     if (!begin(&c, a[17]) || !matrix_of(&c, a[1], &x) || x.dt > DT_F16 ||
-        !norm_of(&c, a[0], params, x.T, x.D, &s, &gates) || !rows_of(&c, a[2], x.T, x.D, -1, 1, &f) ||
+        !norm_of(&c, a[0], params, x.T, x.D, &s, &gates, &mem) || !rows_of(&c, a[2], x.T, x.D, -1, 1, &f) ||
         !rows_of(&c, a[3], x.T, x.D, f.data ? f.dtype : -1, 1, &dy) ||
         !rows_of(&c, a[4], x.T, x.D, x.dt, 1, &dxo) || !rows_of(&c, a[5], x.T, x.D, x.dt, 0, &dx) ||
         !rows_of(&c, a[6], x.T, x.D, f.data ? f.dtype : -1, 1, &df) ||
         !vector_of(&c, a[12], gates * x.D, DT_F32, &g.gate) || !vector_of(&c, a[13], x.D, DT_F32, &g.w_post) ||
         !vector_of(&c, a[14], x.D, DT_F32, &g.b_post) || !vector_of(&c, a[15], x.D, DT_F32, &g.w_pre) ||
-        !vector_of(&c, a[16], x.D, DT_F32, &g.b_pre) || dx.data == x.m.data || !apart(&dx, &x.m, x.T, x.D) ||
-        !apart(&dx, &dxo, x.T, x.D))
+        !vector_of(&c, a[16], x.D, DT_F32, &g.b_pre))
         return unusual();
-    if ((g.gate || g.w_post || g.b_post || g.w_pre || g.b_pre) &&
-        !scratch_of(&c, a[7], f_norm_workspace(&s, x.T, x.D), &ws))
-        return unusual();
+    if (g.gate || g.w_post || g.b_post || g.w_pre || g.b_pre) {
+        const int64_t need = f_norm_workspace(&s, x.T, x.D);
+        if (!scratch_of(&c, a[7], need, &ws)) return unusual();
+        writes(&mem, bytes_of(ws, need), 0);
+    }
+    writes(&mem, span_of(&dx, x.T, x.D), 1);
+    if (df.data) writes(&mem, span_of(&df, x.T, x.D), 0);
+    reads(&mem, span_of(&x.m, x.T, x.D), 0);
+    if (f.data) reads(&mem, span_of(&f, x.T, x.D), 0);
+    if (dy.data) reads(&mem, span_of(&dy, x.T, x.D), 0);
+    if (dxo.data) reads(&mem, span_of(&dxo, x.T, x.D), 1);
+    if (!apart(&mem)) return unusual();
     RUN(f_norm_backward(&s, x.T, x.D, &x.m, OPTIONAL(f), OPTIONAL(dy), OPTIONAL(dxo), &dx, OPTIONAL(df), &g, ws,
                         c.stream));
 }
@@ -420,6 +488,15 @@ static PyObject* codec(PyObject* x, PyObject* x8, PyObject* stream, int encode) 
     if (!begin(&c, stream) || !matrix_of(&c, x, &m) || m.dt > DT_F16 || x8 == Py_None ||
         !act8_of(&c, x8, m.T, m.D, &q))
         return unusual();
+    struct memory mem = {.n_outs = 0};
+    if (encode) {
+        writes8(&mem, &q, m.T, m.D);
+        reads(&mem, span_of(&m.m, m.T, m.D), 0);
+    } else {
+        writes(&mem, span_of(&m.m, m.T, m.D), 0);
+        reads8(&mem, &q, m.T, m.D);
+    }
+    if (!apart(&mem)) return unusual();
     RUN(encode ? f_encode(m.T, m.D, &m.m, &q, c.stream) : f_decode(m.T, m.D, &q, &m.m, c.stream));
 }
 static PyObject* py_encode(PyObject* self, PyObject* const* a, Py_ssize_t count) {
@@ -448,9 +525,15 @@ static PyObject* py_glu_forward(PyObject* self, PyObject* const* a, Py_ssize_t c
     int act;
     if (count != 7 || !act_of(a[0], &act) || !begin(&c, a[6]) || !matrix_of(&c, a[1], &m) || m.dt > DT_F16 ||
         !rows_of(&c, a[2], m.T, m.D, m.dt, 1, &b) || !rows_of(&c, a[3], m.T, m.D, m.dt, 0, &h) ||
-        !act8_of(&c, a[4], m.T, m.D, &a8) || !act8_of(&c, a[5], m.T, m.D, &b8) || !apart(&h, &m.m, m.T, m.D) ||
-        !apart(&h, &b, m.T, m.D))
+        !act8_of(&c, a[4], m.T, m.D, &a8) || !act8_of(&c, a[5], m.T, m.D, &b8))
         return unusual();
+    struct memory mem = {.n_outs = 0};
+    writes(&mem, span_of(&h, m.T, m.D), 1);
+    if (a8.codes) writes8(&mem, &a8, m.T, m.D);
+    if (b8.codes) writes8(&mem, &b8, m.T, m.D);
+    reads(&mem, span_of(&m.m, m.T, m.D), 1);
+    if (b.data) reads(&mem, span_of(&b, m.T, m.D), 1);
+    if (!apart(&mem)) return unusual();
     RUN(f_glu_forward(act, m.T, m.D, &m.m, OPTIONAL(b), &h, OPTIONAL8(a8), OPTIONAL8(b8), c.stream));
 }
 
@@ -465,8 +548,16 @@ static PyObject* py_glu_backward(PyObject* self, PyObject* const* a, Py_ssize_t 
     if (count != 8 || !act_of(a[0], &act) || !begin(&c, a[7]) || !matrix_of(&c, a[1], &m) || m.dt > DT_F16 ||
         a[2] == Py_None || !act8_of(&c, a[2], m.T, m.D, &a8) || !act8_of(&c, a[3], m.T, m.D, &b8) ||
         !rows_of(&c, a[4], m.T, m.D, m.dt, 0, &da) || !rows_of(&c, a[5], m.T, m.D, m.dt, 1, &db) ||
-        !act8_of(&c, a[6], m.T, m.D, &h8) || !apart(&da, &m.m, m.T, m.D) || !apart(&db, &m.m, m.T, m.D))
+        !act8_of(&c, a[6], m.T, m.D, &h8))
         return unusual();
+    struct memory mem = {.n_outs = 0};
+    writes(&mem, span_of(&da, m.T, m.D), 1);
+    if (db.data) writes(&mem, span_of(&db, m.T, m.D), 1);
+    if (h8.codes) writes8(&mem, &h8, m.T, m.D);
+    reads(&mem, span_of(&m.m, m.T, m.D), 1);
+    reads8(&mem, &a8, m.T, m.D);
+    if (b8.codes) reads8(&mem, &b8, m.T, m.D);
+    if (!apart(&mem)) return unusual();
     RUN(f_glu_backward(act, m.T, m.D, &m.m, &a8, OPTIONAL8(b8), &da, OPTIONAL(db), OPTIONAL8(h8), c.stream));
 }
 
@@ -479,9 +570,16 @@ static PyObject* py_weight_grad(PyObject* self, PyObject* const* a, Py_ssize_t c
     void* ws;
     if (count != 6 || !PyBool_Check(a[3]) || !begin(&c, a[5]) || !matrix_of(&c, a[0], &dy) || dy.dt > DT_F16 ||
         !matrix_of(&c, a[2], &dw) || dw.dt > DT_F16 || dw.T != dy.D || a[1] == Py_None ||
-        !act8_of(&c, a[1], dy.T, dw.D, &x) ||
-        !scratch_of(&c, a[4], f_weight_grad_workspace(dy.T, dy.D, dw.D), &ws))
+        !act8_of(&c, a[1], dy.T, dw.D, &x))
         return unusual();
+    const int64_t need = f_weight_grad_workspace(dy.T, dy.D, dw.D);
+    if (!scratch_of(&c, a[4], need, &ws)) return unusual();
+    struct memory mem = {.n_outs = 0};
+    writes(&mem, span_of(&dw.m, dw.T, dw.D), 0);
+    writes(&mem, bytes_of(ws, need), 0);
+    reads(&mem, span_of(&dy.m, dy.T, dy.D), 0);
+    reads8(&mem, &x, dy.T, dw.D);
+    if (!apart(&mem)) return unusual();
     RUN(f_weight_grad(dy.T, dy.D, dw.D, &dy.m, &x, &dw.m, a[3] == Py_True, ws, c.stream));
 }
 

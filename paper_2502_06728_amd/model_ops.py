@@ -3,8 +3,9 @@ library products, next to the optimizer step of binding.py (same library).
 
 Argument checks and marshalling only: device tensors in, raw pointers out; every tensor is given by the
 caller, outputs too, and is written by the kernels on `stream` (the current stream if it is None).
-Matrices are 2-D tensors whose rows may lie any distance apart; their elements are consecutive.  There
-is no CPU fallback.  Calls hand their arguments to csrc_model/marshal.c first, which checks and converts
+Matrices are 2-D tensors whose rows may lie any distance apart; their elements are consecutive.  Written
+matrices, 8-bit forms and workspaces that share memory with each other or with an input are refused, except
+where an operator works in place.  There is no CPU fallback.  Calls hand their arguments to csrc_model/marshal.c first, which checks and converts
 what a program usually passes; what it does not take goes through the checks below, which name what is
 wrong, and so does every call where it cannot be used.
 """
@@ -271,7 +272,7 @@ def _by_ref(s):
 
 
 def _apart(out, *others):
-    """Outputs are not the memory of something else, except where an operator says so: the same rows."""
+    """An output is not the memory of something else, except where an operator says so: the same rows."""
     for name, t in others:
         if t is None or out is None:
             continue
@@ -279,6 +280,34 @@ def _apart(out, *others):
             continue
         if _meet(_span(out), _span(t)):
             raise ValueError(f"an output overlaps {name} without being the same rows")
+
+
+def _disjoint(outs: dict, ins: dict, same=()) -> None:
+    """Outputs (matrices, Act8 and the workspace, a (tensor, bytes)) share no memory with each other, nor with
+    the inputs; the pairs of names in `same` may be the same rows."""
+    outs, ins = _matrices(outs), _matrices(ins)
+    for i, (name, t, span) in enumerate(outs):
+        for other, u, span_u in outs[i + 1:] + ins:
+            if (name, other) in same:
+                _apart(t, (other, u))
+            elif _meet(span, span_u):
+                raise ValueError(f"{name} overlaps {other}")
+
+
+def _matrices(tensors: dict) -> list:
+    out = []
+    for name, t in tensors.items():
+        if isinstance(t, tuple):
+            t, nbytes = t
+            if t is not None and nbytes > 0:
+                out.append((name, t, (t.data_ptr(), 1, 0, nbytes)))
+        elif hasattr(t, "codes"):
+            out += [(name + ".codes", t.codes, _span(t.codes)), (name + ".exps", t.exps, _span(t.exps))]
+        elif t is not None and t.dim() == 2:
+            out.append((name, t, _span(t)))
+        elif t is not None:
+            out.append((name, t, (t.data_ptr(), 1, 0, t.numel() * t.element_size())))
+    return out
 
 
 def _span(t):
@@ -341,7 +370,9 @@ def detonation_token_logprobs(logits, targets, logp, *, lse=None, entropy=None, 
             c.vector(top_idx, "top_idx", T * top, (torch.int32,)),
             c.vector(top_logp, "top_logp", T * top, f32),
             c.vector(stats, "stats", 2 * T, f32))
-    ws = c.scratch(workspace, lib.detonation_token_logprobs_workspace(T, V, top))
+    need = lib.detonation_token_logprobs_workspace(T, V, top)
+    ws = c.scratch(workspace, need)
+    _disjoint({"workspace": (workspace, need)}, {"logits": logits})
     _status(lib.detonation_token_logprobs(T, V, ctypes.byref(x), logit_scale, y,
                                           targets.element_size(), *args, ws, _stream(stream)))
 
@@ -359,7 +390,7 @@ def detonation_token_logprobs_backward(logits, targets, stats, dlogits, *, g_log
     T, V = logits.shape
     x = c.rows(logits, "logits", T, V)
     dx = c.rows(dlogits, "dlogits", T, V, logits.dtype)
-    _apart(dlogits, ("logits", logits))
+    _disjoint({"dlogits": dlogits}, {"logits": logits}, same=(("dlogits", "logits"),))
     f32 = (torch.float32,)
     if g_logp is None and g_entropy is None:
         raise ValueError("g_logp or g_entropy is required")
@@ -424,7 +455,9 @@ def detonation_norm_residual(cfg: NormResidual, x, f, x_out, y, *, y8: Act8 | No
     xo = c.rows(x_out, "x_out", T, D, x.dtype)
     ys = c.rows(y, "y", T, D, None if f is None else f.dtype)
     q = c.act8(y8, "y8", T, D)
-    _apart(x_out, ("x", x))
+    _disjoint({"x_out": x_out, "y": y, "y8": y8},
+              {"x": x, "f": f, "gate": gate, "w_post": w_post, "b_post": b_post, "w_pre": w_pre, "b_pre": b_pre},
+              same=(("x_out", "x"),))
     _status(lib.detonation_norm_residual(ctypes.byref(s), T, D, ctypes.byref(xs), _by_ref(fs),
                                          _by_ref(xo), _by_ref(ys), _by_ref(q), _stream(stream)))
 
@@ -453,12 +486,13 @@ def detonation_norm_residual_backward(cfg: NormResidual, x_out, f, dy, dx_out, d
     g = deto_norm_grads(*(c.vector(t, n, m, f32) for n, t, m in (
         ("dw_pre", dw_pre, D), ("db_pre", db_pre, D), ("dw_post", dw_post, D),
         ("db_post", db_post, D), ("dgate", dgate, gate_rows(cfg, T) * D))))
-    _apart(dx, ("x_out", x_out), ("dx_out", dx_out))
-    if dx is not None and dx.data_ptr() == x_out.data_ptr() and T:
-        raise ValueError("dx overlaps x_out")
     need = lib.detonation_norm_residual_workspace(ctypes.byref(s), T, D)
-    ws = c.scratch(workspace, need if any((dw_pre is not None, db_pre is not None, dgate is not None,
-                                           dw_post is not None, db_post is not None)) else 0)
+    need = need if any((dw_pre is not None, db_pre is not None, dgate is not None, dw_post is not None,
+                        db_post is not None)) else 0
+    ws = c.scratch(workspace, need)
+    _disjoint({"workspace": (workspace, need), "dx": dx, "df": df},
+              {"x_out": x_out, "f": f, "dy": dy, "dx_out": dx_out, "gate": gate, "w_post": w_post,
+               "b_post": b_post, "w_pre": w_pre}, same=(("dx", "dx_out"),))
     _status(lib.detonation_norm_residual_backward(
         ctypes.byref(s), T, D, ctypes.byref(xs), _by_ref(fs), _by_ref(dys), _by_ref(dxo),
         _by_ref(dxs), _by_ref(dfs), ctypes.byref(g), ws, _stream(stream)))
@@ -473,6 +507,7 @@ def detonation_act8_encode(x, x8: Act8, stream=None) -> None:
     lib, c = _load(), _Call()
     T, D = x.shape
     xs, q = c.rows(x, "x", T, D), c.act8(x8, "x8", T, D)
+    _disjoint({"x8": x8}, {"x": x})
     _status(lib.detonation_act8_encode(T, D, ctypes.byref(xs), ctypes.byref(q), _stream(stream)))
 
 
@@ -483,6 +518,7 @@ def detonation_act8_decode(x8: Act8, x, stream=None) -> None:
     lib, c = _load(), _Call()
     T, D = x.shape
     xs, q = c.rows(x, "x", T, D), c.act8(x8, "x8", T, D)
+    _disjoint({"x": x}, {"x8": x8})
     _status(lib.detonation_act8_decode(T, D, ctypes.byref(q), ctypes.byref(xs), _stream(stream)))
 
 
@@ -497,7 +533,7 @@ def detonation_glu_forward(act: int, a, b, h, *, a8: Act8 | None = None, b8: Act
     sa, sb = c.rows(a, "a", T, D), c.rows(b, "b", T, D, a.dtype)
     sh = c.rows(h, "h", T, D, a.dtype)
     qa, qb = c.act8(a8, "a8", T, D), c.act8(b8, "b8", T, D)
-    _apart(h, ("a", a), ("b", b))
+    _disjoint({"h": h, "a8": a8, "b8": b8}, {"a": a, "b": b}, same=(("h", "a"), ("h", "b")))
     _status(lib.detonation_glu_forward(act, T, D, ctypes.byref(sa), _by_ref(sb), ctypes.byref(sh),
                                        _by_ref(qa), _by_ref(qb), _stream(stream)))
 
@@ -513,8 +549,8 @@ def detonation_glu_backward(act: int, dh, a8: Act8, b8: Act8 | None, da, db=None
     sd, sa = c.rows(dh, "dh", T, D), c.rows(da, "da", T, D, dh.dtype)
     sb = c.rows(db, "db", T, D, dh.dtype)
     qa, qb, qh = c.act8(a8, "a8", T, D), c.act8(b8, "b8", T, D), c.act8(h8, "h8", T, D)
-    _apart(da, ("dh", dh))
-    _apart(db, ("dh", dh))
+    _disjoint({"da": da, "db": db, "h8": h8}, {"dh": dh, "a8": a8, "b8": b8},
+              same=(("da", "dh"), ("db", "dh")))
     _status(lib.detonation_glu_backward(act, T, D, ctypes.byref(sd), _by_ref(qa), _by_ref(qb),
                                         ctypes.byref(sa), _by_ref(sb), _by_ref(qh),
                                         _stream(stream)))
@@ -535,7 +571,9 @@ def detonation_act8_weight_grad(dy, x8: Act8, dw, *, accumulate: bool = False, w
     K = dw.shape[1]
     sy, q = c.rows(dy, "dy", T, N), c.act8(x8, "x8", T, K)
     sw = c.rows(dw, "dw", N, K)
-    ws = c.scratch(workspace, lib.detonation_act8_weight_grad_workspace(T, N, K))
+    need = lib.detonation_act8_weight_grad_workspace(T, N, K)
+    ws = c.scratch(workspace, need)
+    _disjoint({"dw": dw, "workspace": (workspace, need)}, {"dy": dy, "x8": x8})
     _status(lib.detonation_act8_weight_grad(T, N, K, ctypes.byref(sy), ctypes.byref(q),
                                             ctypes.byref(sw), int(accumulate), ws,
                                             _stream(stream)))
