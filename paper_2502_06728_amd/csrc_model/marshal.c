@@ -403,11 +403,14 @@ static int norm_of(const struct call* c, PyObject* cfg, PyObject* const* a, long
     for (int i = 0; i < 5; ++i) {
         int dt, contiguous;
         void* p;
-        long long n;
+        long long n, rows, columns;
         *at[i] = NULL;
         if (a[i] == Py_None) continue;
         if (!tensor_of(c, a[i], &dt, &p, &contiguous) || dt > DT_F16 || !contiguous ||
             !call_long(a[i], s_numel, &n) || n != (i ? 1 : *gates) * D || (dtype >= 0 && dt != dtype))
+            return 0;
+        if (i == 0 && *gates > 1 &&          /* as many elements may lie the other way round */
+            (!two(PyObject_GetAttr(a[i], s_shape), &rows, &columns) || rows != *gates || columns != D))
             return 0;
         *at[i] = p;
         dtype = dt;

@@ -143,3 +143,16 @@ def test_the_checks_in_python_name_it():
             ops._disjoint(outs, ins, same)
     ops._disjoint({"workspace": (x, 0)}, {"c": x})
     ops._disjoint({"a": x[:0]}, {"c": x[:0]})
+
+
+def test_gates_of_another_shape(m):  # noqa: F811
+    """As many elements as the gate's rows have, but not those rows: named in Python."""
+    cfg = ops.NormResidual(rows_per_gate=2)
+    x, f, xo, y, ws = mat(T, D), mat(T, D), mat(T, D), mat(T, D), vec(64, torch.uint8)
+    for gate, taken in [(mat(3, D), True), (mat(D, 3), False), (vec(3 * D), False), (mat(2, D), False)]:
+        assert m.norm(cfg, x, f, xo, y, None, gate, None, None, None, None, None) == (0 if taken else -1)
+        assert m.norm_backward(cfg, x, f, y, None, xo, mat(T, D), ws, gate, None, None, None, None, None, None, None, None,
+                               None) == (0 if taken else -1)
+    cfg = ops.NormResidual()
+    for gate in (mat(1, D), vec(D)):
+        assert m.norm(cfg, x, f, xo, y, None, gate, None, None, None, None, None) == 0
