@@ -137,7 +137,8 @@ typedef struct {
 /*
  *   x, x_out   [T, D] of one type; x_out may be x itself (same data and ld).  x_out may be absent if f is
  *   f          [T, D]; absent: x_out = x, no branch (cfg->post NONE, no gate)
- *   y          [T, D] of f's type (any type if f is absent); absent if cfg->pre is NONE
+ *   y          [T, D] of f's type (if f is absent: of x's, or of any where x is fp32); absent if cfg->pre is
+ *              NONE
  *   y8         y in 8 bits, encoded from y before that is rounded; may be absent
  * Types: x is fp32 or of f's type.  D is at most 16384 (else DETO_ERR_UNSUPPORTED).  With cfg->pre other
  * than NONE at least one of y and y8 is there.
