@@ -198,14 +198,6 @@ __device__ __forceinline__ void store8(void* base, int64_t at, const float (&v)[
     }
 }
 
-// parameters of a type known only at run time (the branch is uniform)
-__device__ __forceinline__ void load8_any(const void* base, int dtype, int64_t row, int64_t d, int count,
-                                          float (&v)[8]) {
-    if (dtype == DETO_F32) unpack8<DETO_F32>(load8<DETO_F32>(base, row, d, count), v);
-    else if (dtype == DETO_BF16) unpack8<DETO_BF16>(load8<DETO_BF16>(base, row, d, count), v);
-    else unpack8<DETO_F16>(load8<DETO_F16>(base, row, d, count), v);
-}
-
 // ---- The 8-bit form.  Four lanes in a row hold a group of 32 features, eight each.
 
 // maximum over the four lanes of an aligned group of four
