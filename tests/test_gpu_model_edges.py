@@ -241,3 +241,33 @@ def test_silu_keeps_its_bits(gpu):
     # g (1 + x (1 - g)): the bracket is rounded at its terms' size
     g = torch.sigmoid(v)
     assert bool(((ref.double(da) - ref.act_slope(v, "silu")).abs() <= 16 * 2.0 ** -24 * g * (1 + v.abs())).all())
+
+
+# ------------------------------------------------------------------ weight gradient
+
+@pytest.mark.parametrize("T,N,K,out", [
+    (136, 2051, 6101, F32), (136, 2051, 6101, BF16), (136, 2050, 6100, F16),     # one split; odd strides and whole words
+    (8192, 2049, 2049, F32), (8192, 2049, 2049, BF16),                           # three splits, odd strides
+    (8192, 2048, 2048, F32), (6000, 1537, 1791, F32)])                           # four; five, rows that end inside a step
+@pytest.mark.parametrize("accumulate", [False, True])
+def test_weight_grad_of_large_tiles(gpu, T, N, K, out, accumulate):
+    """bf16 sizes at which tiles are 256 wide: rows at odd strides, T cut into several splits, sums added to what
+    is there."""
+    say(T, N, K, out, accumulate)
+    g = torch.Generator(device=DEV).manual_seed(1)
+    dy = torch.randn((T, N), generator=g, device=DEV).to(BF16)
+    x8 = empty_act8(T, K)
+    ops.detonation_act8_encode(torch.randn((T, K), generator=g, device=DEV), x8)
+    start = torch.randn((N, K), generator=g, device=DEV).to(out)
+    dw = like(N, K, out, 3)
+    dw.copy_(start)
+    ops.detonation_act8_weight_grad(dy, x8, dw, accumulate=accumulate,
+                                    workspace=scratch(ops.act8_weight_grad_workspace(T, N, K)))
+    base.untouched(dw)
+    n = torch.cat([torch.arange(0, N, 61), torch.tensor([N - 1])])               # rows of every tile and of every block of 64
+    d, v = ref.double(dy[:, n]).t().contiguous(), ref.act8_values(x8.codes, x8.exps)
+    want, mag = d @ v, d.abs() @ v.abs()
+    if accumulate:
+        want, mag = want + ref.double(start[n]), mag + ref.double(start[n]).abs()
+    # exact products added in any order, then the splits of T
+    assert_near(dw[n], want, mag, T + 40, "dw")
