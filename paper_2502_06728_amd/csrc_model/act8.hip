@@ -147,7 +147,9 @@ __global__ __launch_bounds__(kThreads) void glu_backward_kernel(Items items, det
     if constexpr (GATED) store8<DT, ONCE>(db.data, at.t * db.ld + at.d, vb, at.count);
 }
 
-// Matrices that the caches do not hold until the next kernel takes them are loaded and stored without a trace there.
+// Matrices that the caches do not hold until the next kernel takes them are loaded and stored without a trace there.  (8,192 x
+// 8,192 bf16, gated SiLU forward and backward, us: 182, with the outputs left there 190; forward with the product that reads h
+// next 285 and 278.)
 template <class F>
 int by_size(int64_t T, int64_t D, int dtype, F f) {
     return T * D * type_size(dtype) >= kCacheBytes / 4 ? f(std::true_type{}) : f(std::false_type{});

@@ -16,8 +16,8 @@
 //
 // Backward.  A stream: p = exp(z - m - log s) from the row's saved m and log s.
 //
-// Measured (8,192 rows of 50,304 bf16): forward 149 us = 5.5 TB/s, about ten vector instructions a value behind the loads;
-// backward 270 us = 6.1 TB/s, memory.  1,021 rows of 32,101 fp16 with the 20 best: 27 us, of which memory is 11: one round
+// Measured (8,192 rows of 50,304 bf16): forward 162 us = 5.1 TB/s, about ten vector instructions a value behind the loads, 132
+// without the entropy; backward 268 us = 6.1 TB/s, memory.  1,021 rows of 32,101 fp16 with the 20 best: 27 us, of which memory is 11: one round
 // of workgroups, each a chain of first look, threshold, second look and ranking.
 #include "device.hip.h"
 

@@ -190,7 +190,9 @@ extern "C" int detonation_norm_residual(const deto_norm_residual* cfg, int64_t T
     const deto_rows none = {};
     Args a = {*cfg, T, static_cast<int>(D), 0, *x, branch ? *f : none, branch ? *x_out : none,
               here(y) ? *y : none, here(y8) ? *y8 : deto_act8{}};
-    // (8,192 x 4,096, fp32 and bf16, us: 79, past the caches 67; 16,384 x 768, which they hold: 25, past them 27)
+    // (8,192 x 4,096, fp32 and bf16, us: 80, past the caches 61; 16,384 x 768, which they hold: 25, past them 27.  With y alone
+    // left there 61 as well: a product that reads it next then takes 0 to 6 % less, but 16,384 x 2,048 with the 8-bit form
+    // written and decoded 91 instead of 82)
     a.once = T * D * type_size(x->dtype) >= kCacheBytes / 4;
     fresh();
     const bool layer = cfg->pre == DETO_NORM_LAYER || cfg->post == DETO_NORM_LAYER || cfg->b_pre || cfg->b_post;
