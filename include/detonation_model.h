@@ -85,7 +85,7 @@ enum { DETO_ACT8_GROUP = 32 };
  *   stats      device, [T, 2] fp32 or NULL: a row's largest logit and log sum_v exp(z_v - largest z),
  *              which the backward pass takes.  (lse is their sum: where logits are large, or all at a
  *              type's lowest value, the sum no longer tells them apart.)
- * logit_scale is finite and above 0.  V is at most 2^31 - 1.
+ * logit_scale is above 0 and at most 2^127.  V is at most 2^31 - 1.
  */
 int detonation_token_logprobs(int64_t T, int64_t V, const deto_rows* logits, float logit_scale,
                               const void* targets, int target_bytes, float* logp, float* lse,

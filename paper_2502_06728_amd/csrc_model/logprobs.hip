@@ -515,6 +515,9 @@ bool bad_shape(int64_t T, int64_t V, int top) {
     return T < 0 || V < 1 || V > 0x7FFFFFFF || top < 0 || top > kMaxTop || top > V;
 }
 
+// (scale / log 2 is a number)
+bool bad_scale(float scale) { return !(scale > 0.f && scale <= 0x1p127f); }
+
 // Few rows take a workgroup of 1,024 threads each (one row of 50,304 bf16 logits with its eight best: 25 pieces and
 // their join 13 us, 1,024 threads 10 us: 3 of them the exponentials of one CU, the rest a chain of latencies).  Rows that are long even for those are cut in pieces.
 constexpr int64_t kFewRows = 512;
@@ -564,7 +567,7 @@ int detonation_token_logprobs(int64_t T, int64_t V, const deto_rows* logits, flo
                               float* entropy, int32_t top, int32_t* top_idx, float* top_logp,
                               float* stats, void* workspace, void* stream) {
     if (bad_shape(T, V, top)) return DETO_ERR_BAD_CONFIG;
-    if (!(logit_scale > 0.f) || !std::isfinite(logit_scale)) return DETO_ERR_BAD_CONFIG;
+    if (bad_scale(logit_scale)) return DETO_ERR_BAD_CONFIG;
     if (target_bytes != 4 && target_bytes != 8) return DETO_ERR_BAD_CONFIG;
     if (T == 0) return DETO_OK;
     const int pieces = pieces_of(T, V);
@@ -618,7 +621,7 @@ int detonation_token_logprobs_backward(int64_t T, int64_t V, const deto_rows* lo
                                        const float* g_logp, const float* g_entropy,
                                        const deto_rows* dlogits, void* stream) {
     if (bad_shape(T, V, 0)) return DETO_ERR_BAD_CONFIG;
-    if (!(logit_scale > 0.f) || !std::isfinite(logit_scale)) return DETO_ERR_BAD_CONFIG;
+    if (bad_scale(logit_scale)) return DETO_ERR_BAD_CONFIG;
     if (target_bytes != 4 && target_bytes != 8) return DETO_ERR_BAD_CONFIG;
     if (T == 0) return DETO_OK;
     if (!here(logits) || !here(dlogits) || !targets || !stats || (!g_logp && !g_entropy) ||

@@ -1,4 +1,5 @@
-"""Which types go together in a norm without a branch, as include/detonation_model.h says."""
+"""Which types go together in a norm without a branch, and which scales logits may have, as
+include/detonation_model.h says."""
 import ctypes
 
 import pytest
@@ -19,4 +20,16 @@ def test_types_of_a_norm_alone(lib, x, y, taken):  # noqa: F811
     grads = ops.deto_norm_grads(w_pre=4096)
     rc = lib.detonation_norm_residual_backward(norm(), 4, 64, rows(dtype=x), None, rows(dtype=y), None, rows(dtype=x), None,
                                                ctypes.byref(grads), None, None)
+    assert rc == (NULL if taken else BAD)
+
+
+@pytest.mark.parametrize("scale,taken", [(2.0 ** 127, True), (2.0 ** 127 * (1 + 2.0 ** -23), False), (3.4e38, False),
+                                         (2.0 ** -126, True), (0.0, False), (float("inf"), False), (float("nan"), False)])
+def test_scales_of_logits(lib, scale, taken):  # noqa: F811
+    """Above 2^127 the scale over log 2 is no number, and equal logits would be NaN apart."""
+    vp = ctypes.c_void_p
+    # (a taken scale goes on to the next check: no targets)
+    rc = lib.detonation_token_logprobs(4, 64, rows(), scale, None, 8, vp(4096), None, None, 0, None, None, None, None, None)
+    assert rc == (NULL if taken else BAD)
+    rc = lib.detonation_token_logprobs_backward(4, 64, rows(), scale, None, 8, vp(4096), None, vp(4096), None, rows(), None)
     assert rc == (NULL if taken else BAD)
