@@ -11,6 +11,12 @@
  *                                                 of them
  *   detonation_act8_weight_grad                   a linear layer's weight gradient out of its input in
  *                                                 8 bits: what detonation_compress takes as gradient
+ *   detonation_rotary                             queries and keys rotated by their positions, and the
+ *                                                 gradient of that
+ *   detonation_attention_forward, .._backward     softmax(scale * q k^T) v over equally long or packed
+ *                                                 sequences, and the gradients of q, k and v
+ *   detonation_dropout                            dropout, alone or onto a residual stream, and its
+ *                                                 gradient
  *
  * Common rules are those of detonation.h: data pointers are device pointers on the current device,
  * the structs that describe them are host memory, read before the call returns; nothing is
@@ -212,6 +218,106 @@ int detonation_act8_weight_grad(int64_t T, int64_t N, int64_t K, const deto_rows
                                 void* workspace, void* stream);
 
 int64_t detonation_act8_weight_grad_workspace(int64_t T, int64_t N, int64_t K);
+
+/* ---- rotary positions -------------------------------------------------------------------------
+ *
+ * A row of x holds `heads` heads of head_dim features.  The first rotary_dim features of a head are pairs (a, b),
+ * pair i < rotary_dim / 2 being the features (i, i + rotary_dim / 2) under HALVES and (2 i, 2 i + 1) under PAIRS.
+ * With the row's position p and the angle  w = p * freqs[i]:
+ *     a' = magnitude * (a cos w - b sin w)        b' = magnitude * (a sin w + b cos w)
+ * and the other features are copied.  `inverse`: w = -p * freqs[i], which makes the call its own gradient.
+ *   x, out      [T, heads * head_dim] of one type; out may be x itself (same data and ld)
+ *   freqs       device, [rotary_dim / 2] doubles: the angle of one position in radians
+ *   positions   device, [T] int32 or int64 (position_bytes 4 or 8); NULL: row t is at first + t % period, or at
+ *               first + t if period is 0.  Angles are taken modulo a turn in 64 bits: those of positions up to
+ *               2^31 are off by less than 2^-19 radians.
+ * rotary_dim is even, 2 ... head_dim; heads * head_dim is at most 2^30; first and period are 0 ... 2^52.
+ */
+typedef enum { DETO_ROTARY_HALVES = 0, DETO_ROTARY_PAIRS = 1 } deto_rotary_layout;
+
+typedef struct {
+    int32_t layout;  /* deto_rotary_layout */
+    int32_t heads, head_dim, rotary_dim;
+    int32_t inverse; /* 0 or 1 */
+    float magnitude; /* finite */
+    int64_t first, period;
+} deto_rotary;
+
+int detonation_rotary(const deto_rotary* cfg, int64_t T, const deto_rows* x, const double* freqs,
+                      const void* positions, int position_bytes, const deto_rows* out, void* stream);
+
+/* ---- attention --------------------------------------------------------------------------------
+ *
+ * Rows are tokens.  A row of q and out holds `heads` heads of head_dim features, a row of k and v kv_heads of them;
+ * head h reads those of k and v number h / (heads / kv_heads).  Rows q_starts[s] ... q_starts[s + 1] - 1 of q are the
+ * queries of sequence s and rows k_starts[s] ... of k and v its keys; without starts each sequence has Tq / sequences
+ * queries and Tk / sequences keys.  For query i of a sequence of Lq queries and Lk keys, over the keys j that it sees
+ * (all of them; under `causal` those with j <= i + Lk - Lq):
+ *     s_j = scale * q_i . k_j      lse = log sum_j exp(s_j)      p_j = exp(s_j - lse)      out_i = sum_j p_j v_j
+ * A query that sees no key, or whose scores are all -infinity, has out = 0 and lse = -infinity.  What a query does not
+ * see does not reach it, whatever it holds; rows of no sequence are neither read into a result nor written.
+ *
+ *   q, out     [Tq, heads * head_dim];  k, v  [Tk, kv_heads * head_dim]: all of one type
+ *   lse        device, [heads, Tq] fp32; may be NULL in the forward call
+ *   q_starts, k_starts   device, [sequences + 1] int32, rising from 0 or more to at most Tq (Tk); either may be
+ *              NULL.  Starts that are out of order or out of range leave results undefined, but no access is out of
+ *              bounds.
+ * head_dim is at most 128 (else DETO_ERR_UNSUPPORTED); kv_heads divides heads, which is at most 65536; scale is above
+ * 0 and finite; Tq, Tk and sequences are at most 2^31 - 1, and without starts a multiple of `sequences`.  Scores,
+ * their statistics and all sums are fp32; p (and ds below) enter the second product rounded to the matrices' type.
+ */
+typedef struct {
+    int32_t heads, kv_heads, head_dim;
+    int32_t causal;          /* 0 or 1 */
+    float scale;
+    int32_t reserved;        /* 0 */
+    int64_t sequences;       /* >= 1 */
+    const int32_t* q_starts;
+    const int32_t* k_starts;
+} deto_attention;
+
+int detonation_attention_forward(const deto_attention* cfg, int64_t Tq, int64_t Tk, const deto_rows* q,
+                                 const deto_rows* k, const deto_rows* v, const deto_rows* out,
+                                 float* lse, void* workspace, void* stream);
+
+/*
+ * Gradients, given that of out (dout), and out and lse as the forward call wrote them:
+ *     dp_j = dout_i . v_j      ds_j = p_j (dp_j - dout_i . out_i)
+ *     dq_i = scale * sum_j ds_j k_j      dk_j = scale * sum_i ds_j q_i      dv_j = sum_i p_j dout_i
+ * with the sums of dk and dv over all heads that read them.  dq, dk and dv are of q's type and shapes, written, not
+ * added to.  Under fp16, ds above 65504 becomes infinite.
+ */
+int detonation_attention_backward(const deto_attention* cfg, int64_t Tq, int64_t Tk, const deto_rows* q,
+                                  const deto_rows* k, const deto_rows* v, const deto_rows* out,
+                                  const float* lse, const deto_rows* dout, const deto_rows* dq,
+                                  const deto_rows* dk, const deto_rows* dv, void* workspace, void* stream);
+
+/* Bytes for either call. */
+int64_t detonation_attention_workspace(const deto_attention* cfg, int64_t Tq, int64_t Tk);
+
+/* ---- dropout ----------------------------------------------------------------------------------
+ *
+ *     out[t][d] = residual[t][d] + (kept ? x[t][d] / (1 - n / 65536) : 0),     n = rate * 65536, rounded
+ * A residual that is absent counts as zeros.  Kept are the elements whose 16 random bits are n or more; nothing about
+ * them is stored: the same call on the gradient of out, without a residual, is the gradient of x.  The bits are those
+ * of Philox 4x32 with ten rounds (Salmon et al., 2011), under the key (seed mod 2^32, seed / 2^32) and the counter
+ * (d / 8, t, o mod 2^32, o / 2^32), o = offset + *device_offset: its four words give the elements 8 (d / 8) ... + 7
+ * their bits, low halves first.  A program gives every dropout of every step an offset of its own; a captured call
+ * reads device_offset, which the program moves on between replays.
+ *   x [T, D];  out [T, D] of x's type, or one of the two is fp32;  residual  of out's type
+ *   out may be x or the residual itself (same data, ld and type).
+ *   device_offset   device, one uint64; may be NULL (0)
+ * rate is 0 ... 1 and not 1; below 2^-17 it drops nothing, and n is at most 65535.  T is at most 2^32, D at most 2^30.
+ */
+typedef struct {
+    uint64_t seed, offset;
+    const uint64_t* device_offset;
+    float rate;
+    int32_t reserved; /* 0 */
+} deto_dropout;
+
+int detonation_dropout(const deto_dropout* cfg, int64_t T, int64_t D, const deto_rows* x,
+                       const deto_rows* residual, const deto_rows* out, void* stream);
 
 #ifdef __cplusplus
 }

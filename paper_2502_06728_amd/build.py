@@ -59,7 +59,8 @@ UNITS = [
 ]
 
 # the operators around the library products of a training step (include/detonation_model.h)
-MODEL_UNITS = ["norm_backward.hip", "norm.hip", "act8.hip", "weight_grad.hip", "logprobs.hip"]
+MODEL_UNITS = ["attention_backward.hip", "attention_forward.hip", "norm_backward.hip", "norm.hip", "act8.hip", "weight_grad.hip",
+               "logprobs.hip", "rotary.hip", "dropout.hip"]
 
 
 def _build_host(out: str, src: str, verbose: bool) -> None:

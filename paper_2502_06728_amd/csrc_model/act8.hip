@@ -13,37 +13,7 @@ namespace deto {
 namespace model {
 namespace {
 
-constexpr int kThreads = 256;
-
-struct Items {
-    FastDiv per_row;    // lane-items of a row, a multiple of 4
-    uint32_t count;     // lane-items of this launch
-    int64_t D;
-    int64_t row0;       // of this launch
-    struct At { int64_t t, d; int count; };
-    // Lanes past the end get count 0 (they still take part in their group's maximum).
-    __device__ __forceinline__ At at(uint32_t item) const {
-        const uint32_t row = per_row.div(item);
-        const int64_t d = int64_t{8} * (item - row * per_row.d);
-        const int64_t left = item < count ? D - d : 0;
-        return {row0 + row, d, left >= 8 ? 8 : left > 0 ? static_cast<int>(left) : 0};
-    }
-};
-
-// One launch for each run of rows whose items can be numbered in 31 bits.
-template <class F>
-int for_items(int64_t T, int64_t D, F launch) {
-    if (T == 0) return DETO_OK;
-    const int64_t per_row = (D + DETO_ACT8_GROUP - 1) / DETO_ACT8_GROUP * (DETO_ACT8_GROUP / 8);
-    const int64_t rows = (int64_t{1} << 31) / per_row - 1;
-    fresh();
-    for (int64_t t = 0; t < T; t += rows) {
-        const int64_t n = (T - t < rows ? T - t : rows) * per_row;
-        launch(Items{FastDiv(static_cast<uint32_t>(per_row)), static_cast<uint32_t>(n), D, t},
-               static_cast<unsigned>((n + kThreads - 1) / kThreads));
-    }
-    return enqueued();
-}
+constexpr int kThreads = kItemThreads;
 
 int check_shape(int64_t T, int64_t D) {
     return T < 0 || D < 1 || D > (int64_t{1} << 30) ? DETO_ERR_BAD_CONFIG : DETO_OK;

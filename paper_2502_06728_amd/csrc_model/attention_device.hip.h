@@ -1,0 +1,425 @@
+// What the kernels of attention share: sequences and their tiles, matrices in LDS, the two products on the matrix cores.
+//
+// Every product is one of 32 x 32 blocks (a wavefront's instruction), in two forms:
+//   rows    C[i][j] = sum_d A[i][d] B[j][d]     over features: scores, and dout . v.  A comes from LDS, B is in registers.
+//   columns C[d][j] += sum_i A[i][d] W[i][j]    over rows i: what the scores weigh.  A comes from LDS turned, W are
+//           results of the first form: a lane holds, of one column j = lane % 32, the rows
+//           (r / 4) * 8 + (lane / 32) * 4 + r % 4 in its registers r = 0 ... 15.  The sum may take its rows in any order:
+//           both operands take them in the one in which W already lies, so W never leaves its lanes.
+// So a lane has one query (or, for the gradients of keys, one key) throughout: its maximum, sum and bounds are one
+// register each.
+#pragma once
+
+#include "device.hip.h"
+
+namespace deto {
+namespace model {
+namespace attention {
+
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x8 __attribute__((ext_vector_type(8)));
+
+constexpr int kSide = 32;               // of a block
+constexpr int kWaves = 4;
+constexpr int kThreads = kWaves * kLanes;
+constexpr float kLog2E = 1.44269504088896341f, kLn2 = 0.693147180559945309f;
+
+// A head's features, padded with zeros to DP.
+template <int DT_, int DP_>
+struct Shape {
+    static constexpr int DT = DT_, DP = DP_;
+    static constexpr int kElem = kSize<DT>;
+    static constexpr int kRow = DP * kElem;         // bytes of a row in LDS
+    static constexpr int kPieces = kRow / 16;       // of 16 bytes
+    static constexpr int kOf = 16 / kElem;          // features of a piece
+    static constexpr int kFrags = kPieces / 2;      // operands of the rows form: two pieces, one for each half of the lanes
+    static constexpr int kBlocks = DP / kSide;      // blocks of features
+};
+
+struct Matrix {
+    char* data;
+    int64_t ld;       // in bytes
+};
+
+struct Args {
+    Matrix q, k, v, out, dout, dq, dk, dv;
+    float* lse;
+    float* delta;                        // [heads, Tq]: dout . out
+    const int32_t *q_starts, *k_starts;
+    int64_t Tq, Tk, sequences;
+    int32_t heads, kv_heads, group, head_dim, causal;
+    float scale;
+    uint32_t tiles;                      // of one head (with starts: at most), see Plan
+    uint32_t per_sequence;               // tiles of one sequence, without starts
+};
+
+// ---- sequences
+struct Sequence {
+    int64_t q0, k0;      // first rows
+    int32_t Lq, Lk;
+};
+
+__device__ __forceinline__ int64_t clamped(int64_t at, int64_t T) { return at < 0 ? 0 : at < T ? at : T; }
+
+__device__ __forceinline__ void span_of(const int32_t* starts, int64_t s, int64_t sequences, int64_t T, int64_t& first,
+                                        int32_t& length) {
+    if (starts) {
+        first = clamped(starts[s], T);
+        const int64_t end = clamped(starts[s + 1], T);
+        length = end > first ? static_cast<int32_t>(end - first) : 0;
+    } else {
+        length = static_cast<int32_t>(T / sequences);
+        first = s * length;
+    }
+}
+
+__device__ __forceinline__ Sequence sequence_of(const Args& a, int64_t s) {
+    Sequence seq;
+    span_of(a.q_starts, s, a.sequences, a.Tq, seq.q0, seq.Lq);
+    span_of(a.k_starts, s, a.sequences, a.Tk, seq.k0, seq.Lk);
+    return seq;
+}
+
+// Tile number `id` of all sequences' rows, `size` rows a tile: its sequence, and which of that one's tiles it is.  False
+// where there are fewer.  The sequences' tiles are counted 64 at a time, a lane each.
+__device__ __forceinline__ bool find_tile(const Args& a, const int32_t* starts, int64_t T, int size, uint32_t id,
+                                          int64_t& s, int32_t& tile, int32_t& tiles) {
+    if (!starts) {
+        s = id / a.per_sequence;
+        tile = static_cast<int32_t>(id % a.per_sequence);
+        tiles = static_cast<int32_t>(a.per_sequence);
+        return true;
+    }
+    const int lane = threadIdx.x % kLanes;
+    int64_t before = 0;
+    for (int64_t base = 0; base < a.sequences; base += kLanes) {
+        int64_t first;
+        int32_t length = 0;
+        if (base + lane < a.sequences) span_of(starts, base + lane, a.sequences, T, first, length);
+        const int32_t own = length / size + (length % size != 0);
+        int64_t upto = own;
+#pragma unroll
+        for (int by = 1; by < kLanes; by *= 2) {
+            const int64_t below = __shfl_up(upto, by);
+            if (lane >= by) upto += below;
+        }
+        const uint64_t past = __ballot(before + upto > static_cast<int64_t>(id));
+        if (past) {
+            const int at = __builtin_ctzll(past);
+            s = base + at;
+            tile = static_cast<int32_t>(id - before - __shfl(upto - own, at));
+            tiles = __shfl(own, at);
+            return true;
+        }
+        before += __shfl(upto, kLanes - 1);
+    }
+    return false;
+}
+
+// Workgroups go to the chip's eight parts in turn; each part takes a run of numbers: the tiles of a head and the heads
+// that share its keys, which its own cache then holds for all of them.
+__device__ __forceinline__ uint32_t number_in_part() {
+    const uint32_t all = gridDim.x, part = blockIdx.x % 8, each = all / 8, more = all % 8;
+    return part * each + (part < more ? part : more) + blockIdx.x / 8;
+}
+
+// ---- matrices in LDS.  Piece p of row r lies at piece p ^ twist(r) of that row: eight lanes that read one piece of
+// rows in a row, and sixteen that read two pieces of four rows (the turned reads), each meet all banks.
+template <class S>
+__device__ __forceinline__ int twist(int row) {
+    if constexpr (S::kPieces >= 16) return ((row & 3) << 2) | ((row >> 2) & 3);
+    else if constexpr (S::kPieces == 8) return ((row & 2) << 1) | ((row >> 2) & 3);
+    else return (row >> 1) & (S::kPieces - 1);
+}
+template <class S>
+__device__ __forceinline__ uint32_t place(int row, int piece) { return row * S::kRow + ((piece ^ twist<S>(row)) << 4); }
+
+// features d ... of a row of which `D` are there (16 bytes, zeros behind)
+template <class S, bool WHOLE>
+__device__ __forceinline__ u32x4 load_piece(const char* row, int piece, int D) {
+    const int d = piece * S::kOf;
+    if constexpr (WHOLE) return *reinterpret_cast<const u32x4_any2*>(row + d * S::kElem);
+    u32x4 r = {0, 0, 0, 0};
+    if (d + S::kOf <= D) return *reinterpret_cast<const u32x4_any2*>(row + d * S::kElem);
+    if (d >= D) return r;
+    if constexpr (S::DT == DETO_F32) {
+#pragma unroll
+        for (int j = 0; j < 3; ++j)
+            if (d + j < D) r[j] = reinterpret_cast<const uint32_t*>(row)[d + j];
+    } else {
+#pragma unroll
+        for (int j = 0; j < 7; ++j)
+            if (d + j < D) r[j / 2] |= static_cast<uint32_t>(reinterpret_cast<const uint16_t*>(row)[d + j]) << (16 * (j % 2));
+    }
+    return r;
+}
+
+// Whether a piece holds an infinity or a NaN; those are made zeros.
+template <class S>
+__device__ __forceinline__ bool take_out_infinities(u32x4& r) {
+    bool any = false;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+        if constexpr (S::DT == DETO_F32) {
+            if ((r[w] & 0x7F800000u) == 0x7F800000u) {
+                any = true;
+                r[w] = 0;
+            }
+        } else {
+            constexpr uint32_t kExponent = S::DT == DETO_BF16 ? 0x7F80u : 0x7C00u;
+            if ((r[w] & kExponent) == kExponent) {
+                any = true;
+                r[w] &= 0xFFFF0000u;
+            }
+            if ((r[w] & kExponent << 16) == kExponent << 16) {
+                any = true;
+                r[w] &= 0xFFFFu;
+            }
+        }
+    }
+    return any;
+}
+
+// ROWS rows on their way from memory to LDS through a workgroup's registers.  Rows past the last one are zeros.
+template <class S, int ROWS, bool WHOLE>
+struct Stage {
+    static constexpr int kUnits = ROWS * S::kPieces / kThreads;
+    static_assert(ROWS * S::kPieces % kThreads == 0, "");
+    u32x4 r[kUnits];
+    static __device__ __forceinline__ int row(int i) { return (threadIdx.x + i * kThreads) / S::kPieces; }
+    static __device__ __forceinline__ int piece(int i) { return (threadIdx.x + i * kThreads) % S::kPieces; }
+
+    // `have` (1 or more) rows from `at` on
+    __device__ __forceinline__ void load(const char* at, int64_t ld, int have, int D) {
+#pragma unroll
+        for (int i = 0; i < kUnits; ++i)
+            r[i] = load_piece<S, WHOLE>(at + (row(i) < have ? row(i) : have - 1) * ld, piece(i), D);
+    }
+    // CLEAN: infinities and NaNs are left out, and their rows' bits are set
+    template <bool CLEAN>
+    __device__ __forceinline__ void store(char* lds, int have, uint32_t* bits) {
+#pragma unroll
+        for (int i = 0; i < kUnits; ++i) {
+            if (row(i) >= have) r[i] = {0, 0, 0, 0};
+            if (CLEAN && take_out_infinities<S>(r[i])) atomicOr(bits + row(i) / kSide, 1u << (row(i) % kSide));
+            *reinterpret_cast<u32x4*>(lds + place<S>(row(i), piece(i))) = r[i];
+        }
+    }
+};
+
+// ---- the rows form
+template <int DT>
+__device__ __forceinline__ f32x16 multiply(const u32x4& a, const u32x4& b, f32x16 c) {
+    if constexpr (DT == DETO_BF16)
+        return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+    else if constexpr (DT == DETO_F16)
+        return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+    else {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) c = __builtin_amdgcn_mfma_f32_32x32x2f32(bits_f32(a[j]), bits_f32(b[j]), c, 0, 0, 0);
+        return c;
+    }
+}
+
+// a lane's row of B: rows of which the lane's one may be missing (zeros)
+template <class S, bool WHOLE>
+__device__ __forceinline__ void load_row(const char* row, bool there, int D, u32x4 (&f)[S::kFrags]) {
+    const int half = (threadIdx.x / kSide) % 2;
+#pragma unroll
+    for (int m = 0; m < S::kFrags; ++m) {
+        f[m] = load_piece<S, WHOLE>(row, 2 * m + half, D);
+        if (!there) f[m] = {0, 0, 0, 0};
+    }
+}
+
+// rows 32 block ... of a matrix in LDS times the lane's row
+template <class S>
+__device__ __forceinline__ f32x16 rows_product(const char* lds, int block, const u32x4 (&b)[S::kFrags]) {
+    const int lane = threadIdx.x % kLanes, row = block * kSide + lane % kSide, half = lane / kSide;
+    f32x16 c = {};
+#pragma unroll
+    for (int m = 0; m < S::kFrags; ++m)
+        c = multiply<S::DT>(*reinterpret_cast<const u32x4*>(lds + place<S>(row, 2 * m + half)), b[m], c);
+    return c;
+}
+
+// ---- the columns form
+typedef __attribute__((address_space(3))) s16x4* TurnedAt;
+
+// W as the second operand: one of two runs of 16 rows
+template <int DT>
+__device__ __forceinline__ u32x4 operand(const f32x16& w, int run) {
+    u32x4 r;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const float lo = w[8 * run + 2 * j], hi = w[8 * run + 2 * j + 1];
+        r[j] = DT == DETO_BF16 ? pack_bf16(lo, hi) : pack_f16(lo, hi);
+    }
+    return r;
+}
+
+template <class S>
+__device__ __forceinline__ void columns_product(const char* lds, int block, const f32x16& w, f32x16 (&c)[S::kBlocks]) {
+    const int lane = threadIdx.x % kLanes, half = lane / kSide;
+    if constexpr (S::DT == DETO_F32) {
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+            const int row = block * kSide + (r / 4) * 8 + half * 4 + r % 4;
+#pragma unroll
+            for (int b = 0; b < S::kBlocks; ++b) {
+                const int d = b * kSide + lane % kSide;
+                const float a = *reinterpret_cast<const float*>(lds + place<S>(row, d / 4) + d % 4 * 4);
+                c[b] = __builtin_amdgcn_mfma_f32_32x32x2f32(a, w[r], c[b], 0, 0, 0);
+            }
+        }
+    } else {
+#pragma unroll
+        for (int run = 0; run < 2; ++run) {
+            const u32x4 own = operand<S::DT>(w, run);
+#pragma unroll
+            for (int b = 0; b < S::kBlocks; ++b) {
+                // Sixteen lanes read four rows of sixteen features, four at a time, and get four rows of one feature.
+                const int row = block * kSide + run * 16 + half * 4 + lane % 16 / 4;
+                const int piece = b * 4 + lane / 16 % 2 * 2 + lane % 4 / 2, odd = lane % 2 * 8;
+                u32x4 a;
+#pragma unroll
+                for (int s = 0; s < 2; ++s) {
+                    const s16x4 four = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                        (TurnedAt)(lds + place<S>(row + 8 * s, piece) + odd));
+                    const u32x2 words = __builtin_bit_cast(u32x2, four);
+                    a[2 * s] = words[0];
+                    a[2 * s + 1] = words[1];
+                }
+                c[b] = multiply<S::DT>(a, own, c[b]);
+            }
+        }
+    }
+}
+
+// The terms of the columns form that infinities and NaNs take part in, for lanes that see their row: `bits` says which
+// rows of the block have any, `rows` is the block's first row in memory.
+template <class S, class Sees>
+__device__ __forceinline__ void add_infinities(uint32_t bits, const char* rows, int64_t ld, int D, const f32x16& w, Sees sees,
+                                               f32x16 (&c)[S::kBlocks]) {
+    const int half = threadIdx.x / kSide % 2;
+    while (bits) {
+        const int n = __builtin_ctz(bits);
+        bits &= bits - 1;
+        float own = 0.f;
+#pragma unroll
+        for (int r = 0; r < 16; ++r)
+            if ((r / 4) * 8 + r % 4 == (n & ~4)) own = w[r];
+        const auto both = __builtin_amdgcn_permlane32_swap(f32_bits(own), f32_bits(own), false, false);
+        const float weight = bits_f32(n & 4 ? both[1] : both[0]);
+        if (!sees(n)) continue;
+#pragma unroll
+        for (int b = 0; b < S::kBlocks; ++b) {
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+                const int d = b * kSide + (r / 4) * 8 + half * 4 + r % 4;
+                if (d >= D) continue;
+                const float v = load1<S::DT>(rows + n * ld, d);
+                if (!(fabsf(v) < __builtin_inff())) c[b][r] += weight * v;
+            }
+        }
+    }
+}
+
+// ---- both halves' maximum and sum of a column
+__device__ __forceinline__ float halves_max(float v) {
+    const auto both = __builtin_amdgcn_permlane32_swap(f32_bits(v), f32_bits(v), false, false);
+    return fmaxf(bits_f32(both[0]), bits_f32(both[1]));
+}
+__device__ __forceinline__ float halves_sum(float v) {
+    const auto both = __builtin_amdgcn_permlane32_swap(f32_bits(v), f32_bits(v), false, false);
+    return bits_f32(both[0]) + bits_f32(both[1]);
+}
+
+// Columns of C times a factor into the lanes' rows of a matrix, 16 bytes a lane: the two halves of the lanes, which hold
+// four features each of every eight, exchange theirs for that.
+template <class S>
+__device__ __forceinline__ void store_columns(const f32x16 (&c)[S::kBlocks], float factor, char* row, bool there, int D) {
+    const int half = threadIdx.x / kSide % 2;
+#pragma unroll
+    for (int b = 0; b < S::kBlocks; ++b) {
+        if constexpr (S::DT == DETO_F32) {
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                const int d = b * kSide + 8 * g + 4 * half;
+                u32x4 v;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) v[j] = f32_bits(c[b][4 * g + j] * factor);
+                if (there && d + 4 <= D) *reinterpret_cast<u32x4_any4*>(row + d * 4) = v;
+                else if (there) {
+#pragma unroll
+                    for (int j = 0; j < 3; ++j)
+                        if (d + j < D) reinterpret_cast<uint32_t*>(row)[d + j] = v[j];
+                }
+            }
+        } else {
+#pragma unroll
+            for (int g = 0; g < 4; g += 2) {
+                uint32_t w[2][2];
+#pragma unroll
+                for (int i = 0; i < 2; ++i)
+#pragma unroll
+                    for (int j = 0; j < 2; ++j) {
+                        const float lo = c[b][4 * (g + i) + 2 * j] * factor, hi = c[b][4 * (g + i) + 2 * j + 1] * factor;
+                        w[i][j] = S::DT == DETO_BF16 ? pack_bf16(lo, hi) : pack_f16(lo, hi);
+                    }
+                const auto x = __builtin_amdgcn_permlane32_swap(w[0][0], w[1][0], false, false);
+                const auto y = __builtin_amdgcn_permlane32_swap(w[0][1], w[1][1], false, false);
+                const u32x4 v = {x[0], y[0], x[1], y[1]};
+                const int d = b * kSide + 8 * (g + half);
+                if (there && d + 8 <= D) *reinterpret_cast<u32x4_any2*>(row + d * 2) = v;
+                else if (there) {
+#pragma unroll
+                    for (int j = 0; j < 7; ++j)
+                        if (d + j < D) reinterpret_cast<uint16_t*>(row)[d + j] = static_cast<uint16_t>(v[j / 2] >> (16 * (j % 2)));
+                }
+            }
+        }
+    }
+}
+
+__device__ __forceinline__ float power2(float x) { return __builtin_amdgcn_exp2f(x); }
+
+// ---- host side
+int check(const deto_attention* cfg, int64_t Tq, int64_t Tk);
+int check_matrix(const deto_attention* cfg, const deto_rows* m, int64_t T, int heads, int dtype);
+Args args_of(const deto_attention* cfg, int64_t Tq, int64_t Tk, const deto_rows* q, const deto_rows* k, const deto_rows* v);
+
+inline Matrix matrix_of(const deto_rows* m) {
+    return {static_cast<char*>(m->data), m->ld * type_size(m->dtype)};
+}
+
+// Tiles of `size` rows of one head, into args; false where a launch cannot number those of all heads.
+inline bool plan(Args& a, const int32_t* starts, int64_t T, int size, int heads) {
+    int64_t tiles;
+    if (starts) {
+        tiles = T / size + (a.sequences < T ? a.sequences : T);
+        a.per_sequence = 1;
+    } else {
+        const int64_t each = (T / a.sequences + size - 1) / size;
+        tiles = each * a.sequences;
+        a.per_sequence = static_cast<uint32_t>(each ? each : 1);
+    }
+    a.tiles = static_cast<uint32_t>(tiles);
+    return tiles * heads < (int64_t{1} << 31) / kThreads * 2;
+}
+
+// f(Shape, whole) for a head's features
+template <int DT, class F>
+inline int by_shape(int head_dim, F f) {
+    if (head_dim == 64) return f(Shape<DT, 64>{}, Type<1>{});
+    if (head_dim == 128) return f(Shape<DT, 128>{}, Type<1>{});
+    if (head_dim <= 64) return f(Shape<DT, 64>{}, Type<0>{});
+    return f(Shape<DT, 128>{}, Type<0>{});
+}
+
+}  // namespace attention
+}  // namespace model
+}  // namespace deto

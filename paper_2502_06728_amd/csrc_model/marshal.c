@@ -35,15 +35,29 @@ static int (*f_weight_grad)(int64_t, int64_t, int64_t, const deto_rows*, const d
                             int, void*, void*);
 static int64_t (*f_weight_grad_workspace)(int64_t, int64_t, int64_t);
 
-enum dt { DT_F32, DT_BF16, DT_F16, DT_I32, DT_I64, DT_I8, DT_U8, DT_COUNT };   /* the first three: deto_dtype */
+/* and in that of setup_block() */
+static int (*f_rotary)(const deto_rotary*, int64_t, const deto_rows*, const double*, const void*, int, const deto_rows*,
+                       void*);
+static int (*f_attention_forward)(const deto_attention*, int64_t, int64_t, const deto_rows*, const deto_rows*,
+                                  const deto_rows*, const deto_rows*, float*, void*, void*);
+static int (*f_attention_backward)(const deto_attention*, int64_t, int64_t, const deto_rows*, const deto_rows*,
+                                   const deto_rows*, const deto_rows*, const float*, const deto_rows*, const deto_rows*,
+                                   const deto_rows*, const deto_rows*, void*, void*);
+static int64_t (*f_attention_workspace)(const deto_attention*, int64_t, int64_t);
+static int (*f_dropout)(const deto_dropout*, int64_t, int64_t, const deto_rows*, const deto_rows*, const deto_rows*,
+                        void*);
+
+enum dt { DT_F32, DT_BF16, DT_F16, DT_I32, DT_I64, DT_I8, DT_U8, DT_F64, DT_COUNT };   /* the first three: deto_dtype */
 static PyObject* dtypes[DT_COUNT];
-static const int dt_size[DT_COUNT] = {4, 2, 2, 4, 8, 1, 1};
+static const int dt_size[DT_COUNT] = {4, 2, 2, 4, 8, 1, 1, 8};
 
 static PyObject *fn_device, *fn_stream;
 static int several;          /* devices: tensors say which one they are on */
 
 static PyObject *s_is_cuda, *s_is_contiguous, *s_shape, *s_stride, *s_numel, *s_dtype, *s_data_ptr,
-    *s_get_device, *s_codes, *s_exps, *s_pre, *s_post, *s_eps_pre, *s_eps_post, *s_scale, *s_rows_per_gate;
+    *s_get_device, *s_codes, *s_exps, *s_pre, *s_post, *s_eps_pre, *s_eps_post, *s_scale, *s_rows_per_gate,
+    *s_heads, *s_kv_heads, *s_head_dim, *s_rotary_dim, *s_layout, *s_magnitude, *s_first, *s_period, *s_causal,
+    *s_sequences, *s_rate, *s_seed;
 
 /* ---- reads; 0 where something is not as usual (a Python error may be set) */
 
@@ -586,6 +600,178 @@ static PyObject* py_weight_grad(PyObject* self, PyObject* const* a, Py_ssize_t c
     RUN(f_weight_grad(dy.T, dy.D, dw.D, &dy.m, &x, &dw.m, a[3] == Py_True, ws, c.stream));
 }
 
+/* a number of 32 bits */
+static int int_of(PyObject* o, PyObject* name, int32_t* out) {
+    long long v;
+    if (!long_of(o, name, &v) || v != (int32_t)v) return 0;
+    *out = (int32_t)v;
+    return 1;
+}
+
+/* a matrix that the call reads, or writes */
+static int part_of(const struct call* c, struct memory* mem, PyObject* t, long long T, long long D, int dt, int written,
+                   deto_rows* out) {
+    if (!rows_of(c, t, T, D, dt, 0, out)) return 0;
+    if (written) writes(mem, span_of(out, T, D), 0);
+    else reads(mem, span_of(out, T, D), 0);
+    return 1;
+}
+
+/* (cfg, x, freqs, out, positions, inverse, stream) */
+static PyObject* py_rotary(PyObject* self, PyObject* const* a, Py_ssize_t count) {
+    (void)self;
+    struct call c;
+    struct matrix x;
+    deto_rows out;
+    deto_rotary s;
+    struct memory mem = {.n_outs = 0};
+    double* freqs;
+    long long first, period;
+    void* positions = NULL;
+    int bytes = 0;
+    if (count != 7 || !PyBool_Check(a[5]) || !int_of(a[0], s_heads, &s.heads) || !int_of(a[0], s_head_dim, &s.head_dim) ||
+        !int_of(a[0], s_rotary_dim, &s.rotary_dim) || !int_of(a[0], s_layout, &s.layout) ||
+        !float_of(a[0], s_magnitude, &s.magnitude) || !long_of(a[0], s_first, &first) ||
+        !long_of(a[0], s_period, &period) || !begin(&c, a[6]) || !matrix_of(&c, a[1], &x) || x.dt > DT_F16 ||
+        x.D != (long long)s.heads * s.head_dim || !rows_of(&c, a[3], x.T, x.D, x.dt, 0, &out))
+        return unusual();
+    if (!s.rotary_dim) s.rotary_dim = s.head_dim;
+    s.inverse = a[5] == Py_True;
+    s.first = first;
+    s.period = period;
+    if (a[2] == Py_None || !vector_of(&c, a[2], s.rotary_dim / 2, DT_F64, &freqs) ||
+        (a[4] != Py_None && !targets_of(&c, a[4], x.T, &positions, &bytes)))
+        return unusual();
+    writes(&mem, span_of(&out, x.T, x.D), 1);
+    reads(&mem, span_of(&x.m, x.T, x.D), 1);
+    reads(&mem, bytes_of(freqs, s.rotary_dim / 2 * 8), 0);
+    if (positions) reads(&mem, bytes_of(positions, x.T * bytes), 0);
+    if (!apart(&mem)) return unusual();
+    RUN(f_rotary(&s, x.T, &x.m, freqs, positions, bytes, &out, c.stream));
+}
+
+/* cfg, and q_starts and k_starts in a[0] and a[1] */
+static int attention_of(const struct call* c, PyObject* cfg, PyObject* const* a, deto_attention* s, struct memory* mem) {
+    long long sequences;
+    int32_t *qs, *ks;
+    if (!int_of(cfg, s_heads, &s->heads) || !int_of(cfg, s_kv_heads, &s->kv_heads) ||
+        !int_of(cfg, s_head_dim, &s->head_dim) || !float_of(cfg, s_scale, &s->scale) ||
+        !long_of(cfg, s_sequences, &sequences) || sequences < 1 || sequences > INT32_MAX ||
+        !vector_of(c, a[0], sequences + 1, DT_I32, &qs) || !vector_of(c, a[1], sequences + 1, DT_I32, &ks))
+        return 0;
+    if (!s->kv_heads) s->kv_heads = s->heads;
+    s->causal = truth_of(cfg, s_causal);
+    s->reserved = 0;
+    s->sequences = sequences;
+    s->q_starts = qs;
+    s->k_starts = ks;
+    if (qs) reads(mem, bytes_of(qs, (sequences + 1) * 4), 0);
+    if (ks) reads(mem, bytes_of(ks, (sequences + 1) * 4), 0);
+    return !PyErr_Occurred();
+}
+
+/* (cfg, q, k, v, out, lse, q_starts, k_starts, workspace, stream) */
+static PyObject* py_attention_forward(PyObject* self, PyObject* const* a, Py_ssize_t count) {
+    (void)self;
+    struct call c;
+    struct matrix q, k;
+    deto_rows v, out;
+    deto_attention s;
+    struct memory mem = {.n_outs = 0};
+    float* lse;
+    void* ws;
+    if (count != 10 || !begin(&c, a[9]) || !attention_of(&c, a[0], a + 6, &s, &mem) || !matrix_of(&c, a[1], &q) ||
+        q.dt > DT_F16 || q.D != (long long)s.heads * s.head_dim || !matrix_of(&c, a[2], &k) || k.dt != q.dt ||
+        k.D != (long long)s.kv_heads * s.head_dim || !part_of(&c, &mem, a[3], k.T, k.D, q.dt, 0, &v) ||
+        !part_of(&c, &mem, a[4], q.T, q.D, q.dt, 1, &out) || !vector_of(&c, a[5], s.heads * q.T, DT_F32, &lse))
+        return unusual();
+    const int64_t need = f_attention_workspace(&s, q.T, k.T);
+    if (!scratch_of(&c, a[8], need, &ws)) return unusual();
+    reads(&mem, span_of(&q.m, q.T, q.D), 0);
+    reads(&mem, span_of(&k.m, k.T, k.D), 0);
+    writes(&mem, bytes_of(lse, s.heads * q.T * 4), 0);
+    writes(&mem, bytes_of(ws, need), 0);
+    if (!apart(&mem)) return unusual();
+    RUN(f_attention_forward(&s, q.T, k.T, &q.m, &k.m, &v, &out, lse, ws, c.stream));
+}
+
+/* (cfg, q, k, v, out, lse, dout, dq, dk, dv, q_starts, k_starts, workspace, stream) */
+static PyObject* py_attention_backward(PyObject* self, PyObject* const* a, Py_ssize_t count) {
+    (void)self;
+    struct call c;
+    struct matrix q, k;
+    deto_rows v, out, dout, dq, dk, dv;
+    deto_attention s;
+    struct memory mem = {.n_outs = 0};
+    float* lse;
+    void* ws;
+    if (count != 14 || !begin(&c, a[13]) || !attention_of(&c, a[0], a + 10, &s, &mem) || !matrix_of(&c, a[1], &q) ||
+        q.dt > DT_F16 || q.D != (long long)s.heads * s.head_dim || !matrix_of(&c, a[2], &k) || k.dt != q.dt ||
+        k.D != (long long)s.kv_heads * s.head_dim || !part_of(&c, &mem, a[3], k.T, k.D, q.dt, 0, &v) ||
+        !part_of(&c, &mem, a[4], q.T, q.D, q.dt, 0, &out) || a[5] == Py_None ||
+        !vector_of(&c, a[5], s.heads * q.T, DT_F32, &lse) || !part_of(&c, &mem, a[6], q.T, q.D, q.dt, 0, &dout) ||
+        !part_of(&c, &mem, a[7], q.T, q.D, q.dt, 1, &dq) || !part_of(&c, &mem, a[8], k.T, k.D, q.dt, 1, &dk) ||
+        !part_of(&c, &mem, a[9], k.T, k.D, q.dt, 1, &dv))
+        return unusual();
+    const int64_t need = f_attention_workspace(&s, q.T, k.T);
+    if (!scratch_of(&c, a[12], need, &ws)) return unusual();
+    reads(&mem, span_of(&q.m, q.T, q.D), 0);
+    reads(&mem, span_of(&k.m, k.T, k.D), 0);
+    reads(&mem, bytes_of(lse, s.heads * q.T * 4), 0);
+    writes(&mem, bytes_of(ws, need), 0);
+    if (!apart(&mem)) return unusual();
+    RUN(f_attention_backward(&s, q.T, k.T, &q.m, &k.m, &v, &out, lse, &dout, &dq, &dk, &dv, ws, c.stream));
+}
+
+/* (cfg, x, out, residual, offset, device_offset, stream) */
+static PyObject* py_dropout(PyObject* self, PyObject* const* a, Py_ssize_t count) {
+    (void)self;
+    struct call c;
+    struct matrix x, out;
+    deto_rows residual;
+    deto_dropout s;
+    struct memory mem = {.n_outs = 0};
+    uint64_t* more;
+    if (count != 7 || !PyLong_Check(a[4]) || !float_of(a[0], s_rate, &s.rate)) return unusual();
+    PyObject* seed = PyObject_GetAttr(a[0], s_seed);
+    if (!seed) return unusual();
+    const int whole = PyLong_Check(seed);
+    s.seed = whole ? PyLong_AsUnsignedLongLong(seed) : 0;
+    Py_DECREF(seed);
+    if (!whole || PyErr_Occurred()) return unusual();
+    s.offset = PyLong_AsUnsignedLongLong(a[4]);
+    s.reserved = 0;
+    if (PyErr_Occurred() || !begin(&c, a[6]) || !matrix_of(&c, a[1], &x) || x.dt > DT_F16 ||
+        !matrix_of(&c, a[2], &out) || out.dt > DT_F16 || out.T != x.T || out.D != x.D ||
+        !rows_of(&c, a[3], x.T, x.D, out.dt, 1, &residual) || !vector_of(&c, a[5], 1, DT_I64, &more))
+        return unusual();
+    s.device_offset = more;
+    /* in place where types are the same: an element's bytes are then its own */
+    writes(&mem, span_of(&out.m, x.T, x.D), 1);
+    reads(&mem, span_of(&x.m, x.T, x.D), x.dt == out.dt);
+    if (residual.data) reads(&mem, span_of(&residual, x.T, x.D), 1);
+    if (more) reads(&mem, bytes_of(more, 8), 0);
+    if (!apart(&mem)) return unusual();
+    RUN(f_dropout(&s, x.T, x.D, &x.m, OPTIONAL(residual), &out.m, c.stream));
+}
+
+/* setup_block(addresses of the entry points of an attention block, in the order of _MARSHALLED_BLOCK) */
+static PyObject* py_setup_block(PyObject* self, PyObject* f) {
+    (void)self;
+    void** const at[] = {(void**)&f_rotary, (void**)&f_attention_forward, (void**)&f_attention_backward,
+                         (void**)&f_attention_workspace, (void**)&f_dropout};
+    const Py_ssize_t entries = (Py_ssize_t)(sizeof(at) / sizeof(at[0]));
+    if (!PyTuple_Check(f) || PyTuple_GET_SIZE(f) != entries) {
+        PyErr_SetString(PyExc_ValueError, "setup_block: wrong number of entry points");
+        return NULL;
+    }
+    for (Py_ssize_t i = 0; i < entries; ++i) {
+        *at[i] = PyLong_AsVoidPtr(PyTuple_GET_ITEM(f, i));
+        if (PyErr_Occurred()) return NULL;
+    }
+    Py_RETURN_NONE;
+}
+
 /* setup(addresses of the entry points, torch's dtypes in the order of enum dt, current device, current stream of
  * a device, devices) */
 static PyObject* py_setup(PyObject* self, PyObject* args) {
@@ -626,7 +812,10 @@ static PyMethodDef methods[] = {
     FAST("logprobs", py_logprobs), FAST("logprobs_backward", py_logprobs_backward), FAST("norm", py_norm),
     FAST("norm_backward", py_norm_backward), FAST("encode", py_encode), FAST("decode", py_decode),
     FAST("glu_forward", py_glu_forward), FAST("glu_backward", py_glu_backward),
-    FAST("weight_grad", py_weight_grad), {NULL, NULL, 0, NULL}};
+    FAST("weight_grad", py_weight_grad),
+    {"setup_block", py_setup_block, METH_O, "entry points of an attention block"}, FAST("rotary", py_rotary),
+    FAST("attention_forward", py_attention_forward), FAST("attention_backward", py_attention_backward),
+    FAST("dropout", py_dropout), {NULL, NULL, 0, NULL}};
 
 static struct PyModuleDef module = {PyModuleDef_HEAD_INIT, "_model_marshal", NULL, -1, methods,
                                     NULL, NULL, NULL, NULL};
@@ -637,7 +826,10 @@ PyMODINIT_FUNC PyInit__model_marshal(void) {
         {&s_stride, "stride"}, {&s_numel, "numel"}, {&s_dtype, "dtype"}, {&s_data_ptr, "data_ptr"},
         {&s_get_device, "get_device"}, {&s_codes, "codes"}, {&s_exps, "exps"}, {&s_pre, "pre"},
         {&s_post, "post"}, {&s_eps_pre, "eps_pre"}, {&s_eps_post, "eps_post"}, {&s_scale, "scale"},
-        {&s_rows_per_gate, "rows_per_gate"}};
+        {&s_rows_per_gate, "rows_per_gate"}, {&s_heads, "heads"}, {&s_kv_heads, "kv_heads"},
+        {&s_head_dim, "head_dim"}, {&s_rotary_dim, "rotary_dim"}, {&s_layout, "layout"}, {&s_magnitude, "magnitude"},
+        {&s_first, "first"}, {&s_period, "period"}, {&s_causal, "causal"}, {&s_sequences, "sequences"},
+        {&s_rate, "rate"}, {&s_seed, "seed"}};
     for (size_t i = 0; i < sizeof(names) / sizeof(names[0]); ++i)
         if (!(*names[i].at = PyUnicode_InternFromString(names[i].name))) return NULL;
     return PyModule_Create(&module);

@@ -21,6 +21,7 @@ from .binding import BF16, F16, F32, DetonationError, _handle
 
 NORM_NONE, NORM_RMS, NORM_LAYER = 0, 1, 2
 ACT_SILU, ACT_GELU, ACT_GELU_TANH, ACT_RELU = 0, 1, 2, 3
+ROTARY_HALVES, ROTARY_PAIRS = 0, 1
 ACT8_GROUP = 32
 MAX_TOP = 32
 MAX_NORM_WIDTH = 16384
@@ -33,7 +34,8 @@ EXPORTS = ("detonation_token_logprobs", "detonation_token_logprobs_backward",
            "detonation_norm_residual_backward", "detonation_norm_residual_workspace",
            "detonation_act8_encode", "detonation_act8_decode", "detonation_glu_forward",
            "detonation_glu_backward", "detonation_act8_weight_grad",
-           "detonation_act8_weight_grad_workspace")
+           "detonation_act8_weight_grad_workspace", "detonation_rotary", "detonation_attention_forward",
+           "detonation_attention_backward", "detonation_attention_workspace", "detonation_dropout")
 
 
 class deto_rows(ctypes.Structure):
@@ -57,6 +59,23 @@ class deto_norm_residual(ctypes.Structure):
 
 class deto_norm_grads(ctypes.Structure):
     _fields_ = [(n, ctypes.c_void_p) for n in ("w_pre", "b_pre", "w_post", "b_post", "gate")]
+
+
+class deto_rotary(ctypes.Structure):
+    _fields_ = [("layout", ctypes.c_int32), ("heads", ctypes.c_int32), ("head_dim", ctypes.c_int32),
+                ("rotary_dim", ctypes.c_int32), ("inverse", ctypes.c_int32), ("magnitude", ctypes.c_float),
+                ("first", ctypes.c_int64), ("period", ctypes.c_int64)]
+
+
+class deto_attention(ctypes.Structure):
+    _fields_ = [("heads", ctypes.c_int32), ("kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32),
+                ("causal", ctypes.c_int32), ("scale", ctypes.c_float), ("reserved", ctypes.c_int32),
+                ("sequences", ctypes.c_int64), ("q_starts", ctypes.c_void_p), ("k_starts", ctypes.c_void_p)]
+
+
+class deto_dropout(ctypes.Structure):
+    _fields_ = [("seed", ctypes.c_uint64), ("offset", ctypes.c_uint64), ("device_offset", ctypes.c_void_p),
+                ("rate", ctypes.c_float), ("reserved", ctypes.c_int32)]
 
 
 @dataclass
@@ -83,6 +102,36 @@ class Act8:
                     torch.empty((T, -(-D // ACT8_GROUP)), dtype=torch.uint8, device=device))
 
 
+@dataclass
+class Rotary:
+    """Heads of head_dim features whose first rotary_dim (0: all) turn in pairs; without a tensor of positions, row t is
+    at first + t % period (period 0: first + t)."""
+    heads: int
+    head_dim: int
+    rotary_dim: int = 0
+    layout: int = ROTARY_HALVES
+    magnitude: float = 1.0
+    first: int = 0
+    period: int = 0
+
+
+@dataclass
+class Attention:
+    """softmax(scale * q k^T) v: heads of queries, kv_heads of keys and values (0: as many)."""
+    heads: int
+    head_dim: int
+    scale: float
+    kv_heads: int = 0
+    causal: bool = True
+    sequences: int = 1
+
+
+@dataclass
+class Dropout:
+    rate: float
+    seed: int = 0
+
+
 _lib = None
 _codes = None          # torch's types by the library's
 
@@ -95,6 +144,7 @@ def _load():
         vp, i64, i32, f32 = ctypes.c_void_p, ctypes.c_int64, ctypes.c_int32, ctypes.c_float
         rows, act8 = ctypes.POINTER(deto_rows), ctypes.POINTER(deto_act8)
         norm, grads = ctypes.POINTER(deto_norm_residual), ctypes.POINTER(deto_norm_grads)
+        attention = ctypes.POINTER(deto_attention)
         for name, args in {
             "token_logprobs": [i64, i64, rows, f32, vp, i32, vp, vp, vp, i32, vp, vp, vp, vp, vp],
             "token_logprobs_backward": [i64, i64, rows, f32, vp, i32, vp, vp, vp, vp, rows, vp],
@@ -106,11 +156,15 @@ def _load():
             "glu_forward": [i32, i64, i64, rows, rows, rows, act8, act8, vp],
             "glu_backward": [i32, i64, i64, rows, act8, act8, rows, rows, act8, vp],
             "act8_weight_grad": [i64, i64, i64, rows, act8, rows, i32, vp, vp],
+            "rotary": [ctypes.POINTER(deto_rotary), i64, rows, vp, vp, i32, rows, vp],
+            "attention_forward": [attention, i64, i64, rows, rows, rows, rows, vp, vp, vp],
+            "attention_backward": [attention, i64, i64, rows, rows, rows, rows, vp, rows, rows, rows, rows, vp, vp],
+            "dropout": [ctypes.POINTER(deto_dropout), i64, i64, rows, rows, rows, vp],
         }.items():
             f = getattr(lib, "detonation_" + name)
             f.argtypes, f.restype = args, i32
         for name, args in {"token_logprobs": [i64, i64, i32], "norm_residual": [norm, i64, i64],
-                           "act8_weight_grad": [i64, i64, i64]}.items():
+                           "act8_weight_grad": [i64, i64, i64], "attention": [attention, i64, i64]}.items():
             f = getattr(lib, f"detonation_{name}_workspace")
             f.argtypes, f.restype = args, i64
         _codes = {torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16}
@@ -127,6 +181,7 @@ class _NoMarshal:
 
     logprobs_backward = norm = norm_backward = encode = decode = logprobs
     glu_forward = glu_backward = weight_grad = logprobs
+    rotary = attention_forward = attention_backward = dropout = logprobs
 
 
 _marshal = None        # csrc_model/marshal.c, or _NoMarshal; set by the first call
@@ -147,11 +202,13 @@ def _marshalling():
 _MARSHALLED = ("token_logprobs", "token_logprobs_backward", "token_logprobs_workspace", "norm_residual",
                "norm_residual_backward", "norm_residual_workspace", "act8_encode", "act8_decode",
                "glu_forward", "glu_backward", "act8_weight_grad", "act8_weight_grad_workspace")
+_MARSHALLED_BLOCK = ("rotary", "attention_forward", "attention_backward", "attention_workspace", "dropout")
 
 
 def _marshal_types():
     import torch
-    return (torch.float32, torch.bfloat16, torch.float16, torch.int32, torch.int64, torch.int8, torch.uint8)
+    return (torch.float32, torch.bfloat16, torch.float16, torch.int32, torch.int64, torch.int8, torch.uint8,
+            torch.float64)
 
 
 def _load_marshal(lib):
@@ -163,9 +220,12 @@ def _load_marshal(lib):
     spec = importlib.util.spec_from_file_location("_model_marshal", MARSHAL_PATH, loader=loader)
     m = importlib.util.module_from_spec(spec)
     loader.exec_module(m)
-    m.setup(tuple(ctypes.cast(getattr(lib, "detonation_" + n), ctypes.c_void_p).value for n in _MARSHALLED),
-            _marshal_types(), torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream,
+    def addresses(names):
+        return tuple(ctypes.cast(getattr(lib, "detonation_" + n), ctypes.c_void_p).value for n in names)
+
+    m.setup(addresses(_MARSHALLED), _marshal_types(), torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream,
             torch.cuda.device_count())
+    m.setup_block(addresses(_MARSHALLED_BLOCK))
     return m
 
 
@@ -577,3 +637,129 @@ def detonation_act8_weight_grad(dy, x8: Act8, dw, *, accumulate: bool = False, w
     _status(lib.detonation_act8_weight_grad(T, N, K, ctypes.byref(sy), ctypes.byref(q),
                                             ctypes.byref(sw), int(accumulate), ws,
                                             _stream(stream)))
+
+
+# ------------------------------------------------------------------ rotary positions
+
+def rotary_frequencies(rotary_dim: int, *, base: float = 10000.0, factor: float = 1.0, trained: int = 0,
+                       once: float = 1.0, often: float = 32.0, device="cuda"):
+    """Angles of one position for rotary_dim / 2 pairs, base ** (-2 i / rotary_dim), in 64 bits on `device`.  For
+    contexts `factor` times as long as the `trained` one, wavelengths that it holds `often` times or more stay, those
+    that it holds `once` or less become factor times as long, and those between are blended by how often it holds
+    them; trained = 0 lengthens all of them."""
+    import math
+
+    import torch
+    if rotary_dim < 2 or rotary_dim % 2 or not base > 0 or not factor > 0 or trained < 0 or not often > once:
+        raise ValueError("an even rotary_dim, base > 0, factor > 0, trained >= 0 and often > once are needed")
+    f = base ** (-torch.arange(0, rotary_dim, 2, dtype=torch.float64) / rotary_dim)
+    keep = ((f * trained / (2 * math.pi) - once) / (often - once)).clamp(0, 1) if trained else torch.zeros_like(f)
+    return (f * (keep + (1 - keep) / factor)).to(device)
+
+
+def detonation_rotary(cfg: Rotary, x, freqs, out, *, positions=None, inverse: bool = False, stream=None) -> None:
+    """out (may be x): the heads of every row of x [T, heads * head_dim] turned by its position (int32 or int64 [T], or
+    as cfg says) times the pairs' freqs (float64 [rotary_dim / 2]); `inverse` turns back, which is the gradient."""
+    if _taken((_marshal or _marshalling()).rotary(cfg, x, freqs, out, positions, inverse, _handle(stream))):
+        return
+    import torch
+    lib, c = _load(), _Call()
+    T, D = x.shape
+    n = cfg.rotary_dim or cfg.head_dim
+    s = deto_rotary(cfg.layout, cfg.heads, cfg.head_dim, n, int(inverse), cfg.magnitude, cfg.first, cfg.period)
+    if D != cfg.heads * cfg.head_dim:
+        raise ValueError(f"x: rows of {cfg.heads} x {cfg.head_dim} features are needed")
+    xs, os_ = c.rows(x, "x", T, D), c.rows(out, "out", T, D, x.dtype)
+    f = c.vector(freqs, "freqs", n // 2, (torch.float64,), optional=False)
+    p = c.vector(positions, "positions", T, (torch.int64, torch.int32))
+    _disjoint({"out": out}, {"x": x, "freqs": freqs, "positions": positions}, same=(("out", "x"),))
+    _status(lib.detonation_rotary(ctypes.byref(s), T, ctypes.byref(xs), f, p, 0 if p is None else positions.element_size(),
+                                  ctypes.byref(os_), _stream(stream)))
+
+
+# ------------------------------------------------------------------ attention
+
+def _attention_struct(c, cfg, q_starts=None, k_starts=None):
+    s = deto_attention(cfg.heads, cfg.kv_heads or cfg.heads, cfg.head_dim, int(cfg.causal), cfg.scale, 0, cfg.sequences)
+    if c is not None:
+        import torch
+        s.q_starts = c.vector(q_starts, "q_starts", cfg.sequences + 1, (torch.int32,))
+        s.k_starts = c.vector(k_starts, "k_starts", cfg.sequences + 1, (torch.int32,))
+    else:       # a size: with starts any number of rows is fine
+        s.q_starts = s.k_starts = 4
+    return s
+
+
+def attention_workspace(cfg: Attention, Tq: int, Tk: int) -> int:
+    """Bytes of scratch for detonation_attention_forward and detonation_attention_backward."""
+    return _size(_load().detonation_attention_workspace(ctypes.byref(_attention_struct(None, cfg)), Tq, Tk))
+
+
+def detonation_attention_forward(cfg: Attention, q, k, v, out, *, lse=None, q_starts=None, k_starts=None, workspace=None,
+                                 stream=None) -> None:
+    """out [Tq, heads * head_dim] from q (the same) and k, v [Tk, kv_heads * head_dim]; lse [heads, Tq], which the
+    backward pass takes.  q_starts, k_starts: int32 [sequences + 1], the first rows of packed sequences and the row
+    behind the last one; None: sequences of one length."""
+    if _taken((_marshal or _marshalling()).attention_forward(cfg, q, k, v, out, lse, q_starts, k_starts, workspace,
+                                                             _handle(stream))):
+        return
+    import torch
+    lib, c = _load(), _Call()
+    Tq, Tk = q.shape[0], k.shape[0]
+    s = _attention_struct(c, cfg, q_starts, k_starts)
+    wide, narrow = cfg.heads * cfg.head_dim, (cfg.kv_heads or cfg.heads) * cfg.head_dim
+    qs, ks, vs = c.rows(q, "q", Tq, wide), c.rows(k, "k", Tk, narrow, q.dtype), c.rows(v, "v", Tk, narrow, q.dtype)
+    os_, ls = c.rows(out, "out", Tq, wide, q.dtype), c.vector(lse, "lse", cfg.heads * Tq, (torch.float32,))
+    need = lib.detonation_attention_workspace(ctypes.byref(s), Tq, Tk)
+    ws = c.scratch(workspace, need)
+    _disjoint({"out": out, "lse": lse, "workspace": (workspace, need)},
+              {"q": q, "k": k, "v": v, "q_starts": q_starts, "k_starts": k_starts})
+    _status(lib.detonation_attention_forward(ctypes.byref(s), Tq, Tk, ctypes.byref(qs), ctypes.byref(ks), ctypes.byref(vs),
+                                             ctypes.byref(os_), ls, ws, _stream(stream)))
+
+
+def detonation_attention_backward(cfg: Attention, q, k, v, out, lse, dout, dq, dk, dv, *, q_starts=None, k_starts=None,
+                                  workspace=None, stream=None) -> None:
+    """dq, dk and dv, given dout, and out and lse as detonation_attention_forward wrote them."""
+    if _taken((_marshal or _marshalling()).attention_backward(cfg, q, k, v, out, lse, dout, dq, dk, dv, q_starts, k_starts,
+                                                              workspace, _handle(stream))):
+        return
+    import torch
+    lib, c = _load(), _Call()
+    Tq, Tk = q.shape[0], k.shape[0]
+    s = _attention_struct(c, cfg, q_starts, k_starts)
+    wide, narrow = cfg.heads * cfg.head_dim, (cfg.kv_heads or cfg.heads) * cfg.head_dim
+    m = {n: c.rows(t, n, Tk if n in ("k", "v", "dk", "dv") else Tq, narrow if n in ("k", "v", "dk", "dv") else wide, q.dtype)
+         for n, t in (("q", q), ("k", k), ("v", v), ("out", out), ("dout", dout), ("dq", dq), ("dk", dk), ("dv", dv))}
+    ls = c.vector(lse, "lse", cfg.heads * Tq, (torch.float32,), optional=False)
+    need = lib.detonation_attention_workspace(ctypes.byref(s), Tq, Tk)
+    ws = c.scratch(workspace, need)
+    _disjoint({"dq": dq, "dk": dk, "dv": dv, "workspace": (workspace, need)},
+              {"q": q, "k": k, "v": v, "out": out, "lse": lse, "dout": dout, "q_starts": q_starts, "k_starts": k_starts})
+    r = {n: _by_ref(x) for n, x in m.items()}
+    _status(lib.detonation_attention_backward(ctypes.byref(s), Tq, Tk, r["q"], r["k"], r["v"], r["out"], ls, r["dout"],
+                                              r["dq"], r["dk"], r["dv"], ws, _stream(stream)))
+
+
+# ------------------------------------------------------------------ dropout
+
+def detonation_dropout(cfg: Dropout, x, out, *, residual=None, offset: int = 0, device_offset=None, stream=None) -> None:
+    """out = residual + x with a share of cfg.rate of x's elements dropped and the others scaled up; out may be x or the
+    residual, if types are the same.  The same call on out's gradient, without a residual, gives x's.  `offset`: one of
+    its own for every dropout of every step, plus that in device_offset (int64, one element), where a captured call
+    finds another one in each replay."""
+    if _taken((_marshal or _marshalling()).dropout(cfg, x, out, residual, offset, device_offset, _handle(stream))):
+        return
+    import torch
+    lib, c = _load(), _Call()
+    T, D = x.shape
+    if not 0 <= cfg.seed < 1 << 64 or not 0 <= offset < 1 << 64:
+        raise ValueError("seed and offset are numbers of 64 bits")
+    xs, os_ = c.rows(x, "x", T, D), c.rows(out, "out", T, D)
+    rs = c.rows(residual, "residual", T, D, out.dtype)
+    at = c.vector(device_offset, "device_offset", 1, (torch.int64,))
+    _disjoint({"out": out}, {"x": x, "residual": residual, "device_offset": device_offset},
+              same=(("out", "x"), ("out", "residual")))
+    s = deto_dropout(cfg.seed, offset, at, cfg.rate, 0)
+    _status(lib.detonation_dropout(ctypes.byref(s), T, D, ctypes.byref(xs), _by_ref(rs), ctypes.byref(os_),
+                                   _stream(stream)))
