@@ -1,7 +1,8 @@
-// Gradients of attention: three launches.  dout . out of every query and head; then the gradients of keys and values, a
-// workgroup for each 128 keys of a head of keys that walks over the queries that see them, of all heads that share it;
-// then those of queries, a workgroup for each 128 queries that walks over the keys they see.  The weights are computed
-// again from lse in both: two of seven products, but every sum has one owner, who adds in a fixed order.
+// Gradients of attention, in two launches: those of queries, a workgroup for each 128 queries of a head that walks over
+// the keys they see; then those of keys and values, a workgroup for each 128 or 256 keys that walks over the queries that
+// see them, of all heads that share the keys.  The weights are computed again from lse in both: two of seven products,
+// but every sum has one owner, who adds in a fixed order.  The first launch leaves dout . out of every query for the
+// second.
 #include "attention_device.hip.h"
 
 namespace deto {
@@ -9,239 +10,307 @@ namespace model {
 namespace attention {
 namespace {
 
-constexpr int kOwn = kWaves * kSide;        // keys, or queries, of a workgroup
-template <int DT> constexpr int kKeys = DT == DETO_F32 ? 32 : 64;      // of a step of the queries' kernel
-constexpr int kQueries = 32;                // of a step of the keys' kernel
-// fp32 rows and sums of 128 features take the registers of two wavefronts
-template <class S> constexpr int kResident = S::DT == DETO_F32 && S::DP == 128 ? 1 : 2;
-
-// ---- delta[h][t] = dout . out
-constexpr int kDotLanes = 16;
-
-template <int DT>
-__global__ __launch_bounds__(kThreads) void dots_kernel(Args a, FastDiv heads, uint32_t count) {
-    const uint32_t id = blockIdx.x * (kThreads / kDotLanes) + threadIdx.x / kDotLanes;
-    const bool there = id < count;
-    const uint32_t t = heads.div(there ? id : 0), h = (there ? id : 0) - t * heads.d;
-    const int D = a.head_dim, d = threadIdx.x % kDotLanes * 8, n = D - d >= 8 ? 8 : D - d > 0 ? D - d : 0;
-    const int64_t col = int64_t{h} * D;
-    float x[8], y[8], sum = 0.f;
-    unpack8<DT>(load8<DT>(a.out.data + t * a.out.ld + col * kSize<DT>, 0, d, n), x);
-    unpack8<DT>(load8<DT>(a.dout.data + t * a.dout.ld + col * kSize<DT>, 0, d, n), y);
-#pragma unroll
-    for (int j = 0; j < 8; ++j) sum = fmaf(x[j], y[j], sum);
-    sum = lanes_sum<kDotLanes>(sum);
-    if (there && d == 0) a.delta[h * a.Tq + t] = sum;
-}
+// ---- dq: the forward kernel's walk.
+template <int DT> constexpr int kKeys = DT == DETO_F32 ? 32 : 64;      // of a step
 
 // A query's lse in powers of two; one that sees nothing gets weights of zero.
 __device__ __forceinline__ float stored_lse(float lse) {
     return lse == -__builtin_inff() ? __builtin_inff() : lse * kLog2E;
 }
 
-// ---- dq
-template <class S, bool WHOLE>
-__global__ __launch_bounds__(kThreads, 2) void queries_kernel(Args a) {
-    constexpr int DT = S::DT, BN = kKeys<DT>, kMatrix = BN * S::kRow;
-    extern __shared__ __align__(16) char lds[];          // two buffers of keys and values
-    __shared__ uint32_t bits[3][2];                      // rows of keys that hold infinities
-    const uint32_t id = number_in_part();
-    const int h = id / a.tiles;
-    int64_t s;
-    int32_t tile, tiles;
-    if (!find_tile(a, a.q_starts, a.Tq, kOwn, id % a.tiles, s, tile, tiles)) return;
-    if (a.causal) tile = tiles - 1 - tile;
-    const Sequence seq = sequence_of(a, s);
-    const int D = a.head_dim, lane = threadIdx.x % kLanes, half = lane / kSide;
-    const int i0 = tile * kOwn, w0 = i0 + threadIdx.x / kLanes * kSide, i = w0 + lane % kSide;
-    const bool there = i < seq.Lq;
+// the sum of the products of two rows, each half of the lanes holding its part of them
+template <class S>
+__device__ __forceinline__ float rows_dot(const u32x4 (&x)[S::kFrags], const u32x4 (&y)[S::kFrags]) {
+    float sum = 0.f;
+#pragma unroll
+    for (int m = 0; m < S::kFrags; ++m)
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+            if constexpr (S::DT == DETO_F32) {
+                sum = fmaf(bits_f32(x[m][w]), bits_f32(y[m][w]), sum);
+            } else if constexpr (S::DT == DETO_BF16) {
+                sum = fmaf(bits_f32(x[m][w] << 16), bits_f32(y[m][w] << 16), sum);
+                sum = fmaf(bits_f32(x[m][w] & 0xFFFF0000u), bits_f32(y[m][w] & 0xFFFF0000u), sum);
+            } else {
+                const uint32_t wx = x[m][w], wy = y[m][w];
+                const f16x2 a = __builtin_bit_cast(f16x2, wx), b = __builtin_bit_cast(f16x2, wy);
+                sum = fmaf(static_cast<float>(a.x), static_cast<float>(b.x), sum);
+                sum = fmaf(static_cast<float>(a.y), static_cast<float>(b.y), sum);
+            }
+        }
+    return halves_sum(sum);
+}
+
+template <class S, int W, bool DIRECT>
+__global__ __launch_bounds__(W * kLanes, 2) void queries_kernel(Args a) {
+    constexpr int DT = S::DT, BM = W * kSide, BN = kKeys<DT>, kMatrix = BN * S::kRow, kStep = 2 * kMatrix;
+    constexpr int AHEAD = kAhead<W, kStep, DIRECT>;
+    extern __shared__ __align__(16) char lds[];          // AHEAD + 1 steps of keys and values
+    __shared__ uint32_t odd;                             // infinities or NaNs among keys that not all queries see
+    Place at;
+    if (!place_of(a, a.q_starts, a.Tq, BM, a.heads, a.causal, at)) return;
+    const Sequence seq = sequence_of(a, at.s);
+    const int D = DIRECT ? S::DP : a.head_dim, lane = threadIdx.x % kLanes, half = lane / kSide;
+    const int i0 = at.tile * BM, w0 = i0 + threadIdx.x / kLanes * kSide, i = w0 + lane % kSide, last = seq.Lq - 1;
+    const bool there = i <= last;
 
     const auto seen = [&](int n) {
         if (!a.causal) return seq.Lk;
-        const int64_t upto = int64_t{n} + seq.Lk - seq.Lq + 1;
-        return static_cast<int>(upto < 0 ? 0 : upto < seq.Lk ? upto : seq.Lk);
+        const int64_t upto = int64_t{n < last ? n : last} + seq.Lk - last;
+        return static_cast<int>(upto < 0 ? 0 : upto);
     };
-    const int last = seq.Lq - 1;
-    const int upto = seen(i0 + kOwn - 1 < last ? i0 + kOwn - 1 : last);
-    const int wave_upto = seen(w0 + kSide - 1 < last ? w0 + kSide - 1 : last);
-    const int own = seen(i);
-    const int steps = (upto + BN - 1) / BN, whole_steps = seen(i0) / BN;
+    const int upto = seen(i0 + BM - 1), wave_upto = seen(w0 + kSide - 1);
+    const int own = seen(i), steps = (upto + BN - 1) / BN, whole_steps = seen(i0) / BN;
 
-    const int64_t kv = int64_t{h / a.group} * D * S::kElem, col = int64_t{h} * D * S::kElem;
+    const int64_t col = int64_t{at.head} * D * S::kElem, kv = int64_t{at.head / a.group} * D * S::kElem;
+    const int64_t row = seq.q0 + (there ? i : last);
     const char* const keys = a.k.data + seq.k0 * a.k.ld + kv;
     const char* const values = a.v.data + seq.k0 * a.v.ld + kv;
-    const int64_t row = seq.q0 + (there ? i : last);
-    u32x4 q[S::kFrags], g[S::kFrags];
-    load_row<S, WHOLE>(a.q.data + row * a.q.ld + col, there, D, q);
-    load_row<S, WHOLE>(a.dout.data + row * a.dout.ld + col, there, D, g);
+    const char* const query = a.q.data + row * a.q.ld + col;
+    const char* const grad = a.dout.data + row * a.dout.ld + col;
+
+    Rows<S, BN, W, DIRECT> rk, rv;
+    const auto buffer = [&](int step) { return lds + step % (AHEAD + 1) * kStep; };
+    const auto begin = [&](int step) {
+        const int have = seq.Lk - step * BN < BN ? seq.Lk - step * BN : BN;
+        rk.begin(buffer(step), keys + int64_t{step} * BN * a.k.ld, a.k.ld, have, D);
+        rv.begin(buffer(step) + kMatrix, values + int64_t{step} * BN * a.v.ld, a.v.ld, have, D);
+    };
+    const auto end = [&](int step) {
+        rk.end(buffer(step));
+        rv.end(buffer(step) + kMatrix);
+    };
+    if (threadIdx.x == 0) odd = 0;
+#pragma unroll
+    for (int n = 0; n < AHEAD; ++n)
+        if (n < steps) begin(n);
+    if (steps > 0) end(0);
+
     const float factor = a.scale * kLog2E;
-    const float lse = there ? stored_lse(a.lse[h * a.Tq + row]) : __builtin_inff();
-    const float delta = there ? a.delta[h * a.Tq + row] : 0.f;
+    u32x4 q[S::kFrags], g[S::kFrags];
+    load_row<S>(grad, there, D, g);
+    load_row<S>(a.out.data + row * a.out.ld + col, there, D, q);
+    const float lse = there ? stored_lse(a.lse[at.head * a.Tq + row]) : __builtin_inff();
+    const float delta = rows_dot<S>(g, q);
+    if (there && half == 0) {
+        a.stats[at.head * a.Tq + row] = lse;
+        a.stats[(a.heads + at.head) * a.Tq + row] = delta;
+    }
+    load_row<S>(query, there, D, q);
     f32x16 dq[S::kBlocks] = {};
 
-    if (threadIdx.x < 6) bits[threadIdx.x / 2][threadIdx.x % 2] = 0;
-    __syncthreads();
-    Stage<S, BN, WHOLE> sk, sv;
-    const auto have = [&](int step) { return seq.Lk - step * BN < BN ? seq.Lk - step * BN : BN; };
-    const auto load = [&](int step) {
-        sk.load(keys + int64_t{step} * BN * a.k.ld, a.k.ld, have(step), D);
-        sv.load(values + int64_t{step} * BN * a.v.ld, a.v.ld, have(step), D);
-    };
-    const auto store = [&](int step) {
-        char* const at = lds + step % 2 * 2 * kMatrix;
-        if (step >= whole_steps) sk.template store<true>(at, have(step), bits[step % 3]);
-        else sk.template store<false>(at, have(step), nullptr);
-        sv.template store<false>(at + kMatrix, have(step), nullptr);
-    };
     const auto compute = [&](int step, auto masked) {
         constexpr bool MASKED = masked.value != 0;
-        const char* const at = lds + step % 2 * 2 * kMatrix;
+        const char* const from = buffer(step);
         const int left = own - step * BN - half * 4;
 #pragma unroll
         for (int b = 0; b < BN / kSide; ++b) {
-            f32x16 x = rows_product<S>(at, b, q);
-            const f32x16 y = rows_product<S>(at + kMatrix, b, g);
+            f32x16 x = rows_product<S>(from, b, q);
+            const f32x16 y = rows_product<S>(from + kMatrix, b, g);
 #pragma unroll
             for (int r = 0; r < 16; ++r) {
                 x[r] = power2(fmaf(x[r], factor, -lse)) * (y[r] - delta);
                 if (MASKED) x[r] = b * kSide + (r / 4) * 8 + r % 4 < left ? x[r] : 0.f;
             }
-            columns_product<S>(at, b, x, dq);
-            if (MASKED) {
-                const uint32_t odd = bits[step % 3][b];
-                if (odd)
-                    add_infinities<S>(odd, keys + (int64_t{step} * BN + b * kSide) * a.k.ld, a.k.ld, D, x,
-                                      [&](int n) { return step * BN + b * kSide + n < own; }, dq);
-            }
+            columns_product<S>(from, b, x, dq);
         }
     };
 
-    if (steps > 0) {
-        load(0);
-        store(0);
-    }
-    __syncthreads();
     for (int step = 0; step < steps; ++step) {
-        if (threadIdx.x < 2) bits[(step + 2) % 3][threadIdx.x] = 0;
-        if (step + 1 < steps) load(step + 1);
-        if (step < whole_steps) compute(step, Type<0>{});
-        else if (step * BN < wave_upto) compute(step, Type<1>{});
-        if (step + 1 < steps) store(step + 1);
-        __syncthreads();
+        if constexpr (DIRECT) arrived_but<2 * Rows<S, BN, W, DIRECT>::kCalls>(min(AHEAD - 1, steps - 1 - step));
+        meet();
+        if (step + AHEAD < steps) begin(step + AHEAD);
+        if (step < whole_steps) {
+            compute(step, Type<0>{});
+        } else {
+            take_out_odd<S, BN, W>(buffer(step), &odd);
+            meet();
+            if (step * BN < wave_upto) compute(step, Type<1>{});
+        }
+        if (step + AHEAD < steps) end(step + AHEAD);
+    }
+
+    if (steps > whole_steps && odd) {
+        for (int j = whole_steps * BN; j < wave_upto; ++j) {
+            const char* const key = keys + j * a.k.ld;
+            if (!row_is_odd<S>(key, D)) continue;
+            const float p = power2(fmaf(slow_dot<S>(query, key, D), factor, -lse));
+            const float ds = p * (slow_dot<S>(grad, values + j * a.v.ld, D) - delta);
+            if (j < own) add_odd<S>(key, D, ds, dq);
+        }
     }
     store_columns<S>(dq, a.scale, a.dq.data + row * a.dq.ld + col, there, D);
 }
 
 // ---- dk, dv
-template <class S, bool WHOLE>
-__global__ __launch_bounds__(kThreads, kResident<S>) void keys_kernel(Args a) {
-    constexpr int BQ = kQueries, kMatrix = BQ * S::kRow;
-    extern __shared__ __align__(16) char lds[];          // two buffers of queries and gradients of outputs
-    __shared__ __align__(16) float stats[2][2][BQ];      // two buffers of lse and delta
-    __shared__ uint32_t bits[3][2];                      // rows of queries, of gradients that hold infinities
-    const uint32_t id = number_in_part();
-    const int hk = id / a.tiles;
-    int64_t s;
-    int32_t tile, tiles;
-    if (!find_tile(a, a.k_starts, a.Tk, kOwn, id % a.tiles, s, tile, tiles)) return;
-    const Sequence seq = sequence_of(a, s);
-    const int D = a.head_dim, lane = threadIdx.x % kLanes, half = lane / kSide;
-    const int j0 = tile * kOwn, w0 = j0 + threadIdx.x / kLanes * kSide, j = w0 + lane % kSide;
-    const bool there = j < seq.Lk;
+template <class S> constexpr int kQueries = S::kRow >= 256 ? 32 : 64;                // of a step
+template <class S, int W, bool DIRECT>
+constexpr int kAheadOfKeys = DIRECT ? (S::kRow > 256 ? 1 : 3) : 1;
+// Sums of fp32 take the registers of two wavefronts with 128 features; 16-bit values of 128 features stay in LDS, which
+// leaves the registers that two wavefronts need beside keys and sums.
+template <class S> constexpr int kResident = S::kRow > 256 ? 1 : 2;
+template <class S> constexpr bool kValuesStay = S::kRow == 256 && S::DT != DETO_F32;
+
+template <class S, int W, bool DIRECT>
+__global__ __launch_bounds__(W * kLanes, kResident<S>) void keys_kernel(Args a) {
+    constexpr int BN = W * kSide, BQ = kQueries<S>, kMatrix = BQ * S::kRow, kStep = 2 * kMatrix;
+    constexpr bool STAY = kValuesStay<S>;
+    constexpr int AHEAD = kAheadOfKeys<S, W, DIRECT>;
+    extern __shared__ __align__(16) char lds[];          // AHEAD + 1 steps of queries and gradients of outputs; values
+    __shared__ __align__(16) float stats[AHEAD + 1][2 * BQ];      // lse and delta
+    __shared__ uint32_t odd;                             // infinities or NaNs among rows that do not see all keys
+    Place at;
+    if (!place_of(a, a.k_starts, a.Tk, BN, a.kv_heads, false, at)) return;
+    const Sequence seq = sequence_of(a, at.s);
+    const int D = DIRECT ? S::DP : a.head_dim, lane = threadIdx.x % kLanes, half = lane / kSide;
+    const int in_tile = threadIdx.x / kLanes * kSide + lane % kSide, j0 = at.tile * BN, j = j0 + in_tile;
+    const int last = seq.Lk - 1;
+    const bool there = j <= last;
 
     // the first query that sees key n
     const auto seen_from = [&](int n) {
         if (!a.causal) return 0;
-        const int64_t from = int64_t{n} - seq.Lk + seq.Lq;
-        return static_cast<int>(from < 0 ? 0 : from < seq.Lq ? from : seq.Lq);
+        const int64_t from = int64_t{n < last ? n : last} - last - 1 + seq.Lq;
+        return static_cast<int>(from < 0 ? 0 : from);
     };
-    const int last = seq.Lk - 1;
     const int first_step = seen_from(j0) / BQ, steps = (seq.Lq + BQ - 1) / BQ - first_step;    // of a head
-    const int all_from = seen_from(j0 + kOwn - 1 < last ? j0 + kOwn - 1 : last);     // seen by these queries in full
-    const int wave_from = seen_from(w0 < last ? w0 : last);
-    const int own = seen_from(there ? j : last);
+    const int all_from = seen_from(j0 + BN - 1);                 // from here on queries see all of these keys
+    const int wave_from = seen_from(j0 + threadIdx.x / kLanes * kSide), own = seen_from(j);
+    const int total = steps * a.group;                           // a head's steps, then the next one's
 
-    const int64_t kv = int64_t{hk} * D * S::kElem;
-    const int64_t row = seq.k0 + (there ? j : last);
-    u32x4 k[S::kFrags], v[S::kFrags];
-    load_row<S, WHOLE>(a.k.data + row * a.k.ld + kv, there, D, k);
-    load_row<S, WHOLE>(a.v.data + row * a.v.ld + kv, there, D, v);
+    const int64_t kv = int64_t{at.head} * D * S::kElem, row = seq.k0 + (there ? j : last);
+    const char* const key = a.k.data + row * a.k.ld + kv;
+    const char* const value = a.v.data + row * a.v.ld + kv;
+
+    Rows<S, BQ, W, DIRECT> rq, rg;
+    float stat[2 * BQ / kLanes];
+    // a step: of which head, from which query on, and its buffer
+    struct Step {
+        int head, query, buffer;
+    };
+    const auto next = [&](Step s) {
+        s.query += BQ;
+        if (s.query >= seq.Lq) {
+            s.query = first_step * BQ;
+            ++s.head;
+        }
+        s.buffer = s.buffer == AHEAD ? 0 : s.buffer + 1;
+        return s;
+    };
+    const auto begin = [&](Step s) {
+        char* const to = lds + s.buffer * kStep;
+        const int have = seq.Lq - s.query < BQ ? seq.Lq - s.query : BQ;
+        const int64_t first = seq.q0 + s.query, col = int64_t{s.head} * D * S::kElem;
+        rq.begin(to, a.q.data + first * a.q.ld + col, a.q.ld, have, D);
+        rg.begin(to + kMatrix, a.dout.data + first * a.dout.ld + col, a.dout.ld, have, D);
+        // lse and delta, 64 at a time, all wavefronts the same
+#pragma unroll
+        for (int c = 0; c < 2 * BQ / kLanes; ++c) {
+            const int n = c * kLanes + lane, t = n % BQ;
+            const float* const from = a.stats + (int64_t{n / BQ} * a.heads + s.head) * a.Tq + first + (t < have ? t : have - 1);
+            if constexpr (DIRECT)
+                __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)from,
+                                                 (__attribute__((address_space(3))) void*)(stats[s.buffer] + c * kLanes), 4, 0, 0);
+            else stat[c] = *from;
+        }
+    };
+    const auto end = [&](Step s) {
+        char* const to = lds + s.buffer * kStep;
+        rq.end(to);
+        rg.end(to + kMatrix);
+        if constexpr (!DIRECT) {
+#pragma unroll
+            for (int c = 0; c < 2 * BQ / kLanes; ++c) stats[s.buffer][c * kLanes + lane] = stat[c];
+        }
+    };
+    if (threadIdx.x == 0) odd = 0;
+    if constexpr (STAY) {
+        Rows<S, BN, W, DIRECT> rv;
+        rv.begin(lds + (AHEAD + 1) * kStep, a.v.data + (seq.k0 + j0) * a.v.ld + kv, a.v.ld, last - j0 < BN ? last - j0 + 1 : BN, D);
+        rv.end(lds + (AHEAD + 1) * kStep);
+    }
+    Step now = {at.head * a.group, first_step * BQ, 0}, ahead = now;
+#pragma unroll
+    for (int n = 0; n < AHEAD; ++n)
+        if (n < total) {
+            begin(ahead);
+            if constexpr (DIRECT) ahead = next(ahead);
+        }
+    if (total > 0 && !DIRECT) {
+        end(ahead);
+        ahead = next(ahead);
+    }
+
+    u32x4 k[S::kFrags], v[STAY ? 1 : S::kFrags];
+    load_row<S>(key, there, D, k);
+    if constexpr (!STAY) load_row<S>(value, there, D, v);
     const float factor = a.scale * kLog2E;
     f32x16 dk[S::kBlocks] = {}, dv[S::kBlocks] = {};
 
-    if (threadIdx.x < 6) bits[threadIdx.x / 2][threadIdx.x % 2] = 0;
-    __syncthreads();
-    Stage<S, BQ, WHOLE> sq, sg;
-    float stat = 0.f;
-    const int total = steps * a.group;                   // a head's steps, then the next one's
-    const auto head = [&](int n) { return hk * a.group + n / steps; };
-    const auto first = [&](int n) { return (first_step + n % steps) * BQ; };
-    const auto have = [&](int n) { return seq.Lq - first(n) < BQ ? seq.Lq - first(n) : BQ; };
-    const auto load = [&](int n) {
-        const int64_t at = seq.q0 + first(n), col = int64_t{head(n)} * D * S::kElem;
-        sq.load(a.q.data + at * a.q.ld + col, a.q.ld, have(n), D);
-        sg.load(a.dout.data + at * a.dout.ld + col, a.dout.ld, have(n), D);
-        const int t = threadIdx.x % BQ;
-        if (threadIdx.x < 2 * BQ && t < have(n)) stat = (threadIdx.x < BQ ? a.lse : a.delta)[head(n) * a.Tq + at + t];
-    };
-    const auto store = [&](int n) {
-        char* const at = lds + n % 2 * 2 * kMatrix;
-        if (first(n) < all_from) {
-            sq.template store<true>(at, have(n), &bits[n % 3][0]);
-            sg.template store<true>(at + kMatrix, have(n), &bits[n % 3][1]);
-        } else {
-            sq.template store<false>(at, have(n), nullptr);
-            sg.template store<false>(at + kMatrix, have(n), nullptr);
-        }
-        if (threadIdx.x < 2 * BQ) {
-            const bool is_lse = threadIdx.x < BQ, past = static_cast<int>(threadIdx.x % BQ) >= have(n);
-            stats[n % 2][!is_lse][threadIdx.x % BQ] =
-                past ? (is_lse ? __builtin_inff() : 0.f) : is_lse ? stored_lse(stat) : stat;
-        }
-    };
-    const auto compute = [&](int n, auto masked) {
+    const auto compute = [&](Step s, auto masked) {
         constexpr bool MASKED = masked.value != 0;
-        const char* const at = lds + n % 2 * 2 * kMatrix;
-        const int from = own - first(n) - half * 4;          // of the step's queries, those that see the key
-        f32x16 p = rows_product<S>(at, 0, k);
+        const char* const from = lds + s.buffer * kStep;
 #pragma unroll
-        for (int r = 0; r < 16; ++r) {
-            const int t = (r / 4) * 8 + r % 4;
-            p[r] = power2(fmaf(p[r], factor, -stats[n % 2][0][t + half * 4]));
-            if (MASKED) p[r] = t >= from ? p[r] : 0.f;
-        }
-        f32x16 ds = rows_product<S>(at + kMatrix, 0, v);
+        for (int b = 0; b < BQ / kSide; ++b) {
+            const int first = s.query + b * kSide + half * 4, upto = seq.Lq - first, own_from = own - first;
+            const float* const stat = stats[s.buffer] + b * kSide + half * 4;
+            f32x16 p = rows_product<S>(from, b, k);
 #pragma unroll
-        for (int r = 0; r < 16; ++r) {
-            const int t = (r / 4) * 8 + r % 4;
-            ds[r] = p[r] * (ds[r] - stats[n % 2][1][t + half * 4]);
-            if (MASKED) ds[r] = t >= from ? ds[r] : 0.f;
-        }
-        columns_product<S>(at + kMatrix, 0, p, dv);
-        columns_product<S>(at, 0, ds, dk);
-        if (MASKED) {
-            const uint32_t odd_q = bits[n % 3][0], odd_g = bits[n % 3][1];
-            if (odd_q | odd_g) {
-                const int64_t at = seq.q0 + first(n), col = int64_t{head(n)} * D * S::kElem;
-                const auto sees = [&](int t) { return first(n) + t >= own; };
-                add_infinities<S>(odd_g, a.dout.data + at * a.dout.ld + col, a.dout.ld, D, p, sees, dv);
-                add_infinities<S>(odd_q, a.q.data + at * a.q.ld + col, a.q.ld, D, ds, sees, dk);
+            for (int r = 0; r < 16; ++r) {
+                const int t = (r / 4) * 8 + r % 4;
+                p[r] = power2(fmaf(p[r], factor, -stat[t]));
+                if (MASKED) p[r] = t >= own_from && t < upto ? p[r] : 0.f;
             }
+            f32x16 ds;
+            if constexpr (STAY) ds = rows_product<S>(from + kMatrix, b, lds + (AHEAD + 1) * kStep, in_tile);
+            else ds = rows_product<S>(from + kMatrix, b, v);
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+                const int t = (r / 4) * 8 + r % 4;
+                ds[r] = p[r] * (ds[r] - stat[BQ + t]);
+                if (MASKED) ds[r] = t >= own_from && t < upto ? ds[r] : 0.f;
+            }
+            columns_product<S>(from + kMatrix, b, p, dv);
+            columns_product<S>(from, b, ds, dk);
         }
     };
 
-    if (total > 0) {
-        load(0);
-        store(0);
-    }
-    __syncthreads();
     for (int n = 0; n < total; ++n) {
-        if (threadIdx.x < 2) bits[(n + 2) % 3][threadIdx.x] = 0;
-        if (n + 1 < total) load(n + 1);
-        if (first(n) >= all_from) compute(n, Type<0>{});
-        else if (first(n) + BQ > wave_from) compute(n, Type<1>{});
-        if (n + 1 < total) store(n + 1);
-        __syncthreads();
+        if constexpr (DIRECT) arrived_but<2 * Rows<S, BQ, W, DIRECT>::kCalls + 2 * BQ / kLanes>(min(AHEAD - 1, total - 1 - n));
+        meet();
+        const bool more = n + AHEAD < total;
+        if (more) begin(ahead);
+        if (now.query >= all_from && now.query + BQ <= seq.Lq) {
+            compute(now, Type<0>{});
+        } else {
+            take_out_odd<S, BQ, W>(lds + now.buffer * kStep, &odd);
+            take_out_odd<S, BQ, W>(lds + now.buffer * kStep + kMatrix, &odd);
+            meet();
+            if (now.query + BQ > wave_from) compute(now, Type<1>{});
+        }
+        if (more) {
+            end(ahead);
+            ahead = next(ahead);
+        }
+        now = next(now);
+    }
+
+    if (total > 0 && odd) {
+        const int tail = seq.Lq / BQ * BQ;                  // steps that were masked: up to all_from, and a short last one
+        for (int h = at.head * a.group; h < (at.head + 1) * a.group; ++h)
+            for (int t = first_step * BQ; t < seq.Lq; ++t) {
+                if (t >= (all_from + BQ - 1) / BQ * BQ && t < tail) t = tail;
+                if (t >= seq.Lq) break;
+                const int64_t at_t = seq.q0 + t, col = int64_t{h} * D * S::kElem;
+                const char *const query = a.q.data + at_t * a.q.ld + col, *const grad = a.dout.data + at_t * a.dout.ld + col;
+                const bool odd_q = row_is_odd<S>(query, D), odd_g = row_is_odd<S>(grad, D);
+                if (!odd_q && !odd_g) continue;
+                const float p = power2(fmaf(slow_dot<S>(query, key, D), factor, -a.stats[h * a.Tq + at_t]));
+                const float ds = p * (slow_dot<S>(grad, value, D) - a.stats[(a.heads + h) * a.Tq + at_t]);
+                if (t < own) continue;
+                add_odd<S>(grad, D, p, dv);
+                add_odd<S>(query, D, ds, dk);
+            }
     }
     store_columns<S>(dk, a.scale, a.dk.data + row * a.dk.ld + kv, there, D);
     store_columns<S>(dv, 1.f, a.dv.data + row * a.dv.ld + kv, there, D);
@@ -276,7 +345,7 @@ int detonation_attention_backward(const deto_attention* cfg, int64_t Tq, int64_t
     if (!is_aligned(lse, 4) || !is_aligned(workspace, 16)) return DETO_ERR_ALIGN;
     Args a = args_of(cfg, Tq, Tk, q, k, v);
     a.lse = const_cast<float*>(lse);
-    a.delta = static_cast<float*>(workspace);
+    a.stats = static_cast<float*>(workspace);
     if (Tq) {
         a.out = matrix_of(out);
         a.dout = matrix_of(dout);
@@ -286,23 +355,36 @@ int detonation_attention_backward(const deto_attention* cfg, int64_t Tq, int64_t
         a.dk = matrix_of(dk);
         a.dv = matrix_of(dv);
     }
-    Args by_keys = a;
-    if (!plan(a, cfg->q_starts, Tq, kOwn, H) || !plan(by_keys, cfg->k_starts, Tk, kOwn, K) || Tq * H >= (int64_t{1} << 31))
-        return DETO_ERR_UNSUPPORTED;
     const hipStream_t on = static_cast<hipStream_t>(stream);
+    int planned = DETO_OK;
     fresh();
     by_type(dtype, [&](auto dt) {
-        const uint32_t dots = static_cast<uint32_t>(Tq * H);
-        constexpr uint32_t kEach = kThreads / kDotLanes;
-        if (dots) dots_kernel<dt.value><<<(dots + kEach - 1) / kEach, kThreads, 0, on>>>(a, FastDiv(static_cast<uint32_t>(H)), dots);
-        return by_shape<dt.value>(cfg->head_dim, [&](auto shape, auto whole) {
+        return by_shape<dt.value>(cfg->head_dim, in_pieces(a.q) && in_pieces(a.k) && in_pieces(a.v) && in_pieces(a.dout),
+                                  [&](auto shape, auto direct) {
             using S = decltype(shape);
-            if (Tk) keys_kernel<S, whole.value != 0><<<by_keys.tiles * K, kThreads, 4 * kQueries * S::kRow, on>>>(by_keys);
-            if (Tq) queries_kernel<S, whole.value != 0><<<a.tiles * H, kThreads, 4 * kKeys<S::DT> * S::kRow, on>>>(a);
-            return 0;
+            constexpr bool DIRECT = direct.value != 0;
+            const auto queries = [&](auto waves) {
+                constexpr int W = waves.value, kStep = 2 * kKeys<S::DT> * S::kRow;
+                if (!plan(a, cfg->q_starts, Tq, W * kSide, H)) return DETO_ERR_UNSUPPORTED;
+                if (Tq) queries_kernel<S, W, DIRECT><<<a.tiles * H, W * kLanes, (kAhead<W, kStep, DIRECT> + 1) * kStep, on>>>(a);
+                return DETO_OK;
+            };
+            const auto keys = [&](auto waves) {
+                constexpr int W = waves.value, kStep = 2 * kQueries<S> * S::kRow;
+                constexpr int kLds = (kAheadOfKeys<S, W, DIRECT> + 1) * kStep + (kValuesStay<S> ? W * kSide * S::kRow : 0);
+                if (!plan(a, cfg->k_starts, Tk, W * kSide, K)) return DETO_ERR_UNSUPPORTED;
+                if (Tk) keys_kernel<S, W, DIRECT><<<a.tiles * K, W * kLanes, kLds, on>>>(a);
+                return DETO_OK;
+            };
+            planned = Tq * H >= int64_t{256} * kCUs ? queries(Type<8>{}) : queries(Type<4>{});
+            if (planned) return planned;
+            if constexpr (kResident<S> == 2) {
+                if (Tk * K >= int64_t{256} * kCUs) return planned = keys(Type<8>{});
+            }
+            return planned = keys(Type<4>{});
         });
     });
-    return enqueued();
+    return planned ? planned : enqueued();
 }
 
 }  // extern "C"

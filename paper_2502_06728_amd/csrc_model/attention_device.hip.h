@@ -23,8 +23,7 @@ typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x8 __attribute__((ext_vector_type(8)));
 
 constexpr int kSide = 32;               // of a block
-constexpr int kWaves = 4;
-constexpr int kThreads = kWaves * kLanes;
+constexpr int kCUs = 256;
 constexpr float kLog2E = 1.44269504088896341f, kLn2 = 0.693147180559945309f;
 
 // A head's features, padded with zeros to DP.
@@ -47,7 +46,7 @@ struct Matrix {
 struct Args {
     Matrix q, k, v, out, dout, dq, dk, dv;
     float* lse;
-    float* delta;                        // [heads, Tq]: dout . out
+    float* stats;                        // [2, heads, Tq]: lse in powers of two, and dout . out
     const int32_t *q_starts, *k_starts;
     int64_t Tq, Tk, sequences;
     int32_t heads, kv_heads, group, head_dim, causal;
@@ -83,16 +82,10 @@ __device__ __forceinline__ Sequence sequence_of(const Args& a, int64_t s) {
     return seq;
 }
 
-// Tile number `id` of all sequences' rows, `size` rows a tile: its sequence, and which of that one's tiles it is.  False
-// where there are fewer.  The sequences' tiles are counted 64 at a time, a lane each.
+// Tile number `id` of all packed sequences' rows, `size` rows a tile: its sequence, and which of that one's tiles it is.
+// False where there are fewer.  The sequences' tiles are counted 64 at a time, a lane each.
 __device__ __forceinline__ bool find_tile(const Args& a, const int32_t* starts, int64_t T, int size, uint32_t id,
                                           int64_t& s, int32_t& tile, int32_t& tiles) {
-    if (!starts) {
-        s = id / a.per_sequence;
-        tile = static_cast<int32_t>(id % a.per_sequence);
-        tiles = static_cast<int32_t>(a.per_sequence);
-        return true;
-    }
     const int lane = threadIdx.x % kLanes;
     int64_t before = 0;
     for (int64_t base = 0; base < a.sequences; base += kLanes) {
@@ -119,11 +112,41 @@ __device__ __forceinline__ bool find_tile(const Args& a, const int32_t* starts, 
     return false;
 }
 
-// Workgroups go to the chip's eight parts in turn; each part takes a run of numbers: the tiles of a head and the heads
-// that share its keys, which its own cache then holds for all of them.
-__device__ __forceinline__ uint32_t number_in_part() {
-    const uint32_t all = gridDim.x, part = blockIdx.x % 8, each = all / 8, more = all % 8;
-    return part * each + (part < more ? part : more) + blockIdx.x / 8;
+// A workgroup's tile and head.  Workgroups go to the chip's eight parts in turn; heads are dealt out so that those in a
+// row, which share keys, meet in one part, whose own cache then holds these for all of them.  Under a mask the longest
+// tiles of all heads come first (`last_first`: those are the last ones), so that no long one is left over at the end;
+// without one, a head's tiles follow each other.
+struct Place {
+    int64_t s;
+    int32_t head, tile;
+};
+__device__ __forceinline__ bool place_of(const Args& a, const int32_t* starts, int64_t T, int size, int heads, bool last_first,
+                                         Place& p) {
+    const uint32_t rows = starts ? a.tiles : a.per_sequence;                 // of the grid: tiles of a column
+    const uint32_t columns = starts ? heads : static_cast<uint32_t>(heads * a.sequences);
+    uint32_t row, column;
+    if (a.causal) {
+        row = blockIdx.x / columns;
+        column = blockIdx.x % columns;
+        if (columns % 8 == 0) column = column % 8 * (columns / 8) + column / 8;
+    } else {
+        const uint32_t all = gridDim.x, part = blockIdx.x % 8, each = all / 8, more = all % 8;
+        const uint32_t n = part * each + (part < more ? part : more) + blockIdx.x / 8;
+        row = n % rows;
+        column = n / rows;
+    }
+    int32_t tiles;
+    if (starts) {
+        p.head = column;
+        if (!find_tile(a, starts, T, size, row, p.s, p.tile, tiles)) return false;
+    } else {
+        p.s = column / heads;
+        p.head = column % heads;
+        p.tile = row;
+        tiles = rows;
+    }
+    if (last_first) p.tile = tiles - 1 - p.tile;
+    return true;
 }
 
 // ---- matrices in LDS.  Piece p of row r lies at piece p ^ twist(r) of that row: eight lanes that read one piece of
@@ -137,11 +160,10 @@ __device__ __forceinline__ int twist(int row) {
 template <class S>
 __device__ __forceinline__ uint32_t place(int row, int piece) { return row * S::kRow + ((piece ^ twist<S>(row)) << 4); }
 
-// features d ... of a row of which `D` are there (16 bytes, zeros behind)
-template <class S, bool WHOLE>
+// piece `piece` of a row of D features: 16 bytes, zeros behind the last feature
+template <class S>
 __device__ __forceinline__ u32x4 load_piece(const char* row, int piece, int D) {
     const int d = piece * S::kOf;
-    if constexpr (WHOLE) return *reinterpret_cast<const u32x4_any2*>(row + d * S::kElem);
     u32x4 r = {0, 0, 0, 0};
     if (d + S::kOf <= D) return *reinterpret_cast<const u32x4_any2*>(row + d * S::kElem);
     if (d >= D) return r;
@@ -157,58 +179,144 @@ __device__ __forceinline__ u32x4 load_piece(const char* row, int piece, int D) {
     return r;
 }
 
-// Whether a piece holds an infinity or a NaN; those are made zeros.
-template <class S>
-__device__ __forceinline__ bool take_out_infinities(u32x4& r) {
-    bool any = false;
+// Rows into LDS by a workgroup of W wavefronts.  Rows that are missing at the end of a sequence are copies of the last
+// one: what they are multiplied with is zero.
+// DIRECT: heads of DP features at multiples of 16 bytes, from memory to LDS without a register: a wavefront's call writes
+// 64 pieces in a row, so its lanes read the pieces that belong there.  begin() starts kCalls of these; who reads the rows
+// waits until they have come (arrived()), and for the other wavefronts' (meet()).
+// Otherwise through registers: begin() loads, end() stores.
+template <class S, int ROWS, int W, bool DIRECT>
+struct Rows {
+    static constexpr int kThreads = W * kLanes, kUnits = DIRECT ? 1 : ROWS * S::kPieces / kThreads;
+    static constexpr int kOfCall = kLanes / S::kPieces, kCalls = ROWS / kOfCall / W;
+    static_assert(ROWS * S::kPieces % kThreads == 0, "");
+    u32x4 r[kUnits];
+
+    // `have` (1 or more) rows from `at` on
+    __device__ __forceinline__ void begin(char* lds, const char* at, int64_t ld, int have, int D) {
+        if constexpr (DIRECT) {
+            const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kLanes), lane = threadIdx.x % kLanes;
 #pragma unroll
-    for (int w = 0; w < 4; ++w) {
-        if constexpr (S::DT == DETO_F32) {
-            if ((r[w] & 0x7F800000u) == 0x7F800000u) {
-                any = true;
-                r[w] = 0;
+            for (int i = 0; i < kCalls; ++i) {
+                const int first = (wave + i * W) * kOfCall, row = first + lane / S::kPieces;
+                const uint32_t off = static_cast<uint32_t>(row < have ? row : have - 1) * static_cast<uint32_t>(ld) +
+                                     ((lane % S::kPieces) ^ twist<S>(row)) * 16;
+                __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(at + off),
+                                                 (__attribute__((address_space(3))) void*)(lds + first * S::kRow), 16, 0, 0);
             }
         } else {
-            constexpr uint32_t kExponent = S::DT == DETO_BF16 ? 0x7F80u : 0x7C00u;
-            if ((r[w] & kExponent) == kExponent) {
-                any = true;
-                r[w] &= 0xFFFF0000u;
-            }
-            if ((r[w] & kExponent << 16) == kExponent << 16) {
-                any = true;
-                r[w] &= 0xFFFFu;
+#pragma unroll
+            for (int i = 0; i < kUnits; ++i) {
+                const int unit = threadIdx.x + i * kThreads, row = unit / S::kPieces;
+                r[i] = load_piece<S>(at + (row < have ? row : have - 1) * ld, unit % S::kPieces, D);
             }
         }
     }
-    return any;
-}
-
-// ROWS rows on their way from memory to LDS through a workgroup's registers.  Rows past the last one are zeros.
-template <class S, int ROWS, bool WHOLE>
-struct Stage {
-    static constexpr int kUnits = ROWS * S::kPieces / kThreads;
-    static_assert(ROWS * S::kPieces % kThreads == 0, "");
-    u32x4 r[kUnits];
-    static __device__ __forceinline__ int row(int i) { return (threadIdx.x + i * kThreads) / S::kPieces; }
-    static __device__ __forceinline__ int piece(int i) { return (threadIdx.x + i * kThreads) % S::kPieces; }
-
-    // `have` (1 or more) rows from `at` on
-    __device__ __forceinline__ void load(const char* at, int64_t ld, int have, int D) {
+    __device__ __forceinline__ void end(char* lds) {
+        if constexpr (!DIRECT) {
 #pragma unroll
-        for (int i = 0; i < kUnits; ++i)
-            r[i] = load_piece<S, WHOLE>(at + (row(i) < have ? row(i) : have - 1) * ld, piece(i), D);
-    }
-    // CLEAN: infinities and NaNs are left out, and their rows' bits are set
-    template <bool CLEAN>
-    __device__ __forceinline__ void store(char* lds, int have, uint32_t* bits) {
-#pragma unroll
-        for (int i = 0; i < kUnits; ++i) {
-            if (row(i) >= have) r[i] = {0, 0, 0, 0};
-            if (CLEAN && take_out_infinities<S>(r[i])) atomicOr(bits + row(i) / kSide, 1u << (row(i) % kSide));
-            *reinterpret_cast<u32x4*>(lds + place<S>(row(i), piece(i))) = r[i];
+            for (int i = 0; i < kUnits; ++i) {
+                const int unit = threadIdx.x + i * kThreads;
+                *reinterpret_cast<u32x4*>(lds + place<S>(unit / S::kPieces, unit % S::kPieces)) = r[i];
+            }
         }
     }
 };
+
+// Steps that are on their way while one is computed: three, where the workgroups that share a CU then have room in its
+// LDS (two of four wavefronts, or one of eight).
+template <int W, int STEP, bool DIRECT>
+constexpr int kAhead = !DIRECT ? 1 : STEP * 4 * (8 / W) <= 144 * 1024 ? 3 : 1;
+
+// All of this wavefront's loads but the last N have come (they come in order).
+template <int N>
+__device__ __forceinline__ void arrived() {
+    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
+}
+// ... but those of the last `more` (0 ... 3) runs of N
+template <int N>
+__device__ __forceinline__ void arrived_but(int more) {
+    if (more >= 3) arrived<3 * N>();
+    else if (more == 2) arrived<2 * N>();
+    else if (more == 1) arrived<N>();
+    else arrived<0>();
+}
+// A barrier that leaves loads on their way.
+__device__ __forceinline__ void meet() {
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+}
+
+template <class S>
+__device__ __forceinline__ bool is_odd(uint32_t word, uint32_t& cleaned) {      // holds an infinity or a NaN
+    cleaned = word;
+    if constexpr (S::DT == DETO_F32) {
+        if ((word & 0x7F800000u) == 0x7F800000u) cleaned = 0;
+    } else {
+        constexpr uint32_t kExponent = S::DT == DETO_BF16 ? 0x7F80u : 0x7C00u;
+        if ((word & kExponent) == kExponent) cleaned &= 0xFFFF0000u;
+        if ((word & kExponent << 16) == kExponent << 16) cleaned &= 0xFFFFu;
+    }
+    return cleaned != word;
+}
+
+// Takes infinities and NaNs out of rows in LDS, and says whether there were any: in a product whose other operand has
+// zeros for what is masked, they would reach what does not see them.  What they give to what does see them is added in
+// the end, by scalar products (see `add_odd`): it is rare, and the kernels' loops stay small.
+template <class S, int ROWS, int W>
+__device__ __forceinline__ void take_out_odd(char* lds, uint32_t* found) {
+    constexpr int kThreads = W * kLanes;
+#pragma unroll
+    for (int i = 0; i < ROWS * S::kPieces / kThreads; ++i) {
+        u32x4* const at = reinterpret_cast<u32x4*>(lds + (threadIdx.x + i * kThreads) * 16);
+        u32x4 r = *at;
+        bool any = false;
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+            uint32_t cleaned;
+            const uint32_t word = r[w];
+            any |= is_odd<S>(word, cleaned);
+            r[w] = cleaned;
+        }
+        if (any) {
+            *at = r;
+            *found = 1;
+        }
+    }
+}
+
+// whether a row in memory holds any (a wavefront's lanes look at its features together)
+template <class S>
+__device__ __forceinline__ bool row_is_odd(const char* row, int D) {
+    bool any = false;
+    for (int d = threadIdx.x % kLanes; d < D; d += kLanes) any |= !(fabsf(load1<S::DT>(row, d)) < __builtin_inff());
+    return __any(any);
+}
+
+// the scalar product of two rows in memory
+template <class S>
+__device__ __forceinline__ float slow_dot(const char* x, const char* y, int D) {
+    float sum = 0.f;
+#pragma unroll 1
+    for (int d = 0; d < D; ++d) sum = fmaf(load1<S::DT>(x, d), load1<S::DT>(y, d), sum);
+    return sum;
+}
+
+// adds to a lane's column what a row's infinities and NaNs give under a weight
+template <class S>
+__device__ __forceinline__ void add_odd(const char* row, int D, float weight, f32x16 (&c)[S::kBlocks]) {
+    const int half = threadIdx.x / kSide % 2;
+#pragma unroll
+    for (int b = 0; b < S::kBlocks; ++b) {
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+            const int d = b * kSide + (r / 4) * 8 + half * 4 + r % 4;
+            const float v = d < D ? load1<S::DT>(row, d) : 0.f;
+            if (!(fabsf(v) < __builtin_inff())) c[b][r] += weight * v;
+        }
+    }
+}
 
 // ---- the rows form
 template <int DT>
@@ -224,13 +332,13 @@ __device__ __forceinline__ f32x16 multiply(const u32x4& a, const u32x4& b, f32x1
     }
 }
 
-// a lane's row of B: rows of which the lane's one may be missing (zeros)
-template <class S, bool WHOLE>
+// a lane's row of B; one that is missing is zeros
+template <class S>
 __device__ __forceinline__ void load_row(const char* row, bool there, int D, u32x4 (&f)[S::kFrags]) {
     const int half = (threadIdx.x / kSide) % 2;
 #pragma unroll
     for (int m = 0; m < S::kFrags; ++m) {
-        f[m] = load_piece<S, WHOLE>(row, 2 * m + half, D);
+        f[m] = load_piece<S>(row, 2 * m + half, D);
         if (!there) f[m] = {0, 0, 0, 0};
     }
 }
@@ -243,6 +351,18 @@ __device__ __forceinline__ f32x16 rows_product(const char* lds, int block, const
 #pragma unroll
     for (int m = 0; m < S::kFrags; ++m)
         c = multiply<S::DT>(*reinterpret_cast<const u32x4*>(lds + place<S>(row, 2 * m + half)), b[m], c);
+    return c;
+}
+
+// the same with B in LDS too, the lane's row being `own` there
+template <class S>
+__device__ __forceinline__ f32x16 rows_product(const char* lds, int block, const char* b, int own) {
+    const int lane = threadIdx.x % kLanes, row = block * kSide + lane % kSide, half = lane / kSide;
+    f32x16 c = {};
+#pragma unroll
+    for (int m = 0; m < S::kFrags; ++m)
+        c = multiply<S::DT>(*reinterpret_cast<const u32x4*>(lds + place<S>(row, 2 * m + half)),
+                            *reinterpret_cast<const u32x4*>(b + place<S>(own, 2 * m + half)), c);
     return c;
 }
 
@@ -261,6 +381,7 @@ __device__ __forceinline__ u32x4 operand(const f32x16& w, int run) {
     return r;
 }
 
+// C += (rows 32 block ... of a matrix in LDS)^T W
 template <class S>
 __device__ __forceinline__ void columns_product(const char* lds, int block, const f32x16& w, f32x16 (&c)[S::kBlocks]) {
     const int lane = threadIdx.x % kLanes, half = lane / kSide;
@@ -294,35 +415,6 @@ __device__ __forceinline__ void columns_product(const char* lds, int block, cons
                     a[2 * s + 1] = words[1];
                 }
                 c[b] = multiply<S::DT>(a, own, c[b]);
-            }
-        }
-    }
-}
-
-// The terms of the columns form that infinities and NaNs take part in, for lanes that see their row: `bits` says which
-// rows of the block have any, `rows` is the block's first row in memory.
-template <class S, class Sees>
-__device__ __forceinline__ void add_infinities(uint32_t bits, const char* rows, int64_t ld, int D, const f32x16& w, Sees sees,
-                                               f32x16 (&c)[S::kBlocks]) {
-    const int half = threadIdx.x / kSide % 2;
-    while (bits) {
-        const int n = __builtin_ctz(bits);
-        bits &= bits - 1;
-        float own = 0.f;
-#pragma unroll
-        for (int r = 0; r < 16; ++r)
-            if ((r / 4) * 8 + r % 4 == (n & ~4)) own = w[r];
-        const auto both = __builtin_amdgcn_permlane32_swap(f32_bits(own), f32_bits(own), false, false);
-        const float weight = bits_f32(n & 4 ? both[1] : both[0]);
-        if (!sees(n)) continue;
-#pragma unroll
-        for (int b = 0; b < S::kBlocks; ++b) {
-#pragma unroll
-            for (int r = 0; r < 16; ++r) {
-                const int d = b * kSide + (r / 4) * 8 + half * 4 + r % 4;
-                if (d >= D) continue;
-                const float v = load1<S::DT>(rows + n * ld, d);
-                if (!(fabsf(v) < __builtin_inff())) c[b][r] += weight * v;
             }
         }
     }
@@ -407,18 +499,21 @@ inline bool plan(Args& a, const int32_t* starts, int64_t T, int size, int heads)
         tiles = each * a.sequences;
         a.per_sequence = static_cast<uint32_t>(each ? each : 1);
     }
-    a.tiles = static_cast<uint32_t>(tiles);
-    return tiles * heads < (int64_t{1} << 31) / kThreads * 2;
+    const bool fits = tiles * heads < (int64_t{1} << 22);          // (2^32 threads are the most of a launch)
+    a.tiles = fits ? static_cast<uint32_t>(tiles) : 0;
+    return fits;
 }
 
-// f(Shape, whole) for a head's features
+// f(Shape, direct) for a head's features; `direct`: every head of the matrices that are walked over starts at a multiple
+// of 16 bytes
 template <int DT, class F>
-inline int by_shape(int head_dim, F f) {
-    if (head_dim == 64) return f(Shape<DT, 64>{}, Type<1>{});
-    if (head_dim == 128) return f(Shape<DT, 128>{}, Type<1>{});
+inline int by_shape(int head_dim, bool direct, F f) {
+    if (head_dim == 64 && direct) return f(Shape<DT, 64>{}, Type<1>{});
+    if (head_dim == 128 && direct) return f(Shape<DT, 128>{}, Type<1>{});
     if (head_dim <= 64) return f(Shape<DT, 64>{}, Type<0>{});
     return f(Shape<DT, 128>{}, Type<0>{});
 }
+inline bool in_pieces(const Matrix& m) { return is_aligned(m.data, 16) && m.ld % 16 == 0 && m.ld < (int64_t{1} << 24); }
 
 }  // namespace attention
 }  // namespace model

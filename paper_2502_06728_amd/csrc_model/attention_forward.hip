@@ -1,8 +1,8 @@
 // softmax(scale q k^T) v and log sum exp, one pass over the keys.
 //
-// A workgroup takes 128 queries of a head, 32 a wavefront, and walks over the keys they see, 64 (fp32: 32) at a time in
-// LDS.  A lane has one query: its running maximum and sum are two registers, and its scores, as they come out of the
-// first product, are the second product's operand.
+// A workgroup takes 128 or 256 queries of a head, 32 a wavefront, and walks over the keys they see, 64 (fp32: 32) at a
+// time in LDS.  A lane has one query: its running maximum and sum are two registers, and its scores, as they come out
+// of the first product, are the second product's operand.
 #include "attention_device.hip.h"
 
 namespace deto {
@@ -10,71 +10,68 @@ namespace model {
 namespace attention {
 namespace {
 
-constexpr int kQueries = kWaves * kSide;    // of a workgroup
 template <int DT> constexpr int kKeys = DT == DETO_F32 ? 32 : 64;      // of a step
 
 // A query's maximum may lag behind by this much (in powers of two): its weights stay below 2^8, and the sums so far need
 // not be scaled down for every new maximum.
 constexpr float kLag = 8.f;
 
-template <class S, bool WHOLE>
-__global__ __launch_bounds__(kThreads, 2) void forward_kernel(Args a) {
-    constexpr int DT = S::DT, BN = kKeys<DT>, kMatrix = BN * S::kRow;
-    extern __shared__ __align__(16) char lds[];          // two buffers of keys and values
-    __shared__ uint32_t bits[3][2];                      // rows of values that hold infinities
-    const uint32_t id = number_in_part();
-    const int h = id / a.tiles;
-    int64_t s;
-    int32_t tile, tiles;
-    if (!find_tile(a, a.q_starts, a.Tq, kQueries, id % a.tiles, s, tile, tiles)) return;
-    if (a.causal) tile = tiles - 1 - tile;               // long ones first
-    const Sequence seq = sequence_of(a, s);
-    const int D = a.head_dim, lane = threadIdx.x % kLanes, half = lane / kSide;
-    const int i0 = tile * kQueries, w0 = i0 + threadIdx.x / kLanes * kSide, i = w0 + lane % kSide;
-    const bool there = i < seq.Lq;
+template <class S, int W, bool DIRECT>
+__global__ __launch_bounds__(W * kLanes, 2) void forward_kernel(Args a) {
+    constexpr int DT = S::DT, BM = W * kSide, BN = kKeys<DT>, kMatrix = BN * S::kRow, kStep = 2 * kMatrix;
+    constexpr int AHEAD = kAhead<W, kStep, DIRECT>;
+    extern __shared__ __align__(16) char lds[];          // AHEAD + 1 steps of keys and values
+    __shared__ uint32_t odd;                             // infinities or NaNs among values that not all queries see
+    Place at;
+    if (!place_of(a, a.q_starts, a.Tq, BM, a.heads, a.causal, at)) return;
+    const Sequence seq = sequence_of(a, at.s);
+    const int D = DIRECT ? S::DP : a.head_dim, lane = threadIdx.x % kLanes, half = lane / kSide;
+    const int i0 = at.tile * BM, w0 = i0 + threadIdx.x / kLanes * kSide, i = w0 + lane % kSide, last = seq.Lq - 1;
+    const bool there = i <= last;
 
     // keys that query n sees
     const auto seen = [&](int n) {
         if (!a.causal) return seq.Lk;
-        const int64_t upto = int64_t{n} + seq.Lk - seq.Lq + 1;
-        return static_cast<int>(upto < 0 ? 0 : upto < seq.Lk ? upto : seq.Lk);
+        const int64_t upto = int64_t{n < last ? n : last} + seq.Lk - last;
+        return static_cast<int>(upto < 0 ? 0 : upto);
     };
-    const int last = seq.Lq - 1;
-    const int upto = seen(i0 + kQueries - 1 < last ? i0 + kQueries - 1 : last);       // by any of the workgroup's
-    const int wave_upto = seen(w0 + kSide - 1 < last ? w0 + kSide - 1 : last);
-    const int own = seen(i);
-    const int steps = (upto + BN - 1) / BN, whole_steps = seen(i0) / BN;
+    const int upto = seen(i0 + BM - 1), wave_upto = seen(w0 + kSide - 1);        // by any of the workgroup's, the wavefront's
+    const int own = seen(i), steps = (upto + BN - 1) / BN, whole_steps = seen(i0) / BN;
 
-    const int64_t kv = int64_t{h / a.group} * D * S::kElem;
+    const int64_t col = int64_t{at.head} * D * S::kElem, kv = int64_t{at.head / a.group} * D * S::kElem;
     const char* const keys = a.k.data + seq.k0 * a.k.ld + kv;
     const char* const values = a.v.data + seq.k0 * a.v.ld + kv;
-    u32x4 q[S::kFrags];
-    load_row<S, WHOLE>(a.q.data + (seq.q0 + (there ? i : last)) * a.q.ld + int64_t{h} * D * S::kElem, there, D, q);
+    const char* const query = a.q.data + (seq.q0 + (there ? i : last)) * a.q.ld + col;
 
+    Rows<S, BN, W, DIRECT> rk, rv;
+    const auto buffer = [&](int step) { return lds + step % (AHEAD + 1) * kStep; };
+    const auto begin = [&](int step) {
+        const int have = seq.Lk - step * BN < BN ? seq.Lk - step * BN : BN;
+        rk.begin(buffer(step), keys + int64_t{step} * BN * a.k.ld, a.k.ld, have, D);
+        rv.begin(buffer(step) + kMatrix, values + int64_t{step} * BN * a.v.ld, a.v.ld, have, D);
+    };
+    const auto end = [&](int step) {
+        rk.end(buffer(step));
+        rv.end(buffer(step) + kMatrix);
+    };
+    if (threadIdx.x == 0) odd = 0;
+#pragma unroll
+    for (int n = 0; n < AHEAD; ++n)
+        if (n < steps) begin(n);
+    if (steps > 0) end(0);
+
+    u32x4 q[S::kFrags];
+    load_row<S>(query, there, D, q);
     const float factor = a.scale * kLog2E;       // of scores, to powers of two
     float m = -__builtin_inff(), base = 0.f, l = 0.f;
     f32x16 o[S::kBlocks] = {};
 
-    if (threadIdx.x < 6) bits[threadIdx.x / 2][threadIdx.x % 2] = 0;
-    __syncthreads();
-    Stage<S, BN, WHOLE> sk, sv;
-    const auto have = [&](int step) { return seq.Lk - step * BN < BN ? seq.Lk - step * BN : BN; };
-    const auto load = [&](int step) {
-        sk.load(keys + int64_t{step} * BN * a.k.ld, a.k.ld, have(step), D);
-        sv.load(values + int64_t{step} * BN * a.v.ld, a.v.ld, have(step), D);
-    };
-    const auto store = [&](int step) {
-        char* const at = lds + step % 2 * 2 * kMatrix;
-        sk.template store<false>(at, have(step), nullptr);
-        if (step >= whole_steps) sv.template store<true>(at + kMatrix, have(step), bits[step % 3]);
-        else sv.template store<false>(at + kMatrix, have(step), nullptr);
-    };
     const auto compute = [&](int step, auto masked) {
         constexpr bool MASKED = masked.value != 0;
-        const char* const at = lds + step % 2 * 2 * kMatrix;
+        const char* const from = buffer(step);
         f32x16 x[BN / kSide];
 #pragma unroll
-        for (int b = 0; b < BN / kSide; ++b) x[b] = rows_product<S>(at, b, q);
+        for (int b = 0; b < BN / kSide; ++b) x[b] = rows_product<S>(from, b, q);
         const int left = own - step * BN - half * 4;         // of the keys that the query sees
         float top = -__builtin_inff();
 #pragma unroll
@@ -106,36 +103,36 @@ __global__ __launch_bounds__(kThreads, 2) void forward_kernel(Args a) {
             }
         l += sum;
 #pragma unroll
-        for (int b = 0; b < BN / kSide; ++b) {
-            columns_product<S>(at + kMatrix, b, x[b], o);
-            if (MASKED) {
-                const uint32_t odd = bits[step % 3][b];
-                if (odd)
-                    add_infinities<S>(odd, values + (int64_t{step} * BN + b * kSide) * a.v.ld, a.v.ld, D, x[b],
-                                      [&](int n) { return step * BN + b * kSide + n < own; }, o);
-            }
-        }
+        for (int b = 0; b < BN / kSide; ++b) columns_product<S>(from + kMatrix, b, x[b], o);
     };
 
-    if (steps > 0) {
-        load(0);
-        store(0);
-    }
-    __syncthreads();
     for (int step = 0; step < steps; ++step) {
-        if (threadIdx.x < 2) bits[(step + 2) % 3][threadIdx.x] = 0;
-        if (step + 1 < steps) load(step + 1);
-        if (step < whole_steps) compute(step, Type<0>{});
-        else if (step * BN < wave_upto) compute(step, Type<1>{});
-        if (step + 1 < steps) store(step + 1);
-        __syncthreads();
+        if constexpr (DIRECT) arrived_but<2 * Rows<S, BN, W, DIRECT>::kCalls>(min(AHEAD - 1, steps - 1 - step));
+        meet();
+        if (step + AHEAD < steps) begin(step + AHEAD);
+        if (step < whole_steps) {
+            compute(step, Type<0>{});
+        } else {
+            take_out_odd<S, BN, W>(buffer(step) + kMatrix, &odd);
+            meet();
+            if (step * BN < wave_upto) compute(step, Type<1>{});
+        }
+        if (step + AHEAD < steps) end(step + AHEAD);
     }
 
+    if (steps > whole_steps && odd) {
+        for (int j = whole_steps * BN; j < wave_upto; ++j) {
+            const char* const value = values + j * a.v.ld;
+            if (!row_is_odd<S>(value, D)) continue;
+            const float weight = power2(fmaf(slow_dot<S>(query, keys + j * a.k.ld, D), factor, -base));
+            if (j < own) add_odd<S>(value, D, weight, o);
+        }
+    }
     l = halves_sum(l);
     const int64_t row = seq.q0 + i;
-    store_columns<S>(o, l == 0.f ? 0.f : 1.f / l, a.out.data + row * a.out.ld + int64_t{h} * D * S::kElem, there, D);
+    store_columns<S>(o, l == 0.f ? 0.f : 1.f / l, a.out.data + row * a.out.ld + col, there, D);
     if (a.lse && there && half == 0)
-        a.lse[h * a.Tq + row] = l == 0.f ? -__builtin_inff() : (base + __builtin_amdgcn_logf(l)) * kLn2;
+        a.lse[at.head * a.Tq + row] = l == 0.f ? -__builtin_inff() : (base + __builtin_amdgcn_logf(l)) * kLn2;
 }
 
 }  // namespace
@@ -193,7 +190,7 @@ extern "C" {
 
 int64_t detonation_attention_workspace(const deto_attention* cfg, int64_t Tq, int64_t Tk) {
     if (check(cfg, Tq, Tk) != DETO_OK) return -1;
-    return cfg->heads * Tq * static_cast<int64_t>(sizeof(float));
+    return 2 * cfg->heads * Tq * static_cast<int64_t>(sizeof(float));
 }
 
 int detonation_attention_forward(const deto_attention* cfg, int64_t Tq, int64_t Tk, const deto_rows* q,
@@ -211,16 +208,25 @@ int detonation_attention_forward(const deto_attention* cfg, int64_t Tq, int64_t 
     Args a = args_of(cfg, Tq, Tk, q, k, v);
     a.out = matrix_of(out);
     a.lse = lse;
-    if (!plan(a, cfg->q_starts, Tq, kQueries, cfg->heads)) return DETO_ERR_UNSUPPORTED;
+    int planned = DETO_OK;
+    const bool wide = Tq * cfg->heads >= int64_t{256} * kCUs;
     fresh();
     by_type(q->dtype, [&](auto dt) {
-        return by_shape<dt.value>(cfg->head_dim, [&](auto shape, auto whole) {
+        return by_shape<dt.value>(cfg->head_dim, in_pieces(a.k) && in_pieces(a.v), [&](auto shape, auto direct) {
             using S = decltype(shape);
-            forward_kernel<S, whole.value != 0><<<a.tiles * cfg->heads, kThreads, 4 * kKeys<S::DT> * S::kRow,
-                                                  static_cast<hipStream_t>(stream)>>>(a);
-            return 0;
+            const auto run = [&](auto waves) {
+                constexpr int W = waves.value;
+                constexpr bool DIRECT = direct.value != 0;
+                if (!plan(a, cfg->q_starts, Tq, W * kSide, cfg->heads)) return planned = DETO_ERR_UNSUPPORTED;
+                constexpr int kStep = 2 * kKeys<S::DT> * S::kRow;
+                forward_kernel<S, W, DIRECT><<<a.tiles * cfg->heads, W * kLanes, (kAhead<W, kStep, DIRECT> + 1) * kStep,
+                                               static_cast<hipStream_t>(stream)>>>(a);
+                return 0;
+            };
+            return wide ? run(Type<8>{}) : run(Type<4>{});
         });
     });
+    if (planned) return planned;
     return enqueued();
 }
 
