@@ -41,6 +41,11 @@ __device__ __forceinline__ float rows_dot(const u32x4 (&x)[S::kFrags], const u32
     return halves_sum(sum);
 }
 
+// Steps that are on their way while one is computed: three, where the workgroups that share a CU then have room in its
+// LDS (two of four wavefronts, or one of eight).
+template <int W, int STEP, bool DIRECT>
+constexpr int kAhead = !DIRECT ? 1 : STEP * 4 * (8 / W) <= 144 * 1024 ? 3 : 1;
+
 template <class S, int W, bool DIRECT>
 __global__ __launch_bounds__(W * kLanes, 2) void queries_kernel(Args a) {
     constexpr int DT = S::DT, BM = W * kSide, BN = kKeys<DT>, kMatrix = BN * S::kRow, kStep = 2 * kMatrix;
@@ -51,7 +56,7 @@ __global__ __launch_bounds__(W * kLanes, 2) void queries_kernel(Args a) {
     if (!place_of(a, a.q_starts, a.Tq, BM, a.heads, a.causal, at)) return;
     const Sequence seq = sequence_of(a, at.s);
     const int D = DIRECT ? S::DP : a.head_dim, lane = threadIdx.x % kLanes, half = lane / kSide;
-    const int i0 = at.tile * BM, w0 = i0 + threadIdx.x / kLanes * kSide, i = w0 + lane % kSide, last = seq.Lq - 1;
+    const int i0 = at.tile * BM, w0 = i0 + uniform(static_cast<int32_t>(threadIdx.x / kLanes)) * kSide, i = w0 + lane % kSide, last = seq.Lq - 1;
     const bool there = i <= last;
 
     const auto seen = [&](int n) {
@@ -69,14 +74,14 @@ __global__ __launch_bounds__(W * kLanes, 2) void queries_kernel(Args a) {
     const char* const query = a.q.data + row * a.q.ld + col;
     const char* const grad = a.dout.data + row * a.dout.ld + col;
 
-    Rows<S, BN, W, DIRECT> rk, rv;
+    Rows<S, BN, W, DIRECT> rk(a.k.ld), rv(a.v.ld);
     const auto buffer = [&](int step) { return lds + step % (AHEAD + 1) * kStep; };
-    const auto begin = [&](int step) {
+    const auto begin = [&](int step) __attribute__((always_inline)) {
         const int have = seq.Lk - step * BN < BN ? seq.Lk - step * BN : BN;
         rk.begin(buffer(step), keys + int64_t{step} * BN * a.k.ld, a.k.ld, have, D);
         rv.begin(buffer(step) + kMatrix, values + int64_t{step} * BN * a.v.ld, a.v.ld, have, D);
     };
-    const auto end = [&](int step) {
+    const auto end = [&](int step) __attribute__((always_inline)) {
         rk.end(buffer(step));
         rv.end(buffer(step) + kMatrix);
     };
@@ -87,59 +92,68 @@ __global__ __launch_bounds__(W * kLanes, 2) void queries_kernel(Args a) {
     if (steps > 0) end(0);
 
     const float factor = a.scale * kLog2E;
-    u32x4 q[S::kFrags], g[S::kFrags];
-    load_row<S>(grad, there, D, g);
-    load_row<S>(a.out.data + row * a.out.ld + col, there, D, q);
+    u32x4 q[1][S::kFrags], g[1][S::kFrags];
+    load_row<S>(grad, there, D, g[0]);
+    load_row<S>(a.out.data + row * a.out.ld + col, there, D, q[0]);
     const float lse = there ? stored_lse(a.lse[at.head * a.Tq + row]) : __builtin_inff();
-    const float delta = rows_dot<S>(g, q);
+    const float delta = rows_dot<S>(g[0], q[0]);
     if (there && half == 0) {
         a.stats[at.head * a.Tq + row] = lse;
         a.stats[(a.heads + at.head) * a.Tq + row] = delta;
     }
-    load_row<S>(query, there, D, q);
-    f32x16 dq[S::kBlocks] = {};
+    load_row<S>(query, there, D, q[0]);
+    f32x16 dq[1][S::kBlocks] = {};
 
-    const auto compute = [&](int step, auto masked) {
+    const Places places = places_of<S>();
+    const auto compute = [&](int step, auto masked) __attribute__((always_inline)) {
         constexpr bool MASKED = masked.value != 0;
         const char* const from = buffer(step);
         const int left = own - step * BN - half * 4;
 #pragma unroll
         for (int b = 0; b < BN / kSide; ++b) {
-            f32x16 x = rows_product<S>(from, b, q);
-            const f32x16 y = rows_product<S>(from + kMatrix, b, g);
+            f32x16 x[1][1], y[1][1];
+            rows_product<S, 1, 1>(from + b * kSide * S::kRow, places, q, x);
+            rows_product<S, 1, 1>(from + kMatrix + b * kSide * S::kRow, places, g, y);
 #pragma unroll
             for (int r = 0; r < 16; ++r) {
-                x[r] = power2(fmaf(x[r], factor, -lse)) * (y[r] - delta);
-                if (MASKED) x[r] = b * kSide + (r / 4) * 8 + r % 4 < left ? x[r] : 0.f;
+                x[0][0][r] = power2(fmaf(x[0][0][r], factor, -lse)) * (y[0][0][r] - delta);
+                if (MASKED) x[0][0][r] = b * kSide + (r / 4) * 8 + r % 4 < left ? x[0][0][r] : 0.f;
             }
-            columns_product<S>(from, b, x, dq);
+            columns_product<S, 1>(from + b * kSide * S::kRow, places, x[0], dq);
         }
     };
 
-    for (int step = 0; step < steps; ++step) {
-        if constexpr (DIRECT) arrived_but<2 * Rows<S, BN, W, DIRECT>::kCalls>(min(AHEAD - 1, steps - 1 - step));
-        meet();
-        if (step + AHEAD < steps) begin(step + AHEAD);
-        if (step < whole_steps) {
-            compute(step, Type<0>{});
-        } else {
-            take_out_odd<S, BN, W>(buffer(step), &odd);
+    // (two loops: a branch between the two forms in one would keep a second set of sums)
+    const auto walk = [&](int& step, int to, auto masked) __attribute__((always_inline)) {
+        for (; step < to; ++step) {
+            if constexpr (DIRECT) arrived_but<2 * Rows<S, BN, W, DIRECT>::kCalls>(min(AHEAD - 1, steps - 1 - step));
             meet();
-            if (step * BN < wave_upto) compute(step, Type<1>{});
+            if (step + AHEAD < steps) begin(step + AHEAD);
+            if constexpr (masked.value != 0) {
+                take_out_odd<S, BN, W>(buffer(step), &odd);
+                meet();
+                if (step * BN < wave_upto) compute(step, masked);
+            } else {
+                compute(step, masked);
+            }
+            if (step + AHEAD < steps) end(step + AHEAD);
         }
-        if (step + AHEAD < steps) end(step + AHEAD);
-    }
+    };
+    int step = 0;
+    walk(step, whole_steps, Type<0>{});
+    walk(step, steps, Type<1>{});
 
+    store_columns<S>(dq[0], a.scale, a.dq.data + row * a.dq.ld + col, there, D);
     if (steps > whole_steps && odd) {
+        stored();
         for (int j = whole_steps * BN; j < wave_upto; ++j) {
             const char* const key = keys + j * a.k.ld;
             if (!row_is_odd<S>(key, D)) continue;
             const float p = power2(fmaf(slow_dot<S>(query, key, D), factor, -lse));
             const float ds = p * (slow_dot<S>(grad, values + j * a.v.ld, D) - delta);
-            if (j < own) add_odd<S>(key, D, ds, dq);
+            if (there && j < own) add_odd<S>(a.dq.data + row * a.dq.ld + col, key, D, ds * a.scale);
         }
     }
-    store_columns<S>(dq, a.scale, a.dq.data + row * a.dq.ld + col, there, D);
 }
 
 // ---- dk, dv
@@ -175,20 +189,20 @@ __global__ __launch_bounds__(W * kLanes, kResident<S>) void keys_kernel(Args a) 
     };
     const int first_step = seen_from(j0) / BQ, steps = (seq.Lq + BQ - 1) / BQ - first_step;    // of a head
     const int all_from = seen_from(j0 + BN - 1);                 // from here on queries see all of these keys
-    const int wave_from = seen_from(j0 + threadIdx.x / kLanes * kSide), own = seen_from(j);
+    const int wave_from = seen_from(j0 + uniform(static_cast<int32_t>(threadIdx.x / kLanes)) * kSide), own = seen_from(j);
     const int total = steps * a.group;                           // a head's steps, then the next one's
 
     const int64_t kv = int64_t{at.head} * D * S::kElem, row = seq.k0 + (there ? j : last);
     const char* const key = a.k.data + row * a.k.ld + kv;
     const char* const value = a.v.data + row * a.v.ld + kv;
 
-    Rows<S, BQ, W, DIRECT> rq, rg;
+    Rows<S, BQ, W, DIRECT> rq(a.q.ld), rg(a.dout.ld);
     float stat[2 * BQ / kLanes];
     // a step: of which head, from which query on, and its buffer
     struct Step {
         int head, query, buffer;
     };
-    const auto next = [&](Step s) {
+    const auto next = [&](Step s) __attribute__((always_inline)) {
         s.query += BQ;
         if (s.query >= seq.Lq) {
             s.query = first_step * BQ;
@@ -197,7 +211,7 @@ __global__ __launch_bounds__(W * kLanes, kResident<S>) void keys_kernel(Args a) 
         s.buffer = s.buffer == AHEAD ? 0 : s.buffer + 1;
         return s;
     };
-    const auto begin = [&](Step s) {
+    const auto begin = [&](Step s) __attribute__((always_inline)) {
         char* const to = lds + s.buffer * kStep;
         const int have = seq.Lq - s.query < BQ ? seq.Lq - s.query : BQ;
         const int64_t first = seq.q0 + s.query, col = int64_t{s.head} * D * S::kElem;
@@ -214,7 +228,7 @@ __global__ __launch_bounds__(W * kLanes, kResident<S>) void keys_kernel(Args a) 
             else stat[c] = *from;
         }
     };
-    const auto end = [&](Step s) {
+    const auto end = [&](Step s) __attribute__((always_inline)) {
         char* const to = lds + s.buffer * kStep;
         rq.end(to);
         rg.end(to + kMatrix);
@@ -225,7 +239,7 @@ __global__ __launch_bounds__(W * kLanes, kResident<S>) void keys_kernel(Args a) 
     };
     if (threadIdx.x == 0) odd = 0;
     if constexpr (STAY) {
-        Rows<S, BN, W, DIRECT> rv;
+        Rows<S, BN, W, DIRECT> rv(a.v.ld);
         rv.begin(lds + (AHEAD + 1) * kStep, a.v.data + (seq.k0 + j0) * a.v.ld + kv, a.v.ld, last - j0 < BN ? last - j0 + 1 : BN, D);
         rv.end(lds + (AHEAD + 1) * kStep);
     }
@@ -241,61 +255,77 @@ __global__ __launch_bounds__(W * kLanes, kResident<S>) void keys_kernel(Args a) 
         ahead = next(ahead);
     }
 
-    u32x4 k[S::kFrags], v[STAY ? 1 : S::kFrags];
-    load_row<S>(key, there, D, k);
-    if constexpr (!STAY) load_row<S>(value, there, D, v);
+    u32x4 k[1][S::kFrags], v[1][STAY ? 1 : S::kFrags];
+    load_row<S>(key, there, D, k[0]);
+    if constexpr (!STAY) load_row<S>(value, there, D, v[0]);
     const float factor = a.scale * kLog2E;
-    f32x16 dk[S::kBlocks] = {}, dv[S::kBlocks] = {};
+    f32x16 dk[1][S::kBlocks] = {}, dv[1][S::kBlocks] = {};
 
-    const auto compute = [&](Step s, auto masked) {
+    const Places places = places_of<S>();
+    const char* const own_values = lds + (AHEAD + 1) * kStep + threadIdx.x / kLanes * kSide * S::kRow;
+    const auto compute = [&](Step s, auto masked) __attribute__((always_inline)) {
         constexpr bool MASKED = masked.value != 0;
         const char* const from = lds + s.buffer * kStep;
 #pragma unroll
         for (int b = 0; b < BQ / kSide; ++b) {
             const int first = s.query + b * kSide + half * 4, upto = seq.Lq - first, own_from = own - first;
             const float* const stat = stats[s.buffer] + b * kSide + half * 4;
-            f32x16 p = rows_product<S>(from, b, k);
+            const char *const rows_q = from + b * kSide * S::kRow, *const rows_g = rows_q + kMatrix;
+            f32x16 p[1][1], ds[1][1];
+            rows_product<S, 1, 1>(rows_q, places, k, p);
 #pragma unroll
             for (int r = 0; r < 16; ++r) {
                 const int t = (r / 4) * 8 + r % 4;
-                p[r] = power2(fmaf(p[r], factor, -stat[t]));
-                if (MASKED) p[r] = t >= own_from && t < upto ? p[r] : 0.f;
+                p[0][0][r] = power2(fmaf(p[0][0][r], factor, -stat[t]));
+                if (MASKED) p[0][0][r] = t >= own_from && t < upto ? p[0][0][r] : 0.f;
             }
-            f32x16 ds;
-            if constexpr (STAY) ds = rows_product<S>(from + kMatrix, b, lds + (AHEAD + 1) * kStep, in_tile);
-            else ds = rows_product<S>(from + kMatrix, b, v);
+            if constexpr (STAY) rows_product<S, 1, 1>(rows_g, places, own_values, ds);
+            else rows_product<S, 1, 1>(rows_g, places, v, ds);
 #pragma unroll
             for (int r = 0; r < 16; ++r) {
                 const int t = (r / 4) * 8 + r % 4;
-                ds[r] = p[r] * (ds[r] - stat[BQ + t]);
-                if (MASKED) ds[r] = t >= own_from && t < upto ? ds[r] : 0.f;
+                ds[0][0][r] = p[0][0][r] * (ds[0][0][r] - stat[BQ + t]);
+                if (MASKED) ds[0][0][r] = t >= own_from && t < upto ? ds[0][0][r] : 0.f;
             }
-            columns_product<S>(from + kMatrix, b, p, dv);
-            columns_product<S>(from, b, ds, dk);
+            columns_product<S, 1>(rows_g, places, p[0], dv);
+            columns_product<S, 1>(rows_q, places, ds[0], dk);
         }
     };
 
-    for (int n = 0; n < total; ++n) {
-        if constexpr (DIRECT) arrived_but<2 * Rows<S, BQ, W, DIRECT>::kCalls + 2 * BQ / kLanes>(min(AHEAD - 1, total - 1 - n));
-        meet();
-        const bool more = n + AHEAD < total;
-        if (more) begin(ahead);
-        if (now.query >= all_from && now.query + BQ <= seq.Lq) {
-            compute(now, Type<0>{});
-        } else {
-            take_out_odd<S, BQ, W>(lds + now.buffer * kStep, &odd);
-            take_out_odd<S, BQ, W>(lds + now.buffer * kStep + kMatrix, &odd);
+    // steps of one form, as long as they are (loops of their own: a branch between the two in one would keep a second set
+    // of sums)
+    const auto walk = [&](int& n, auto masked) __attribute__((always_inline)) {
+        constexpr bool MASKED = masked.value != 0;
+        while (n < total && (now.query >= all_from && now.query + BQ <= seq.Lq) != MASKED) {
+            if constexpr (DIRECT) arrived_but<2 * Rows<S, BQ, W, DIRECT>::kCalls + 2 * BQ / kLanes>(min(AHEAD - 1, total - 1 - n));
             meet();
-            if (now.query + BQ > wave_from) compute(now, Type<1>{});
+            const bool more = n + AHEAD < total;
+            if (more) begin(ahead);
+            if constexpr (MASKED) {
+                take_out_odd<S, BQ, W>(lds + now.buffer * kStep, &odd);
+                take_out_odd<S, BQ, W>(lds + now.buffer * kStep + kMatrix, &odd);
+                meet();
+                if (now.query + BQ > wave_from) compute(now, masked);
+            } else {
+                compute(now, masked);
+            }
+            if (more) {
+                end(ahead);
+                ahead = next(ahead);
+            }
+            now = next(now);
+            ++n;
         }
-        if (more) {
-            end(ahead);
-            ahead = next(ahead);
-        }
-        now = next(now);
+    };
+    for (int n = 0; n < total;) {
+        walk(n, Type<0>{});
+        walk(n, Type<1>{});
     }
 
+    store_columns<S>(dk[0], a.scale, a.dk.data + row * a.dk.ld + kv, there, D);
+    store_columns<S>(dv[0], 1.f, a.dv.data + row * a.dv.ld + kv, there, D);
     if (total > 0 && odd) {
+        stored();
         const int tail = seq.Lq / BQ * BQ;                  // steps that were masked: up to all_from, and a short last one
         for (int h = at.head * a.group; h < (at.head + 1) * a.group; ++h)
             for (int t = first_step * BQ; t < seq.Lq; ++t) {
@@ -307,13 +337,11 @@ __global__ __launch_bounds__(W * kLanes, kResident<S>) void keys_kernel(Args a) 
                 if (!odd_q && !odd_g) continue;
                 const float p = power2(fmaf(slow_dot<S>(query, key, D), factor, -a.stats[h * a.Tq + at_t]));
                 const float ds = p * (slow_dot<S>(grad, value, D) - a.stats[(a.heads + h) * a.Tq + at_t]);
-                if (t < own) continue;
-                add_odd<S>(grad, D, p, dv);
-                add_odd<S>(query, D, ds, dk);
+                if (t < own || !there) continue;
+                add_odd<S>(a.dv.data + row * a.dv.ld + kv, grad, D, p);
+                add_odd<S>(a.dk.data + row * a.dk.ld + kv, query, D, ds * a.scale);
             }
     }
-    store_columns<S>(dk, a.scale, a.dk.data + row * a.dk.ld + kv, there, D);
-    store_columns<S>(dv, 1.f, a.dv.data + row * a.dv.ld + kv, there, D);
 }
 
 }  // namespace

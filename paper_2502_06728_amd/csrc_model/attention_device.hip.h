@@ -75,11 +75,18 @@ __device__ __forceinline__ void span_of(const int32_t* starts, int64_t s, int64_
     }
 }
 
+// what is the same in all lanes, in a scalar register
+__device__ __forceinline__ int32_t uniform(int32_t v) { return __builtin_amdgcn_readfirstlane(v); }
+__device__ __forceinline__ int64_t uniform(int64_t v) {
+    const uint32_t lo = uniform(static_cast<int32_t>(v)), hi = uniform(static_cast<int32_t>(v >> 32));
+    return static_cast<int64_t>(uint64_t{hi} << 32 | lo);
+}
+
 __device__ __forceinline__ Sequence sequence_of(const Args& a, int64_t s) {
     Sequence seq;
     span_of(a.q_starts, s, a.sequences, a.Tq, seq.q0, seq.Lq);
     span_of(a.k_starts, s, a.sequences, a.Tk, seq.k0, seq.Lk);
-    return seq;
+    return {uniform(seq.q0), uniform(seq.k0), uniform(seq.Lq), uniform(seq.Lk)};
 }
 
 // Tile number `id` of all packed sequences' rows, `size` rows a tile: its sequence, and which of that one's tiles it is.
@@ -102,9 +109,9 @@ __device__ __forceinline__ bool find_tile(const Args& a, const int32_t* starts, 
         const uint64_t past = __ballot(before + upto > static_cast<int64_t>(id));
         if (past) {
             const int at = __builtin_ctzll(past);
-            s = base + at;
-            tile = static_cast<int32_t>(id - before - __shfl(upto - own, at));
-            tiles = __shfl(own, at);
+            s = uniform(base + at);
+            tile = uniform(static_cast<int32_t>(id - before - __shfl(upto - own, at)));
+            tiles = uniform(__shfl(own, at));
             return true;
         }
         before += __shfl(upto, kLanes - 1);
@@ -149,16 +156,33 @@ __device__ __forceinline__ bool place_of(const Args& a, const int32_t* starts, i
     return true;
 }
 
-// ---- matrices in LDS.  Piece p of row r lies at piece p ^ twist(r) of that row: eight lanes that read one piece of
-// rows in a row, and sixteen that read two pieces of four rows (the turned reads), each meet all banks.
+// ---- matrices in LDS.  Four rows lie together, in blocks of 256 bytes: four pieces of each row side by side, in an
+// order of their own for each of four such fours.  So the rows form (a piece of each of 16 rows) and the columns form
+// (four pieces of four rows) both read 256 bytes of different banks, and a lane's places differ by constants but for two
+// in each form.
 template <class S>
-__device__ __forceinline__ int twist(int row) {
-    if constexpr (S::kPieces >= 16) return ((row & 3) << 2) | ((row >> 2) & 3);
-    else if constexpr (S::kPieces == 8) return ((row & 2) << 1) | ((row >> 2) & 3);
-    else return (row >> 1) & (S::kPieces - 1);
+__device__ __forceinline__ uint32_t place(int row, int piece) {
+    return row / 4 * 4 * S::kRow + piece / 4 * 256 + row % 4 * 64 + ((piece ^ row / 4) & 3) * 16;
 }
+
+struct Places {
+    uint32_t rows[2];       // of a lane's piece 0 and 2 (or 1 and 3) of its row: the others are 256 bytes apart
+    uint32_t turned[2];     // of what it reads for the columns form in the first and the second eight rows
+};
 template <class S>
-__device__ __forceinline__ uint32_t place(int row, int piece) { return row * S::kRow + ((piece ^ twist<S>(row)) << 4); }
+__device__ __forceinline__ Places places_of() {
+    const int lane = threadIdx.x % kLanes, half = lane / kSide;
+    Places p;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        p.rows[i] = place<S>(lane % kSide, 2 * i + half);
+        if constexpr (S::DT == DETO_F32)
+            p.turned[i] = place<S>(8 * i + 4 * half, lane % kSide / 4) + lane % 4 * 4;
+        else        // sixteen lanes read four rows of sixteen features, four at a time, and get four rows of one feature
+            p.turned[i] = place<S>(8 * i + 4 * half + lane % 16 / 4, lane / 16 % 2 * 2 + lane % 4 / 2) + lane % 2 * 8;
+    }
+    return p;
+}
 
 // piece `piece` of a row of D features: 16 bytes, zeros behind the last feature
 template <class S>
@@ -188,21 +212,43 @@ __device__ __forceinline__ u32x4 load_piece(const char* row, int piece, int D) {
 template <class S, int ROWS, int W, bool DIRECT>
 struct Rows {
     static constexpr int kThreads = W * kLanes, kUnits = DIRECT ? 1 : ROWS * S::kPieces / kThreads;
-    static constexpr int kOfCall = kLanes / S::kPieces, kCalls = ROWS / kOfCall / W;
+    static constexpr int kCalls = ROWS * S::kPieces / kThreads;
     static_assert(ROWS * S::kPieces % kThreads == 0, "");
     u32x4 r[kUnits];
+    uint32_t off[DIRECT ? kCalls : 1];      // what a lane reads in each call, in bytes from the first row, if all rows are there
+
+    // (the inverse of place)
+    static __device__ __forceinline__ int row_of(int slot) { return slot / (4 * S::kPieces) * 4 + slot / 4 % 4; }
+    static __device__ __forceinline__ int piece_of(int slot) {
+        return slot / 16 % (S::kPieces / 4) * 4 + ((slot ^ slot / (4 * S::kPieces)) & 3);
+    }
+    __device__ __forceinline__ explicit Rows(int64_t ld) {
+        if constexpr (DIRECT) {
+#pragma unroll
+            for (int i = 0; i < kCalls; ++i) {
+                const int slot = threadIdx.x + i * kThreads;
+                off[i] = static_cast<uint32_t>(row_of(slot)) * static_cast<uint32_t>(ld) + piece_of(slot) * 16;
+            }
+        }
+    }
 
     // `have` (1 or more) rows from `at` on
     __device__ __forceinline__ void begin(char* lds, const char* at, int64_t ld, int have, int D) {
         if constexpr (DIRECT) {
-            const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kLanes), lane = threadIdx.x % kLanes;
+            const int wave = uniform(static_cast<int32_t>(threadIdx.x / kLanes));
+            const auto call = [&](int i, uint32_t from) {
+                __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(at + from),
+                                                 (__attribute__((address_space(3))) void*)(lds + (wave + i * W) * kLanes * 16), 16, 0, 0);
+            };
+            if (have == ROWS) {
 #pragma unroll
-            for (int i = 0; i < kCalls; ++i) {
-                const int first = (wave + i * W) * kOfCall, row = first + lane / S::kPieces;
-                const uint32_t off = static_cast<uint32_t>(row < have ? row : have - 1) * static_cast<uint32_t>(ld) +
-                                     ((lane % S::kPieces) ^ twist<S>(row)) * 16;
-                __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(at + off),
-                                                 (__attribute__((address_space(3))) void*)(lds + first * S::kRow), 16, 0, 0);
+                for (int i = 0; i < kCalls; ++i) call(i, off[i]);
+            } else {
+#pragma unroll
+                for (int i = 0; i < kCalls; ++i) {
+                    const int slot = threadIdx.x + i * kThreads, row = row_of(slot);
+                    call(i, static_cast<uint32_t>(row < have ? row : have - 1) * static_cast<uint32_t>(ld) + piece_of(slot) * 16);
+                }
             }
         } else {
 #pragma unroll
@@ -223,10 +269,10 @@ struct Rows {
     }
 };
 
-// Steps that are on their way while one is computed: three, where the workgroups that share a CU then have room in its
-// LDS (two of four wavefronts, or one of eight).
-template <int W, int STEP, bool DIRECT>
-constexpr int kAhead = !DIRECT ? 1 : STEP * 4 * (8 / W) <= 144 * 1024 ? 3 : 1;
+// A walk has the rows of two steps in LDS, which it computes with, and kLead - 2 steps more on their way; staged through
+// registers one in these.
+template <bool DIRECT> constexpr int kLead = DIRECT ? 3 : 2;
+template <bool DIRECT> constexpr int kBuffers = kLead<DIRECT> + 1;
 
 // All of this wavefront's loads but the last N have come (they come in order).
 template <int N>
@@ -303,20 +349,18 @@ __device__ __forceinline__ float slow_dot(const char* x, const char* y, int D) {
     return sum;
 }
 
-// adds to a lane's column what a row's infinities and NaNs give under a weight
+// Adds what a row's infinities and NaNs give under a weight to a row of results that is in memory already (the halves of
+// the lanes take turns at the features).
 template <class S>
-__device__ __forceinline__ void add_odd(const char* row, int D, float weight, f32x16 (&c)[S::kBlocks]) {
-    const int half = threadIdx.x / kSide % 2;
-#pragma unroll
-    for (int b = 0; b < S::kBlocks; ++b) {
-#pragma unroll
-        for (int r = 0; r < 16; ++r) {
-            const int d = b * kSide + (r / 4) * 8 + half * 4 + r % 4;
-            const float v = d < D ? load1<S::DT>(row, d) : 0.f;
-            if (!(fabsf(v) < __builtin_inff())) c[b][r] += weight * v;
-        }
+__device__ __forceinline__ void add_odd(char* to, const char* row, int D, float weight) {
+#pragma unroll 1
+    for (int d = threadIdx.x / kSide % 2; d < D; d += 2) {
+        const float v = load1<S::DT>(row, d);
+        if (!(fabsf(v) < __builtin_inff())) store1<S::DT>(to, d, load1<S::DT>(to, d) + weight * v);
     }
 }
+// this wavefront's stores are there for its loads
+__device__ __forceinline__ void stored() { __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "workgroup"); }
 
 // ---- the rows form
 template <int DT>
@@ -343,27 +387,43 @@ __device__ __forceinline__ void load_row(const char* row, bool there, int D, u32
     }
 }
 
-// rows 32 block ... of a matrix in LDS times the lane's row
-template <class S>
-__device__ __forceinline__ f32x16 rows_product(const char* lds, int block, const u32x4 (&b)[S::kFrags]) {
-    const int lane = threadIdx.x % kLanes, row = block * kSide + lane % kSide, half = lane / kSide;
-    f32x16 c = {};
+// BLOCKS blocks of 32 rows of a matrix in LDS times each of the lane's N rows
+template <class S, int BLOCKS, int N>
+__device__ __forceinline__ void rows_product(const char* lds, const Places& at, const u32x4 (&b)[N][S::kFrags],
+                                             f32x16 (&c)[BLOCKS][N]) {
+#pragma unroll
+    for (int k = 0; k < BLOCKS; ++k)
+#pragma unroll
+        for (int n = 0; n < N; ++n) c[k][n] = f32x16{};
 #pragma unroll
     for (int m = 0; m < S::kFrags; ++m)
-        c = multiply<S::DT>(*reinterpret_cast<const u32x4*>(lds + place<S>(row, 2 * m + half)), b[m], c);
-    return c;
+#pragma unroll
+        for (int k = 0; k < BLOCKS; ++k) {
+            const u32x4 a = *reinterpret_cast<const u32x4*>(lds + at.rows[m % 2] + m / 2 * 256 + k * kSide * S::kRow);
+#pragma unroll
+            for (int n = 0; n < N; ++n) c[k][n] = multiply<S::DT>(a, b[n][m], c[k][n]);
+        }
 }
 
-// the same with B in LDS too, the lane's row being `own` there
-template <class S>
-__device__ __forceinline__ f32x16 rows_product(const char* lds, int block, const char* b, int own) {
-    const int lane = threadIdx.x % kLanes, row = block * kSide + lane % kSide, half = lane / kSide;
-    f32x16 c = {};
+// the same with the lane's rows in LDS too, among 32 N rows at `b`
+template <class S, int BLOCKS, int N>
+__device__ __forceinline__ void rows_product(const char* lds, const Places& at, const char* b, f32x16 (&c)[BLOCKS][N]) {
 #pragma unroll
-    for (int m = 0; m < S::kFrags; ++m)
-        c = multiply<S::DT>(*reinterpret_cast<const u32x4*>(lds + place<S>(row, 2 * m + half)),
-                            *reinterpret_cast<const u32x4*>(b + place<S>(own, 2 * m + half)), c);
-    return c;
+    for (int k = 0; k < BLOCKS; ++k)
+#pragma unroll
+        for (int n = 0; n < N; ++n) c[k][n] = f32x16{};
+#pragma unroll
+    for (int m = 0; m < S::kFrags; ++m) {
+        u32x4 own[N];
+#pragma unroll
+        for (int n = 0; n < N; ++n) own[n] = *reinterpret_cast<const u32x4*>(b + at.rows[m % 2] + m / 2 * 256 + n * kSide * S::kRow);
+#pragma unroll
+        for (int k = 0; k < BLOCKS; ++k) {
+            const u32x4 a = *reinterpret_cast<const u32x4*>(lds + at.rows[m % 2] + m / 2 * 256 + k * kSide * S::kRow);
+#pragma unroll
+            for (int n = 0; n < N; ++n) c[k][n] = multiply<S::DT>(a, own[n], c[k][n]);
+        }
+    }
 }
 
 // ---- the columns form
@@ -381,40 +441,38 @@ __device__ __forceinline__ u32x4 operand(const f32x16& w, int run) {
     return r;
 }
 
-// C += (rows 32 block ... of a matrix in LDS)^T W
-template <class S>
-__device__ __forceinline__ void columns_product(const char* lds, int block, const f32x16& w, f32x16 (&c)[S::kBlocks]) {
-    const int lane = threadIdx.x % kLanes, half = lane / kSide;
+// C[n] += (32 rows of a matrix in LDS)^T W[n]
+template <class S, int N>
+__device__ __forceinline__ void columns_product(const char* lds, const Places& at, const f32x16 (&w)[N], f32x16 (&c)[N][S::kBlocks]) {
     if constexpr (S::DT == DETO_F32) {
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
-            const int row = block * kSide + (r / 4) * 8 + half * 4 + r % 4;
 #pragma unroll
             for (int b = 0; b < S::kBlocks; ++b) {
-                const int d = b * kSide + lane % kSide;
-                const float a = *reinterpret_cast<const float*>(lds + place<S>(row, d / 4) + d % 4 * 4);
-                c[b] = __builtin_amdgcn_mfma_f32_32x32x2f32(a, w[r], c[b], 0, 0, 0);
+                const float a = *reinterpret_cast<const float*>(lds + at.turned[r / 4 % 2] + r / 8 * 16 * S::kRow + r % 4 * 64 + b * 512);
+#pragma unroll
+                for (int n = 0; n < N; ++n) c[n][b] = __builtin_amdgcn_mfma_f32_32x32x2f32(a, w[n][r], c[n][b], 0, 0, 0);
             }
         }
     } else {
 #pragma unroll
         for (int run = 0; run < 2; ++run) {
-            const u32x4 own = operand<S::DT>(w, run);
+            u32x4 own[N];
+#pragma unroll
+            for (int n = 0; n < N; ++n) own[n] = operand<S::DT>(w[n], run);
 #pragma unroll
             for (int b = 0; b < S::kBlocks; ++b) {
-                // Sixteen lanes read four rows of sixteen features, four at a time, and get four rows of one feature.
-                const int row = block * kSide + run * 16 + half * 4 + lane % 16 / 4;
-                const int piece = b * 4 + lane / 16 % 2 * 2 + lane % 4 / 2, odd = lane % 2 * 8;
                 u32x4 a;
 #pragma unroll
                 for (int s = 0; s < 2; ++s) {
                     const s16x4 four = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                        (TurnedAt)(lds + place<S>(row + 8 * s, piece) + odd));
+                        (TurnedAt)(lds + at.turned[s] + run * 16 * S::kRow + b * 256));
                     const u32x2 words = __builtin_bit_cast(u32x2, four);
                     a[2 * s] = words[0];
                     a[2 * s + 1] = words[1];
                 }
-                c[b] = multiply<S::DT>(a, own, c[b]);
+#pragma unroll
+                for (int n = 0; n < N; ++n) c[n][b] = multiply<S::DT>(a, own[n], c[n][b]);
             }
         }
     }

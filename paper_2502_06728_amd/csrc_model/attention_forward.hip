@@ -12,22 +12,23 @@ namespace {
 
 template <int DT> constexpr int kKeys = DT == DETO_F32 ? 32 : 64;      // of a step
 
-// A query's maximum may lag behind by this much (in powers of two): its weights stay below 2^8, and the sums so far need
-// not be scaled down for every new maximum.
-constexpr float kLag = 8.f;
+// Weights are powers of two of a score less the query's base.  The base is the largest score of the first keys, and it
+// stays until a step's weights, which a lane adds up anyway, pass this: no step needs its scores' maximum, and the sums
+// so far are seldom scaled down.  (Weights this large are numbers in fp16, and have as many bits as others.)
+constexpr float kMost = 8192.f;
 
-template <class S, int W, bool DIRECT>
-__global__ __launch_bounds__(W * kLanes, 2) void forward_kernel(Args a) {
-    constexpr int DT = S::DT, BM = W * kSide, BN = kKeys<DT>, kMatrix = BN * S::kRow, kStep = 2 * kMatrix;
-    constexpr int AHEAD = kAhead<W, kStep, DIRECT>;
-    extern __shared__ __align__(16) char lds[];          // AHEAD + 1 steps of keys and values
+template <class S, int W, int N, bool DIRECT>
+__global__ __launch_bounds__(W * kLanes, N == 1 ? 2 : 1) __attribute__((amdgpu_waves_per_eu(N == 1 ? 2 : 1, N == 1 ? 2 : 1)))
+void forward_kernel(Args a) {
+    constexpr int DT = S::DT, BM = W * kSide * N, BN = kKeys<DT>, kMatrix = BN * S::kRow, kStep = 2 * kMatrix;
+    constexpr int LEAD = kLead<DIRECT>, NB = BN / kSide;
+    extern __shared__ __align__(16) char lds[];          // steps of keys and values
     __shared__ uint32_t odd;                             // infinities or NaNs among values that not all queries see
     Place at;
     if (!place_of(a, a.q_starts, a.Tq, BM, a.heads, a.causal, at)) return;
     const Sequence seq = sequence_of(a, at.s);
     const int D = DIRECT ? S::DP : a.head_dim, lane = threadIdx.x % kLanes, half = lane / kSide;
-    const int i0 = at.tile * BM, w0 = i0 + threadIdx.x / kLanes * kSide, i = w0 + lane % kSide, last = seq.Lq - 1;
-    const bool there = i <= last;
+    const int i0 = at.tile * BM, w0 = i0 + uniform(static_cast<int32_t>(threadIdx.x / kLanes)) * kSide * N, last = seq.Lq - 1;
 
     // keys that query n sees
     const auto seen = [&](int n) {
@@ -35,104 +36,168 @@ __global__ __launch_bounds__(W * kLanes, 2) void forward_kernel(Args a) {
         const int64_t upto = int64_t{n < last ? n : last} + seq.Lk - last;
         return static_cast<int>(upto < 0 ? 0 : upto);
     };
-    const int upto = seen(i0 + BM - 1), wave_upto = seen(w0 + kSide - 1);        // by any of the workgroup's, the wavefront's
-    const int own = seen(i), steps = (upto + BN - 1) / BN, whole_steps = seen(i0) / BN;
+    const int upto = seen(i0 + BM - 1), wave_upto = seen(w0 + kSide * N - 1);        // by any of the workgroup's, the wavefront's
+    const int steps = (upto + BN - 1) / BN, whole_steps = seen(i0) / BN;
 
     const int64_t col = int64_t{at.head} * D * S::kElem, kv = int64_t{at.head / a.group} * D * S::kElem;
     const char* const keys = a.k.data + seq.k0 * a.k.ld + kv;
     const char* const values = a.v.data + seq.k0 * a.v.ld + kv;
-    const char* const query = a.q.data + (seq.q0 + (there ? i : last)) * a.q.ld + col;
+    const char* const queries = a.q.data + seq.q0 * a.q.ld + col;
 
-    Rows<S, BN, W, DIRECT> rk, rv;
-    const auto buffer = [&](int step) { return lds + step % (AHEAD + 1) * kStep; };
-    const auto begin = [&](int step) {
+    Rows<S, BN, W, DIRECT> rk(a.k.ld), rv(a.v.ld);
+    const auto buffer = [&](int step) { return lds + step % kBuffers<DIRECT> * kStep; };
+    const auto begin = [&](int step) __attribute__((always_inline)) {
         const int have = seq.Lk - step * BN < BN ? seq.Lk - step * BN : BN;
         rk.begin(buffer(step), keys + int64_t{step} * BN * a.k.ld, a.k.ld, have, D);
         rv.begin(buffer(step) + kMatrix, values + int64_t{step} * BN * a.v.ld, a.v.ld, have, D);
     };
-    const auto end = [&](int step) {
+    const auto end = [&](int step) __attribute__((always_inline)) {
         rk.end(buffer(step));
         rv.end(buffer(step) + kMatrix);
     };
     if (threadIdx.x == 0) odd = 0;
 #pragma unroll
-    for (int n = 0; n < AHEAD; ++n)
-        if (n < steps) begin(n);
-    if (steps > 0) end(0);
-
-    u32x4 q[S::kFrags];
-    load_row<S>(query, there, D, q);
-    const float factor = a.scale * kLog2E;       // of scores, to powers of two
-    float m = -__builtin_inff(), base = 0.f, l = 0.f;
-    f32x16 o[S::kBlocks] = {};
-
-    const auto compute = [&](int step, auto masked) {
-        constexpr bool MASKED = masked.value != 0;
-        const char* const from = buffer(step);
-        f32x16 x[BN / kSide];
-#pragma unroll
-        for (int b = 0; b < BN / kSide; ++b) x[b] = rows_product<S>(from, b, q);
-        const int left = own - step * BN - half * 4;         // of the keys that the query sees
-        float top = -__builtin_inff();
-#pragma unroll
-        for (int b = 0; b < BN / kSide; ++b)
-#pragma unroll
-            for (int r = 0; r < 16; ++r) {
-                if (MASKED) x[b][r] = b * kSide + (r / 4) * 8 + r % 4 < left ? x[b][r] : -__builtin_inff();
-                top = fmaxf(top, x[b][r]);
-            }
-        top = halves_max(top);
-        if (__any((top - m) * factor > kLag)) {
-            m = fmaxf(m, top);
-            const float before = base;
-            base = m > -__builtin_inff() ? m * factor : 0.f;
-            const float less = power2(before - base);
-            l *= less;
-#pragma unroll
-            for (int b = 0; b < S::kBlocks; ++b)
-#pragma unroll
-                for (int r = 0; r < 16; ++r) o[b][r] *= less;
+    for (int n = 0; n < LEAD; ++n)
+        if (n < steps) {
+            begin(n);
+            end(n);
         }
-        float sum = 0.f;
+
+    const float factor = a.scale * kLog2E;       // of scores, to powers of two
+    u32x4 q[N][S::kFrags];
+    int own[N];
+    float base[N], l[N];
+    f32x16 o[N][S::kBlocks] = {};
 #pragma unroll
-        for (int b = 0; b < BN / kSide; ++b)
+    for (int n = 0; n < N; ++n) {
+        const int i = w0 + n * kSide + lane % kSide;
+        load_row<S>(queries + (i < last ? i : last) * a.q.ld, i <= last, D, q[n]);
+        own[n] = seen(i);
+        base[n] = own[n] > 0 ? -__builtin_inff() : 0.f;
+        l[n] = 0.f;
+    }
+    const Places places = places_of<S>();
+    f32x16 x[NB][N];                                     // scores of a step, computed in the one before
+
+    // weights of a step's scores, their products with its values, and the next step's scores (the last step's again
+    // behind it: a branch here would keep the three from sharing the time)
+    const auto compute = [&](int step) __attribute__((always_inline)) {
+        f32x16 next[NB][N], p[NB][N];
+        rows_product<S, NB, N>(buffer(step + 1 < steps ? step + 1 : step), places, q, next);
+        float sum[N];
+        bool high = false;
 #pragma unroll
-            for (int r = 0; r < 16; ++r) {
-                x[b][r] = power2(fmaf(x[b][r], factor, -base));
-                sum += x[b][r];
+        for (int n = 0; n < N; ++n) {
+            sum[n] = 0.f;
+#pragma unroll
+            for (int b = 0; b < NB; ++b)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) {
+                    p[b][n][r] = power2(fmaf(x[b][n][r], factor, -base[n]));
+                    sum[n] += p[b][n][r];
+                }
+            high |= !(sum[n] <= kMost);                  // (or none yet)
+        }
+        if (__any(high)) {
+#pragma unroll
+            for (int n = 0; n < N; ++n) {
+                const uint64_t lanes = __ballot(!(sum[n] <= kMost));
+                if (!((lanes | lanes << kSide | lanes >> kSide) >> lane & 1)) continue;       // (a query's two lanes do the same)
+                float top = -__builtin_inff();
+#pragma unroll
+                for (int b = 0; b < NB; ++b)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) top = fmaxf(top, x[b][n][r]);
+                const float to = fmaxf(base[n], halves_max(top) * factor), less = to > base[n] ? power2(base[n] - to) : 1.f;
+                base[n] = to;
+                const float from = to > -__builtin_inff() ? to : 0.f;
+                l[n] *= less;
+                sum[n] = 0.f;
+#pragma unroll
+                for (int b = 0; b < S::kBlocks; ++b)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) o[n][b][r] *= less;
+#pragma unroll
+                for (int b = 0; b < NB; ++b)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) {
+                        p[b][n][r] = power2(fmaf(x[b][n][r], factor, -from));
+                        sum[n] += p[b][n][r];
+                    }
             }
-        l += sum;
+        }
 #pragma unroll
-        for (int b = 0; b < BN / kSide; ++b) columns_product<S>(from + kMatrix, b, x[b], o);
+        for (int n = 0; n < N; ++n) l[n] += sum[n];
+#pragma unroll
+        for (int b = 0; b < NB; ++b) columns_product<S, N>(buffer(step) + kMatrix + b * kSide * S::kRow, places, p[b], o);
+#pragma unroll
+        for (int b = 0; b < NB; ++b)
+#pragma unroll
+            for (int n = 0; n < N; ++n) x[b][n] = next[b][n];
     };
 
-    for (int step = 0; step < steps; ++step) {
-        if constexpr (DIRECT) arrived_but<2 * Rows<S, BN, W, DIRECT>::kCalls>(min(AHEAD - 1, steps - 1 - step));
+    constexpr int kLoads = 2 * Rows<S, BN, W, DIRECT>::kCalls;
+    if (steps > 0) {
+        if constexpr (DIRECT) arrived_but<kLoads>(min(LEAD - 1, steps - 1));
         meet();
-        if (step + AHEAD < steps) begin(step + AHEAD);
-        if (step < whole_steps) {
-            compute(step, Type<0>{});
-        } else {
-            take_out_odd<S, BN, W>(buffer(step) + kMatrix, &odd);
+        rows_product<S, NB, N>(buffer(0), places, q, x);
+    }
+    // (two loops: a branch between the two forms in one would keep a second set of sums)
+    const auto walk = [&](int& step, int to, auto masked) __attribute__((always_inline)) {
+        for (; step < to; ++step) {
+            if constexpr (DIRECT) arrived_but<kLoads>(max(0, min(LEAD - 2, steps - 2 - step)));
             meet();
-            if (step * BN < wave_upto) compute(step, Type<1>{});
+            if (step + LEAD < steps) begin(step + LEAD);
+            if constexpr (masked.value != 0) {
+                take_out_odd<S, BN, W>(buffer(step) + kMatrix, &odd);
+                meet();
+                if (step * BN < wave_upto) {
+#pragma unroll
+                    for (int n = 0; n < N; ++n) {
+                        const int left = own[n] - step * BN - half * 4;         // of the keys that the query sees
+#pragma unroll
+                        for (int b = 0; b < NB; ++b)
+#pragma unroll
+                            for (int r = 0; r < 16; ++r)
+                                x[b][n][r] = b * kSide + (r / 4) * 8 + r % 4 < left ? x[b][n][r] : -__builtin_inff();
+                    }
+                    compute(step);
+                }
+            } else {
+                compute(step);
+            }
+            if (step + LEAD < steps) end(step + LEAD);
         }
-        if (step + AHEAD < steps) end(step + AHEAD);
-    }
+    };
+    int step = 0;
+    walk(step, whole_steps, Type<0>{});
+    walk(step, steps, Type<1>{});
 
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+        const int i = w0 + n * kSide + lane % kSide;
+        const int64_t row = seq.q0 + i;
+        const float total = halves_sum(l[n]);
+        const float to_one = total == 0.f ? 0.f : 1.f / total;
+        store_columns<S>(o[n], to_one, a.out.data + row * a.out.ld + col, i <= last, D);
+        if (a.lse && i <= last && half == 0)
+            a.lse[at.head * a.Tq + row] = total == 0.f ? -__builtin_inff() : (base[n] + __builtin_amdgcn_logf(total)) * kLn2;
+        l[n] = to_one;
+    }
     if (steps > whole_steps && odd) {
+        stored();
         for (int j = whole_steps * BN; j < wave_upto; ++j) {
-            const char* const value = values + j * a.v.ld;
+            const char *const value = values + j * a.v.ld, *const key = keys + j * a.k.ld;
             if (!row_is_odd<S>(value, D)) continue;
-            const float weight = power2(fmaf(slow_dot<S>(query, keys + j * a.k.ld, D), factor, -base));
-            if (j < own) add_odd<S>(value, D, weight, o);
+#pragma unroll
+            for (int n = 0; n < N; ++n) {
+                const int i = w0 + n * kSide + lane % kSide;
+                const float score = slow_dot<S>(queries + (i < last ? i : last) * a.q.ld, key, D);
+                if (i <= last && j < own[n])
+                    add_odd<S>(a.out.data + (seq.q0 + i) * a.out.ld + col, value, D, power2(fmaf(score, factor, -base[n])) * l[n]);
+            }
         }
     }
-    l = halves_sum(l);
-    const int64_t row = seq.q0 + i;
-    store_columns<S>(o, l == 0.f ? 0.f : 1.f / l, a.out.data + row * a.out.ld + col, there, D);
-    if (a.lse && there && half == 0)
-        a.lse[at.head * a.Tq + row] = l == 0.f ? -__builtin_inff() : (base + __builtin_amdgcn_logf(l)) * kLn2;
 }
 
 }  // namespace
@@ -214,16 +279,17 @@ int detonation_attention_forward(const deto_attention* cfg, int64_t Tq, int64_t 
     by_type(q->dtype, [&](auto dt) {
         return by_shape<dt.value>(cfg->head_dim, in_pieces(a.k) && in_pieces(a.v), [&](auto shape, auto direct) {
             using S = decltype(shape);
-            const auto run = [&](auto waves) {
-                constexpr int W = waves.value;
+            const auto run = [&](auto waves, auto blocks) {
+                constexpr int W = waves.value, N = blocks.value;
                 constexpr bool DIRECT = direct.value != 0;
-                if (!plan(a, cfg->q_starts, Tq, W * kSide, cfg->heads)) return planned = DETO_ERR_UNSUPPORTED;
+                if (!plan(a, cfg->q_starts, Tq, W * kSide * N, cfg->heads)) return planned = DETO_ERR_UNSUPPORTED;
                 constexpr int kStep = 2 * kKeys<S::DT> * S::kRow;
-                forward_kernel<S, W, DIRECT><<<a.tiles * cfg->heads, W * kLanes, (kAhead<W, kStep, DIRECT> + 1) * kStep,
+                forward_kernel<S, W, N, DIRECT><<<a.tiles * cfg->heads, W * kLanes, kBuffers<DIRECT> * kStep,
                                                static_cast<hipStream_t>(stream)>>>(a);
                 return 0;
             };
-            return wide ? run(Type<8>{}) : run(Type<4>{});
+            if (wide) return run(Type<8>{}, Type<1>{});
+            return run(Type<4>{}, Type<1>{});
         });
     });
     if (planned) return planned;
