@@ -11,8 +11,6 @@ namespace attention {
 namespace {
 
 // ---- dq: the forward kernel's walk.
-template <int DT> constexpr int kKeys = DT == DETO_F32 ? 32 : 64;      // of a step
-
 // A query's lse in powers of two; one that sees nothing gets weights of zero.
 __device__ __forceinline__ float stored_lse(float lse) {
     return lse == -__builtin_inff() ? __builtin_inff() : lse * kLog2E;
@@ -47,8 +45,8 @@ template <int W, int STEP, bool DIRECT>
 constexpr int kAhead = !DIRECT ? 1 : STEP * 4 * (8 / W) <= 144 * 1024 ? 3 : 1;
 
 template <class S, int W, bool DIRECT>
-__global__ __launch_bounds__(W * kLanes, 2) void queries_kernel(Args a) {
-    constexpr int DT = S::DT, BM = W * kSide, BN = kKeys<DT>, kMatrix = BN * S::kRow, kStep = 2 * kMatrix;
+__global__ __launch_bounds__(W * kLanes) __attribute__((amdgpu_waves_per_eu(kResident<S>, kResident<S>))) void queries_kernel(Args a) {
+    constexpr int DT = S::DT, BM = W * kSide, BN = kKeys<S>, kMatrix = BN * S::kRow, kStep = 2 * kMatrix;
     constexpr int AHEAD = kAhead<W, kStep, DIRECT>;
     extern __shared__ __align__(16) char lds[];          // AHEAD + 1 steps of keys and values
     __shared__ uint32_t odd;                             // infinities or NaNs among keys that not all queries see
@@ -65,7 +63,10 @@ __global__ __launch_bounds__(W * kLanes, 2) void queries_kernel(Args a) {
         return static_cast<int>(upto < 0 ? 0 : upto);
     };
     const int upto = seen(i0 + BM - 1), wave_upto = seen(w0 + kSide - 1);
-    const int own = seen(i), steps = (upto + BN - 1) / BN, whole_steps = seen(i0) / BN;
+    const int own = seen(i), all_steps = (upto + BN - 1) / BN, splits = gridDim.y, split = blockIdx.y;
+    // of which this workgroup takes one part
+    const int from = static_cast<int>(int64_t{all_steps} * split / splits), steps = static_cast<int>(int64_t{all_steps} * (split + 1) / splits);
+    const int whole_steps = min(max(seen(i0) / BN, from), steps);
 
     const int64_t col = int64_t{at.head} * D * S::kElem, kv = int64_t{at.head / a.group} * D * S::kElem;
     const int64_t row = seq.q0 + (there ? i : last);
@@ -88,8 +89,8 @@ __global__ __launch_bounds__(W * kLanes, 2) void queries_kernel(Args a) {
     if (threadIdx.x == 0) odd = 0;
 #pragma unroll
     for (int n = 0; n < AHEAD; ++n)
-        if (n < steps) begin(n);
-    if (steps > 0) end(0);
+        if (from + n < steps) begin(from + n);
+    if (from < steps) end(from);
 
     const float factor = a.scale * kLog2E;
     u32x4 q[1][S::kFrags], g[1][S::kFrags];
@@ -97,7 +98,7 @@ __global__ __launch_bounds__(W * kLanes, 2) void queries_kernel(Args a) {
     load_row<S>(a.out.data + row * a.out.ld + col, there, D, q[0]);
     const float lse = there ? stored_lse(a.lse[at.head * a.Tq + row]) : __builtin_inff();
     const float delta = rows_dot<S>(g[0], q[0]);
-    if (there && half == 0) {
+    if (there && half == 0 && split == 0) {
         a.stats[at.head * a.Tq + row] = lse;
         a.stats[(a.heads + at.head) * a.Tq + row] = delta;
     }
@@ -139,45 +140,110 @@ __global__ __launch_bounds__(W * kLanes, 2) void queries_kernel(Args a) {
             if (step + AHEAD < steps) end(step + AHEAD);
         }
     };
-    int step = 0;
+    int step = from;
     walk(step, whole_steps, Type<0>{});
     walk(step, steps, Type<1>{});
 
-    store_columns<S>(dq[0], a.scale, a.dq.data + row * a.dq.ld + col, there, D);
+    float* const part = a.parts + ((int64_t{split} * a.heads + at.head) * a.Tq + row) * part_row(D);
+    if (splits == 1) store_columns<S>(dq[0], a.scale, a.dq.data + row * a.dq.ld + col, there, D);
+    else store_part<S>(dq[0], part, there, D);
     if (steps > whole_steps && odd) {
         stored();
-        for (int j = whole_steps * BN; j < wave_upto; ++j) {
+        for (int j = whole_steps * BN; j < min(wave_upto, steps * BN); ++j) {
             const char* const key = keys + j * a.k.ld;
             if (!row_is_odd<S>(key, D)) continue;
             const float p = power2(fmaf(slow_dot<S>(query, key, D), factor, -lse));
             const float ds = p * (slow_dot<S>(grad, values + j * a.v.ld, D) - delta);
-            if (there && j < own) add_odd<S>(a.dq.data + row * a.dq.ld + col, key, D, ds * a.scale);
+            if (!there || j >= own) continue;
+            if (splits == 1) add_odd<S>(a.dq.data + row * a.dq.ld + col, key, D, ds * a.scale);
+            else add_odd<S, DETO_F32>(part, key, D, ds);
         }
     }
 }
 
+// A tile's rows of dq out of what the splits left: a wavefront for each, its lanes two features each.
+template <class S, int W>
+__global__ __launch_bounds__(W * kLanes) void join_kernel(Args a, int splits) {
+    constexpr int BM = W * kSide;
+    Place at;
+    if (!place_of(a, a.q_starts, a.Tq, BM, a.heads, a.causal, at)) return;
+    const Sequence seq = sequence_of(a, at.s);
+    const int D = a.head_dim, P = part_row(D), lane = threadIdx.x % kLanes;
+    if (2 * lane >= D) return;
+    const int i = at.tile * BM + blockIdx.y * W + threadIdx.x / kLanes;
+    if (i < seq.Lq) {
+        const float* const part = a.parts + (at.head * a.Tq + seq.q0 + i) * P + 2 * lane;
+        float x = 0.f, y = 0.f;
+#pragma unroll 8
+        for (int s = 0; s < splits; ++s) {
+            const f32x2 v = *reinterpret_cast<const f32x2*>(part + s * a.heads * a.Tq * P);
+            x += v.x;
+            y += v.y;
+        }
+        char* const dq = a.dq.data + (seq.q0 + i) * a.dq.ld + int64_t{at.head} * D * S::kElem;
+        store1<S::DT>(dq, 2 * lane, x * a.scale);
+        if (2 * lane + 1 < D) store1<S::DT>(dq, 2 * lane + 1, y * a.scale);
+    }
+}
+
 // ---- dk, dv
-template <class S> constexpr int kQueries = S::kRow >= 256 ? 32 : 64;                // of a step
-template <class S, int W, bool DIRECT>
-constexpr int kAheadOfKeys = DIRECT ? (S::kRow > 256 ? 1 : 3) : 1;
+template <class S> constexpr int kQueries = 32;                // of a step
+// HEADS of the heads that share keys are taken at a time, by wavefronts of their own, which add up their sums in the end:
+// so that a few long walks are cut where there are not many workgroups.  Their rows leave room for fewer steps ahead.
+template <class S, int HEADS, bool DIRECT>
+constexpr int kAheadOfKeys = !DIRECT || S::kRow > 256 || HEADS == 4 ? 1 : HEADS == 2 ? 2 : 3;
 // Sums of fp32 take the registers of two wavefronts with 128 features; 16-bit values of 128 features stay in LDS, which
 // leaves the registers that two wavefronts need beside keys and sums.
-template <class S> constexpr int kResident = S::kRow > 256 ? 1 : 2;
+template <class S> constexpr int kResidentKeys = S::kRow > 256 ? 1 : 2;
 template <class S> constexpr bool kValuesStay = S::kRow == 256 && S::DT != DETO_F32;
 
-template <class S, int W, bool DIRECT>
-__global__ __launch_bounds__(W * kLanes, kResident<S>) void keys_kernel(Args a) {
-    constexpr int BN = W * kSide, BQ = kQueries<S>, kMatrix = BQ * S::kRow, kStep = 2 * kMatrix;
+template <class S, int BLOCKS, int HEADS>
+__device__ __forceinline__ void add_heads(char* lds, const f32x16 (&c)[S::kBlocks], int own_block, int own_head, float factor,
+                                          char* row, bool there, int D) {
+    typedef float f32x4 __attribute__((ext_vector_type(4)));
+    static_assert(S::kBlocks % HEADS == 0, "");
+    constexpr int kSums = S::kBlocks * 16 * kLanes * 4;          // bytes of a wavefront's
+    const int lane = threadIdx.x % kLanes;
+    f32x4* const own = reinterpret_cast<f32x4*>(lds + (own_head * BLOCKS + own_block) * kSums) + lane;
+    __syncthreads();
+#pragma unroll
+    for (int b = 0; b < S::kBlocks; ++b)
+#pragma unroll
+        for (int g = 0; g < 4; ++g)
+            own[(4 * b + g) * kLanes] = f32x4{c[b][4 * g], c[b][4 * g + 1], c[b][4 * g + 2], c[b][4 * g + 3]};
+    __syncthreads();
+#pragma unroll
+    for (int n = 0; n < S::kBlocks / HEADS; ++n) {
+        const int b = n * HEADS + own_head;
+        f32x16 sum = {};
+#pragma unroll
+        for (int h = 0; h < HEADS; ++h) {
+            const f32x4* const from = reinterpret_cast<const f32x4*>(lds + (h * BLOCKS + own_block) * kSums) + 4 * b * kLanes + lane;
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                const f32x4 v = from[g * kLanes];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) sum[4 * g + j] += v[j];
+            }
+        }
+        store_block<S>(sum, b, factor, row, there, D);
+    }
+}
+
+template <class S, int W, int HEADS, bool DIRECT>
+__global__ __launch_bounds__(W * kLanes) __attribute__((amdgpu_waves_per_eu(kResidentKeys<S>, kResidentKeys<S>))) void keys_kernel(Args a) {
+    constexpr int BLOCKS = W / HEADS, BN = BLOCKS * kSide, BQ = kQueries<S>, kMatrix = BQ * S::kRow, kStep = 2 * HEADS * kMatrix;
     constexpr bool STAY = kValuesStay<S>;
-    constexpr int AHEAD = kAheadOfKeys<S, W, DIRECT>;
+    constexpr int AHEAD = kAheadOfKeys<S, HEADS, DIRECT>;
     extern __shared__ __align__(16) char lds[];          // AHEAD + 1 steps of queries and gradients of outputs; values
-    __shared__ __align__(16) float stats[AHEAD + 1][2 * BQ];      // lse and delta
+    __shared__ __align__(16) float stats[AHEAD + 1][HEADS][2 * BQ];      // lse and delta
     __shared__ uint32_t odd;                             // infinities or NaNs among rows that do not see all keys
     Place at;
     if (!place_of(a, a.k_starts, a.Tk, BN, a.kv_heads, false, at)) return;
     const Sequence seq = sequence_of(a, at.s);
     const int D = DIRECT ? S::DP : a.head_dim, lane = threadIdx.x % kLanes, half = lane / kSide;
-    const int in_tile = threadIdx.x / kLanes * kSide + lane % kSide, j0 = at.tile * BN, j = j0 + in_tile;
+    const int wave = uniform(static_cast<int32_t>(threadIdx.x / kLanes)), own_block = wave % BLOCKS, own_head = wave / BLOCKS;
+    const int j0 = at.tile * BN, j = j0 + own_block * kSide + lane % kSide;
     const int last = seq.Lk - 1;
     const bool there = j <= last;
 
@@ -189,16 +255,16 @@ __global__ __launch_bounds__(W * kLanes, kResident<S>) void keys_kernel(Args a) 
     };
     const int first_step = seen_from(j0) / BQ, steps = (seq.Lq + BQ - 1) / BQ - first_step;    // of a head
     const int all_from = seen_from(j0 + BN - 1);                 // from here on queries see all of these keys
-    const int wave_from = seen_from(j0 + uniform(static_cast<int32_t>(threadIdx.x / kLanes)) * kSide), own = seen_from(j);
-    const int total = steps * a.group;                           // a head's steps, then the next one's
+    const int wave_from = seen_from(j0 + own_block * kSide), own = seen_from(j);
+    const int total = steps * (a.group / HEADS);                 // those of the first heads, then of the next ones
 
     const int64_t kv = int64_t{at.head} * D * S::kElem, row = seq.k0 + (there ? j : last);
     const char* const key = a.k.data + row * a.k.ld + kv;
     const char* const value = a.v.data + row * a.v.ld + kv;
 
     Rows<S, BQ, W, DIRECT> rq(a.q.ld), rg(a.dout.ld);
-    float stat[2 * BQ / kLanes];
-    // a step: of which head, from which query on, and its buffer
+    float stat[HEADS][2 * BQ / kLanes];
+    // a step: of which heads, from which query on, and its buffer
     struct Step {
         int head, query, buffer;
     };
@@ -206,7 +272,7 @@ __global__ __launch_bounds__(W * kLanes, kResident<S>) void keys_kernel(Args a) 
         s.query += BQ;
         if (s.query >= seq.Lq) {
             s.query = first_step * BQ;
-            ++s.head;
+            s.head += HEADS;
         }
         s.buffer = s.buffer == AHEAD ? 0 : s.buffer + 1;
         return s;
@@ -214,27 +280,33 @@ __global__ __launch_bounds__(W * kLanes, kResident<S>) void keys_kernel(Args a) 
     const auto begin = [&](Step s) __attribute__((always_inline)) {
         char* const to = lds + s.buffer * kStep;
         const int have = seq.Lq - s.query < BQ ? seq.Lq - s.query : BQ;
-        const int64_t first = seq.q0 + s.query, col = int64_t{s.head} * D * S::kElem;
-        rq.begin(to, a.q.data + first * a.q.ld + col, a.q.ld, have, D);
-        rg.begin(to + kMatrix, a.dout.data + first * a.dout.ld + col, a.dout.ld, have, D);
-        // lse and delta, 64 at a time, all wavefronts the same
+        const int64_t first = seq.q0 + s.query;
 #pragma unroll
-        for (int c = 0; c < 2 * BQ / kLanes; ++c) {
-            const int n = c * kLanes + lane, t = n % BQ;
-            const float* const from = a.stats + (int64_t{n / BQ} * a.heads + s.head) * a.Tq + first + (t < have ? t : have - 1);
-            if constexpr (DIRECT)
-                __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)from,
-                                                 (__attribute__((address_space(3))) void*)(stats[s.buffer] + c * kLanes), 4, 0, 0);
-            else stat[c] = *from;
+        for (int h = 0; h < HEADS; ++h) {
+            const int64_t col = int64_t{s.head + h} * D * S::kElem;
+            rq.begin(to + 2 * h * kMatrix, a.q.data + first * a.q.ld + col, a.q.ld, have, D);
+            rg.begin(to + (2 * h + 1) * kMatrix, a.dout.data + first * a.dout.ld + col, a.dout.ld, have, D);
+            // lse and delta, 64 at a time, all wavefronts the same
+#pragma unroll
+            for (int c = 0; c < 2 * BQ / kLanes; ++c) {
+                const int n = c * kLanes + lane, t = n % BQ;
+                const float* const from =
+                    a.stats + (int64_t{n / BQ} * a.heads + s.head + h) * a.Tq + first + (t < have ? t : have - 1);
+                if constexpr (DIRECT)
+                    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)from,
+                                                     (__attribute__((address_space(3))) void*)(stats[s.buffer][h] + c * kLanes),
+                                                     4, 0, 0);
+                else stat[h][c] = *from;
+            }
         }
     };
     const auto end = [&](Step s) __attribute__((always_inline)) {
         char* const to = lds + s.buffer * kStep;
-        rq.end(to);
+        rq.end(to);                                      // (one head at a time)
         rg.end(to + kMatrix);
         if constexpr (!DIRECT) {
 #pragma unroll
-            for (int c = 0; c < 2 * BQ / kLanes; ++c) stats[s.buffer][c * kLanes + lane] = stat[c];
+            for (int c = 0; c < 2 * BQ / kLanes; ++c) stats[s.buffer][0][c * kLanes + lane] = stat[0][c];
         }
     };
     if (threadIdx.x == 0) odd = 0;
@@ -262,14 +334,14 @@ __global__ __launch_bounds__(W * kLanes, kResident<S>) void keys_kernel(Args a) 
     f32x16 dk[1][S::kBlocks] = {}, dv[1][S::kBlocks] = {};
 
     const Places places = places_of<S>();
-    const char* const own_values = lds + (AHEAD + 1) * kStep + threadIdx.x / kLanes * kSide * S::kRow;
+    const char* const own_values = lds + (AHEAD + 1) * kStep + own_block * kSide * S::kRow;
     const auto compute = [&](Step s, auto masked) __attribute__((always_inline)) {
         constexpr bool MASKED = masked.value != 0;
-        const char* const from = lds + s.buffer * kStep;
+        const char* const from = lds + s.buffer * kStep + 2 * own_head * kMatrix;
 #pragma unroll
         for (int b = 0; b < BQ / kSide; ++b) {
             const int first = s.query + b * kSide + half * 4, upto = seq.Lq - first, own_from = own - first;
-            const float* const stat = stats[s.buffer] + b * kSide + half * 4;
+            const float* const stat = stats[s.buffer][own_head] + b * kSide + half * 4;
             const char *const rows_q = from + b * kSide * S::kRow, *const rows_g = rows_q + kMatrix;
             f32x16 p[1][1], ds[1][1];
             rows_product<S, 1, 1>(rows_q, places, k, p);
@@ -297,13 +369,12 @@ __global__ __launch_bounds__(W * kLanes, kResident<S>) void keys_kernel(Args a) 
     const auto walk = [&](int& n, auto masked) __attribute__((always_inline)) {
         constexpr bool MASKED = masked.value != 0;
         while (n < total && (now.query >= all_from && now.query + BQ <= seq.Lq) != MASKED) {
-            if constexpr (DIRECT) arrived_but<2 * Rows<S, BQ, W, DIRECT>::kCalls + 2 * BQ / kLanes>(min(AHEAD - 1, total - 1 - n));
+            if constexpr (DIRECT) arrived_but<HEADS * (2 * Rows<S, BQ, W, DIRECT>::kCalls + 2 * BQ / kLanes)>(min(AHEAD - 1, total - 1 - n));
             meet();
             const bool more = n + AHEAD < total;
             if (more) begin(ahead);
             if constexpr (MASKED) {
-                take_out_odd<S, BQ, W>(lds + now.buffer * kStep, &odd);
-                take_out_odd<S, BQ, W>(lds + now.buffer * kStep + kMatrix, &odd);
+                take_out_odd<S, 2 * HEADS * BQ, W>(lds + now.buffer * kStep, &odd);
                 meet();
                 if (now.query + BQ > wave_from) compute(now, masked);
             } else {
@@ -322,10 +393,22 @@ __global__ __launch_bounds__(W * kLanes, kResident<S>) void keys_kernel(Args a) 
         walk(n, Type<1>{});
     }
 
-    store_columns<S>(dk[0], a.scale, a.dk.data + row * a.dk.ld + kv, there, D);
-    store_columns<S>(dv[0], 1.f, a.dv.data + row * a.dv.ld + kv, there, D);
+    char *const to_k = a.dk.data + row * a.dk.ld + kv, *const to_v = a.dv.data + row * a.dv.ld + kv;
+    if constexpr (HEADS == 1) {
+        store_columns<S>(dk[0], a.scale, to_k, there, D);
+        store_columns<S>(dv[0], 1.f, to_v, there, D);
+    } else {
+        // a wavefront adds up the heads' sums of every HEADS-th block of features, in their order
+        add_heads<S, BLOCKS, HEADS>(lds, dk[0], own_block, own_head, a.scale, to_k, there, D);
+        add_heads<S, BLOCKS, HEADS>(lds, dv[0], own_block, own_head, 1.f, to_v, there, D);
+    }
     if (total > 0 && odd) {
-        stored();
+        if constexpr (HEADS == 1) {
+            stored();
+        } else {
+            __syncthreads();
+            if (own_head) return;
+        }
         const int tail = seq.Lq / BQ * BQ;                  // steps that were masked: up to all_from, and a short last one
         for (int h = at.head * a.group; h < (at.head + 1) * a.group; ++h)
             for (int t = first_step * BQ; t < seq.Lq; ++t) {
@@ -374,6 +457,8 @@ int detonation_attention_backward(const deto_attention* cfg, int64_t Tq, int64_t
     Args a = args_of(cfg, Tq, Tk, q, k, v);
     a.lse = const_cast<float*>(lse);
     a.stats = static_cast<float*>(workspace);
+    a.parts = a.stats + stats_floats(cfg, Tq);
+    const int splits = splits_of(cfg, Tq, Tk, dtype == DETO_F32);
     if (Tq) {
         a.out = matrix_of(out);
         a.dout = matrix_of(dout);
@@ -387,29 +472,40 @@ int detonation_attention_backward(const deto_attention* cfg, int64_t Tq, int64_t
     int planned = DETO_OK;
     fresh();
     by_type(dtype, [&](auto dt) {
-        return by_shape<dt.value>(cfg->head_dim, in_pieces(a.q) && in_pieces(a.k) && in_pieces(a.v) && in_pieces(a.dout),
+        return by_shape<dt.value>(cfg->head_dim, in_words(a.q) && in_words(a.k) && in_words(a.v) && in_words(a.dout),
                                   [&](auto shape, auto direct) {
             using S = decltype(shape);
             constexpr bool DIRECT = direct.value != 0;
             const auto queries = [&](auto waves) {
-                constexpr int W = waves.value, kStep = 2 * kKeys<S::DT> * S::kRow;
+                constexpr int W = waves.value, kStep = 2 * kKeys<S> * S::kRow;
                 if (!plan(a, cfg->q_starts, Tq, W * kSide, H)) return DETO_ERR_UNSUPPORTED;
-                if (Tq) queries_kernel<S, W, DIRECT><<<a.tiles * H, W * kLanes, (kAhead<W, kStep, DIRECT> + 1) * kStep, on>>>(a);
+                if (Tq) {
+                    const dim3 grid(a.tiles * H, splits);
+                    queries_kernel<S, W, DIRECT><<<grid, W * kLanes, (kAhead<W, kStep, DIRECT> + 1) * kStep, on>>>(a);
+                    if (splits > 1) join_kernel<S, W><<<dim3(grid.x, kSide), W * kLanes, 0, on>>>(a, splits);
+                }
                 return DETO_OK;
             };
-            const auto keys = [&](auto waves) {
-                constexpr int W = waves.value, kStep = 2 * kQueries<S> * S::kRow;
-                constexpr int kLds = (kAheadOfKeys<S, W, DIRECT> + 1) * kStep + (kValuesStay<S> ? W * kSide * S::kRow : 0);
-                if (!plan(a, cfg->k_starts, Tk, W * kSide, K)) return DETO_ERR_UNSUPPORTED;
-                if (Tk) keys_kernel<S, W, DIRECT><<<a.tiles * K, W * kLanes, kLds, on>>>(a);
+            const auto keys = [&](auto waves, auto heads) {
+                constexpr int W = waves.value, HEADS = heads.value, BN = W / HEADS * kSide, kStep = 2 * HEADS * kQueries<S> * S::kRow;
+                constexpr int kLds = (kAheadOfKeys<S, HEADS, DIRECT> + 1) * kStep + (kValuesStay<S> ? BN * S::kRow : 0);
+                if (!plan(a, cfg->k_starts, Tk, BN, K)) return DETO_ERR_UNSUPPORTED;
+                if (Tk) keys_kernel<S, W, HEADS, DIRECT><<<a.tiles * K, W * kLanes, kLds, on>>>(a);
                 return DETO_OK;
             };
-            planned = Tq * H >= int64_t{256} * kCUs ? queries(Type<8>{}) : queries(Type<4>{});
+            constexpr bool kWide = S::DP == 128;
+            if constexpr (kWide) planned = Tq * H >= int64_t{256} * kCUs ? queries(Type<8>{}) : queries(Type<4>{});
+            else planned = queries(Type<4>{});
             if (planned) return planned;
-            if constexpr (kResident<S> == 2) {
-                if (Tk * K >= int64_t{256} * kCUs) return planned = keys(Type<8>{});
+            if constexpr (kWide && kResidentKeys<S> == 2) {
+                if constexpr (DIRECT) {
+                    const bool few = Tk * K < int64_t{256} * 2 * kCUs;
+                    if (few && a.group % 4 == 0) return planned = keys(Type<8>{}, Type<4>{});
+                    if (few && a.group % 2 == 0) return planned = keys(Type<8>{}, Type<2>{});
+                }
+                if (Tk * K >= int64_t{256} * kCUs) return planned = keys(Type<8>{}, Type<1>{});
             }
-            return planned = keys(Type<4>{});
+            return planned = keys(Type<4>{}, Type<1>{});
         });
     });
     return planned ? planned : enqueued();

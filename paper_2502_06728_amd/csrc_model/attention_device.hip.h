@@ -24,6 +24,8 @@ typedef uint32_t u32x8 __attribute__((ext_vector_type(8)));
 
 constexpr int kSide = 32;               // of a block
 constexpr int kCUs = 256;
+
+
 constexpr float kLog2E = 1.44269504088896341f, kLn2 = 0.693147180559945309f;
 
 // A head's features, padded with zeros to DP.
@@ -37,6 +39,11 @@ struct Shape {
     static constexpr int kFrags = kPieces / 2;      // operands of the rows form: two pieces, one for each half of the lanes
     static constexpr int kBlocks = DP / kSide;      // blocks of features
 };
+
+// The wavefronts that a SIMD has registers for: two with 128 features, four with 64 and fewer.
+template <class S> constexpr int kResident = S::DP == 64 && S::DT != DETO_F32 ? 3 : 2;
+// Keys of a step of a walk over keys
+template <class S> constexpr int kKeys = S::DT == DETO_F32 || S::DP == 64 ? 32 : 64;
 
 struct Matrix {
     char* data;
@@ -53,7 +60,12 @@ struct Args {
     float scale;
     uint32_t tiles;                      // of one head (with starts: at most), see Plan
     uint32_t per_sequence;               // tiles of one sequence, without starts
+    float* parts;                        // [splits, heads * Tq, part_row(head_dim)], where a walk is cut into several
 };
+
+// A split's sums for a query are a row of floats: a head's features, in whole pieces of four.  Behind all of those the
+// forward pass has two planes of splits * heads * Tq: bases and sums of weights.
+__host__ __device__ __forceinline__ int part_row(int head_dim) { return (head_dim + 3) / 4 * 4; }
 
 // ---- sequences
 struct Sequence {
@@ -205,7 +217,7 @@ __device__ __forceinline__ u32x4 load_piece(const char* row, int piece, int D) {
 
 // Rows into LDS by a workgroup of W wavefronts.  Rows that are missing at the end of a sequence are copies of the last
 // one: what they are multiplied with is zero.
-// DIRECT: heads of DP features at multiples of 16 bytes, from memory to LDS without a register: a wavefront's call writes
+// DIRECT: heads of DP features at multiples of 4 bytes, from memory to LDS without a register: a wavefront's call writes
 // 64 pieces in a row, so its lanes read the pieces that belong there.  begin() starts kCalls of these; who reads the rows
 // waits until they have come (arrived()), and for the other wavefronts' (meet()).
 // Otherwise through registers: begin() loads, end() stores.
@@ -351,12 +363,12 @@ __device__ __forceinline__ float slow_dot(const char* x, const char* y, int D) {
 
 // Adds what a row's infinities and NaNs give under a weight to a row of results that is in memory already (the halves of
 // the lanes take turns at the features).
-template <class S>
-__device__ __forceinline__ void add_odd(char* to, const char* row, int D, float weight) {
+template <class S, int OUT = S::DT>
+__device__ __forceinline__ void add_odd(void* to, const char* row, int D, float weight) {
 #pragma unroll 1
     for (int d = threadIdx.x / kSide % 2; d < D; d += 2) {
         const float v = load1<S::DT>(row, d);
-        if (!(fabsf(v) < __builtin_inff())) store1<S::DT>(to, d, load1<S::DT>(to, d) + weight * v);
+        if (!(fabsf(v) < __builtin_inff())) store1<OUT>(to, d, load1<OUT>(to, d) + weight * v);
     }
 }
 // this wavefront's stores are there for its loads
@@ -491,48 +503,66 @@ __device__ __forceinline__ float halves_sum(float v) {
 // Columns of C times a factor into the lanes' rows of a matrix, 16 bytes a lane: the two halves of the lanes, which hold
 // four features each of every eight, exchange theirs for that.
 template <class S>
-__device__ __forceinline__ void store_columns(const f32x16 (&c)[S::kBlocks], float factor, char* row, bool there, int D) {
+__device__ __forceinline__ void store_block(const f32x16& c, int b, float factor, char* row, bool there, int D) {
     const int half = threadIdx.x / kSide % 2;
+    if constexpr (S::DT == DETO_F32) {
 #pragma unroll
-    for (int b = 0; b < S::kBlocks; ++b) {
-        if constexpr (S::DT == DETO_F32) {
+        for (int g = 0; g < 4; ++g) {
+            const int d = b * kSide + 8 * g + 4 * half;
+            u32x4 v;
 #pragma unroll
-            for (int g = 0; g < 4; ++g) {
-                const int d = b * kSide + 8 * g + 4 * half;
-                u32x4 v;
+            for (int j = 0; j < 4; ++j) v[j] = f32_bits(c[4 * g + j] * factor);
+            if (there && d + 4 <= D) *reinterpret_cast<u32x4_any4*>(row + d * 4) = v;
+            else if (there) {
 #pragma unroll
-                for (int j = 0; j < 4; ++j) v[j] = f32_bits(c[b][4 * g + j] * factor);
-                if (there && d + 4 <= D) *reinterpret_cast<u32x4_any4*>(row + d * 4) = v;
-                else if (there) {
-#pragma unroll
-                    for (int j = 0; j < 3; ++j)
-                        if (d + j < D) reinterpret_cast<uint32_t*>(row)[d + j] = v[j];
-                }
+                for (int j = 0; j < 3; ++j)
+                    if (d + j < D) reinterpret_cast<uint32_t*>(row)[d + j] = v[j];
             }
-        } else {
+        }
+    } else {
 #pragma unroll
-            for (int g = 0; g < 4; g += 2) {
-                uint32_t w[2][2];
+        for (int g = 0; g < 4; g += 2) {
+            uint32_t w[2][2];
 #pragma unroll
-                for (int i = 0; i < 2; ++i)
+            for (int i = 0; i < 2; ++i)
 #pragma unroll
-                    for (int j = 0; j < 2; ++j) {
-                        const float lo = c[b][4 * (g + i) + 2 * j] * factor, hi = c[b][4 * (g + i) + 2 * j + 1] * factor;
-                        w[i][j] = S::DT == DETO_BF16 ? pack_bf16(lo, hi) : pack_f16(lo, hi);
-                    }
-                const auto x = __builtin_amdgcn_permlane32_swap(w[0][0], w[1][0], false, false);
-                const auto y = __builtin_amdgcn_permlane32_swap(w[0][1], w[1][1], false, false);
-                const u32x4 v = {x[0], y[0], x[1], y[1]};
-                const int d = b * kSide + 8 * (g + half);
-                if (there && d + 8 <= D) *reinterpret_cast<u32x4_any2*>(row + d * 2) = v;
-                else if (there) {
-#pragma unroll
-                    for (int j = 0; j < 7; ++j)
-                        if (d + j < D) reinterpret_cast<uint16_t*>(row)[d + j] = static_cast<uint16_t>(v[j / 2] >> (16 * (j % 2)));
+                for (int j = 0; j < 2; ++j) {
+                    const float lo = c[4 * (g + i) + 2 * j] * factor, hi = c[4 * (g + i) + 2 * j + 1] * factor;
+                    w[i][j] = S::DT == DETO_BF16 ? pack_bf16(lo, hi) : pack_f16(lo, hi);
                 }
+            const auto x = __builtin_amdgcn_permlane32_swap(w[0][0], w[1][0], false, false);
+            const auto y = __builtin_amdgcn_permlane32_swap(w[0][1], w[1][1], false, false);
+            const u32x4 v = {x[0], y[0], x[1], y[1]};
+            const int d = b * kSide + 8 * (g + half);
+            if (there && d + 8 <= D) *reinterpret_cast<u32x4_any2*>(row + d * 2) = v;
+            else if (there) {
+#pragma unroll
+                for (int j = 0; j < 7; ++j)
+                    if (d + j < D) reinterpret_cast<uint16_t*>(row)[d + j] = static_cast<uint16_t>(v[j / 2] >> (16 * (j % 2)));
             }
         }
     }
+}
+template <class S>
+__device__ __forceinline__ void store_columns(const f32x16 (&c)[S::kBlocks], float factor, char* row, bool there, int D) {
+#pragma unroll
+    for (int b = 0; b < S::kBlocks; ++b) store_block<S>(c[b], b, factor, row, there, D);
+}
+
+// the same as fp32 sums, as they are
+template <class S>
+__device__ __forceinline__ void store_part(const f32x16 (&c)[S::kBlocks], float* row, bool there, int D) {
+    const int half = threadIdx.x / kSide % 2;
+#pragma unroll
+    for (int b = 0; b < S::kBlocks; ++b)
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+            const int d = b * kSide + 8 * g + 4 * half;
+            u32x4 v;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) v[j] = f32_bits(c[b][4 * g + j]);
+            if (there && d < D) *reinterpret_cast<u32x4*>(row + d) = v;
+        }
 }
 
 __device__ __forceinline__ float power2(float x) { return __builtin_amdgcn_exp2f(x); }
@@ -544,6 +574,27 @@ Args args_of(const deto_attention* cfg, int64_t Tq, int64_t Tk, const deto_rows*
 
 inline Matrix matrix_of(const deto_rows* m) {
     return {static_cast<char*>(m->data), m->ld * type_size(m->dtype)};
+}
+
+// Into how many parts the walks over keys are cut.  Where fewer workgroups than CUs would walk over many keys, a second
+// launch that adds up what parts of 64 keys leave costs less than the rest of the walk.  (Sequences of equal length are
+// assumed; the parts are equal shares of each tile's own walk, whatever its length.)  fp32 steps take longer: it is cut
+// from 128 keys on, 16-bit types from 512 on.
+inline int splits_of(const deto_attention* cfg, int64_t Tq, int64_t Tk, bool f32) {
+    if (!Tq || !Tk) return 1;
+    const int64_t queried = cfg->sequences < Tq ? cfg->sequences : Tq;
+    const int64_t groups = cfg->heads * ((Tq + 127) / 128 > queried ? (Tq + 127) / 128 : queried);
+    const int64_t keys = Tk / (cfg->sequences < Tk ? cfg->sequences : Tk);
+    if (groups >= kCUs || keys < (f32 ? 128 : 512)) return 1;
+    int64_t n = 2 * kCUs / groups;
+    n = n < keys / 64 ? n : keys / 64;
+    return static_cast<int>(n < 32 ? n : 32);
+}
+inline int64_t stats_floats(const deto_attention* cfg, int64_t Tq) {        // of the backward pass, to whole pieces
+    return (2 * cfg->heads * Tq + 3) / 4 * 4;
+}
+inline int64_t part_floats(const deto_attention* cfg, int64_t Tq, int splits) {
+    return splits > 1 ? splits * cfg->heads * Tq * (part_row(cfg->head_dim) + 2) : 0;
 }
 
 // Tiles of `size` rows of one head, into args; false where a launch cannot number those of all heads.
@@ -562,8 +613,8 @@ inline bool plan(Args& a, const int32_t* starts, int64_t T, int size, int heads)
     return fits;
 }
 
-// f(Shape, direct) for a head's features; `direct`: every head of the matrices that are walked over starts at a multiple
-// of 16 bytes
+// f(Shape, direct) for a head's features; `direct`: every row of the matrices that are walked over starts at a multiple
+// of 4 bytes
 template <int DT, class F>
 inline int by_shape(int head_dim, bool direct, F f) {
     if (head_dim == 64 && direct) return f(Shape<DT, 64>{}, Type<1>{});
@@ -571,7 +622,7 @@ inline int by_shape(int head_dim, bool direct, F f) {
     if (head_dim <= 64) return f(Shape<DT, 64>{}, Type<0>{});
     return f(Shape<DT, 128>{}, Type<0>{});
 }
-inline bool in_pieces(const Matrix& m) { return is_aligned(m.data, 16) && m.ld % 16 == 0 && m.ld < (int64_t{1} << 24); }
+inline bool in_words(const Matrix& m) { return is_aligned(m.data, 4) && m.ld % 4 == 0 && m.ld < (int64_t{1} << 24); }
 
 }  // namespace attention
 }  // namespace model

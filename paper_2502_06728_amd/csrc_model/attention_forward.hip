@@ -10,17 +10,15 @@ namespace model {
 namespace attention {
 namespace {
 
-template <int DT> constexpr int kKeys = DT == DETO_F32 ? 32 : 64;      // of a step
-
 // Weights are powers of two of a score less the query's base.  The base is the largest score of the first keys, and it
 // stays until a step's weights, which a lane adds up anyway, pass this: no step needs its scores' maximum, and the sums
 // so far are seldom scaled down.  (Weights this large are numbers in fp16, and have as many bits as others.)
 constexpr float kMost = 8192.f;
 
 template <class S, int W, int N, bool DIRECT>
-__global__ __launch_bounds__(W * kLanes, N == 1 ? 2 : 1) __attribute__((amdgpu_waves_per_eu(N == 1 ? 2 : 1, N == 1 ? 2 : 1)))
+__global__ __launch_bounds__(W * kLanes) __attribute__((amdgpu_waves_per_eu(kResident<S>, kResident<S>)))
 void forward_kernel(Args a) {
-    constexpr int DT = S::DT, BM = W * kSide * N, BN = kKeys<DT>, kMatrix = BN * S::kRow, kStep = 2 * kMatrix;
+    constexpr int DT = S::DT, BM = W * kSide * N, BN = kKeys<S>, kMatrix = BN * S::kRow, kStep = 2 * kMatrix;
     constexpr int LEAD = kLead<DIRECT>, NB = BN / kSide;
     extern __shared__ __align__(16) char lds[];          // steps of keys and values
     __shared__ uint32_t odd;                             // infinities or NaNs among values that not all queries see
@@ -37,7 +35,10 @@ void forward_kernel(Args a) {
         return static_cast<int>(upto < 0 ? 0 : upto);
     };
     const int upto = seen(i0 + BM - 1), wave_upto = seen(w0 + kSide * N - 1);        // by any of the workgroup's, the wavefront's
-    const int steps = (upto + BN - 1) / BN, whole_steps = seen(i0) / BN;
+    const int all_steps = (upto + BN - 1) / BN, splits = gridDim.y, split = blockIdx.y;
+    // of which this workgroup takes one part
+    const int from = static_cast<int>(int64_t{all_steps} * split / splits), steps = static_cast<int>(int64_t{all_steps} * (split + 1) / splits);
+    const int whole_steps = min(max(seen(i0) / BN, from), steps);
 
     const int64_t col = int64_t{at.head} * D * S::kElem, kv = int64_t{at.head / a.group} * D * S::kElem;
     const char* const keys = a.k.data + seq.k0 * a.k.ld + kv;
@@ -58,9 +59,9 @@ void forward_kernel(Args a) {
     if (threadIdx.x == 0) odd = 0;
 #pragma unroll
     for (int n = 0; n < LEAD; ++n)
-        if (n < steps) {
-            begin(n);
-            end(n);
+        if (from + n < steps) {
+            begin(from + n);
+            end(from + n);
         }
 
     const float factor = a.scale * kLog2E;       // of scores, to powers of two
@@ -137,10 +138,10 @@ void forward_kernel(Args a) {
     };
 
     constexpr int kLoads = 2 * Rows<S, BN, W, DIRECT>::kCalls;
-    if (steps > 0) {
-        if constexpr (DIRECT) arrived_but<kLoads>(min(LEAD - 1, steps - 1));
+    if (from < steps) {
+        if constexpr (DIRECT) arrived_but<kLoads>(min(LEAD - 1, steps - 1 - from));
         meet();
-        rows_product<S, NB, N>(buffer(0), places, q, x);
+        rows_product<S, NB, N>(buffer(from), places, q, x);
     }
     // (two loops: a branch between the two forms in one would keep a second set of sums)
     const auto walk = [&](int& step, int to, auto masked) __attribute__((always_inline)) {
@@ -169,7 +170,7 @@ void forward_kernel(Args a) {
             if (step + LEAD < steps) end(step + LEAD);
         }
     };
-    int step = 0;
+    int step = from;
     walk(step, whole_steps, Type<0>{});
     walk(step, steps, Type<1>{});
 
@@ -179,24 +180,77 @@ void forward_kernel(Args a) {
         const int64_t row = seq.q0 + i;
         const float total = halves_sum(l[n]);
         const float to_one = total == 0.f ? 0.f : 1.f / total;
-        store_columns<S>(o[n], to_one, a.out.data + row * a.out.ld + col, i <= last, D);
-        if (a.lse && i <= last && half == 0)
-            a.lse[at.head * a.Tq + row] = total == 0.f ? -__builtin_inff() : (base[n] + __builtin_amdgcn_logf(total)) * kLn2;
-        l[n] = to_one;
+        if (splits == 1) {
+            store_columns<S>(o[n], to_one, a.out.data + row * a.out.ld + col, i <= last, D);
+            if (a.lse && i <= last && half == 0)
+                a.lse[at.head * a.Tq + row] = total == 0.f ? -__builtin_inff() : (base[n] + __builtin_amdgcn_logf(total)) * kLn2;
+            l[n] = to_one;
+        } else {
+            const int64_t rows = a.heads * a.Tq, part = split * rows + at.head * a.Tq + row;
+            store_part<S>(o[n], a.parts + part * part_row(D), i <= last, D);
+            if (i <= last && half == 0) {
+                float* const stats = a.parts + splits * rows * part_row(D) + part;
+                stats[0] = base[n];
+                stats[splits * rows] = total;
+            }
+            l[n] = 1.f;
+        }
     }
     if (steps > whole_steps && odd) {
         stored();
-        for (int j = whole_steps * BN; j < wave_upto; ++j) {
+        for (int j = whole_steps * BN; j < min(wave_upto, steps * BN); ++j) {
             const char *const value = values + j * a.v.ld, *const key = keys + j * a.k.ld;
             if (!row_is_odd<S>(value, D)) continue;
 #pragma unroll
             for (int n = 0; n < N; ++n) {
                 const int i = w0 + n * kSide + lane % kSide;
                 const float score = slow_dot<S>(queries + (i < last ? i : last) * a.q.ld, key, D);
-                if (i <= last && j < own[n])
-                    add_odd<S>(a.out.data + (seq.q0 + i) * a.out.ld + col, value, D, power2(fmaf(score, factor, -base[n])) * l[n]);
+                const float weight = power2(fmaf(score, factor, -base[n])) * l[n];
+                if (i > last || j >= own[n]) continue;
+                const int64_t row = seq.q0 + i;
+                if (splits == 1) add_odd<S>(a.out.data + row * a.out.ld + col, value, D, weight);
+                else add_odd<S, DETO_F32>(a.parts + ((int64_t{split} * a.heads + at.head) * a.Tq + row) * part_row(D), value, D, weight);
             }
         }
+    }
+}
+
+// A tile's queries out of what the splits left of them: a wavefront for each, its lanes two features each
+// (a workgroup for every W of the 32 W queries).
+template <class S, int W>
+__global__ __launch_bounds__(W * kLanes) void join_kernel(Args a, int splits) {
+    constexpr int BM = W * kSide;
+    Place at;
+    if (!place_of(a, a.q_starts, a.Tq, BM, a.heads, a.causal, at)) return;
+    const Sequence seq = sequence_of(a, at.s);
+    const int D = a.head_dim, P = part_row(D), lane = threadIdx.x % kLanes;
+    const int64_t rows = a.heads * a.Tq;
+    const int i = at.tile * BM + blockIdx.y * W + threadIdx.x / kLanes;
+    if (i < seq.Lq) {
+        const int64_t row = at.head * a.Tq + seq.q0 + i;
+        const float* const bases = a.parts + splits * rows * P + row;
+        // a lane looks at one split's base and sum (there are at most 32)
+        const bool own = lane < splits;
+        const float base = own ? bases[lane * rows] : -__builtin_inff(), sum = own ? bases[(splits + lane) * rows] : 0.f;
+        float top = base;
+#pragma unroll
+        for (int by = 1; by < kLanes; by *= 2) top = fmaxf(top, __shfl_xor(top, by));
+        const float less = sum == 0.f ? 0.f : power2(base - top);          // (of a part that the query sees nothing of: 0)
+        const float total = wave_sum(sum * less);
+        const float* const part = a.parts + row * P + 2 * (2 * lane < D ? lane : 0);
+        float x = 0.f, y = 0.f;
+#pragma unroll 8
+        for (int s = 0; s < splits; ++s) {
+            const f32x2 v = *reinterpret_cast<const f32x2*>(part + s * rows * P);
+            const float w = __shfl(less, s);
+            x += w == 0.f ? 0.f : v.x * w;
+            y += w == 0.f ? 0.f : v.y * w;
+        }
+        const float to_one = total == 0.f ? 0.f : 1.f / total;
+        char* const out = a.out.data + (seq.q0 + i) * a.out.ld + int64_t{at.head} * D * S::kElem;
+        if (2 * lane < D) store1<S::DT>(out, 2 * lane, x * to_one);
+        if (2 * lane + 1 < D) store1<S::DT>(out, 2 * lane + 1, y * to_one);
+        if (a.lse && lane == 0) a.lse[row] = total == 0.f ? -__builtin_inff() : (top + __builtin_amdgcn_logf(total)) * kLn2;
     }
 }
 
@@ -255,7 +309,8 @@ extern "C" {
 
 int64_t detonation_attention_workspace(const deto_attention* cfg, int64_t Tq, int64_t Tk) {
     if (check(cfg, Tq, Tk) != DETO_OK) return -1;
-    return 2 * cfg->heads * Tq * static_cast<int64_t>(sizeof(float));
+    // (fp32 is cut into at least as many parts as the others)
+    return (stats_floats(cfg, Tq) + part_floats(cfg, Tq, splits_of(cfg, Tq, Tk, true))) * static_cast<int64_t>(sizeof(float));
 }
 
 int detonation_attention_forward(const deto_attention* cfg, int64_t Tq, int64_t Tk, const deto_rows* q,
@@ -269,26 +324,34 @@ int detonation_attention_forward(const deto_attention* cfg, int64_t Tq, int64_t 
                      check_matrix(cfg, v, Tk, cfg->kv_heads, q->dtype), check_matrix(cfg, out, Tq, cfg->heads, q->dtype));
     if (rc) return rc;
     if (!is_aligned(lse, 4)) return DETO_ERR_ALIGN;
-    (void)workspace;
+    const int splits = splits_of(cfg, Tq, Tk, q->dtype == DETO_F32);
+    if (splits > 1 && !workspace) return DETO_ERR_NULL;
+    if (!is_aligned(workspace, 16)) return DETO_ERR_ALIGN;
     Args a = args_of(cfg, Tq, Tk, q, k, v);
     a.out = matrix_of(out);
     a.lse = lse;
+    a.parts = static_cast<float*>(workspace);
     int planned = DETO_OK;
+    // (8 x 2,048 bf16 rows of 16 heads of 128: eight wavefronts 92 us, four 103; 64 x 197 of 12 heads of 64: 37 and 27)
     const bool wide = Tq * cfg->heads >= int64_t{256} * kCUs;
     fresh();
     by_type(q->dtype, [&](auto dt) {
-        return by_shape<dt.value>(cfg->head_dim, in_pieces(a.k) && in_pieces(a.v), [&](auto shape, auto direct) {
+        return by_shape<dt.value>(cfg->head_dim, in_words(a.k) && in_words(a.v), [&](auto shape, auto direct) {
             using S = decltype(shape);
             const auto run = [&](auto waves, auto blocks) {
                 constexpr int W = waves.value, N = blocks.value;
                 constexpr bool DIRECT = direct.value != 0;
                 if (!plan(a, cfg->q_starts, Tq, W * kSide * N, cfg->heads)) return planned = DETO_ERR_UNSUPPORTED;
-                constexpr int kStep = 2 * kKeys<S::DT> * S::kRow;
-                forward_kernel<S, W, N, DIRECT><<<a.tiles * cfg->heads, W * kLanes, kBuffers<DIRECT> * kStep,
-                                               static_cast<hipStream_t>(stream)>>>(a);
+                constexpr int kStep = 2 * kKeys<S> * S::kRow;
+                const hipStream_t on = static_cast<hipStream_t>(stream);
+                const dim3 grid(a.tiles * cfg->heads, splits);
+                forward_kernel<S, W, N, DIRECT><<<grid, W * kLanes, kBuffers<DIRECT> * kStep, on>>>(a);
+                if (splits > 1) join_kernel<S, W><<<dim3(grid.x, Tq < kSide ? Tq : kSide), W * kLanes, 0, on>>>(a, splits);
                 return 0;
             };
-            if (wide) return run(Type<8>{}, Type<1>{});
+            if constexpr (S::DP == 128) {
+                if (wide) return run(Type<8>{}, Type<1>{});
+            }
             return run(Type<4>{}, Type<1>{});
         });
     });

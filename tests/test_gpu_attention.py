@@ -76,7 +76,8 @@ def even(sequences, length):
     (1, 257, 257, 4, 2, 80, True, 1, 3), (2, 128, 128, 2, 2, 128, True, 0, 0), (1, 5, 300, 2, 1, 128, True, 0, 0),
     (2, 1, 200, 3, 3, 96, True, 7, 1), (1, 300, 5, 2, 2, 64, True, 0, 0), (1, 140, 96, 2, 1, 7, False, 0, 5),
     (2, 64, 192, 8, 1, 32, True, 0, 0), (1, 1, 1100, 2, 2, 64, False, 0, 0), (1, 31, 64, 1, 1, 127, True, 2, 0),
-    (1, 96, 160, 2, 2, 65, False, 0, 0), (1, 200, 200, 1, 1, 33, True, 3, 1)])
+    (1, 96, 160, 2, 2, 65, False, 0, 0), (1, 200, 200, 1, 1, 33, True, 3, 1), (2, 3, 700, 4, 2, 128, True, 0, 0),
+    (1, 150, 1500, 2, 1, 64, True, 0, 0), (1, 1, 2111, 2, 2, 7, True, 1, 1)])
 def test_attention(gpu, dtype, sequences, Lq, Lk, heads, kv_heads, head_dim, causal, pad, offset):
     say(dtype, sequences, Lq, Lk, heads, kv_heads, head_dim, causal)
     c = Case(dtype, even(sequences, Lq), even(sequences, Lk), heads, kv_heads, head_dim, causal, pad, offset, packed=False)
