@@ -46,7 +46,7 @@ constexpr int kAhead = !DIRECT ? 1 : STEP * 4 * (8 / W) <= 144 * 1024 ? 3 : 1;
 
 template <class S, int W, bool DIRECT>
 __global__ __launch_bounds__(W * kLanes) __attribute__((amdgpu_waves_per_eu(kResident<S>, kResident<S>))) void queries_kernel(Args a) {
-    constexpr int DT = S::DT, BM = W * kSide, BN = kKeys<S>, kMatrix = BN * S::kRow, kStep = 2 * kMatrix;
+    constexpr int DT = S::DT, BM = W * kSide, BN = kKeys<S, W>, kMatrix = BN * S::kRow, kStep = 2 * kMatrix;
     constexpr int AHEAD = kAhead<W, kStep, DIRECT>;
     extern __shared__ __align__(16) char lds[];          // AHEAD + 1 steps of keys and values
     __shared__ uint32_t odd;                             // infinities or NaNs among keys that not all queries see
@@ -477,7 +477,7 @@ int detonation_attention_backward(const deto_attention* cfg, int64_t Tq, int64_t
             using S = decltype(shape);
             constexpr bool DIRECT = direct.value != 0;
             const auto queries = [&](auto waves) {
-                constexpr int W = waves.value, kStep = 2 * kKeys<S> * S::kRow;
+                constexpr int W = waves.value, kStep = 2 * kKeys<S, W> * S::kRow;
                 if (!plan(a, cfg->q_starts, Tq, W * kSide, H)) return DETO_ERR_UNSUPPORTED;
                 if (Tq) {
                     const dim3 grid(a.tiles * H, splits);
@@ -494,7 +494,7 @@ int detonation_attention_backward(const deto_attention* cfg, int64_t Tq, int64_t
                 return DETO_OK;
             };
             constexpr bool kWide = S::DP == 128;
-            if constexpr (kWide) planned = Tq * H >= int64_t{256} * kCUs ? queries(Type<8>{}) : queries(Type<4>{});
+            if constexpr (kWide) planned = Tq * H >= int64_t{256} * kCUs && Tq / cfg->sequences >= 2048 ? queries(Type<8>{}) : queries(Type<4>{});
             else planned = queries(Type<4>{});
             if (planned) return planned;
             if constexpr (kWide && kResidentKeys<S> == 2) {

@@ -43,7 +43,7 @@ struct Shape {
 // The wavefronts that a SIMD has registers for: two with 128 features, four with 64 and fewer.
 template <class S> constexpr int kResident = S::DP == 64 && S::DT != DETO_F32 ? 3 : 2;
 // Keys of a step of a walk over keys
-template <class S> constexpr int kKeys = S::DT == DETO_F32 || S::DP == 64 ? 32 : 64;
+template <class S, int W> constexpr int kKeys = S::DT == DETO_F32 || S::DP == 64 || W == 4 ? 32 : 64;
 
 struct Matrix {
     char* data;

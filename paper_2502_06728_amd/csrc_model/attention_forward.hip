@@ -18,7 +18,7 @@ constexpr float kMost = 8192.f;
 template <class S, int W, int N, bool DIRECT>
 __global__ __launch_bounds__(W * kLanes) __attribute__((amdgpu_waves_per_eu(kResident<S>, kResident<S>)))
 void forward_kernel(Args a) {
-    constexpr int DT = S::DT, BM = W * kSide * N, BN = kKeys<S>, kMatrix = BN * S::kRow, kStep = 2 * kMatrix;
+    constexpr int DT = S::DT, BM = W * kSide * N, BN = kKeys<S, W>, kMatrix = BN * S::kRow, kStep = 2 * kMatrix;
     constexpr int LEAD = kLead<DIRECT>, NB = BN / kSide;
     extern __shared__ __align__(16) char lds[];          // steps of keys and values
     __shared__ uint32_t odd;                             // infinities or NaNs among values that not all queries see
@@ -80,57 +80,71 @@ void forward_kernel(Args a) {
     const Places places = places_of<S>();
     f32x16 x[NB][N];                                     // scores of a step, computed in the one before
 
-    // weights of a step's scores, their products with its values, and the next step's scores (the last step's again
-    // behind it: a branch here would keep the three from sharing the time)
-    const auto compute = [&](int step) __attribute__((always_inline)) {
-        f32x16 next[NB][N], p[NB][N];
-        rows_product<S, NB, N>(buffer(step + 1 < steps ? step + 1 : step), places, q, next);
-        float sum[N];
-        bool high = false;
+    const auto hide = [&](int step) __attribute__((always_inline)) {
 #pragma unroll
         for (int n = 0; n < N; ++n) {
-            sum[n] = 0.f;
+            const int left = own[n] - step * BN - half * 4;         // of the keys that the query sees
 #pragma unroll
             for (int b = 0; b < NB; ++b)
 #pragma unroll
-                for (int r = 0; r < 16; ++r) {
-                    p[b][n][r] = power2(fmaf(x[b][n][r], factor, -base[n]));
-                    sum[n] += p[b][n][r];
-                }
-            high |= !(sum[n] <= kMost);                  // (or none yet)
+                for (int r = 0; r < 16; ++r)
+                    x[b][n][r] = b * kSide + (r / 4) * 8 + r % 4 < left ? x[b][n][r] : -__builtin_inff();
         }
-        if (__any(high)) {
+    };
+    // scores into weights, and their sum
+    const auto weigh = [&](int n, float from) __attribute__((always_inline)) {
+        float sum = 0.f;
+#pragma unroll
+        for (int b = 0; b < NB; ++b)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+                x[b][n][r] = power2(fmaf(x[b][n][r], factor, -from));
+                sum += x[b][n][r];
+            }
+        return sum;
+    };
+    // weights of a step's scores, their products with its values, and the next step's scores (the last step's again
+    // behind it: a branch here would keep the three from sharing the time)
+    const auto compute = [&](int step, auto masked) __attribute__((always_inline)) {
+        constexpr bool MASKED = masked.value != 0;
+        f32x16 next[NB][N];
+        if (MASKED) hide(step);
+        rows_product<S, NB, N>(buffer(step + 1 < steps ? step + 1 : step), places, q, next);
+        float sum[N];
+        uint64_t high = 0;                               // (or none yet)
+#pragma unroll
+        for (int n = 0; n < N; ++n) {
+            sum[n] = weigh(n, base[n]);
+            high |= __ballot(!(sum[n] <= kMost));
+        }
+        if (high) {
+            rows_product<S, NB, N>(buffer(step), places, q, x);
+            if (MASKED) hide(step);
 #pragma unroll
             for (int n = 0; n < N; ++n) {
-                const uint64_t lanes = __ballot(!(sum[n] <= kMost));
-                if (!((lanes | lanes << kSide | lanes >> kSide) >> lane & 1)) continue;       // (a query's two lanes do the same)
                 float top = -__builtin_inff();
 #pragma unroll
                 for (int b = 0; b < NB; ++b)
 #pragma unroll
                     for (int r = 0; r < 16; ++r) top = fmaxf(top, x[b][n][r]);
-                const float to = fmaxf(base[n], halves_max(top) * factor), less = to > base[n] ? power2(base[n] - to) : 1.f;
-                base[n] = to;
-                const float from = to > -__builtin_inff() ? to : 0.f;
+                top = halves_max(top) * factor;
+                // (a query's two lanes do the same, whatever the others do)
+                const uint64_t lanes = __ballot(!(sum[n] <= kMost));
+                const bool rise = (lanes | lanes << kSide | lanes >> kSide) >> lane & 1 && top > base[n];
+                const float less = rise ? power2(base[n] - top) : 1.f;
+                base[n] = rise ? top : base[n];
                 l[n] *= less;
-                sum[n] = 0.f;
 #pragma unroll
                 for (int b = 0; b < S::kBlocks; ++b)
 #pragma unroll
                     for (int r = 0; r < 16; ++r) o[n][b][r] *= less;
-#pragma unroll
-                for (int b = 0; b < NB; ++b)
-#pragma unroll
-                    for (int r = 0; r < 16; ++r) {
-                        p[b][n][r] = power2(fmaf(x[b][n][r], factor, -from));
-                        sum[n] += p[b][n][r];
-                    }
+                sum[n] = weigh(n, base[n] > -__builtin_inff() ? base[n] : 0.f);
             }
         }
 #pragma unroll
         for (int n = 0; n < N; ++n) l[n] += sum[n];
 #pragma unroll
-        for (int b = 0; b < NB; ++b) columns_product<S, N>(buffer(step) + kMatrix + b * kSide * S::kRow, places, p[b], o);
+        for (int b = 0; b < NB; ++b) columns_product<S, N>(buffer(step) + kMatrix + b * kSide * S::kRow, places, x[b], o);
 #pragma unroll
         for (int b = 0; b < NB; ++b)
 #pragma unroll
@@ -142,6 +156,16 @@ void forward_kernel(Args a) {
         if constexpr (DIRECT) arrived_but<kLoads>(min(LEAD - 1, steps - 1 - from));
         meet();
         rows_product<S, NB, N>(buffer(from), places, q, x);
+#pragma unroll
+        for (int n = 0; n < N; ++n) {                    // what is masked among these makes no base too low
+            float top = x[0][n][0];
+#pragma unroll
+            for (int b = 0; b < NB; ++b)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) top = fmaxf(top, x[b][n][r]);
+            top = halves_max(top) * factor;
+            if (own[n] > 0 && from < whole_steps) base[n] = top;
+        }
     }
     // (two loops: a branch between the two forms in one would keep a second set of sums)
     const auto walk = [&](int& step, int to, auto masked) __attribute__((always_inline)) {
@@ -152,20 +176,9 @@ void forward_kernel(Args a) {
             if constexpr (masked.value != 0) {
                 take_out_odd<S, BN, W>(buffer(step) + kMatrix, &odd);
                 meet();
-                if (step * BN < wave_upto) {
-#pragma unroll
-                    for (int n = 0; n < N; ++n) {
-                        const int left = own[n] - step * BN - half * 4;         // of the keys that the query sees
-#pragma unroll
-                        for (int b = 0; b < NB; ++b)
-#pragma unroll
-                            for (int r = 0; r < 16; ++r)
-                                x[b][n][r] = b * kSide + (r / 4) * 8 + r % 4 < left ? x[b][n][r] : -__builtin_inff();
-                    }
-                    compute(step);
-                }
+                if (step * BN < wave_upto) compute(step, masked);
             } else {
-                compute(step);
+                compute(step, masked);
             }
             if (step + LEAD < steps) end(step + LEAD);
         }
@@ -333,7 +346,7 @@ int detonation_attention_forward(const deto_attention* cfg, int64_t Tq, int64_t 
     a.parts = static_cast<float*>(workspace);
     int planned = DETO_OK;
     // (8 x 2,048 bf16 rows of 16 heads of 128: eight wavefronts 92 us, four 103; 64 x 197 of 12 heads of 64: 37 and 27)
-    const bool wide = Tq * cfg->heads >= int64_t{256} * kCUs;
+    const bool wide = Tq * cfg->heads >= int64_t{256} * kCUs && Tq / cfg->sequences >= 2048;
     fresh();
     by_type(q->dtype, [&](auto dt) {
         return by_shape<dt.value>(cfg->head_dim, in_words(a.k) && in_words(a.v), [&](auto shape, auto direct) {
@@ -342,7 +355,7 @@ int detonation_attention_forward(const deto_attention* cfg, int64_t Tq, int64_t 
                 constexpr int W = waves.value, N = blocks.value;
                 constexpr bool DIRECT = direct.value != 0;
                 if (!plan(a, cfg->q_starts, Tq, W * kSide * N, cfg->heads)) return planned = DETO_ERR_UNSUPPORTED;
-                constexpr int kStep = 2 * kKeys<S> * S::kRow;
+                constexpr int kStep = 2 * kKeys<S, W> * S::kRow;
                 const hipStream_t on = static_cast<hipStream_t>(stream);
                 const dim3 grid(a.tiles * cfg->heads, splits);
                 forward_kernel<S, W, N, DIRECT><<<grid, W * kLanes, kBuffers<DIRECT> * kStep, on>>>(a);
