@@ -62,7 +62,7 @@ __global__ __launch_bounds__(W * kLanes) __attribute__((amdgpu_waves_per_eu(kRes
         const int64_t upto = int64_t{n < last ? n : last} + seq.Lk - last;
         return static_cast<int>(upto < 0 ? 0 : upto);
     };
-    const int upto = seen(i0 + BM - 1), wave_upto = seen(w0 + kSide - 1);
+    const int upto = seen(i0 + BM - 1), wave_upto = w0 > last ? 0 : seen(w0 + kSide - 1);
     const int own = seen(i), all_steps = (upto + BN - 1) / BN, splits = gridDim.y, split = blockIdx.y;
     // of which this workgroup takes one part
     const int from = static_cast<int>(int64_t{all_steps} * split / splits), steps = static_cast<int>(int64_t{all_steps} * (split + 1) / splits);
@@ -133,10 +133,8 @@ __global__ __launch_bounds__(W * kLanes) __attribute__((amdgpu_waves_per_eu(kRes
             if constexpr (masked.value != 0) {
                 take_out_odd<S, BN, W>(buffer(step), &odd);
                 meet();
-                if (step * BN < wave_upto) compute(step, masked);
-            } else {
-                compute(step, masked);
             }
+            if (step * BN < wave_upto) compute(step, masked);
             if (step + AHEAD < steps) end(step + AHEAD);
         }
     };
@@ -255,7 +253,7 @@ __global__ __launch_bounds__(W * kLanes) __attribute__((amdgpu_waves_per_eu(kRes
     };
     const int first_step = seen_from(j0) / BQ, steps = (seq.Lq + BQ - 1) / BQ - first_step;    // of a head
     const int all_from = seen_from(j0 + BN - 1);                 // from here on queries see all of these keys
-    const int wave_from = seen_from(j0 + own_block * kSide), own = seen_from(j);
+    const int wave_from = j0 + own_block * kSide > last ? seq.Lq + BQ : seen_from(j0 + own_block * kSide), own = seen_from(j);
     const int total = steps * (a.group / HEADS);                 // those of the first heads, then of the next ones
 
     const int64_t kv = int64_t{at.head} * D * S::kElem, row = seq.k0 + (there ? j : last);
@@ -376,10 +374,8 @@ __global__ __launch_bounds__(W * kLanes) __attribute__((amdgpu_waves_per_eu(kRes
             if constexpr (MASKED) {
                 take_out_odd<S, 2 * HEADS * BQ, W>(lds + now.buffer * kStep, &odd);
                 meet();
-                if (now.query + BQ > wave_from) compute(now, masked);
-            } else {
-                compute(now, masked);
             }
+            if (now.query + BQ > wave_from) compute(now, masked);
             if (more) {
                 end(ahead);
                 ahead = next(ahead);

@@ -577,7 +577,7 @@ inline Matrix matrix_of(const deto_rows* m) {
 }
 
 // Into how many parts the walks over keys are cut.  Where fewer workgroups than CUs would walk over many keys, a second
-// launch that adds up what parts of 64 keys leave costs less than the rest of the walk.  (Sequences of equal length are
+// launch that adds up what parts of 64 (fp32: 32) keys leave costs less than the rest of the walk.  (Sequences of equal length are
 // assumed; the parts are equal shares of each tile's own walk, whatever its length.)  fp32 steps take longer: it is cut
 // from 128 keys on, 16-bit types from 512 on.
 inline int splits_of(const deto_attention* cfg, int64_t Tq, int64_t Tk, bool f32) {
@@ -586,8 +586,8 @@ inline int splits_of(const deto_attention* cfg, int64_t Tq, int64_t Tk, bool f32
     const int64_t groups = cfg->heads * ((Tq + 127) / 128 > queried ? (Tq + 127) / 128 : queried);
     const int64_t keys = Tk / (cfg->sequences < Tk ? cfg->sequences : Tk);
     if (groups >= kCUs || keys < (f32 ? 128 : 512)) return 1;
-    int64_t n = 2 * kCUs / groups;
-    n = n < keys / 64 ? n : keys / 64;
+    int64_t n = (f32 ? 4 : 2) * kCUs / groups;
+    n = n < keys / (f32 ? 32 : 64) ? n : keys / (f32 ? 32 : 64);
     return static_cast<int>(n < 32 ? n : 32);
 }
 inline int64_t stats_floats(const deto_attention* cfg, int64_t Tq) {        // of the backward pass, to whole pieces

@@ -34,7 +34,7 @@ void forward_kernel(Args a) {
         const int64_t upto = int64_t{n < last ? n : last} + seq.Lk - last;
         return static_cast<int>(upto < 0 ? 0 : upto);
     };
-    const int upto = seen(i0 + BM - 1), wave_upto = seen(w0 + kSide * N - 1);        // by any of the workgroup's, the wavefront's
+    const int upto = seen(i0 + BM - 1), wave_upto = w0 > last ? 0 : seen(w0 + kSide * N - 1);        // by any of the workgroup's, the wavefront's
     const int all_steps = (upto + BN - 1) / BN, splits = gridDim.y, split = blockIdx.y;
     // of which this workgroup takes one part
     const int from = static_cast<int>(int64_t{all_steps} * split / splits), steps = static_cast<int>(int64_t{all_steps} * (split + 1) / splits);
@@ -176,10 +176,8 @@ void forward_kernel(Args a) {
             if constexpr (masked.value != 0) {
                 take_out_odd<S, BN, W>(buffer(step) + kMatrix, &odd);
                 meet();
-                if (step * BN < wave_upto) compute(step, masked);
-            } else {
-                compute(step, masked);
             }
+            if (step * BN < wave_upto) compute(step, masked);
             if (step + LEAD < steps) end(step + LEAD);
         }
     };
@@ -228,43 +226,46 @@ void forward_kernel(Args a) {
     }
 }
 
-// A tile's queries out of what the splits left of them: a wavefront for each, its lanes two features each
-// (a workgroup for every W of the 32 W queries).
-template <class S, int W>
-__global__ __launch_bounds__(W * kLanes) void join_kernel(Args a, int splits) {
-    constexpr int BM = W * kSide;
+// Queries out of what the splits left of them: a wavefront for each of a tile, its lanes two features each.
+constexpr int kJoinWaves = 4;
+
+template <class S, int BM>
+__global__ __launch_bounds__(kJoinWaves * kLanes) void join_kernel(Args a, int splits) {
     Place at;
     if (!place_of(a, a.q_starts, a.Tq, BM, a.heads, a.causal, at)) return;
     const Sequence seq = sequence_of(a, at.s);
+    const int i = at.tile * BM + blockIdx.y * kJoinWaves + threadIdx.x / kLanes;
+    if (i >= seq.Lq) return;
     const int D = a.head_dim, P = part_row(D), lane = threadIdx.x % kLanes;
-    const int64_t rows = a.heads * a.Tq;
-    const int i = at.tile * BM + blockIdx.y * W + threadIdx.x / kLanes;
-    if (i < seq.Lq) {
-        const int64_t row = at.head * a.Tq + seq.q0 + i;
-        const float* const bases = a.parts + splits * rows * P + row;
-        // a lane looks at one split's base and sum (there are at most 32)
-        const bool own = lane < splits;
-        const float base = own ? bases[lane * rows] : -__builtin_inff(), sum = own ? bases[(splits + lane) * rows] : 0.f;
-        float top = base;
+    const int64_t rows = a.heads * a.Tq, row = at.head * a.Tq + seq.q0 + i;
+    const float* const bases = a.parts + splits * rows * P + row;
+    // a lane looks at one split's base and sum (there are at most 32)
+    const bool own = lane < splits;
+    const float base = own ? bases[lane * rows] : -__builtin_inff(), sum = own ? bases[(splits + lane) * rows] : 0.f;
+    float top = base;
 #pragma unroll
-        for (int by = 1; by < kLanes; by *= 2) top = fmaxf(top, __shfl_xor(top, by));
-        const float less = sum == 0.f ? 0.f : power2(base - top);          // (of a part that the query sees nothing of: 0)
-        const float total = wave_sum(sum * less);
-        const float* const part = a.parts + row * P + 2 * (2 * lane < D ? lane : 0);
-        float x = 0.f, y = 0.f;
-#pragma unroll 8
-        for (int s = 0; s < splits; ++s) {
-            const f32x2 v = *reinterpret_cast<const f32x2*>(part + s * rows * P);
-            const float w = __shfl(less, s);
-            x += w == 0.f ? 0.f : v.x * w;
-            y += w == 0.f ? 0.f : v.y * w;
+    for (int by = 1; by < kLanes; by *= 2) top = fmaxf(top, __shfl_xor(top, by));
+    const float less = sum == 0.f ? 0.f : power2(base - top);          // (of a part that the query sees nothing of: 0)
+    const float total = wave_sum(sum * less);
+    const float* const part = a.parts + row * P + 2 * (2 * lane < D ? lane : 0);
+    float x = 0.f, y = 0.f;
+    constexpr int kOnce = 16;                                           // splits' loads in flight
+    for (int first = 0; first < splits; first += kOnce) {
+        f32x2 v[kOnce];
+#pragma unroll
+        for (int n = 0; n < kOnce; ++n) v[n] = *reinterpret_cast<const f32x2*>(part + min(first + n, splits - 1) * rows * P);
+#pragma unroll
+        for (int n = 0; n < kOnce; ++n) {
+            const float w = __shfl(less, first + n);                    // (0 behind the last one)
+            x += w == 0.f ? 0.f : v[n].x * w;
+            y += w == 0.f ? 0.f : v[n].y * w;
         }
-        const float to_one = total == 0.f ? 0.f : 1.f / total;
-        char* const out = a.out.data + (seq.q0 + i) * a.out.ld + int64_t{at.head} * D * S::kElem;
-        if (2 * lane < D) store1<S::DT>(out, 2 * lane, x * to_one);
-        if (2 * lane + 1 < D) store1<S::DT>(out, 2 * lane + 1, y * to_one);
-        if (a.lse && lane == 0) a.lse[row] = total == 0.f ? -__builtin_inff() : (top + __builtin_amdgcn_logf(total)) * kLn2;
     }
+    const float to_one = total == 0.f ? 0.f : 1.f / total;
+    char* const out = a.out.data + (seq.q0 + i) * a.out.ld + int64_t{at.head} * D * S::kElem;
+    if (2 * lane < D) store1<S::DT>(out, 2 * lane, x * to_one);
+    if (2 * lane + 1 < D) store1<S::DT>(out, 2 * lane + 1, y * to_one);
+    if (a.lse && lane == 0) a.lse[row] = total == 0.f ? -__builtin_inff() : (top + __builtin_amdgcn_logf(total)) * kLn2;
 }
 
 }  // namespace
@@ -359,7 +360,11 @@ int detonation_attention_forward(const deto_attention* cfg, int64_t Tq, int64_t 
                 const hipStream_t on = static_cast<hipStream_t>(stream);
                 const dim3 grid(a.tiles * cfg->heads, splits);
                 forward_kernel<S, W, N, DIRECT><<<grid, W * kLanes, kBuffers<DIRECT> * kStep, on>>>(a);
-                if (splits > 1) join_kernel<S, W><<<dim3(grid.x, Tq < kSide ? Tq : kSide), W * kLanes, 0, on>>>(a, splits);
+                if (splits > 1) {
+                    constexpr int BM = W * kSide * N;
+                    const unsigned of_tile = (min(int64_t{BM}, Tq) + kJoinWaves - 1) / kJoinWaves;
+                    join_kernel<S, BM><<<dim3(grid.x, of_tile), kJoinWaves * kLanes, 0, on>>>(a, splits);
+                }
                 return 0;
             };
             if constexpr (S::DP == 128) {
