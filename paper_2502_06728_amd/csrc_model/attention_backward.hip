@@ -11,6 +11,25 @@ namespace attention {
 namespace {
 
 // ---- dq: the forward kernel's walk.
+//
+// `out` is rounded, and dout . out with it, by as much as 2^-9 of |dout| |out| in bf16: more than ds may be where a query
+// sees few keys, or one outweighs the others.  What is missing is the sum of a query's ds, since its p are 1 together.  So
+// the gradients of keys get the sum back with dout . out; those of queries take it times the sum of p k back in the end.
+//   kMean    that sum is a second one of as many registers, out of the same reads of LDS
+//   kTwice   no room for it (128 features): what ds loses by rounding is multiplied too, which takes away as much of the
+//            error where a query sees many keys (errors of dq over 2,048 keys, bf16: neither 2.7e-3, kTwice 2.2e-3, kMean
+//            2.4e-3, rounding dq alone 1.7e-3; over two keys 6.1e-3, 6.3e-3, 2.4e-3)
+//   kPlain   fp32
+enum Form { kPlain, kMean, kTwice };
+// fewer keys a sequence take kMean for every type
+constexpr int64_t kFewKeys = 512;
+
+template <int DT>
+__device__ __forceinline__ float rounded(float v) {
+    if constexpr (DT == DETO_BF16) return bits_f32(pack_bf16(v, 0.f) << 16);
+    else return static_cast<float>(static_cast<_Float16>(v));
+}
+
 // A query's lse in powers of two; one that sees nothing gets weights of zero.
 __device__ __forceinline__ float stored_lse(float lse) {
     return lse == -__builtin_inff() ? __builtin_inff() : lse * kLog2E;
@@ -44,7 +63,7 @@ __device__ __forceinline__ float rows_dot(const u32x4 (&x)[S::kFrags], const u32
 template <int W, int STEP, bool DIRECT>
 constexpr int kAhead = !DIRECT ? 1 : STEP * 4 * (8 / W) <= 144 * 1024 ? 3 : 1;
 
-template <class S, int W, bool DIRECT>
+template <class S, int W, int FORM, bool DIRECT>
 __global__ __launch_bounds__(W * kLanes) __attribute__((amdgpu_waves_per_eu(kResident<S>, kResident<S>))) void queries_kernel(Args a) {
     constexpr int DT = S::DT, BM = W * kSide, BN = kKeys<S, W>, kMatrix = BN * S::kRow, kStep = 2 * kMatrix;
     constexpr int AHEAD = kAhead<W, kStep, DIRECT>;
@@ -53,7 +72,7 @@ __global__ __launch_bounds__(W * kLanes) __attribute__((amdgpu_waves_per_eu(kRes
     Place at;
     if (!place_of(a, a.q_starts, a.Tq, BM, a.heads, a.causal, at)) return;
     const Sequence seq = sequence_of(a, at.s);
-    const int D = DIRECT ? S::DP : a.head_dim, lane = threadIdx.x % kLanes, half = lane / kSide;
+    const int D = a.head_dim, lane = threadIdx.x % kLanes, half = lane / kSide;
     const int i0 = at.tile * BM, w0 = i0 + uniform(static_cast<int32_t>(threadIdx.x / kLanes)) * kSide, i = w0 + lane % kSide, last = seq.Lq - 1;
     const bool there = i <= last;
 
@@ -87,6 +106,7 @@ __global__ __launch_bounds__(W * kLanes) __attribute__((amdgpu_waves_per_eu(kRes
         rv.end(buffer(step) + kMatrix);
     };
     if (threadIdx.x == 0) odd = 0;
+    if constexpr (DIRECT) clear<S, W>(lds, (AHEAD + 1) * kStep, D);
 #pragma unroll
     for (int n = 0; n < AHEAD; ++n)
         if (from + n < steps) begin(from + n);
@@ -94,16 +114,17 @@ __global__ __launch_bounds__(W * kLanes) __attribute__((amdgpu_waves_per_eu(kRes
 
     const float factor = a.scale * kLog2E;
     u32x4 q[1][S::kFrags], g[1][S::kFrags];
-    load_row<S>(grad, there, D, g[0]);
-    load_row<S>(a.out.data + row * a.out.ld + col, there, D, q[0]);
+    load_row<S, DIRECT>(grad, there, D, g[0]);
+    load_row<S, DIRECT>(a.out.data + row * a.out.ld + col, there, D, q[0]);
     const float lse = there ? stored_lse(a.lse[at.head * a.Tq + row]) : __builtin_inff();
     const float delta = rows_dot<S>(g[0], q[0]);
     if (there && half == 0 && split == 0) {
         a.stats[at.head * a.Tq + row] = lse;
         a.stats[(a.heads + at.head) * a.Tq + row] = delta;
     }
-    load_row<S>(query, there, D, q[0]);
-    f32x16 dq[1][S::kBlocks] = {};
+    load_row<S, DIRECT>(query, there, D, q[0]);
+    f32x16 dq[1][S::kBlocks] = {}, mean[FORM == kMean ? S::kBlocks : 1] = {};
+    float rest = 0.f;
 
     const Places places = places_of<S>();
     const auto compute = [&](int step, auto masked) __attribute__((always_inline)) {
@@ -117,10 +138,22 @@ __global__ __launch_bounds__(W * kLanes) __attribute__((amdgpu_waves_per_eu(kRes
             rows_product<S, 1, 1>(from + kMatrix + b * kSide * S::kRow, places, g, y);
 #pragma unroll
             for (int r = 0; r < 16; ++r) {
-                x[0][0][r] = power2(fmaf(x[0][0][r], factor, -lse)) * (y[0][0][r] - delta);
+                x[0][0][r] = power2(fmaf(x[0][0][r], factor, -lse));
                 if (MASKED) x[0][0][r] = b * kSide + (r / 4) * 8 + r % 4 < left ? x[0][0][r] : 0.f;
+                y[0][0][r] = x[0][0][r] * (y[0][0][r] - delta);
+                if (MASKED) y[0][0][r] = b * kSide + (r / 4) * 8 + r % 4 < left ? y[0][0][r] : 0.f;
+                if (FORM != kPlain) rest += y[0][0][r];
             }
-            columns_product<S, 1>(from + b * kSide * S::kRow, places, x[0], dq);
+            if constexpr (FORM == kMean) {
+                columns_products<S>(from + b * kSide * S::kRow, places, y[0][0], x[0][0], dq[0], mean);
+            } else if constexpr (FORM == kTwice) {
+                // (what is left of ds takes the place of p)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) x[0][0][r] = y[0][0][r] - rounded<DT>(y[0][0][r]);
+                columns_products<S>(from + b * kSide * S::kRow, places, y[0][0], x[0][0], dq[0], dq[0]);
+            } else {
+                columns_product<S, 1>(from + b * kSide * S::kRow, places, y[0], dq);
+            }
         }
     };
 
@@ -143,6 +176,21 @@ __global__ __launch_bounds__(W * kLanes) __attribute__((amdgpu_waves_per_eu(kRes
     walk(step, steps, Type<1>{});
 
     float* const part = a.parts + ((int64_t{split} * a.heads + at.head) * a.Tq + row) * part_row(D);
+    if constexpr (FORM != kPlain) {
+        rest = halves_sum(rest);
+        if (splits > 1) {
+            if constexpr (FORM == kMean) store_part<S>(mean, part + splits * a.heads * a.Tq * part_row(D), there, D);
+            if (there && half == 0) a.parts[(2 * splits * part_row(D) + split) * a.heads * a.Tq + at.head * a.Tq + row] = rest;
+        } else {
+            if constexpr (FORM == kMean) {
+#pragma unroll
+                for (int b = 0; b < S::kBlocks; ++b)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) dq[0][b][r] -= rest * mean[b][r];
+            }
+            if (there && half == 0) a.stats[(a.heads + at.head) * a.Tq + row] = delta + rest;
+        }
+    }
     if (splits == 1) store_columns<S>(dq[0], a.scale, a.dq.data + row * a.dq.ld + col, there, D);
     else store_part<S>(dq[0], part, there, D);
     if (steps > whole_steps && odd) {
@@ -160,28 +208,38 @@ __global__ __launch_bounds__(W * kLanes) __attribute__((amdgpu_waves_per_eu(kRes
 }
 
 // A tile's rows of dq out of what the splits left: a wavefront for each, its lanes two features each.
-template <class S, int W>
+template <class S, int W, int FORM>
 __global__ __launch_bounds__(W * kLanes) void join_kernel(Args a, int splits) {
     constexpr int BM = W * kSide;
     Place at;
     if (!place_of(a, a.q_starts, a.Tq, BM, a.heads, a.causal, at)) return;
     const Sequence seq = sequence_of(a, at.s);
-    const int D = a.head_dim, P = part_row(D), lane = threadIdx.x % kLanes;
-    if (2 * lane >= D) return;
     const int i = at.tile * BM + blockIdx.y * W + threadIdx.x / kLanes;
-    if (i < seq.Lq) {
-        const float* const part = a.parts + (at.head * a.Tq + seq.q0 + i) * P + 2 * lane;
-        float x = 0.f, y = 0.f;
+    if (i >= seq.Lq) return;
+    const int D = a.head_dim, P = part_row(D), lane = threadIdx.x % kLanes;
+    const int64_t rows = a.heads * a.Tq, row = at.head * a.Tq + seq.q0 + i;
+    const float* const part = a.parts + row * P + 2 * (2 * lane < D ? lane : 0);
+    f32x2 x = {0.f, 0.f}, mean = {0.f, 0.f};
 #pragma unroll 8
-        for (int s = 0; s < splits; ++s) {
-            const f32x2 v = *reinterpret_cast<const f32x2*>(part + s * a.heads * a.Tq * P);
-            x += v.x;
-            y += v.y;
+    for (int s = 0; s < splits; ++s) {
+        const f32x2 v = *reinterpret_cast<const f32x2*>(part + s * rows * P);
+        x.x += v.x;
+        x.y += v.y;
+        if constexpr (FORM == kMean) {
+            const f32x2 m = *reinterpret_cast<const f32x2*>(part + (splits + s) * rows * P);
+            mean.x += m.x;
+            mean.y += m.y;
         }
-        char* const dq = a.dq.data + (seq.q0 + i) * a.dq.ld + int64_t{at.head} * D * S::kElem;
-        store1<S::DT>(dq, 2 * lane, x * a.scale);
-        if (2 * lane + 1 < D) store1<S::DT>(dq, 2 * lane + 1, y * a.scale);
     }
+    if constexpr (FORM != kPlain) {
+        const float rest = wave_sum(lane < splits ? a.parts[(2 * splits * P + lane) * rows + row] : 0.f);    // (at most 32)
+        x.x -= rest * mean.x;
+        x.y -= rest * mean.y;
+        if (lane == 0) a.stats[rows + row] += rest;
+    }
+    char* const dq = a.dq.data + (seq.q0 + i) * a.dq.ld + int64_t{at.head} * D * S::kElem;
+    if (2 * lane < D) store1<S::DT>(dq, 2 * lane, x.x * a.scale);
+    if (2 * lane + 1 < D) store1<S::DT>(dq, 2 * lane + 1, x.y * a.scale);
 }
 
 // ---- dk, dv
@@ -199,8 +257,7 @@ template <class S, int BLOCKS, int HEADS>
 __device__ __forceinline__ void add_heads(char* lds, const f32x16 (&c)[S::kBlocks], int own_block, int own_head, float factor,
                                           char* row, bool there, int D) {
     typedef float f32x4 __attribute__((ext_vector_type(4)));
-    static_assert(S::kBlocks % HEADS == 0, "");
-    constexpr int kSums = S::kBlocks * 16 * kLanes * 4;          // bytes of a wavefront's
+        constexpr int kSums = S::kBlocks * 16 * kLanes * 4;          // bytes of a wavefront's
     const int lane = threadIdx.x % kLanes;
     f32x4* const own = reinterpret_cast<f32x4*>(lds + (own_head * BLOCKS + own_block) * kSums) + lane;
     __syncthreads();
@@ -211,8 +268,9 @@ __device__ __forceinline__ void add_heads(char* lds, const f32x16 (&c)[S::kBlock
             own[(4 * b + g) * kLanes] = f32x4{c[b][4 * g], c[b][4 * g + 1], c[b][4 * g + 2], c[b][4 * g + 3]};
     __syncthreads();
 #pragma unroll
-    for (int n = 0; n < S::kBlocks / HEADS; ++n) {
+    for (int n = 0; n < (S::kBlocks + HEADS - 1) / HEADS; ++n) {
         const int b = n * HEADS + own_head;
+        if (b >= S::kBlocks) continue;
         f32x16 sum = {};
 #pragma unroll
         for (int h = 0; h < HEADS; ++h) {
@@ -239,7 +297,7 @@ __global__ __launch_bounds__(W * kLanes) __attribute__((amdgpu_waves_per_eu(kRes
     Place at;
     if (!place_of(a, a.k_starts, a.Tk, BN, a.kv_heads, false, at)) return;
     const Sequence seq = sequence_of(a, at.s);
-    const int D = DIRECT ? S::DP : a.head_dim, lane = threadIdx.x % kLanes, half = lane / kSide;
+    const int D = a.head_dim, lane = threadIdx.x % kLanes, half = lane / kSide;
     const int wave = uniform(static_cast<int32_t>(threadIdx.x / kLanes)), own_block = wave % BLOCKS, own_head = wave / BLOCKS;
     const int j0 = at.tile * BN, j = j0 + own_block * kSide + lane % kSide;
     const int last = seq.Lk - 1;
@@ -308,6 +366,7 @@ __global__ __launch_bounds__(W * kLanes) __attribute__((amdgpu_waves_per_eu(kRes
         }
     };
     if (threadIdx.x == 0) odd = 0;
+    if constexpr (DIRECT) clear<S, W>(lds, (AHEAD + 1) * kStep + (STAY ? BN * S::kRow : 0), D);
     if constexpr (STAY) {
         Rows<S, BN, W, DIRECT> rv(a.v.ld);
         rv.begin(lds + (AHEAD + 1) * kStep, a.v.data + (seq.k0 + j0) * a.v.ld + kv, a.v.ld, last - j0 < BN ? last - j0 + 1 : BN, D);
@@ -326,8 +385,8 @@ __global__ __launch_bounds__(W * kLanes) __attribute__((amdgpu_waves_per_eu(kRes
     }
 
     u32x4 k[1][S::kFrags], v[1][STAY ? 1 : S::kFrags];
-    load_row<S>(key, there, D, k[0]);
-    if constexpr (!STAY) load_row<S>(value, there, D, v[0]);
+    load_row<S, DIRECT>(key, there, D, k[0]);
+    if constexpr (!STAY) load_row<S, DIRECT>(value, there, D, v[0]);
     const float factor = a.scale * kLog2E;
     f32x16 dk[1][S::kBlocks] = {}, dv[1][S::kBlocks] = {};
 
@@ -472,13 +531,13 @@ int detonation_attention_backward(const deto_attention* cfg, int64_t Tq, int64_t
                                   [&](auto shape, auto direct) {
             using S = decltype(shape);
             constexpr bool DIRECT = direct.value != 0;
-            const auto queries = [&](auto waves) {
-                constexpr int W = waves.value, kStep = 2 * kKeys<S, W> * S::kRow;
+            const auto queries = [&](auto waves, auto form) {
+                constexpr int W = waves.value, FORM = form.value, kStep = 2 * kKeys<S, W> * S::kRow;
                 if (!plan(a, cfg->q_starts, Tq, W * kSide, H)) return DETO_ERR_UNSUPPORTED;
                 if (Tq) {
                     const dim3 grid(a.tiles * H, splits);
-                    queries_kernel<S, W, DIRECT><<<grid, W * kLanes, (kAhead<W, kStep, DIRECT> + 1) * kStep, on>>>(a);
-                    if (splits > 1) join_kernel<S, W><<<dim3(grid.x, kSide), W * kLanes, 0, on>>>(a, splits);
+                    queries_kernel<S, W, FORM, DIRECT><<<grid, W * kLanes, (kAhead<W, kStep, DIRECT> + 1) * kStep, on>>>(a);
+                    if (splits > 1) join_kernel<S, W, FORM><<<dim3(grid.x, kSide), W * kLanes, 0, on>>>(a, splits);
                 }
                 return DETO_OK;
             };
@@ -490,8 +549,21 @@ int detonation_attention_backward(const deto_attention* cfg, int64_t Tq, int64_t
                 return DETO_OK;
             };
             constexpr bool kWide = S::DP == 128;
-            if constexpr (kWide) planned = Tq * H >= int64_t{256} * kCUs && Tq / cfg->sequences >= 2048 ? queries(Type<8>{}) : queries(Type<4>{});
-            else planned = queries(Type<4>{});
+            const bool wide = kWide && Tq * H >= int64_t{256} * kCUs && Tq / cfg->sequences >= 2048;
+            const auto by_waves = [&](auto form) {
+                if constexpr (kWide) {
+                    if (wide) return queries(Type<8>{}, form);
+                }
+                return queries(Type<4>{}, form);
+            };
+            const bool few = Tk / cfg->sequences < kFewKeys;
+            if constexpr (S::DT == DETO_F32) {
+                planned = few ? queries(Type<4>{}, Type<kMean>{}) : by_waves(Type<kPlain>{});
+            } else if constexpr (S::DU == 128) {
+                planned = few ? queries(Type<4>{}, Type<kMean>{}) : by_waves(Type<kTwice>{});
+            } else {
+                planned = by_waves(Type<kMean>{});
+            }
             if (planned) return planned;
             if constexpr (kWide && kResidentKeys<S> == 2) {
                 if constexpr (DIRECT) {

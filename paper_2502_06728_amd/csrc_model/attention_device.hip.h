@@ -28,16 +28,16 @@ constexpr int kCUs = 256;
 
 constexpr float kLog2E = 1.44269504088896341f, kLn2 = 0.693147180559945309f;
 
-// A head's features, padded with zeros to DP.
-template <int DT_, int DP_>
+// A head's features: rows of DP in LDS, of which products take the first DU (zeros behind the last feature).
+template <int DT_, int DP_, int DU_>
 struct Shape {
-    static constexpr int DT = DT_, DP = DP_;
+    static constexpr int DT = DT_, DP = DP_, DU = DU_;
     static constexpr int kElem = kSize<DT>;
-    static constexpr int kRow = DP * kElem;         // bytes of a row in LDS
-    static constexpr int kPieces = kRow / 16;       // of 16 bytes
-    static constexpr int kOf = 16 / kElem;          // features of a piece
-    static constexpr int kFrags = kPieces / 2;      // operands of the rows form: two pieces, one for each half of the lanes
-    static constexpr int kBlocks = DP / kSide;      // blocks of features
+    static constexpr int kRow = DP * kElem;             // bytes of a row in LDS
+    static constexpr int kPieces = kRow / 16;           // of 16 bytes
+    static constexpr int kOf = 16 / kElem;              // features of a piece
+    static constexpr int kFrags = DU * kElem / 32;      // operands of the rows form: two pieces, one for each half of the lanes
+    static constexpr int kBlocks = DU / kSide;          // blocks of features
 };
 
 // The wavefronts that a SIMD has registers for: two with 128 features, four with 64 and fewer.
@@ -64,7 +64,8 @@ struct Args {
 };
 
 // A split's sums for a query are a row of floats: a head's features, in whole pieces of four.  Behind all of those the
-// forward pass has two planes of splits * heads * Tq: bases and sums of weights.
+// forward pass has two planes of splits * heads * Tq: bases and sums of weights; the backward pass as many rows again, the
+// sums of p k, and one plane, the sums of ds.
 __host__ __device__ __forceinline__ int part_row(int head_dim) { return (head_dim + 3) / 4 * 4; }
 
 // ---- sequences
@@ -197,10 +198,15 @@ __device__ __forceinline__ Places places_of() {
 }
 
 // piece `piece` of a row of D features: 16 bytes, zeros behind the last feature
-template <class S>
+// (WHOLE: there are no parts of a piece)
+template <class S, bool WHOLE>
 __device__ __forceinline__ u32x4 load_piece(const char* row, int piece, int D) {
     const int d = piece * S::kOf;
     u32x4 r = {0, 0, 0, 0};
+    if constexpr (WHOLE) {
+        const u32x4 v = *reinterpret_cast<const u32x4_any2*>(row + (d < D ? d : 0) * S::kElem);
+        return d < D ? v : r;
+    }
     if (d + S::kOf <= D) return *reinterpret_cast<const u32x4_any2*>(row + d * S::kElem);
     if (d >= D) return r;
     if constexpr (S::DT == DETO_F32) {
@@ -217,8 +223,8 @@ __device__ __forceinline__ u32x4 load_piece(const char* row, int piece, int D) {
 
 // Rows into LDS by a workgroup of W wavefronts.  Rows that are missing at the end of a sequence are copies of the last
 // one: what they are multiplied with is zero.
-// DIRECT: heads of DP features at multiples of 4 bytes, from memory to LDS without a register: a wavefront's call writes
-// 64 pieces in a row, so its lanes read the pieces that belong there.  begin() starts kCalls of these; who reads the rows
+// DIRECT: heads of whole pieces at multiples of 4 bytes, from memory to LDS without a register: a wavefront's call writes
+// 64 pieces in a row, so its lanes read the pieces that belong there (those behind the last feature stay as they are).  begin() starts kCalls of these; who reads the rows
 // waits until they have come (arrived()), and for the other wavefronts' (meet()).
 // Otherwise through registers: begin() loads, end() stores.
 template <class S, int ROWS, int W, bool DIRECT>
@@ -252,21 +258,22 @@ struct Rows {
                 __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(at + from),
                                                  (__attribute__((address_space(3))) void*)(lds + (wave + i * W) * kLanes * 16), 16, 0, 0);
             };
-            if (have == ROWS) {
+            if (have == ROWS && D == S::DP) {
 #pragma unroll
                 for (int i = 0; i < kCalls; ++i) call(i, off[i]);
             } else {
 #pragma unroll
                 for (int i = 0; i < kCalls; ++i) {
-                    const int slot = threadIdx.x + i * kThreads, row = row_of(slot);
-                    call(i, static_cast<uint32_t>(row < have ? row : have - 1) * static_cast<uint32_t>(ld) + piece_of(slot) * 16);
+                    const int slot = threadIdx.x + i * kThreads, row = row_of(slot), piece = piece_of(slot);
+                    if (piece * S::kOf < D)
+                        call(i, static_cast<uint32_t>(row < have ? row : have - 1) * static_cast<uint32_t>(ld) + piece * 16);
                 }
             }
         } else {
 #pragma unroll
             for (int i = 0; i < kUnits; ++i) {
                 const int unit = threadIdx.x + i * kThreads, row = unit / S::kPieces;
-                r[i] = load_piece<S>(at + (row < have ? row : have - 1) * ld, unit % S::kPieces, D);
+                r[i] = load_piece<S, false>(at + (row < have ? row : have - 1) * ld, unit % S::kPieces, D);
             }
         }
     }
@@ -285,6 +292,14 @@ struct Rows {
 // registers one in these.
 template <bool DIRECT> constexpr int kLead = DIRECT ? 3 : 2;
 template <bool DIRECT> constexpr int kBuffers = kLead<DIRECT> + 1;
+
+// Zeros behind the last feature, before the first begin().
+template <class S, int W>
+__device__ __forceinline__ void clear(char* lds, int bytes, int D) {
+    if (D == S::DP) return;
+    for (int at = threadIdx.x * 16; at < bytes; at += W * kLanes * 16) *reinterpret_cast<u32x4*>(lds + at) = {0, 0, 0, 0};
+    __syncthreads();
+}
 
 // All of this wavefront's loads but the last N have come (they come in order).
 template <int N>
@@ -389,12 +404,12 @@ __device__ __forceinline__ f32x16 multiply(const u32x4& a, const u32x4& b, f32x1
 }
 
 // a lane's row of B; one that is missing is zeros
-template <class S>
+template <class S, bool WHOLE>
 __device__ __forceinline__ void load_row(const char* row, bool there, int D, u32x4 (&f)[S::kFrags]) {
     const int half = (threadIdx.x / kSide) % 2;
 #pragma unroll
     for (int m = 0; m < S::kFrags; ++m) {
-        f[m] = load_piece<S>(row, 2 * m + half, D);
+        f[m] = load_piece<S, WHOLE>(row, 2 * m + half, D);
         if (!there) f[m] = {0, 0, 0, 0};
     }
 }
@@ -485,6 +500,41 @@ __device__ __forceinline__ void columns_product(const char* lds, const Places& a
                 }
 #pragma unroll
                 for (int n = 0; n < N; ++n) c[n][b] = multiply<S::DT>(a, own[n], c[n][b]);
+            }
+        }
+    }
+}
+
+// C += A^T W and E += A^T V with the same 32 rows A
+template <class S>
+__device__ __forceinline__ void columns_products(const char* lds, const Places& at, const f32x16& w, const f32x16& v,
+                                                 f32x16 (&c)[S::kBlocks], f32x16 (&e)[S::kBlocks]) {
+    if constexpr (S::DT == DETO_F32) {
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+#pragma unroll
+            for (int b = 0; b < S::kBlocks; ++b) {
+                const float a = *reinterpret_cast<const float*>(lds + at.turned[r / 4 % 2] + r / 8 * 16 * S::kRow + r % 4 * 64 + b * 512);
+                c[b] = __builtin_amdgcn_mfma_f32_32x32x2f32(a, w[r], c[b], 0, 0, 0);
+            }
+        }
+    } else {
+#pragma unroll
+        for (int run = 0; run < 2; ++run) {
+            const u32x4 own = operand<S::DT>(w, run), other = operand<S::DT>(v, run);
+#pragma unroll
+            for (int b = 0; b < S::kBlocks; ++b) {
+                u32x4 a;
+#pragma unroll
+                for (int s = 0; s < 2; ++s) {
+                    const s16x4 four = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                        (TurnedAt)(lds + at.turned[s] + run * 16 * S::kRow + b * 256));
+                    const u32x2 words = __builtin_bit_cast(u32x2, four);
+                    a[2 * s] = words[0];
+                    a[2 * s + 1] = words[1];
+                }
+                c[b] = multiply<S::DT>(a, own, c[b]);
+                e[b] = multiply<S::DT>(a, other, e[b]);
             }
         }
     }
@@ -594,7 +644,7 @@ inline int64_t stats_floats(const deto_attention* cfg, int64_t Tq) {        // o
     return (2 * cfg->heads * Tq + 3) / 4 * 4;
 }
 inline int64_t part_floats(const deto_attention* cfg, int64_t Tq, int splits) {
-    return splits > 1 ? splits * cfg->heads * Tq * (part_row(cfg->head_dim) + 2) : 0;
+    return splits > 1 ? splits * cfg->heads * Tq * (2 * part_row(cfg->head_dim) + 2) : 0;
 }
 
 // Tiles of `size` rows of one head, into args; false where a launch cannot number those of all heads.
@@ -613,14 +663,17 @@ inline bool plan(Args& a, const int32_t* starts, int64_t T, int size, int heads)
     return fits;
 }
 
-// f(Shape, direct) for a head's features; `direct`: every row of the matrices that are walked over starts at a multiple
+// f(Shape, direct) for a head's features; `words`: every row of the matrices that are walked over starts at a multiple
 // of 4 bytes
 template <int DT, class F>
-inline int by_shape(int head_dim, bool direct, F f) {
-    if (head_dim == 64 && direct) return f(Shape<DT, 64>{}, Type<1>{});
-    if (head_dim == 128 && direct) return f(Shape<DT, 128>{}, Type<1>{});
-    if (head_dim <= 64) return f(Shape<DT, 64>{}, Type<0>{});
-    return f(Shape<DT, 128>{}, Type<0>{});
+inline int by_shape(int head_dim, bool words, F f) {
+    const auto by_way = [&](auto shape) {
+        return words && head_dim % decltype(shape)::kOf == 0 ? f(shape, Type<1>{}) : f(shape, Type<0>{});
+    };
+    if (head_dim <= 32) return by_way(Shape<DT, 64, 32>{});
+    if (head_dim <= 64) return by_way(Shape<DT, 64, 64>{});
+    if (head_dim <= 96) return by_way(Shape<DT, 128, 96>{});
+    return by_way(Shape<DT, 128, 128>{});
 }
 inline bool in_words(const Matrix& m) { return is_aligned(m.data, 4) && m.ld % 4 == 0 && m.ld < (int64_t{1} << 24); }
 

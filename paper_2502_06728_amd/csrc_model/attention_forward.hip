@@ -25,7 +25,7 @@ void forward_kernel(Args a) {
     Place at;
     if (!place_of(a, a.q_starts, a.Tq, BM, a.heads, a.causal, at)) return;
     const Sequence seq = sequence_of(a, at.s);
-    const int D = DIRECT ? S::DP : a.head_dim, lane = threadIdx.x % kLanes, half = lane / kSide;
+    const int D = a.head_dim, lane = threadIdx.x % kLanes, half = lane / kSide;
     const int i0 = at.tile * BM, w0 = i0 + uniform(static_cast<int32_t>(threadIdx.x / kLanes)) * kSide * N, last = seq.Lq - 1;
 
     // keys that query n sees
@@ -57,6 +57,7 @@ void forward_kernel(Args a) {
         rv.end(buffer(step) + kMatrix);
     };
     if (threadIdx.x == 0) odd = 0;
+    if constexpr (DIRECT) clear<S, W>(lds, kBuffers<DIRECT> * kStep, D);
 #pragma unroll
     for (int n = 0; n < LEAD; ++n)
         if (from + n < steps) {
@@ -72,7 +73,7 @@ void forward_kernel(Args a) {
 #pragma unroll
     for (int n = 0; n < N; ++n) {
         const int i = w0 + n * kSide + lane % kSide;
-        load_row<S>(queries + (i < last ? i : last) * a.q.ld, i <= last, D, q[n]);
+        load_row<S, DIRECT>(queries + (i < last ? i : last) * a.q.ld, i <= last, D, q[n]);
         own[n] = seen(i);
         base[n] = own[n] > 0 ? -__builtin_inff() : 0.f;
         l[n] = 0.f;
