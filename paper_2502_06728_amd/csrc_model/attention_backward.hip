@@ -14,21 +14,19 @@ namespace {
 //
 // `out` is rounded, and dout . out with it, by as much as 2^-9 of |dout| |out| in bf16: more than ds may be where a query
 // sees few keys, or one outweighs the others.  What is missing is the sum of a query's ds, since its p are 1 together.  So
-// the gradients of keys get the sum back with dout . out; those of queries take it times the sum of p k back in the end.
-//   kMean    that sum is a second one of as many registers, out of the same reads of LDS
-//   kTwice   no room for it (128 features): what ds loses by rounding is multiplied too, which takes away as much of the
-//            error where a query sees many keys (errors of dq over 2,048 keys, bf16: neither 2.7e-3, kTwice 2.2e-3, kMean
-//            2.4e-3, rounding dq alone 1.7e-3; over two keys 6.1e-3, 6.3e-3, 2.4e-3)
-//   kPlain   fp32
-enum Form { kPlain, kMean, kTwice };
-// fewer keys a sequence take kMean for every type
-constexpr int64_t kFewKeys = 512;
-
-template <int DT>
-__device__ __forceinline__ float rounded(float v) {
-    if constexpr (DT == DETO_BF16) return bits_f32(pack_bf16(v, 0.f) << 16);
-    else return static_cast<float>(static_cast<_Float16>(v));
-}
+// the gradients of keys get the sum back with dout . out; those of queries take it times the sum of p k back in the end
+// (MEAN: that sum takes as many registers as dq, and shares its reads of LDS).  TWICE: what ds loses by rounding is
+// multiplied too.  Errors of dq in bf16, where rounding dq itself is 1.7e-3:
+//                  neither   MEAN     TWICE    both
+//   2,048 keys     2.7e-3    2.4e-3   2.2e-3   1.7e-3
+//   2 keys         6.1e-3    2.4e-3   6.3e-3   1.7e-3
+// 16-bit types take MEAN but for long walks over 128 features, whose registers it does not leave (4 x 2,048 tokens of 16
+// heads, MEAN 189 us, TWICE 158, neither 120), fp32 where there are few keys; TWICE where there is time for it
+// (8 x 114 queries of 12 heads over 512 keys, fp32: MEAN 46 us, without 36, errors 5.7e-7 both).
+// fewer keys a sequence take MEAN
+template <int DT> constexpr int64_t kFewKeys = DT == DETO_F32 ? 128 : 512;
+// rows of all heads, up to which no CU has two workgroups of a kernel, and it takes TWICE
+constexpr int64_t kFewRows = int64_t{128} * kCUs;
 
 // A query's lse in powers of two; one that sees nothing gets weights of zero.
 __device__ __forceinline__ float stored_lse(float lse) {
@@ -63,9 +61,9 @@ __device__ __forceinline__ float rows_dot(const u32x4 (&x)[S::kFrags], const u32
 template <int W, int STEP, bool DIRECT>
 constexpr int kAhead = !DIRECT ? 1 : STEP * 4 * (8 / W) <= 144 * 1024 ? 3 : 1;
 
-template <class S, int W, int FORM, bool DIRECT>
+template <class S, int W, bool MEAN, bool TWICE, bool DIRECT>
 __global__ __launch_bounds__(W * kLanes) __attribute__((amdgpu_waves_per_eu(kResident<S>, kResident<S>))) void queries_kernel(Args a) {
-    constexpr int DT = S::DT, BM = W * kSide, BN = kKeys<S, W>, kMatrix = BN * S::kRow, kStep = 2 * kMatrix;
+    constexpr int BM = W * kSide, BN = kKeys<S, W>, kMatrix = BN * S::kRow, kStep = 2 * kMatrix;
     constexpr int AHEAD = kAhead<W, kStep, DIRECT>;
     extern __shared__ __align__(16) char lds[];          // AHEAD + 1 steps of keys and values
     __shared__ uint32_t odd;                             // infinities or NaNs among keys that not all queries see
@@ -113,17 +111,17 @@ __global__ __launch_bounds__(W * kLanes) __attribute__((amdgpu_waves_per_eu(kRes
     if (from < steps) end(from);
 
     const float factor = a.scale * kLog2E;
-    u32x4 q[1][S::kFrags], g[1][S::kFrags];
-    load_row<S, DIRECT>(grad, there, D, g[0]);
-    load_row<S, DIRECT>(a.out.data + row * a.out.ld + col, there, D, q[0]);
+    u32x4 q[S::kFrags], g[S::kFrags];
+    load_row<S, DIRECT>(grad, there, D, g);
+    load_row<S, DIRECT>(a.out.data + row * a.out.ld + col, there, D, q);
     const float lse = there ? stored_lse(a.lse[at.head * a.Tq + row]) : __builtin_inff();
-    const float delta = rows_dot<S>(g[0], q[0]);
+    const float delta = rows_dot<S>(g, q);
     if (there && half == 0 && split == 0) {
         a.stats[at.head * a.Tq + row] = lse;
         a.stats[(a.heads + at.head) * a.Tq + row] = delta;
     }
-    load_row<S, DIRECT>(query, there, D, q[0]);
-    f32x16 dq[1][S::kBlocks] = {}, mean[FORM == kMean ? S::kBlocks : 1] = {};
+    load_row<S, DIRECT>(query, there, D, q);
+    f32x16 dq[S::kBlocks] = {}, mean[MEAN ? S::kBlocks : 1] = {};
     float rest = 0.f;
 
     const Places places = places_of<S>();
@@ -133,27 +131,18 @@ __global__ __launch_bounds__(W * kLanes) __attribute__((amdgpu_waves_per_eu(kRes
         const int left = own - step * BN - half * 4;
 #pragma unroll
         for (int b = 0; b < BN / kSide; ++b) {
-            f32x16 x[1][1], y[1][1];
-            rows_product<S, 1, 1>(from + b * kSide * S::kRow, places, q, x);
-            rows_product<S, 1, 1>(from + kMatrix + b * kSide * S::kRow, places, g, y);
+            const char* const rows_k = from + b * kSide * S::kRow;
+            f32x16 p = block_product<S>(rows_k, places, q), ds = block_product<S>(rows_k + kMatrix, places, g);
 #pragma unroll
             for (int r = 0; r < 16; ++r) {
-                x[0][0][r] = power2(fmaf(x[0][0][r], factor, -lse));
-                if (MASKED) x[0][0][r] = b * kSide + (r / 4) * 8 + r % 4 < left ? x[0][0][r] : 0.f;
-                y[0][0][r] = x[0][0][r] * (y[0][0][r] - delta);
-                if (MASKED) y[0][0][r] = b * kSide + (r / 4) * 8 + r % 4 < left ? y[0][0][r] : 0.f;
-                if (FORM != kPlain) rest += y[0][0][r];
+                const bool shown = b * kSide + (r / 4) * 8 + r % 4 < left;
+                p[r] = power2(fmaf(p[r], factor, -lse));
+                if (MASKED) p[r] = shown ? p[r] : 0.f;
+                ds[r] = p[r] * (ds[r] - delta);
+                if (MASKED) ds[r] = shown ? ds[r] : 0.f;
+                if (S::DT != DETO_F32 || MEAN) rest += ds[r];
             }
-            if constexpr (FORM == kMean) {
-                columns_products<S>(from + b * kSide * S::kRow, places, y[0][0], x[0][0], dq[0], mean);
-            } else if constexpr (FORM == kTwice) {
-                // (what is left of ds takes the place of p)
-#pragma unroll
-                for (int r = 0; r < 16; ++r) x[0][0][r] = y[0][0][r] - rounded<DT>(y[0][0][r]);
-                columns_products<S>(from + b * kSide * S::kRow, places, y[0][0], x[0][0], dq[0], dq[0]);
-            } else {
-                columns_product<S, 1>(from + b * kSide * S::kRow, places, y[0], dq);
-            }
+            columns_products<S, TWICE, MEAN>(rows_k, places, ds, p, dq, mean);
         }
     };
 
@@ -176,23 +165,25 @@ __global__ __launch_bounds__(W * kLanes) __attribute__((amdgpu_waves_per_eu(kRes
     walk(step, steps, Type<1>{});
 
     float* const part = a.parts + ((int64_t{split} * a.heads + at.head) * a.Tq + row) * part_row(D);
-    if constexpr (FORM != kPlain) {
-        rest = halves_sum(rest);
-        if (splits > 1) {
-            if constexpr (FORM == kMean) store_part<S>(mean, part + splits * a.heads * a.Tq * part_row(D), there, D);
-            if (there && half == 0) a.parts[(2 * splits * part_row(D) + split) * a.heads * a.Tq + at.head * a.Tq + row] = rest;
-        } else {
-            if constexpr (FORM == kMean) {
+    rest = halves_sum(rest);
+    // (the weight of a query's only key does not change; a NaN stays one)
+    const bool alone = own <= 1 && fabsf(rest) < __builtin_inff();
 #pragma unroll
-                for (int b = 0; b < S::kBlocks; ++b)
+    for (int b = 0; b < S::kBlocks; ++b)
 #pragma unroll
-                    for (int r = 0; r < 16; ++r) dq[0][b][r] -= rest * mean[b][r];
-            }
-            if (there && half == 0) a.stats[(a.heads + at.head) * a.Tq + row] = delta + rest;
+        for (int r = 0; r < 16; ++r) {
+            if (MEAN && splits == 1) dq[b][r] -= rest * mean[MEAN ? b : 0][r];
+            dq[b][r] = alone ? 0.f : dq[b][r];
+            if (MEAN) mean[MEAN ? b : 0][r] = alone ? 0.f : mean[MEAN ? b : 0][r];
         }
+    if (splits == 1) {
+        store_columns<S>(dq, a.scale, a.dq.data + row * a.dq.ld + col, there, D);
+        if (there && half == 0) a.stats[(a.heads + at.head) * a.Tq + row] = delta + rest;
+    } else {
+        store_part<S>(dq, part, there, D);
+        if constexpr (MEAN) store_part<S>(mean, part + splits * a.heads * a.Tq * part_row(D), there, D);
+        if (there && half == 0) a.parts[(2 * splits * part_row(D) + split) * a.heads * a.Tq + at.head * a.Tq + row] = rest;
     }
-    if (splits == 1) store_columns<S>(dq[0], a.scale, a.dq.data + row * a.dq.ld + col, there, D);
-    else store_part<S>(dq[0], part, there, D);
     if (steps > whole_steps && odd) {
         stored();
         for (int j = whole_steps * BN; j < min(wave_upto, steps * BN); ++j) {
@@ -208,7 +199,7 @@ __global__ __launch_bounds__(W * kLanes) __attribute__((amdgpu_waves_per_eu(kRes
 }
 
 // A tile's rows of dq out of what the splits left: a wavefront for each, its lanes two features each.
-template <class S, int W, int FORM>
+template <class S, int W, bool MEAN>
 __global__ __launch_bounds__(W * kLanes) void join_kernel(Args a, int splits) {
     constexpr int BM = W * kSide;
     Place at;
@@ -225,25 +216,25 @@ __global__ __launch_bounds__(W * kLanes) void join_kernel(Args a, int splits) {
         const f32x2 v = *reinterpret_cast<const f32x2*>(part + s * rows * P);
         x.x += v.x;
         x.y += v.y;
-        if constexpr (FORM == kMean) {
+        if constexpr (MEAN) {
             const f32x2 m = *reinterpret_cast<const f32x2*>(part + (splits + s) * rows * P);
             mean.x += m.x;
             mean.y += m.y;
         }
     }
-    if constexpr (FORM != kPlain) {
-        const float rest = wave_sum(lane < splits ? a.parts[(2 * splits * P + lane) * rows + row] : 0.f);    // (at most 32)
+    const float rest = wave_sum(lane < splits ? a.parts[(2 * splits * P + lane) * rows + row] : 0.f);    // (at most 32)
+    if constexpr (MEAN) {
         x.x -= rest * mean.x;
         x.y -= rest * mean.y;
-        if (lane == 0) a.stats[rows + row] += rest;
     }
+    if (lane == 0) a.stats[rows + row] += rest;
     char* const dq = a.dq.data + (seq.q0 + i) * a.dq.ld + int64_t{at.head} * D * S::kElem;
     if (2 * lane < D) store1<S::DT>(dq, 2 * lane, x.x * a.scale);
     if (2 * lane + 1 < D) store1<S::DT>(dq, 2 * lane + 1, x.y * a.scale);
 }
 
 // ---- dk, dv
-template <class S> constexpr int kQueries = 32;                // of a step
+constexpr int kQueries = kSide;       // of a step
 // HEADS of the heads that share keys are taken at a time, by wavefronts of their own, which add up their sums in the end:
 // so that a few long walks are cut where there are not many workgroups.  Their rows leave room for fewer steps ahead.
 template <class S, int HEADS, bool DIRECT>
@@ -253,11 +244,34 @@ constexpr int kAheadOfKeys = !DIRECT || S::kRow > 256 || HEADS == 4 ? 1 : HEADS 
 template <class S> constexpr int kResidentKeys = S::kRow > 256 ? 1 : 2;
 template <class S> constexpr bool kValuesStay = S::kRow == 256 && S::DT != DETO_F32;
 
+// fp32: after so many steps the sums go to the results, and start again from zero.  Added up in one run, those of 8 heads of
+// 2,100 queries were off by 2.4e-6 (sums of a head's products by 1.2e-6).
+constexpr int kSumSteps = 32;
+
+template <class S>
+__device__ __forceinline__ void add_columns(f32x16 (&c)[S::kBlocks], float factor, char* row, bool there, int D, bool more) {
+    if (more) {
+        const int half = threadIdx.x / kSide % 2;
+        const float* const from = reinterpret_cast<const float*>(row);
+#pragma unroll
+        for (int b = 0; b < S::kBlocks; ++b)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+                const int d = b * kSide + r / 4 * 8 + 4 * half + r % 4;
+                c[b][r] = c[b][r] * factor + (there && d < D ? from[d] : 0.f);
+            }
+        factor = 1.f;
+    }
+    store_columns<S>(c, factor, row, there, D);
+#pragma unroll
+    for (int b = 0; b < S::kBlocks; ++b) c[b] = f32x16{};
+}
+
 template <class S, int BLOCKS, int HEADS>
 __device__ __forceinline__ void add_heads(char* lds, const f32x16 (&c)[S::kBlocks], int own_block, int own_head, float factor,
                                           char* row, bool there, int D) {
     typedef float f32x4 __attribute__((ext_vector_type(4)));
-        constexpr int kSums = S::kBlocks * 16 * kLanes * 4;          // bytes of a wavefront's
+    constexpr int kSums = S::kBlocks * 16 * kLanes * 4;              // bytes of a wavefront's
     const int lane = threadIdx.x % kLanes;
     f32x4* const own = reinterpret_cast<f32x4*>(lds + (own_head * BLOCKS + own_block) * kSums) + lane;
     __syncthreads();
@@ -286,9 +300,9 @@ __device__ __forceinline__ void add_heads(char* lds, const f32x16 (&c)[S::kBlock
     }
 }
 
-template <class S, int W, int HEADS, bool DIRECT>
+template <class S, int W, int HEADS, bool TWICE, bool DIRECT>
 __global__ __launch_bounds__(W * kLanes) __attribute__((amdgpu_waves_per_eu(kResidentKeys<S>, kResidentKeys<S>))) void keys_kernel(Args a) {
-    constexpr int BLOCKS = W / HEADS, BN = BLOCKS * kSide, BQ = kQueries<S>, kMatrix = BQ * S::kRow, kStep = 2 * HEADS * kMatrix;
+    constexpr int BLOCKS = W / HEADS, BN = BLOCKS * kSide, BQ = kQueries, kMatrix = BQ * S::kRow, kStep = 2 * HEADS * kMatrix;
     constexpr bool STAY = kValuesStay<S>;
     constexpr int AHEAD = kAheadOfKeys<S, HEADS, DIRECT>;
     extern __shared__ __align__(16) char lds[];          // AHEAD + 1 steps of queries and gradients of outputs; values
@@ -384,11 +398,11 @@ __global__ __launch_bounds__(W * kLanes) __attribute__((amdgpu_waves_per_eu(kRes
         ahead = next(ahead);
     }
 
-    u32x4 k[1][S::kFrags], v[1][STAY ? 1 : S::kFrags];
-    load_row<S, DIRECT>(key, there, D, k[0]);
-    if constexpr (!STAY) load_row<S, DIRECT>(value, there, D, v[0]);
+    u32x4 k[S::kFrags], v[S::kFrags];
+    load_row<S, DIRECT>(key, there, D, k);
+    if constexpr (!STAY) load_row<S, DIRECT>(value, there, D, v);
     const float factor = a.scale * kLog2E;
-    f32x16 dk[1][S::kBlocks] = {}, dv[1][S::kBlocks] = {};
+    f32x16 dk[S::kBlocks] = {}, dv[S::kBlocks] = {};
 
     const Places places = places_of<S>();
     const char* const own_values = lds + (AHEAD + 1) * kStep + own_block * kSide * S::kRow;
@@ -400,32 +414,31 @@ __global__ __launch_bounds__(W * kLanes) __attribute__((amdgpu_waves_per_eu(kRes
             const int first = s.query + b * kSide + half * 4, upto = seq.Lq - first, own_from = own - first;
             const float* const stat = stats[s.buffer][own_head] + b * kSide + half * 4;
             const char *const rows_q = from + b * kSide * S::kRow, *const rows_g = rows_q + kMatrix;
-            f32x16 p[1][1], ds[1][1];
-            rows_product<S, 1, 1>(rows_q, places, k, p);
+            f32x16 p = block_product<S>(rows_q, places, k), ds;
 #pragma unroll
             for (int r = 0; r < 16; ++r) {
                 const int t = (r / 4) * 8 + r % 4;
-                p[0][0][r] = power2(fmaf(p[0][0][r], factor, -stat[t]));
-                if (MASKED) p[0][0][r] = t >= own_from && t < upto ? p[0][0][r] : 0.f;
+                p[r] = power2(fmaf(p[r], factor, -stat[t]));
+                if (MASKED) p[r] = t >= own_from && t < upto ? p[r] : 0.f;
             }
-            if constexpr (STAY) rows_product<S, 1, 1>(rows_g, places, own_values, ds);
-            else rows_product<S, 1, 1>(rows_g, places, v, ds);
+            if constexpr (STAY) ds = block_product<S>(rows_g, places, own_values);
+            else ds = block_product<S>(rows_g, places, v);
 #pragma unroll
             for (int r = 0; r < 16; ++r) {
                 const int t = (r / 4) * 8 + r % 4;
-                ds[0][0][r] = p[0][0][r] * (ds[0][0][r] - stat[BQ + t]);
-                if (MASKED) ds[0][0][r] = t >= own_from && t < upto ? ds[0][0][r] : 0.f;
+                ds[r] = p[r] * (ds[r] - stat[BQ + t]);
+                if (MASKED) ds[r] = t >= own_from && t < upto ? ds[r] : 0.f;
             }
-            columns_product<S, 1>(rows_g, places, p[0], dv);
-            columns_product<S, 1>(rows_q, places, ds[0], dk);
+            columns_product<S, TWICE>(rows_g, places, p, dv);
+            columns_product<S, TWICE>(rows_q, places, ds, dk);
         }
     };
 
     // steps of one form, as long as they are (loops of their own: a branch between the two in one would keep a second set
     // of sums)
-    const auto walk = [&](int& n, auto masked) __attribute__((always_inline)) {
+    const auto walk = [&](int& n, int upto, auto masked) __attribute__((always_inline)) {
         constexpr bool MASKED = masked.value != 0;
-        while (n < total && (now.query >= all_from && now.query + BQ <= seq.Lq) != MASKED) {
+        while (n < upto && (now.query >= all_from && now.query + BQ <= seq.Lq) != MASKED) {
             if constexpr (DIRECT) arrived_but<HEADS * (2 * Rows<S, BQ, W, DIRECT>::kCalls + 2 * BQ / kLanes)>(min(AHEAD - 1, total - 1 - n));
             meet();
             const bool more = n + AHEAD < total;
@@ -443,19 +456,33 @@ __global__ __launch_bounds__(W * kLanes) __attribute__((amdgpu_waves_per_eu(kRes
             ++n;
         }
     };
-    for (int n = 0; n < total;) {
-        walk(n, Type<0>{});
-        walk(n, Type<1>{});
-    }
-
     char *const to_k = a.dk.data + row * a.dk.ld + kv, *const to_v = a.dv.data + row * a.dv.ld + kv;
-    if constexpr (HEADS == 1) {
-        store_columns<S>(dk[0], a.scale, to_k, there, D);
-        store_columns<S>(dv[0], 1.f, to_v, there, D);
+    const auto all = [&](int& n, int upto) __attribute__((always_inline)) {
+        while (n < upto) {
+            walk(n, upto, Type<0>{});
+            walk(n, upto, Type<1>{});
+        }
+    };
+    int n = 0;
+    if constexpr (S::DT == DETO_F32) {
+        do {
+            const bool more = n > 0;
+            all(n, min(total, n + kSumSteps));
+            add_columns<S>(dk, a.scale, to_k, there, D, more);
+            add_columns<S>(dv, 1.f, to_v, there, D, more);
+        } while (n < total);
+    } else {
+        all(n, total);
+    }
+    if constexpr (S::DT == DETO_F32) {
+        // (they are there)
+    } else if constexpr (HEADS == 1) {
+        store_columns<S>(dk, a.scale, to_k, there, D);
+        store_columns<S>(dv, 1.f, to_v, there, D);
     } else {
         // a wavefront adds up the heads' sums of every HEADS-th block of features, in their order
-        add_heads<S, BLOCKS, HEADS>(lds, dk[0], own_block, own_head, a.scale, to_k, there, D);
-        add_heads<S, BLOCKS, HEADS>(lds, dv[0], own_block, own_head, 1.f, to_v, there, D);
+        add_heads<S, BLOCKS, HEADS>(lds, dk, own_block, own_head, a.scale, to_k, there, D);
+        add_heads<S, BLOCKS, HEADS>(lds, dv, own_block, own_head, 1.f, to_v, there, D);
     }
     if (total > 0 && odd) {
         if constexpr (HEADS == 1) {
@@ -531,49 +558,57 @@ int detonation_attention_backward(const deto_attention* cfg, int64_t Tq, int64_t
                                   [&](auto shape, auto direct) {
             using S = decltype(shape);
             constexpr bool DIRECT = direct.value != 0;
-            const auto queries = [&](auto waves, auto form) {
-                constexpr int W = waves.value, FORM = form.value, kStep = 2 * kKeys<S, W> * S::kRow;
+            const auto queries = [&](auto waves, auto mean, auto twice) {
+                constexpr int W = waves.value, kStep = 2 * kKeys<S, W> * S::kRow;
+                constexpr bool MEAN = mean.value, TWICE = twice.value;
                 if (!plan(a, cfg->q_starts, Tq, W * kSide, H)) return DETO_ERR_UNSUPPORTED;
                 if (Tq) {
                     const dim3 grid(a.tiles * H, splits);
-                    queries_kernel<S, W, FORM, DIRECT><<<grid, W * kLanes, (kAhead<W, kStep, DIRECT> + 1) * kStep, on>>>(a);
-                    if (splits > 1) join_kernel<S, W, FORM><<<dim3(grid.x, kSide), W * kLanes, 0, on>>>(a, splits);
+                    queries_kernel<S, W, MEAN, TWICE, DIRECT><<<grid, W * kLanes, (kAhead<W, kStep, DIRECT> + 1) * kStep, on>>>(a);
+                    if (splits > 1) join_kernel<S, W, MEAN><<<dim3(grid.x, kSide), W * kLanes, 0, on>>>(a, splits);
                 }
                 return DETO_OK;
             };
-            const auto keys = [&](auto waves, auto heads) {
-                constexpr int W = waves.value, HEADS = heads.value, BN = W / HEADS * kSide, kStep = 2 * HEADS * kQueries<S> * S::kRow;
+            const auto keys = [&](auto waves, auto heads, auto twice) {
+                constexpr int W = waves.value, HEADS = heads.value, BN = W / HEADS * kSide, kStep = 2 * HEADS * kQueries * S::kRow;
                 constexpr int kLds = (kAheadOfKeys<S, HEADS, DIRECT> + 1) * kStep + (kValuesStay<S> ? BN * S::kRow : 0);
                 if (!plan(a, cfg->k_starts, Tk, BN, K)) return DETO_ERR_UNSUPPORTED;
-                if (Tk) keys_kernel<S, W, HEADS, DIRECT><<<a.tiles * K, W * kLanes, kLds, on>>>(a);
+                if (Tk) keys_kernel<S, W, HEADS, twice.value, DIRECT><<<a.tiles * K, W * kLanes, kLds, on>>>(a);
                 return DETO_OK;
             };
             constexpr bool kWide = S::DP == 128;
             const bool wide = kWide && Tq * H >= int64_t{256} * kCUs && Tq / cfg->sequences >= 2048;
-            const auto by_waves = [&](auto form) {
+            const auto by_waves = [&](auto mean, auto twice) {
                 if constexpr (kWide) {
-                    if (wide) return queries(Type<8>{}, form);
+                    if (wide) return queries(Type<8>{}, mean, twice);
                 }
-                return queries(Type<4>{}, form);
+                return queries(Type<4>{}, mean, twice);
             };
-            const bool few = Tk / cfg->sequences < kFewKeys;
+            const bool few = Tk / cfg->sequences < kFewKeys<S::DT>, spare = Tq * H <= kFewRows;
             if constexpr (S::DT == DETO_F32) {
-                planned = few ? queries(Type<4>{}, Type<kMean>{}) : by_waves(Type<kPlain>{});
+                planned = few ? queries(Type<4>{}, Type<1>{}, Type<0>{}) : by_waves(Type<0>{}, Type<0>{});
             } else if constexpr (S::DU == 128) {
-                planned = few ? queries(Type<4>{}, Type<kMean>{}) : by_waves(Type<kTwice>{});
+                planned = !few ? by_waves(Type<0>{}, Type<1>{}) : spare ? queries(Type<4>{}, Type<1>{}, Type<1>{})
+                                                                        : queries(Type<4>{}, Type<1>{}, Type<0>{});
             } else {
-                planned = by_waves(Type<kMean>{});
+                planned = spare ? queries(Type<4>{}, Type<1>{}, Type<1>{}) : by_waves(Type<1>{}, Type<0>{});
             }
             if (planned) return planned;
-            if constexpr (kWide && kResidentKeys<S> == 2) {
-                if constexpr (DIRECT) {
-                    const bool few = Tk * K < int64_t{256} * 2 * kCUs;
-                    if (few && a.group % 4 == 0) return planned = keys(Type<8>{}, Type<4>{});
-                    if (few && a.group % 2 == 0) return planned = keys(Type<8>{}, Type<2>{});
+            const auto by_heads = [&](auto twice) {
+                if constexpr (kWide && kResidentKeys<S> == 2) {
+                    if constexpr (DIRECT) {
+                        const bool short_of_work = Tk * K < int64_t{256} * 2 * kCUs;
+                        if (short_of_work && a.group % 4 == 0) return keys(Type<8>{}, Type<4>{}, twice);
+                        if (short_of_work && a.group % 2 == 0) return keys(Type<8>{}, Type<2>{}, twice);
+                    }
+                    if (!twice.value && Tk * K >= int64_t{256} * kCUs) return keys(Type<8>{}, Type<1>{}, Type<0>{});
                 }
-                if (Tk * K >= int64_t{256} * kCUs) return planned = keys(Type<8>{}, Type<1>{});
+                return keys(Type<4>{}, Type<1>{}, twice);
+            };
+            if constexpr (S::DT != DETO_F32) {
+                if (Tk * K <= kFewRows) return planned = by_heads(Type<1>{});
             }
-            return planned = keys(Type<4>{}, Type<1>{});
+            return planned = by_heads(Type<0>{});
         });
     });
     return planned ? planned : enqueued();

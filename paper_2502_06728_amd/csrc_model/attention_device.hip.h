@@ -20,12 +20,9 @@ typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
-typedef uint32_t u32x8 __attribute__((ext_vector_type(8)));
 
 constexpr int kSide = 32;               // of a block
 constexpr int kCUs = 256;
-
-
 constexpr float kLog2E = 1.44269504088896341f, kLn2 = 0.693147180559945309f;
 
 // A head's features: rows of DP in LDS, of which products take the first DU (zeros behind the last feature).
@@ -224,8 +221,9 @@ __device__ __forceinline__ u32x4 load_piece(const char* row, int piece, int D) {
 // Rows into LDS by a workgroup of W wavefronts.  Rows that are missing at the end of a sequence are copies of the last
 // one: what they are multiplied with is zero.
 // DIRECT: heads of whole pieces at multiples of 4 bytes, from memory to LDS without a register: a wavefront's call writes
-// 64 pieces in a row, so its lanes read the pieces that belong there (those behind the last feature stay as they are).  begin() starts kCalls of these; who reads the rows
-// waits until they have come (arrived()), and for the other wavefronts' (meet()).
+// 64 pieces in a row, so its lanes read the pieces that belong there (those behind the last feature stay as they are).
+// begin() starts kCalls of these; who reads the rows waits until they have come (arrived()), and for the other wavefronts'
+// (meet()).
 // Otherwise through registers: begin() loads, end() stores.
 template <class S, int ROWS, int W, bool DIRECT>
 struct Rows {
@@ -414,49 +412,42 @@ __device__ __forceinline__ void load_row(const char* row, bool there, int D, u32
     }
 }
 
-// BLOCKS blocks of 32 rows of a matrix in LDS times each of the lane's N rows
-template <class S, int BLOCKS, int N>
-__device__ __forceinline__ void rows_product(const char* lds, const Places& at, const u32x4 (&b)[N][S::kFrags],
-                                             f32x16 (&c)[BLOCKS][N]) {
+// BLOCKS blocks of 32 rows of a matrix in LDS times the lane's row
+template <class S, int BLOCKS>
+__device__ __forceinline__ void rows_product(const char* lds, const Places& at, const u32x4 (&b)[S::kFrags], f32x16 (&c)[BLOCKS]) {
 #pragma unroll
-    for (int k = 0; k < BLOCKS; ++k)
-#pragma unroll
-        for (int n = 0; n < N; ++n) c[k][n] = f32x16{};
+    for (int k = 0; k < BLOCKS; ++k) c[k] = f32x16{};
 #pragma unroll
     for (int m = 0; m < S::kFrags; ++m)
 #pragma unroll
         for (int k = 0; k < BLOCKS; ++k) {
             const u32x4 a = *reinterpret_cast<const u32x4*>(lds + at.rows[m % 2] + m / 2 * 256 + k * kSide * S::kRow);
-#pragma unroll
-            for (int n = 0; n < N; ++n) c[k][n] = multiply<S::DT>(a, b[n][m], c[k][n]);
+            c[k] = multiply<S::DT>(a, b[m], c[k]);
         }
 }
 
-// the same with the lane's rows in LDS too, among 32 N rows at `b`
-template <class S, int BLOCKS, int N>
-__device__ __forceinline__ void rows_product(const char* lds, const Places& at, const char* b, f32x16 (&c)[BLOCKS][N]) {
-#pragma unroll
-    for (int k = 0; k < BLOCKS; ++k)
-#pragma unroll
-        for (int n = 0; n < N; ++n) c[k][n] = f32x16{};
+// a block of rows with the lane's row in LDS too, among the 32 at `b`
+template <class S>
+__device__ __forceinline__ f32x16 block_product(const char* lds, const Places& at, const char* b) {
+    f32x16 c = {};
 #pragma unroll
     for (int m = 0; m < S::kFrags; ++m) {
-        u32x4 own[N];
-#pragma unroll
-        for (int n = 0; n < N; ++n) own[n] = *reinterpret_cast<const u32x4*>(b + at.rows[m % 2] + m / 2 * 256 + n * kSide * S::kRow);
-#pragma unroll
-        for (int k = 0; k < BLOCKS; ++k) {
-            const u32x4 a = *reinterpret_cast<const u32x4*>(lds + at.rows[m % 2] + m / 2 * 256 + k * kSide * S::kRow);
-#pragma unroll
-            for (int n = 0; n < N; ++n) c[k][n] = multiply<S::DT>(a, own[n], c[k][n]);
-        }
+        const uint32_t from = at.rows[m % 2] + m / 2 * 256;
+        c = multiply<S::DT>(*reinterpret_cast<const u32x4*>(lds + from), *reinterpret_cast<const u32x4*>(b + from), c);
     }
+    return c;
+}
+template <class S>
+__device__ __forceinline__ f32x16 block_product(const char* lds, const Places& at, const u32x4 (&b)[S::kFrags]) {
+    f32x16 c[1];
+    rows_product<S, 1>(lds, at, b, c);
+    return c[0];
 }
 
 // ---- the columns form
 typedef __attribute__((address_space(3))) s16x4* TurnedAt;
 
-// W as the second operand: one of two runs of 16 rows
+// W as the second operand: one of two runs of 16 rows, rounded
 template <int DT>
 __device__ __forceinline__ u32x4 operand(const f32x16& w, int run) {
     u32x4 r;
@@ -467,48 +458,32 @@ __device__ __forceinline__ u32x4 operand(const f32x16& w, int run) {
     }
     return r;
 }
-
-// C[n] += (32 rows of a matrix in LDS)^T W[n]
-template <class S, int N>
-__device__ __forceinline__ void columns_product(const char* lds, const Places& at, const f32x16 (&w)[N], f32x16 (&c)[N][S::kBlocks]) {
-    if constexpr (S::DT == DETO_F32) {
+// ... and what the rounding took away, rounded in its turn
+template <int DT>
+__device__ __forceinline__ u32x4 operand_rest(const f32x16& w, int run, const u32x4& rounded) {
+    u32x4 r;
 #pragma unroll
-        for (int r = 0; r < 16; ++r) {
-#pragma unroll
-            for (int b = 0; b < S::kBlocks; ++b) {
-                const float a = *reinterpret_cast<const float*>(lds + at.turned[r / 4 % 2] + r / 8 * 16 * S::kRow + r % 4 * 64 + b * 512);
-#pragma unroll
-                for (int n = 0; n < N; ++n) c[n][b] = __builtin_amdgcn_mfma_f32_32x32x2f32(a, w[n][r], c[n][b], 0, 0, 0);
-            }
-        }
-    } else {
-#pragma unroll
-        for (int run = 0; run < 2; ++run) {
-            u32x4 own[N];
-#pragma unroll
-            for (int n = 0; n < N; ++n) own[n] = operand<S::DT>(w[n], run);
-#pragma unroll
-            for (int b = 0; b < S::kBlocks; ++b) {
-                u32x4 a;
-#pragma unroll
-                for (int s = 0; s < 2; ++s) {
-                    const s16x4 four = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                        (TurnedAt)(lds + at.turned[s] + run * 16 * S::kRow + b * 256));
-                    const u32x2 words = __builtin_bit_cast(u32x2, four);
-                    a[2 * s] = words[0];
-                    a[2 * s + 1] = words[1];
-                }
-#pragma unroll
-                for (int n = 0; n < N; ++n) c[n][b] = multiply<S::DT>(a, own[n], c[n][b]);
-            }
+    for (int j = 0; j < 4; ++j) {
+        const uint32_t two = rounded[j];
+        float lo = w[8 * run + 2 * j], hi = w[8 * run + 2 * j + 1];
+        if constexpr (DT == DETO_BF16) {
+            lo -= bits_f32(two << 16);
+            hi -= bits_f32(two & 0xFFFF0000u);
+            r[j] = pack_bf16(lo, hi);
+        } else {
+            const f16x2 h = __builtin_bit_cast(f16x2, two);
+            lo -= static_cast<float>(h.x);
+            hi -= static_cast<float>(h.y);
+            r[j] = pack_f16(lo, hi);
         }
     }
+    return r;
 }
 
-// C += A^T W and E += A^T V with the same 32 rows A
-template <class S>
+// C += A^T W and E += A^T V with the same 32 rows A in LDS (SECOND: otherwise C alone); TWICE: W to twice the bits
+template <class S, bool TWICE, bool SECOND>
 __device__ __forceinline__ void columns_products(const char* lds, const Places& at, const f32x16& w, const f32x16& v,
-                                                 f32x16 (&c)[S::kBlocks], f32x16 (&e)[S::kBlocks]) {
+                                                 f32x16 (&c)[S::kBlocks], f32x16* e) {
     if constexpr (S::DT == DETO_F32) {
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
@@ -516,12 +491,16 @@ __device__ __forceinline__ void columns_products(const char* lds, const Places& 
             for (int b = 0; b < S::kBlocks; ++b) {
                 const float a = *reinterpret_cast<const float*>(lds + at.turned[r / 4 % 2] + r / 8 * 16 * S::kRow + r % 4 * 64 + b * 512);
                 c[b] = __builtin_amdgcn_mfma_f32_32x32x2f32(a, w[r], c[b], 0, 0, 0);
+                if constexpr (SECOND) e[b] = __builtin_amdgcn_mfma_f32_32x32x2f32(a, v[r], e[b], 0, 0, 0);
             }
         }
     } else {
 #pragma unroll
         for (int run = 0; run < 2; ++run) {
-            const u32x4 own = operand<S::DT>(w, run), other = operand<S::DT>(v, run);
+            const u32x4 own = operand<S::DT>(w, run);
+            u32x4 rest, other;
+            if constexpr (TWICE) rest = operand_rest<S::DT>(w, run, own);
+            if constexpr (SECOND) other = operand<S::DT>(v, run);
 #pragma unroll
             for (int b = 0; b < S::kBlocks; ++b) {
                 u32x4 a;
@@ -534,10 +513,15 @@ __device__ __forceinline__ void columns_products(const char* lds, const Places& 
                     a[2 * s + 1] = words[1];
                 }
                 c[b] = multiply<S::DT>(a, own, c[b]);
-                e[b] = multiply<S::DT>(a, other, e[b]);
+                if constexpr (TWICE) c[b] = multiply<S::DT>(a, rest, c[b]);
+                if constexpr (SECOND) e[b] = multiply<S::DT>(a, other, e[b]);
             }
         }
     }
+}
+template <class S, bool TWICE = false>
+__device__ __forceinline__ void columns_product(const char* lds, const Places& at, const f32x16& w, f32x16 (&c)[S::kBlocks]) {
+    columns_products<S, TWICE, false>(lds, at, w, w, c, nullptr);
 }
 
 // ---- both halves' maximum and sum of a column

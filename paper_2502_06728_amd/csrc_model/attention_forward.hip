@@ -15,10 +15,10 @@ namespace {
 // so far are seldom scaled down.  (Weights this large are numbers in fp16, and have as many bits as others.)
 constexpr float kMost = 8192.f;
 
-template <class S, int W, int N, bool DIRECT>
+template <class S, int W, bool DIRECT>
 __global__ __launch_bounds__(W * kLanes) __attribute__((amdgpu_waves_per_eu(kResident<S>, kResident<S>)))
 void forward_kernel(Args a) {
-    constexpr int DT = S::DT, BM = W * kSide * N, BN = kKeys<S, W>, kMatrix = BN * S::kRow, kStep = 2 * kMatrix;
+    constexpr int BM = W * kSide, BN = kKeys<S, W>, kMatrix = BN * S::kRow, kStep = 2 * kMatrix;
     constexpr int LEAD = kLead<DIRECT>, NB = BN / kSide;
     extern __shared__ __align__(16) char lds[];          // steps of keys and values
     __shared__ uint32_t odd;                             // infinities or NaNs among values that not all queries see
@@ -26,7 +26,7 @@ void forward_kernel(Args a) {
     if (!place_of(a, a.q_starts, a.Tq, BM, a.heads, a.causal, at)) return;
     const Sequence seq = sequence_of(a, at.s);
     const int D = a.head_dim, lane = threadIdx.x % kLanes, half = lane / kSide;
-    const int i0 = at.tile * BM, w0 = i0 + uniform(static_cast<int32_t>(threadIdx.x / kLanes)) * kSide * N, last = seq.Lq - 1;
+    const int i0 = at.tile * BM, w0 = i0 + uniform(static_cast<int32_t>(threadIdx.x / kLanes)) * kSide, last = seq.Lq - 1;
 
     // keys that query n sees
     const auto seen = [&](int n) {
@@ -34,7 +34,7 @@ void forward_kernel(Args a) {
         const int64_t upto = int64_t{n < last ? n : last} + seq.Lk - last;
         return static_cast<int>(upto < 0 ? 0 : upto);
     };
-    const int upto = seen(i0 + BM - 1), wave_upto = w0 > last ? 0 : seen(w0 + kSide * N - 1);        // by any of the workgroup's, the wavefront's
+    const int upto = seen(i0 + BM - 1), wave_upto = w0 > last ? 0 : seen(w0 + kSide - 1);    // by any of the workgroup's, the wavefront's
     const int all_steps = (upto + BN - 1) / BN, splits = gridDim.y, split = blockIdx.y;
     // of which this workgroup takes one part
     const int from = static_cast<int>(int64_t{all_steps} * split / splits), steps = static_cast<int>(int64_t{all_steps} * (split + 1) / splits);
@@ -66,107 +66,80 @@ void forward_kernel(Args a) {
         }
 
     const float factor = a.scale * kLog2E;       // of scores, to powers of two
-    u32x4 q[N][S::kFrags];
-    int own[N];
-    float base[N], l[N];
-    f32x16 o[N][S::kBlocks] = {};
-#pragma unroll
-    for (int n = 0; n < N; ++n) {
-        const int i = w0 + n * kSide + lane % kSide;
-        load_row<S, DIRECT>(queries + (i < last ? i : last) * a.q.ld, i <= last, D, q[n]);
-        own[n] = seen(i);
-        base[n] = own[n] > 0 ? -__builtin_inff() : 0.f;
-        l[n] = 0.f;
-    }
+    const int i = w0 + lane % kSide, own = seen(i);
+    u32x4 q[S::kFrags];
+    load_row<S, DIRECT>(queries + (i < last ? i : last) * a.q.ld, i <= last, D, q);
+    float base = own > 0 ? -__builtin_inff() : 0.f, l = 0.f;
+    f32x16 o[S::kBlocks] = {};
     const Places places = places_of<S>();
-    f32x16 x[NB][N];                                     // scores of a step, computed in the one before
+    f32x16 x[NB];                                        // scores of a step, computed in the one before
 
     const auto hide = [&](int step) __attribute__((always_inline)) {
+        const int left = own - step * BN - half * 4;            // of the keys that the query sees
 #pragma unroll
-        for (int n = 0; n < N; ++n) {
-            const int left = own[n] - step * BN - half * 4;         // of the keys that the query sees
+        for (int b = 0; b < NB; ++b)
 #pragma unroll
-            for (int b = 0; b < NB; ++b)
-#pragma unroll
-                for (int r = 0; r < 16; ++r)
-                    x[b][n][r] = b * kSide + (r / 4) * 8 + r % 4 < left ? x[b][n][r] : -__builtin_inff();
-        }
+            for (int r = 0; r < 16; ++r) x[b][r] = b * kSide + (r / 4) * 8 + r % 4 < left ? x[b][r] : -__builtin_inff();
     };
     // scores into weights, and their sum
-    const auto weigh = [&](int n, float from) __attribute__((always_inline)) {
+    const auto weigh = [&](float from) __attribute__((always_inline)) {
         float sum = 0.f;
 #pragma unroll
         for (int b = 0; b < NB; ++b)
 #pragma unroll
             for (int r = 0; r < 16; ++r) {
-                x[b][n][r] = power2(fmaf(x[b][n][r], factor, -from));
-                sum += x[b][n][r];
+                x[b][r] = power2(fmaf(x[b][r], factor, -from));
+                sum += x[b][r];
             }
         return sum;
+    };
+    // the largest score, in powers of two
+    const auto largest = [&]() __attribute__((always_inline)) {
+        float top = -__builtin_inff();
+#pragma unroll
+        for (int b = 0; b < NB; ++b)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) top = fmaxf(top, x[b][r]);
+        return halves_max(top) * factor;
     };
     // weights of a step's scores, their products with its values, and the next step's scores (the last step's again
     // behind it: a branch here would keep the three from sharing the time)
     const auto compute = [&](int step, auto masked) __attribute__((always_inline)) {
         constexpr bool MASKED = masked.value != 0;
-        f32x16 next[NB][N];
+        f32x16 next[NB];
         if (MASKED) hide(step);
-        rows_product<S, NB, N>(buffer(step + 1 < steps ? step + 1 : step), places, q, next);
-        float sum[N];
-        uint64_t high = 0;                               // (or none yet)
-#pragma unroll
-        for (int n = 0; n < N; ++n) {
-            sum[n] = weigh(n, base[n]);
-            high |= __ballot(!(sum[n] <= kMost));
-        }
+        rows_product<S, NB>(buffer(step + 1 < steps ? step + 1 : step), places, q, next);
+        float sum = weigh(base);
+        const uint64_t high = __ballot(!(sum <= kMost));         // (or no base yet)
         if (high) {
-            rows_product<S, NB, N>(buffer(step), places, q, x);
+            rows_product<S, NB>(buffer(step), places, q, x);
             if (MASKED) hide(step);
+            const float top = largest();
+            // (a query's two lanes do the same, whatever the others do)
+            const bool rise = (high | high << kSide | high >> kSide) >> lane & 1 && top > base;
+            const float less = rise ? power2(base - top) : 1.f;
+            base = rise ? top : base;
+            l *= less;
 #pragma unroll
-            for (int n = 0; n < N; ++n) {
-                float top = -__builtin_inff();
+            for (int b = 0; b < S::kBlocks; ++b)
 #pragma unroll
-                for (int b = 0; b < NB; ++b)
-#pragma unroll
-                    for (int r = 0; r < 16; ++r) top = fmaxf(top, x[b][n][r]);
-                top = halves_max(top) * factor;
-                // (a query's two lanes do the same, whatever the others do)
-                const uint64_t lanes = __ballot(!(sum[n] <= kMost));
-                const bool rise = (lanes | lanes << kSide | lanes >> kSide) >> lane & 1 && top > base[n];
-                const float less = rise ? power2(base[n] - top) : 1.f;
-                base[n] = rise ? top : base[n];
-                l[n] *= less;
-#pragma unroll
-                for (int b = 0; b < S::kBlocks; ++b)
-#pragma unroll
-                    for (int r = 0; r < 16; ++r) o[n][b][r] *= less;
-                sum[n] = weigh(n, base[n] > -__builtin_inff() ? base[n] : 0.f);
-            }
+                for (int r = 0; r < 16; ++r) o[b][r] *= less;
+            sum = weigh(base > -__builtin_inff() ? base : 0.f);
         }
+        l += sum;
 #pragma unroll
-        for (int n = 0; n < N; ++n) l[n] += sum[n];
+        for (int b = 0; b < NB; ++b) columns_product<S>(buffer(step) + kMatrix + b * kSide * S::kRow, places, x[b], o);
 #pragma unroll
-        for (int b = 0; b < NB; ++b) columns_product<S, N>(buffer(step) + kMatrix + b * kSide * S::kRow, places, x[b], o);
-#pragma unroll
-        for (int b = 0; b < NB; ++b)
-#pragma unroll
-            for (int n = 0; n < N; ++n) x[b][n] = next[b][n];
+        for (int b = 0; b < NB; ++b) x[b] = next[b];
     };
 
     constexpr int kLoads = 2 * Rows<S, BN, W, DIRECT>::kCalls;
     if (from < steps) {
         if constexpr (DIRECT) arrived_but<kLoads>(min(LEAD - 1, steps - 1 - from));
         meet();
-        rows_product<S, NB, N>(buffer(from), places, q, x);
-#pragma unroll
-        for (int n = 0; n < N; ++n) {                    // what is masked among these makes no base too low
-            float top = x[0][n][0];
-#pragma unroll
-            for (int b = 0; b < NB; ++b)
-#pragma unroll
-                for (int r = 0; r < 16; ++r) top = fmaxf(top, x[b][n][r]);
-            top = halves_max(top) * factor;
-            if (own[n] > 0 && from < whole_steps) base[n] = top;
-        }
+        rows_product<S, NB>(buffer(from), places, q, x);
+        const float top = largest();
+        if (own > 0 && from < whole_steps) base = top;           // (what is masked makes no base too low)
     }
     // (two loops: a branch between the two forms in one would keep a second set of sums)
     const auto walk = [&](int& step, int to, auto masked) __attribute__((always_inline)) {
@@ -186,43 +159,33 @@ void forward_kernel(Args a) {
     walk(step, whole_steps, Type<0>{});
     walk(step, steps, Type<1>{});
 
-#pragma unroll
-    for (int n = 0; n < N; ++n) {
-        const int i = w0 + n * kSide + lane % kSide;
-        const int64_t row = seq.q0 + i;
-        const float total = halves_sum(l[n]);
-        const float to_one = total == 0.f ? 0.f : 1.f / total;
-        if (splits == 1) {
-            store_columns<S>(o[n], to_one, a.out.data + row * a.out.ld + col, i <= last, D);
-            if (a.lse && i <= last && half == 0)
-                a.lse[at.head * a.Tq + row] = total == 0.f ? -__builtin_inff() : (base[n] + __builtin_amdgcn_logf(total)) * kLn2;
-            l[n] = to_one;
-        } else {
-            const int64_t rows = a.heads * a.Tq, part = split * rows + at.head * a.Tq + row;
-            store_part<S>(o[n], a.parts + part * part_row(D), i <= last, D);
-            if (i <= last && half == 0) {
-                float* const stats = a.parts + splits * rows * part_row(D) + part;
-                stats[0] = base[n];
-                stats[splits * rows] = total;
-            }
-            l[n] = 1.f;
+    const float total = halves_sum(l), to_one = total == 0.f ? 0.f : 1.f / total;
+    const bool there = i <= last;
+    const int64_t row = seq.q0 + (there ? i : last);
+    char* const out = a.out.data + row * a.out.ld + col;
+    const int64_t rows = a.heads * a.Tq, of_part = split * rows + at.head * a.Tq + row;
+    float* const part = a.parts + of_part * part_row(D);
+    if (splits == 1) {
+        store_columns<S>(o, to_one, out, there, D);
+        if (a.lse && there && half == 0)
+            a.lse[at.head * a.Tq + row] = total == 0.f ? -__builtin_inff() : (base + __builtin_amdgcn_logf(total)) * kLn2;
+    } else {
+        store_part<S>(o, part, there, D);
+        if (there && half == 0) {
+            float* const stats = a.parts + splits * rows * part_row(D) + of_part;
+            stats[0] = base;
+            stats[splits * rows] = total;
         }
     }
     if (steps > whole_steps && odd) {
         stored();
         for (int j = whole_steps * BN; j < min(wave_upto, steps * BN); ++j) {
-            const char *const value = values + j * a.v.ld, *const key = keys + j * a.k.ld;
+            const char* const value = values + j * a.v.ld;
             if (!row_is_odd<S>(value, D)) continue;
-#pragma unroll
-            for (int n = 0; n < N; ++n) {
-                const int i = w0 + n * kSide + lane % kSide;
-                const float score = slow_dot<S>(queries + (i < last ? i : last) * a.q.ld, key, D);
-                const float weight = power2(fmaf(score, factor, -base[n])) * l[n];
-                if (i > last || j >= own[n]) continue;
-                const int64_t row = seq.q0 + i;
-                if (splits == 1) add_odd<S>(a.out.data + row * a.out.ld + col, value, D, weight);
-                else add_odd<S, DETO_F32>(a.parts + ((int64_t{split} * a.heads + at.head) * a.Tq + row) * part_row(D), value, D, weight);
-            }
+            const float weight = power2(fmaf(slow_dot<S>(queries + (there ? i : last) * a.q.ld, keys + j * a.k.ld, D), factor, -base));
+            if (!there || j >= own) continue;
+            if (splits == 1) add_odd<S>(out, value, D, weight * to_one);
+            else add_odd<S, DETO_F32>(part, value, D, weight);
         }
     }
 }
@@ -353,25 +316,23 @@ int detonation_attention_forward(const deto_attention* cfg, int64_t Tq, int64_t 
     by_type(q->dtype, [&](auto dt) {
         return by_shape<dt.value>(cfg->head_dim, in_words(a.k) && in_words(a.v), [&](auto shape, auto direct) {
             using S = decltype(shape);
-            const auto run = [&](auto waves, auto blocks) {
-                constexpr int W = waves.value, N = blocks.value;
+            const auto run = [&](auto waves) {
+                constexpr int W = waves.value, BM = W * kSide, kStep = 2 * kKeys<S, W> * S::kRow;
                 constexpr bool DIRECT = direct.value != 0;
-                if (!plan(a, cfg->q_starts, Tq, W * kSide * N, cfg->heads)) return planned = DETO_ERR_UNSUPPORTED;
-                constexpr int kStep = 2 * kKeys<S, W> * S::kRow;
+                if (!plan(a, cfg->q_starts, Tq, BM, cfg->heads)) return planned = DETO_ERR_UNSUPPORTED;
                 const hipStream_t on = static_cast<hipStream_t>(stream);
                 const dim3 grid(a.tiles * cfg->heads, splits);
-                forward_kernel<S, W, N, DIRECT><<<grid, W * kLanes, kBuffers<DIRECT> * kStep, on>>>(a);
+                forward_kernel<S, W, DIRECT><<<grid, W * kLanes, kBuffers<DIRECT> * kStep, on>>>(a);
                 if (splits > 1) {
-                    constexpr int BM = W * kSide * N;
                     const unsigned of_tile = (min(int64_t{BM}, Tq) + kJoinWaves - 1) / kJoinWaves;
                     join_kernel<S, BM><<<dim3(grid.x, of_tile), kJoinWaves * kLanes, 0, on>>>(a, splits);
                 }
-                return 0;
+                return planned = DETO_OK;
             };
             if constexpr (S::DP == 128) {
-                if (wide) return run(Type<8>{}, Type<1>{});
+                if (wide) return run(Type<8>{});
             }
-            return run(Type<4>{}, Type<1>{});
+            return run(Type<4>{});
         });
     });
     if (planned) return planned;

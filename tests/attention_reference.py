@@ -142,3 +142,26 @@ def assert_within(got, want, bound, what):
         at = int(torch.argmax(off))
         raise AssertionError(f"{what}: {got[there][at]} is not {want[there][at]} to {bound[there][at]} "
                              f"(element {int(torch.nonzero(there.flatten())[at])} of {tuple(got.shape)})")
+
+
+def whole(q, k, v, dout, heads, kv_heads, scale, causal, sequences):
+    """out, dq, dk and dv of sequences of equal length, all heads at once in 64 bits where the matrices are."""
+    def apart(x, n):
+        return x.double().reshape(sequences, -1, n, x.shape[1] // n).transpose(1, 2)
+
+    def together(x):
+        return x.transpose(1, 2).reshape(sequences * x.shape[2], -1)
+
+    group = heads // kv_heads
+    q, dout = apart(q, heads), apart(dout, heads)
+    k, v = (apart(t, kv_heads).repeat_interleave(group, 1).contiguous() for t in (k, v))
+    s = q @ k.transpose(2, 3).contiguous() * scale
+    if causal:
+        nq, nk = s.shape[2:]
+        s.masked_fill_(torch.ones((nq, nk), dtype=torch.bool, device=s.device).triu(nk - nq + 1), -math.inf)
+    p = torch.softmax(s, 3)
+    out = p @ v
+    ds = p * (dout @ v.transpose(2, 3).contiguous() - (dout * out).sum(3, keepdim=True))
+    dk, dv = ds.transpose(2, 3).contiguous() @ q * scale, p.transpose(2, 3).contiguous() @ dout
+    dk, dv = (t.unflatten(1, (kv_heads, group)).sum(2) for t in (dk, dv))
+    return {"out": together(out), "dq": together(ds @ k * scale), "dk": together(dk), "dv": together(dv)}

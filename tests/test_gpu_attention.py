@@ -239,6 +239,47 @@ def test_long_sequence(gpu):
         assert bool(((c.out[i].double() - p @ v).abs() <= bound).all()), i
 
 
+@pytest.mark.parametrize("dtype,sequences,L,heads,kv_heads,head_dim,causal", [
+    (BF16, 1, 2100, 32, 8, 128, True), (F16, 1, 2100, 32, 32, 128, False), (BF16, 20, 130, 16, 8, 128, True),
+    (BF16, 9, 1000, 32, 8, 128, True), (F16, 9, 1000, 16, 8, 96, False), (BF16, 1, 2100, 32, 32, 96, True),
+    (BF16, 20, 130, 16, 16, 64, False), (BF16, 9, 1000, 16, 2, 40, True), (F32, 1, 2100, 32, 4, 128, True),
+    (F32, 20, 130, 16, 16, 128, False), (BF16, 30, 2, 8, 2, 64, False), (F16, 50, 2, 4, 4, 128, False),
+    (BF16, 50, 3, 4, 1, 96, True), (F32, 50, 3, 4, 2, 32, True)])
+def test_as_exact_as_the_type(gpu, dtype, sequences, L, heads, kv_heads, head_dim, causal):
+    """Results are rounded, and so are the weights (or their gradients) that are multiplied: two errors spread over half a
+    step u, u / sqrt(3) each, as is a third that the written `out` may bring into the gradients: u together.  In fp32 a
+    score of 64 additions of partial sums around 2 is off by some sqrt(64) half units, its product with a factor and lse
+    by up to 16 each, and a sum over 2,100 terms by sqrt(2100) / 4: 64 together.  A row has 4 times as much of its own."""
+    n = sequences * L
+    c = Case(dtype, even(sequences, L), even(sequences, L), heads, kv_heads, head_dim, causal, packed=False)
+    c.q.mul_(2.0)                                    # scores of a standard deviation of two
+    c.forward()
+    c.backward()
+    want = ref.whole(c.q, c.k, c.v, c.dout, heads, kv_heads, c.cfg.scale, causal, sequences)
+    u = 64 * ref.FINE if dtype == F32 else ref.UNIT[dtype]
+    for name, w in want.items():
+        got = getattr(c, name).double()
+        assert got.shape == w.shape == (n, w.shape[1])
+        off, size = (got - w).norm(dim=1), w.norm(dim=1)
+        say(name, float(off.norm() / size.norm()) / u)
+        assert float(off.norm()) <= u * float(size.norm()), name
+        assert bool((off <= 4 * u * torch.maximum(size, size.norm() / n ** 0.5)).all()), name
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("head_dim", [64, 128])
+@pytest.mark.parametrize("Lq,Lk,causal", [(1, 1, True), (300, 1, False), (7, 7, True), (3, 1, True), (600, 600, True)])
+def test_one_key(gpu, dtype, head_dim, Lq, Lk, causal):
+    """The weight of a query's only key is 1 whatever its score: no gradient reaches the query."""
+    c = Case(dtype, [0, Lq], [0, Lk], 2, 1, head_dim, causal)
+    c.forward()
+    c.backward()
+    sees = torch.arange(Lq) + Lk - Lq + 1 if causal else torch.full((Lq,), Lk)
+    assert not bool(c.dq[(sees <= 1).to(DEV)].any())
+    if Lk == 1:
+        assert not bool(c.dk.any())
+
+
 def test_same_bits_and_other_stream(gpu):
     for args in ((BF16, [0, 300, 420], [0, 300, 420], 4, 2, 64, True), (F32, [0, 5], [0, 3000], 2, 2, 64, False)):
         c = Case(*args)
