@@ -3,6 +3,12 @@
 // see them, of all heads that share the keys.  The weights are computed again from lse in both: two of seven products,
 // but every sum has one owner, who adds in a fixed order.  The first launch leaves dout . out of every query for the
 // second.
+//
+// What bounds them: two wavefronts a SIMD, whose matrix products, exponentials and LDS reads only partly share the time;
+// sums of two gradients, or operands in two terms, fill the registers.  4 x 2,048 tokens of 16 heads of 128 under the mask,
+// bf16: queries 151 us (910 TFLOP/s in four products), keys 182 (755 in four); without what makes dout . out exact,
+// queries 120.  64 x 197 tokens of 12 heads of 64 in fp16: 41 and 48.  fp32, 8 x 114 queries over 512 keys: 35 + 11 (the
+// join) and 43, chains of a few steps each.
 #include "attention_device.hip.h"
 
 namespace deto {
@@ -25,8 +31,9 @@ namespace {
 // (8 x 114 queries of 12 heads over 512 keys, fp32: MEAN 46 us, without 36, errors 5.7e-7 both).
 // fewer keys a sequence take MEAN
 template <int DT> constexpr int64_t kFewKeys = DT == DETO_F32 ? 128 : 512;
-// rows of all heads, up to which no CU has two workgroups of a kernel, and it takes TWICE
-constexpr int64_t kFewRows = int64_t{128} * kCUs;
+// rows of all heads, up to which there is time for it in both kernels: a row's error may stand out among few, and the chip
+// is not full.  (16,384 rows of keys, 1 x 2,048 tokens of 32 heads over 8: 277 us without, 316 with it)
+constexpr int64_t kFewRows = 32 * kCUs;
 
 // A query's lse in powers of two; one that sees nothing gets weights of zero.
 __device__ __forceinline__ float stored_lse(float lse) {
@@ -57,7 +64,7 @@ __device__ __forceinline__ float rows_dot(const u32x4 (&x)[S::kFrags], const u32
 }
 
 // Steps that are on their way while one is computed: three, where the workgroups that share a CU then have room in its
-// LDS (two of four wavefronts, or one of eight).
+// LDS (two of four wavefronts, or one of eight); a step that goes through registers is the only one.
 template <int W, int STEP, bool DIRECT>
 constexpr int kAhead = !DIRECT ? 1 : STEP * 4 * (8 / W) <= 144 * 1024 ? 3 : 1;
 
@@ -594,14 +601,18 @@ int detonation_attention_backward(const deto_attention* cfg, int64_t Tq, int64_t
                 planned = spare ? queries(Type<4>{}, Type<1>{}, Type<1>{}) : by_waves(Type<1>{}, Type<0>{});
             }
             if (planned) return planned;
+            // (groups of four heads of 128, bf16, both passes of gradients, four and two heads at a time: 2 x 2,048 tokens of
+            // 32 heads 375 us and 424, 1 x 4,200 706 and 808, 1 x 6,000 1,338 and 1,315, 1 x 8,100 2,198 and 2,045; 12 packed
+            // sequences of up to 1,500, one at a time 520 us, two 399, four 445, the keys' kernel alone)
             const auto by_heads = [&](auto twice) {
                 if constexpr (kWide && kResidentKeys<S> == 2) {
                     if constexpr (DIRECT) {
-                        const bool short_of_work = Tk * K < int64_t{256} * 2 * kCUs;
-                        if (short_of_work && a.group % 4 == 0) return keys(Type<8>{}, Type<4>{}, twice);
-                        if (short_of_work && a.group % 2 == 0) return keys(Type<8>{}, Type<2>{}, twice);
+                        if (Tk * K < int64_t{160} * kCUs && a.group % 4 == 0) return keys(Type<8>{}, Type<4>{}, twice);
+                        if (Tk * K < int64_t{512} * kCUs && a.group % 2 == 0) return keys(Type<8>{}, Type<2>{}, twice);
                     }
-                    if (!twice.value && Tk * K >= int64_t{256} * kCUs) return keys(Type<8>{}, Type<1>{}, Type<0>{});
+                    if constexpr (!twice.value) {
+                        if (Tk * K >= int64_t{256} * kCUs) return keys(Type<8>{}, Type<1>{}, twice);
+                    }
                 }
                 return keys(Type<4>{}, Type<1>{}, twice);
             };

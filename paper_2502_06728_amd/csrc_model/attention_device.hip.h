@@ -37,7 +37,7 @@ struct Shape {
     static constexpr int kBlocks = DU / kSide;          // blocks of features
 };
 
-// The wavefronts that a SIMD has registers for: two with 128 features, four with 64 and fewer.
+// The wavefronts that a SIMD is given registers for (three with up to 64 features of 16 bits: four would spill).
 template <class S> constexpr int kResident = S::DP == 64 && S::DT != DETO_F32 ? 3 : 2;
 // Keys of a step of a walk over keys
 template <class S, int W> constexpr int kKeys = S::DT == DETO_F32 || S::DP == 64 || W == 4 ? 32 : 64;
@@ -286,8 +286,8 @@ struct Rows {
     }
 };
 
-// A walk has the rows of two steps in LDS, which it computes with, and kLead - 2 steps more on their way; staged through
-// registers one in these.
+// The forward walk has the rows of two steps in LDS, which it computes with, and kLead - 2 steps more on their way; staged
+// through registers, one in these.
 template <bool DIRECT> constexpr int kLead = DIRECT ? 3 : 2;
 template <bool DIRECT> constexpr int kBuffers = kLead<DIRECT> + 1;
 
@@ -611,9 +611,10 @@ inline Matrix matrix_of(const deto_rows* m) {
 }
 
 // Into how many parts the walks over keys are cut.  Where fewer workgroups than CUs would walk over many keys, a second
-// launch that adds up what parts of 64 (fp32: 32) keys leave costs less than the rest of the walk.  (Sequences of equal length are
-// assumed; the parts are equal shares of each tile's own walk, whatever its length.)  fp32 steps take longer: it is cut
-// from 128 keys on, 16-bit types from 512 on.
+// launch that adds up what parts of 64 (fp32: 32) keys leave costs less than the rest of the walk.  (Sequences of equal
+// length are assumed; the parts are equal shares of each tile's own walk, whatever its length.)  fp32 steps take longer: it
+// is cut from 128 keys on, 16-bit types from 512 on.  Forward, in one part and in several: one query over 2,048 keys of 16
+// heads of 128, bf16, 45 us and 12; 8 x 114 queries over 512 keys of 12 heads of 64, fp32, 48 and 42.
 inline int splits_of(const deto_attention* cfg, int64_t Tq, int64_t Tk, bool f32) {
     if (!Tq || !Tk) return 1;
     const int64_t queried = cfg->sequences < Tq ? cfg->sequences : Tq;

@@ -1,8 +1,14 @@
 // softmax(scale q k^T) v and log sum exp, one pass over the keys.
 //
-// A workgroup takes 128 or 256 queries of a head, 32 a wavefront, and walks over the keys they see, 64 (fp32: 32) at a
-// time in LDS.  A lane has one query: its running maximum and sum are two registers, and its scores, as they come out
-// of the first product, are the second product's operand.
+// A workgroup takes 128 or 256 queries of a head, 32 a wavefront, and walks over the keys they see, 32 or 64 at a time in
+// LDS.  A lane has one query: its base and sum are two registers, and its scores, as they come out of the first product,
+// are the second product's operand.  A step's exponentials and second product share the time with the next step's scores.
+//
+// What bounds it: long sequences the matrix cores, at the chip's power (16,384 tokens of 16 heads of 128 under the mask,
+// bf16: 1,020 us, 1.08 PFLOP/s; the library's products of 8,192^3 run at 1.06); 4 x 2,048 tokens (95 us, 0.72) also the
+// tiles' unequal lengths; 64 features the exponentials (64 x 197 tokens of 12 heads, fp16: 28 us); few queries a chain of
+// loads (one query over 2,048 keys of 16 heads: 7.4 us + 3.8 to join 16 parts, 45 in one part).  64 queries a wavefront
+// (one wavefront a SIMD) took 205 us at 4 x 2,048.
 #include "attention_device.hip.h"
 
 namespace deto {
@@ -310,7 +316,7 @@ int detonation_attention_forward(const deto_attention* cfg, int64_t Tq, int64_t 
     a.lse = lse;
     a.parts = static_cast<float*>(workspace);
     int planned = DETO_OK;
-    // (8 x 2,048 bf16 rows of 16 heads of 128: eight wavefronts 92 us, four 103; 64 x 197 of 12 heads of 64: 37 and 27)
+    // (4 x 2,048 bf16 rows of 16 heads of 128: eight wavefronts 92 us, four 103; 64 x 197 of 12 heads of 64: 37 and 27)
     const bool wide = Tq * cfg->heads >= int64_t{256} * kCUs && Tq / cfg->sequences >= 2048;
     fresh();
     by_type(q->dtype, [&](auto dt) {

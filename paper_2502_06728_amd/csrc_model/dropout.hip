@@ -5,7 +5,8 @@
 //
 // Philox 4x32 (Salmon, Moraes, Dror and Shaw, 2011): ten rounds of two 32 x 32 -> 64 bit products, which the vector
 // units do at a quarter of their rate.  32 bits an element would take two counters and make the products the bound for
-// 16-bit matrices.
+// 16-bit matrices.  Bound by memory: 16,384 x 2,048, bf16 onto an fp32 residual 61 us (5.5 TB/s), its gradient 28 (7.2: part
+// of it stays in the caches); 197 x 771 fp16 2.8 (a launch).
 #include "device.hip.h"
 
 namespace deto {
