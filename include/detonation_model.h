@@ -263,8 +263,9 @@ int detonation_rotary(const deto_rotary* cfg, int64_t T, const deto_rows* x, con
  *              NULL.  Starts that are out of order or out of range leave results undefined, but no access is out of
  *              bounds.
  * head_dim is at most 128 (else DETO_ERR_UNSUPPORTED); kv_heads divides heads, which is at most 65536; scale is above
- * 0 and finite; Tq, Tk and sequences are at most 2^31 - 1, and without starts a multiple of `sequences`.  Scores,
- * their statistics and all sums are fp32; p (and ds below) enter the second product rounded to the matrices' type.
+ * 0 and finite; Tq, Tk and sequences are at most 2^31 - 1, and without starts a multiple of `sequences`.  Tiles of 128
+ * rows, with one more for each sequence, times heads are below 2^22 (else DETO_ERR_UNSUPPORTED).  Scores, their
+ * statistics and all sums are fp32; p (and ds below) enter the second product rounded to the matrices' type.
  */
 typedef struct {
     int32_t heads, kv_heads, head_dim;
@@ -285,14 +286,16 @@ int detonation_attention_forward(const deto_attention* cfg, int64_t Tq, int64_t 
  *     dp_j = dout_i . v_j      ds_j = p_j (dp_j - dout_i . out_i)
  *     dq_i = scale * sum_j ds_j k_j      dk_j = scale * sum_i ds_j q_i      dv_j = sum_i p_j dout_i
  * with the sums of dk and dv over all heads that read them.  dq, dk and dv are of q's type and shapes, written, not
- * added to.  Under fp16, ds above 65504 becomes infinite.
+ * added to.  Under fp16, ds above 65504 becomes infinite.  dout_i . out_i is taken as if out were not rounded, and ds
+ * of a query's only key as 0.
  */
 int detonation_attention_backward(const deto_attention* cfg, int64_t Tq, int64_t Tk, const deto_rows* q,
                                   const deto_rows* k, const deto_rows* v, const deto_rows* out,
                                   const float* lse, const deto_rows* dout, const deto_rows* dq,
                                   const deto_rows* dk, const deto_rows* dv, void* workspace, void* stream);
 
-/* Bytes for either call. */
+/* Bytes for either call, at 16 bytes.  The forward call needs them where it cuts its walks over keys (few queries, many
+ * keys: else the workspace may be NULL, which is otherwise DETO_ERR_NULL). */
 int64_t detonation_attention_workspace(const deto_attention* cfg, int64_t Tq, int64_t Tk);
 
 /* ---- dropout ----------------------------------------------------------------------------------
