@@ -250,8 +250,20 @@ def test_as_exact_as_the_type(gpu, dtype, sequences, L, heads, kv_heads, head_di
     step u, u / sqrt(3) each, as is a third that the written `out` may bring into the gradients: u together.  In fp32 a
     score of 64 additions of partial sums around 2 is off by some sqrt(64) half units, its product with a factor and lse
     by up to 16 each, and a sum over 2,100 terms by sqrt(2100) / 4: 64 together.  A row has 4 times as much of its own."""
+    check_whole(dtype, sequences, L, heads, kv_heads, head_dim, causal)
+
+
+@pytest.mark.parametrize("dtype,sequences,L,heads,kv_heads,head_dim,causal,pad", [
+    (BF16, 1, 2100, 32, 8, 128, True, 1), (F16, 9, 1000, 16, 8, 96, True, 3), (BF16, 20, 130, 16, 16, 127, False, 0),
+    (F32, 1, 2100, 32, 32, 99, False, 0)])
+def test_as_exact_from_any_address(gpu, dtype, sequences, L, heads, kv_heads, head_dim, causal, pad):
+    """The same where rows start at odd elements, or heads are no whole pieces."""
+    check_whole(dtype, sequences, L, heads, kv_heads, head_dim, causal, pad)
+
+
+def check_whole(dtype, sequences, L, heads, kv_heads, head_dim, causal, pad=0):
     n = sequences * L
-    c = Case(dtype, even(sequences, L), even(sequences, L), heads, kv_heads, head_dim, causal, packed=False)
+    c = Case(dtype, even(sequences, L), even(sequences, L), heads, kv_heads, head_dim, causal, pad, packed=False)
     c.q.mul_(2.0)                                    # scores of a standard deviation of two
     c.forward()
     c.backward()
