@@ -487,7 +487,9 @@ __global__ __launch_bounds__(W * kLanes) __attribute__((amdgpu_waves_per_eu(kRes
         store_columns<S>(dk, a.scale, to_k, there, D);
         store_columns<S>(dv, 1.f, to_v, there, D);
     } else {
-        // a wavefront adds up the heads' sums of every HEADS-th block of features, in their order
+        // a wavefront adds up the heads' sums of every HEADS-th block of features, in their order (in LDS, where the copy of
+        // the values may still be on its way if no step has waited for it: a sequence may have no queries)
+        if constexpr (DIRECT) arrived<0>();
         add_heads<S, BLOCKS, HEADS>(lds, dk, own_block, own_head, a.scale, to_k, there, D);
         add_heads<S, BLOCKS, HEADS>(lds, dv, own_block, own_head, 1.f, to_v, there, D);
     }
