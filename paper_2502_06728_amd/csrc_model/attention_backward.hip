@@ -132,7 +132,7 @@ __global__ __launch_bounds__(W * kLanes) __attribute__((amdgpu_waves_per_eu(kRes
     float rest = 0.f;
 
     const Places places = places_of<S>();
-    const auto compute = [&](int step, auto masked) __attribute__((always_inline)) {
+    const auto compute = [&](int step, auto masked, auto clean) __attribute__((always_inline)) {
         constexpr bool MASKED = masked.value != 0;
         const char* const from = buffer(step);
         const int left = own - step * BN - half * 4;
@@ -149,27 +149,38 @@ __global__ __launch_bounds__(W * kLanes) __attribute__((amdgpu_waves_per_eu(kRes
                 if (MASKED) ds[r] = shown ? ds[r] : 0.f;
                 if (S::DT != DETO_F32 || MEAN) rest += ds[r];
             }
-            columns_products<S, TWICE, MEAN>(rows_k, places, ds, p, dq, mean);
+            columns_products<S, TWICE, MEAN, clean.value != 0>(rows_k, places, ds, p, dq, mean);
         }
     };
 
-    // (two loops: a branch between the two forms in one would keep a second set of sums)
-    const auto walk = [&](int& step, int to, auto masked) __attribute__((always_inline)) {
-        for (; step < to; ++step) {
-            if constexpr (DIRECT) arrived_but<2 * Rows<S, BN, W, DIRECT>::kCalls>(min(AHEAD - 1, steps - 1 - step));
-            meet();
-            if (step + AHEAD < steps) begin(step + AHEAD);
-            if constexpr (masked.value != 0) {
-                take_out_odd<S, BN, W>(buffer(step), &odd);
-                meet();
-            }
-            if (step * BN < wave_upto) compute(step, masked);
-            if (step + AHEAD < steps) end(step + AHEAD);
-        }
+    const auto arrive = [&](int step) __attribute__((always_inline)) {
+        if constexpr (DIRECT) arrived_but<2 * Rows<S, BN, W, DIRECT>::kCalls>(min(AHEAD - 1, steps - 1 - step));
+        meet();
+        if (step + AHEAD < steps) begin(step + AHEAD);
     };
+    // (loops of their own: a branch between the forms in one would keep a second set of sums)
     int step = from;
-    walk(step, whole_steps, Type<0>{});
-    walk(step, steps, Type<1>{});
+    for (; step < whole_steps; ++step) {
+        arrive(step);
+        if (step * BN < wave_upto) compute(step, Type<0>{}, Type<0>{});
+        if (step + AHEAD < steps) end(step + AHEAD);
+    }
+    for (; step < steps; ++step) {
+        arrive(step);
+        find_odd<S, BN, W>(buffer(step), &odd);
+        meet();
+        if (uniform(static_cast<int32_t>(odd))) break;
+        if (step * BN < wave_upto) compute(step, Type<1>{}, Type<0>{});
+        if (step + AHEAD < steps) end(step + AHEAD);
+    }
+    // From the first step on that has infinities or NaNs among the keys, the second product goes without them: its other
+    // operand has zeros for what is masked, which they would pass by.  (The scores keep them: one that is -infinity is no
+    // weight.)  What they give to the queries that see them is added behind the stores.
+    for (const int first = step; step < steps; ++step) {
+        if (step > first) arrive(step);
+        if (step * BN < wave_upto) compute(step, Type<1>{}, Type<1>{});
+        if (step + AHEAD < steps) end(step + AHEAD);
+    }
 
     float* const part = a.parts + ((int64_t{split} * a.heads + at.head) * a.Tq + row) * part_row(D);
     rest = halves_sum(rest);

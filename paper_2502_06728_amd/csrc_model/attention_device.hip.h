@@ -357,6 +357,24 @@ __device__ __forceinline__ void take_out_odd(char* lds, uint32_t* found) {
     }
 }
 
+// Says whether there are any, and leaves them: for rows that the scores are computed from as well.
+template <class S, int ROWS, int W>
+__device__ __forceinline__ void find_odd(const char* lds, uint32_t* found) {
+    constexpr int kThreads = W * kLanes;
+    // (an exponent of all ones, and nothing else, carries into the bit above it)
+    constexpr uint32_t kExponent = S::DT == DETO_F32 ? 0x7F800000u : S::DT == DETO_BF16 ? 0x7F807F80u : 0x7C007C00u;
+    constexpr uint32_t kLowest = S::DT == DETO_F32 ? 0x00800000u : S::DT == DETO_BF16 ? 0x00800080u : 0x04000400u;
+    constexpr uint32_t kAbove = S::DT == DETO_F32 ? 0x80000000u : 0x80008000u;
+    uint32_t any = 0;
+#pragma unroll
+    for (int i = 0; i < ROWS * S::kPieces / kThreads; ++i) {
+        const u32x4 r = *reinterpret_cast<const u32x4*>(lds + (threadIdx.x + i * kThreads) * 16);
+#pragma unroll
+        for (int w = 0; w < 4; ++w) any |= (r[w] & kExponent) + kLowest;
+    }
+    if (any & kAbove) *found = 1;
+}
+
 // whether a row in memory holds any (a wavefront's lanes look at its features together)
 template <class S>
 __device__ __forceinline__ bool row_is_odd(const char* row, int D) {
@@ -480,8 +498,9 @@ __device__ __forceinline__ u32x4 operand_rest(const f32x16& w, int run, const u3
     return r;
 }
 
-// C += A^T W and E += A^T V with the same 32 rows A in LDS (SECOND: otherwise C alone); TWICE: W to twice the bits
-template <class S, bool TWICE, bool SECOND>
+// C += A^T W and E += A^T V with the same 32 rows A in LDS (SECOND: otherwise C alone); TWICE: W to twice the bits; CLEAN:
+// without A's infinities and NaNs
+template <class S, bool TWICE, bool SECOND, bool CLEAN = false>
 __device__ __forceinline__ void columns_products(const char* lds, const Places& at, const f32x16& w, const f32x16& v,
                                                  f32x16 (&c)[S::kBlocks], f32x16* e) {
     if constexpr (S::DT == DETO_F32) {
@@ -489,7 +508,9 @@ __device__ __forceinline__ void columns_products(const char* lds, const Places& 
         for (int r = 0; r < 16; ++r) {
 #pragma unroll
             for (int b = 0; b < S::kBlocks; ++b) {
-                const float a = *reinterpret_cast<const float*>(lds + at.turned[r / 4 % 2] + r / 8 * 16 * S::kRow + r % 4 * 64 + b * 512);
+                uint32_t word = *reinterpret_cast<const uint32_t*>(lds + at.turned[r / 4 % 2] + r / 8 * 16 * S::kRow + r % 4 * 64 + b * 512);
+                if constexpr (CLEAN) is_odd<S>(word, word);
+                const float a = bits_f32(word);
                 c[b] = __builtin_amdgcn_mfma_f32_32x32x2f32(a, w[r], c[b], 0, 0, 0);
                 if constexpr (SECOND) e[b] = __builtin_amdgcn_mfma_f32_32x32x2f32(a, v[r], e[b], 0, 0, 0);
             }
@@ -511,6 +532,14 @@ __device__ __forceinline__ void columns_products(const char* lds, const Places& 
                     const u32x2 words = __builtin_bit_cast(u32x2, four);
                     a[2 * s] = words[0];
                     a[2 * s + 1] = words[1];
+                }
+                if constexpr (CLEAN) {
+#pragma unroll
+                    for (int w = 0; w < 4; ++w) {
+                        uint32_t cleaned;
+                        is_odd<S>(a[w], cleaned);
+                        a[w] = cleaned;
+                    }
                 }
                 c[b] = multiply<S::DT>(a, own, c[b]);
                 if constexpr (TWICE) c[b] = multiply<S::DT>(a, rest, c[b]);

@@ -68,3 +68,66 @@ def test_keys_without_queries(gpu, dtype, heads, kv_heads, head_dim):
     c.check()
     assert not bool(c.dk[:140].any()) and not bool(c.dv[:140].any())
     assert not bool(c.dk[290:355].any()) and not bool(c.dv[290:355].any())
+
+
+# ------------------------------------------------------------------ infinities that are seen
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("n,at,causal,heads,kv_heads,head_dim", [
+    (150, 75, True, 2, 1, 64), (150, 140, False, 2, 1, 64), (150, 10, False, 2, 1, 128), (150, 149, False, 2, 2, 128),
+    (140, 130, True, 4, 1, 128), (600, 595, True, 2, 2, 128), (150, 64, True, 2, 2, 33), (2100, 2090, True, 32, 8, 128)])
+def test_key_of_minus_infinity(gpu, dtype, n, at, causal, heads, kv_heads, head_dim):
+    """A key that makes a score -infinity has no weight: only its own feature of a query's gradient is 0 * infinity, the others
+    and the other keys' gradients are as if it were not there.  Whether the step is masked or not."""
+    feature = 5
+    c = Case(dtype, [0, n], [0, n], heads, kv_heads, head_dim, causal, packed=False)
+    c.q[:, feature::head_dim] = c.q[:, feature::head_dim].abs() + 0.25
+    c.k[at, feature::head_dim] = -INF
+    c.forward()
+    c.backward()
+    want, _ = defined(c)
+    u = unit(dtype)
+    other = torch.arange(heads * head_dim, device=DEV) % head_dim != feature
+    assert_rows(c.out, want["out"], u, "out")
+    assert_rows(c.dq[:, other], want["dq"][:, other], u, "dq")
+    assert_rows(c.dk, want["dk"], u, "dk")
+    assert_rows(c.dv, want["dv"], u, "dv")
+    assert not bool(c.dk[at].any()) and not bool(c.dv[at].any())
+    seen = torch.arange(n, device=DEV) >= (at if causal else 0)
+    assert bool(torch.isnan(c.dq[seen][:, ~other]).all())
+    if causal:
+        assert_rows(c.dq[:at], want["dq"][:at], u, "dq of those that do not see it")
+
+
+@pytest.mark.parametrize("dtype", [BF16, F16])
+@pytest.mark.parametrize("bad", [INF, -INF, NAN])
+def test_four_heads_and_infinities(gpu, dtype, bad):
+    """Groups of four heads: a row that holds infinities or NaNs changes the gradients of what it sees alone, whichever of
+    the four it belongs to."""
+    at, n = 75, 150
+    fine = Case(dtype, [0, n, 2 * n], [0, n, 2 * n], 4, 1, 128, True)
+    fine.forward()
+    fine.backward()
+    for head in (0, 3):
+        for name in ("q", "dout"):
+            c = Case(dtype, [0, n, 2 * n], [0, n, 2 * n], 4, 1, 128, True)
+            getattr(c, name)[at, 128 * head + 7:128 * (head + 1):9] = bad
+            c.forward()
+            c.backward()
+            assert torch.equal(c.dk[at + 1:], fine.dk[at + 1:]) and torch.equal(c.dv[at + 1:], fine.dv[at + 1:]), (head, name)
+            assert not bool(torch.isfinite((c.dk if name == "q" else c.dv)[:at + 1, 7::9]).any()), (head, name)
+            same = torch.arange(2 * n, device=DEV) != at
+            assert torch.equal(c.dq[same], fine.dq[same]), (head, name)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_hundreds_of_sequences(gpu, dtype):
+    """Tiles are counted 64 sequences at a time: a few hundred, some of none, and a long one at the end."""
+    starts = [0]
+    for s in range(300):
+        starts.append(starts[-1] + s % 5)
+    starts.append(starts[-1] + 200)
+    c = Case(dtype, starts, starts, 2, 1, 64, True, behind=3)
+    c.forward()
+    c.backward()
+    c.check()
