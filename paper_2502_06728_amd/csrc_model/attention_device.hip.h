@@ -61,7 +61,7 @@ struct Args {
 };
 
 // A split's sums for a query are a row of floats: a head's features, in whole pieces of four.  Behind all of those the
-// forward pass has two planes of splits * heads * Tq: bases and sums of weights; the backward pass as many rows again, the
+// forward pass has three planes of splits * heads * Tq: bases (two) and sums of weights; the backward pass as many rows again, the
 // sums of p k, and one plane, the sums of ds.
 __host__ __device__ __forceinline__ int part_row(int head_dim) { return (head_dim + 3) / 4 * 4; }
 
@@ -629,6 +629,33 @@ __device__ __forceinline__ void store_part(const f32x16 (&c)[S::kBlocks], float*
 }
 
 __device__ __forceinline__ float power2(float x) { return __builtin_amdgcn_exp2f(x); }
+
+// of scores, to powers of two
+__device__ __forceinline__ float factor_of(float scale) { return fminf(scale * kLog2E, 3.402823466e38f); }
+
+// What weights are relative to: that of score x is 2^((x - score) * factor - power).  One of the two is zero.  Of scores in
+// reach it is `score`: the difference to a rounded power is exact in one operation, and the rounding is the same for all
+// weights.  Out of it a power would be rounded by more than a weight may be off by, up to all of its range, so there the
+// scores are subtracted first.
+constexpr float kReach = 1 << 20;
+struct Base {
+    float score, power;
+    __device__ __forceinline__ bool far() const { return score != 0.f; }
+    __device__ __forceinline__ float above(float x, float factor) const { return fmaf(x - score, factor, -power); }
+    // how far this one is above another one, in powers of two
+    __device__ __forceinline__ float over(const Base& other, float factor) const {
+        return fmaf(score - other.score, factor, power - other.power);
+    }
+};
+// (-infinity stays a power: of nothing)
+__device__ __forceinline__ Base base_of(float score, float factor) {
+    const float power = score * factor;
+    const bool far = score > -__builtin_inff() && !(fabsf(power) < kReach);
+    return {far ? score : 0.f, far ? 0.f : power};
+}
+__device__ __forceinline__ float log_sum(const Base& base, float total, float scale) {
+    return total == 0.f ? -__builtin_inff() : fmaf(base.score, scale, (base.power + __builtin_amdgcn_logf(total)) * kLn2);
+}
 
 // ---- host side
 int check(const deto_attention* cfg, int64_t Tq, int64_t Tk);

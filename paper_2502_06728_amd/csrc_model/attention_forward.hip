@@ -71,11 +71,12 @@ void forward_kernel(Args a) {
             end(from + n);
         }
 
-    const float factor = a.scale * kLog2E;       // of scores, to powers of two
+    const float factor = factor_of(a.scale);
     const int i = w0 + lane % kSide, own = seen(i);
     u32x4 q[S::kFrags];
     load_row<S, DIRECT>(queries + (i < last ? i : last) * a.q.ld, i <= last, D, q);
-    float base = own > 0 ? -__builtin_inff() : 0.f, l = 0.f;
+    Base base = {0.f, own > 0 ? -__builtin_inff() : 0.f};
+    float l = 0.f, most = kMost;
     f32x16 o[S::kBlocks] = {};
     const Places places = places_of<S>();
     f32x16 x[NB];                                        // scores of a step, computed in the one before
@@ -88,25 +89,30 @@ void forward_kernel(Args a) {
             for (int r = 0; r < 16; ++r) x[b][r] = b * kSide + (r / 4) * 8 + r % 4 < left ? x[b][r] : -__builtin_inff();
     };
     // scores into weights, and their sum
-    const auto weigh = [&](float from) __attribute__((always_inline)) {
+    const auto weigh = [&](Base from) __attribute__((always_inline)) {
         float sum = 0.f;
 #pragma unroll
         for (int b = 0; b < NB; ++b)
 #pragma unroll
             for (int r = 0; r < 16; ++r) {
-                x[b][r] = power2(fmaf(x[b][r], factor, -from));
+                x[b][r] = power2(from.above(x[b][r], factor));
                 sum += x[b][r];
             }
         return sum;
     };
-    // the largest score, in powers of two
+    // the largest score
     const auto largest = [&]() __attribute__((always_inline)) {
         float top = -__builtin_inff();
 #pragma unroll
         for (int b = 0; b < NB; ++b)
 #pragma unroll
             for (int r = 0; r < 16; ++r) top = fmaxf(top, x[b][r]);
-        return halves_max(top) * factor;
+        return halves_max(top);
+    };
+    // (a far base's weights are always taken the second way)
+    const auto set = [&](Base to) __attribute__((always_inline)) {
+        base = to;
+        most = to.far() ? -1.f : kMost;
     };
     // weights of a step's scores, their products with its values, and the next step's scores (the last step's again
     // behind it: a branch here would keep the three from sharing the time)
@@ -115,22 +121,24 @@ void forward_kernel(Args a) {
         f32x16 next[NB];
         if (MASKED) hide(step);
         rows_product<S, NB>(buffer(step + 1 < steps ? step + 1 : step), places, q, next);
-        float sum = weigh(base);
-        const uint64_t high = __ballot(!(sum <= kMost));         // (or no base yet)
+        float sum = weigh({0.f, base.power});
+        const uint64_t high = __ballot(!(sum <= most));          // (or no base yet)
         if (high) {
             rows_product<S, NB>(buffer(step), places, q, x);
             if (MASKED) hide(step);
             const float top = largest();
             // (a query's two lanes do the same, whatever the others do)
-            const bool rise = (high | high << kSide | high >> kSide) >> lane & 1 && top > base;
-            const float less = rise ? power2(base - top) : 1.f;
-            base = rise ? top : base;
-            l *= less;
+            if ((high | high << kSide | high >> kSide) >> lane & 1 && base.above(top, factor) > 0.f) {
+                const Base risen = base_of(top, factor);
+                const float less = power2(base.over(risen, factor));
+                set(risen);
+                l *= less;
 #pragma unroll
-            for (int b = 0; b < S::kBlocks; ++b)
+                for (int b = 0; b < S::kBlocks; ++b)
 #pragma unroll
-                for (int r = 0; r < 16; ++r) o[b][r] *= less;
-            sum = weigh(base > -__builtin_inff() ? base : 0.f);
+                    for (int r = 0; r < 16; ++r) o[b][r] *= less;
+            }
+            sum = weigh({base.score, base.power > -__builtin_inff() ? base.power : 0.f});
         }
         l += sum;
 #pragma unroll
@@ -145,7 +153,7 @@ void forward_kernel(Args a) {
         meet();
         rows_product<S, NB>(buffer(from), places, q, x);
         const float top = largest();
-        if (own > 0 && from < whole_steps) base = top;           // (what is masked makes no base too low)
+        if (own > 0 && from < whole_steps) set(base_of(top, factor));           // (what is masked makes no base too low)
     }
     // (two loops: a branch between the two forms in one would keep a second set of sums)
     const auto walk = [&](int& step, int to, auto masked) __attribute__((always_inline)) {
@@ -174,13 +182,14 @@ void forward_kernel(Args a) {
     if (splits == 1) {
         store_columns<S>(o, to_one, out, there, D);
         if (a.lse && there && half == 0)
-            a.lse[at.head * a.Tq + row] = total == 0.f ? -__builtin_inff() : (base + __builtin_amdgcn_logf(total)) * kLn2;
+            a.lse[at.head * a.Tq + row] = log_sum(base, total, a.scale);
     } else {
         store_part<S>(o, part, there, D);
         if (there && half == 0) {
             float* const stats = a.parts + splits * rows * part_row(D) + of_part;
-            stats[0] = base;
-            stats[splits * rows] = total;
+            stats[0] = base.score;
+            stats[splits * rows] = base.power;
+            stats[2 * splits * rows] = total;
         }
     }
     if (steps > whole_steps && odd) {
@@ -188,7 +197,7 @@ void forward_kernel(Args a) {
         for (int j = whole_steps * BN; j < min(wave_upto, steps * BN); ++j) {
             const char* const value = values + j * a.v.ld;
             if (!row_is_odd<S>(value, D)) continue;
-            const float weight = power2(fmaf(slow_dot<S>(queries + (there ? i : last) * a.q.ld, keys + j * a.k.ld, D), factor, -base));
+            const float weight = power2(base.above(slow_dot<S>(queries + (there ? i : last) * a.q.ld, keys + j * a.k.ld, D), factor));
             if (!there || j >= own) continue;
             if (splits == 1) add_odd<S>(out, value, D, weight * to_one);
             else add_odd<S, DETO_F32>(part, value, D, weight);
@@ -211,11 +220,21 @@ __global__ __launch_bounds__(kJoinWaves * kLanes) void join_kernel(Args a, int s
     const float* const bases = a.parts + splits * rows * P + row;
     // a lane looks at one split's base and sum (there are at most 32)
     const bool own = lane < splits;
-    const float base = own ? bases[lane * rows] : -__builtin_inff(), sum = own ? bases[(splits + lane) * rows] : 0.f;
-    float top = base;
+    const Base base = {own ? bases[lane * rows] : 0.f, own ? bases[(splits + lane) * rows] : -__builtin_inff()};
+    const float sum = own ? bases[(2 * splits + lane) * rows] : 0.f, factor = factor_of(a.scale);
+    // the highest one: by its power, and the far ones that are rounded to the same by their scores
+    const float power = base.far() ? base.score * factor : base.power;
+    float top = power;
 #pragma unroll
     for (int by = 1; by < kLanes; by *= 2) top = fmaxf(top, __shfl_xor(top, by));
-    const float less = sum == 0.f ? 0.f : power2(base - top);          // (of a part that the query sees nothing of: 0)
+    Base highest = {0.f, top};
+    if (!(fabsf(top) < kReach)) {
+        float score = power == top && base.far() ? base.score : -__builtin_inff();
+#pragma unroll
+        for (int by = 1; by < kLanes; by *= 2) score = fmaxf(score, __shfl_xor(score, by));
+        if (score > -__builtin_inff()) highest = {score, 0.f};
+    }
+    const float less = sum == 0.f ? 0.f : power2(base.over(highest, factor));          // (of a part that the query sees nothing of: 0)
     const float total = wave_sum(sum * less);
     const float* const part = a.parts + row * P + 2 * (2 * lane < D ? lane : 0);
     float x = 0.f, y = 0.f;
@@ -235,7 +254,7 @@ __global__ __launch_bounds__(kJoinWaves * kLanes) void join_kernel(Args a, int s
     char* const out = a.out.data + (seq.q0 + i) * a.out.ld + int64_t{at.head} * D * S::kElem;
     if (2 * lane < D) store1<S::DT>(out, 2 * lane, x * to_one);
     if (2 * lane + 1 < D) store1<S::DT>(out, 2 * lane + 1, y * to_one);
-    if (a.lse && lane == 0) a.lse[row] = total == 0.f ? -__builtin_inff() : (top + __builtin_amdgcn_logf(total)) * kLn2;
+    if (a.lse && lane == 0) a.lse[row] = log_sum(highest, total, a.scale);
 }
 
 }  // namespace

@@ -131,3 +131,56 @@ def test_hundreds_of_sequences(gpu, dtype):
     c.forward()
     c.backward()
     c.check()
+
+
+# ------------------------------------------------------------------ scores of any size
+
+def far_case(dtype, n, m, causal, heads, kv_heads, head_dim, q0, k0, k1, scale):
+    """Scores scale * (q0 * k0[j] + k1[j]), whose sums fp32 holds exactly; the other features of the keys do not count, as
+    those of the queries are zeros."""
+    c = Case(dtype, [0, n], [0, m], heads, kv_heads, head_dim, causal, packed=False, scale=scale)
+    c.q.zero_()
+    c.q[:, 0::head_dim] = q0
+    c.q[:, 1::head_dim] = 1.0
+    j = torch.arange(m)
+    c.k[:, 0::head_dim] = k0(j).to(dtype).to(DEV)[:, None]
+    c.k[:, 1::head_dim] = k1(j).to(dtype).to(DEV)[:, None]
+    c.dout.mul_(2.0 ** -6)
+    return c
+
+
+# name: q0, k0, k1, scale.  63 is no power of two, so a score's product with a factor is rounded, by up to half of
+#   a million 2^-4, 8 million 1/2, 2,000 million 2^7, 2^116 2^92     (in powers of two)
+SCORES = {"a million": (9 * 2.0 ** 7, lambda j: 7 * 2.0 ** 7 + 0 * j, lambda j: j * 31 % 97 / 8, 1.0),
+          "minus a million": (-9 * 2.0 ** 7, lambda j: 7 * 2.0 ** 7 + 0 * j, lambda j: j * 31 % 97 / 8, 1.0),
+          "8 million": (9 * 2.0 ** 10, lambda j: 7 * 2.0 ** 7 + 0 * j, lambda j: j * 3 % 4, 1.0),
+          "2,000 million": (9 * 2.0 ** 10, lambda j: torch.where(j % 50 == 33, 7, 6) * 2.0 ** 10, lambda j: 0.0 * j, 32.0),
+          "minus 2,000 million": (-9 * 2.0 ** 10, lambda j: torch.where(j % 50 == 33, 7, 8) * 2.0 ** 10, lambda j: 0.0 * j, 32.0),
+          "2^116": (9 * 2.0 ** 10, lambda j: torch.where(j % 50 == 33, 7, 6) * 2.0 ** 10, lambda j: 0.0 * j, 2.0 ** 90)}
+LENGTHS = [(150, 150, True, 2, 1, 64), (40, 700, False, 2, 2, 128), (1, 2111, False, 2, 2, 64), (600, 600, True, 4, 1, 128),
+           (33, 1111, True, 2, 2, 80)]
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("name", SCORES)
+@pytest.mark.parametrize("n,m,causal,heads,kv_heads,head_dim", LENGTHS)
+def test_far_scores(gpu, dtype, name, n, m, causal, heads, kv_heads, head_dim):
+    """Finite scores of any size: weights depend on their differences alone, which are small, or so large that only the
+    best keys count, alike."""
+    c = far_case(dtype, n, m, causal, heads, kv_heads, head_dim, *SCORES[name])
+    c.forward()
+    want, size = defined(c)
+    u = unit(dtype)
+    assert_rows(c.out, want["out"], u, "out")
+    # two roundings of a sum as large as lse itself, and its own
+    assert bool(((c.lse.double() - want["lse"]).abs() <= 2.0 ** -22 * want["lse"].abs()).all())
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("n,m,causal,heads,kv_heads,head_dim", LENGTHS)
+def test_scores_above_fp32(gpu, dtype, n, m, causal, heads, kv_heads, head_dim):
+    """The product of q and k is a number, that with the scale is not: the best keys are."""
+    c = far_case(dtype, n, m, causal, heads, kv_heads, head_dim, *SCORES["2,000 million"][:3], 2.0 ** 110)
+    c.forward()
+    assert_rows(c.out, defined(c)[0]["out"], unit(dtype), "out")
+    assert bool((c.lse == INF).all())
