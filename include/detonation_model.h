@@ -255,7 +255,8 @@ int detonation_rotary(const deto_rotary* cfg, int64_t T, const deto_rows* x, con
  * (all of them; under `causal` those with j <= i + Lk - Lq):
  *     s_j = scale * q_i . k_j      lse = log sum_j exp(s_j)      p_j = exp(s_j - lse)      out_i = sum_j p_j v_j
  * A query that sees no key, or whose scores are all -infinity, has out = 0 and lse = -infinity.  What a query does not
- * see does not reach it, whatever it holds; rows of no sequence are neither read into a result nor written.
+ * see does not reach it, whatever it holds; rows of no sequence are neither read into a result nor written.  Products
+ * q_i . k_j of any size that fp32 holds are taken, with the scale above it as well: lse is infinite then, and out right.
  *
  *   q, out     [Tq, heads * head_dim];  k, v  [Tk, kv_heads * head_dim]: all of one type
  *   lse        device, [heads, Tq] fp32; may be NULL in the forward call

@@ -40,6 +40,11 @@ __device__ __forceinline__ float stored_lse(float lse) {
     return lse == -__builtin_inff() ? __builtin_inff() : lse * kLog2E;
 }
 
+// lse is as it was written, rounded in proportion to its size: above this, in powers of two, by as much as 2^-13 (weights are
+// off by 1e-4 then, about what a score of that size is, whose product is rounded as well).  Such a query's largest score and
+// its sum are taken again, in a walk of their own, and its base is both of them.
+constexpr float kFarLse = 1024.f;
+
 // the sum of the products of two rows, each half of the lanes holding its part of them
 template <class S>
 __device__ __forceinline__ float rows_dot(const u32x4 (&x)[S::kFrags], const u32x4 (&y)[S::kFrags]) {
@@ -74,11 +79,12 @@ __global__ __launch_bounds__(W * kLanes) __attribute__((amdgpu_waves_per_eu(kRes
     constexpr int AHEAD = kAhead<W, kStep, DIRECT>;
     extern __shared__ __align__(16) char lds[];          // AHEAD + 1 steps of keys and values
     __shared__ uint32_t odd;                             // infinities or NaNs among keys that not all queries see
+    __shared__ uint32_t far[W];                          // queries of a wavefront with a far lse
     Place at;
     if (!place_of(a, a.q_starts, a.Tq, BM, a.heads, a.causal, at)) return;
     const Sequence seq = sequence_of(a, at.s);
-    const int D = a.head_dim, lane = threadIdx.x % kLanes, half = lane / kSide;
-    const int i0 = at.tile * BM, w0 = i0 + uniform(static_cast<int32_t>(threadIdx.x / kLanes)) * kSide, i = w0 + lane % kSide, last = seq.Lq - 1;
+    const int D = a.head_dim, lane = threadIdx.x % kLanes, half = lane / kSide, wave = uniform(static_cast<int32_t>(threadIdx.x / kLanes));
+    const int i0 = at.tile * BM, w0 = i0 + wave * kSide, i = w0 + lane % kSide, last = seq.Lq - 1;
     const bool there = i <= last;
 
     const auto seen = [&](int n) {
@@ -110,30 +116,90 @@ __global__ __launch_bounds__(W * kLanes) __attribute__((amdgpu_waves_per_eu(kRes
         rk.end(buffer(step));
         rv.end(buffer(step) + kMatrix);
     };
+    // a walk's first steps on their way; the wait for one of its steps, and another one on its way
+    const auto start = [&](int first, int to) __attribute__((always_inline)) {
+#pragma unroll
+        for (int n = 0; n < AHEAD; ++n)
+            if (first + n < to) begin(first + n);
+        if (first < to) end(first);
+    };
+    const auto arrive = [&](int step, int to) __attribute__((always_inline)) {
+        if constexpr (DIRECT) arrived_but<2 * Rows<S, BN, W, DIRECT>::kCalls>(min(AHEAD - 1, to - 1 - step));
+        meet();
+        if (step + AHEAD < to) begin(step + AHEAD);
+    };
+    const auto leave = [&](int step, int to) __attribute__((always_inline)) {
+        if (step + AHEAD < to) end(step + AHEAD);
+    };
     if (threadIdx.x == 0) odd = 0;
     if constexpr (DIRECT) clear<S, W>(lds, (AHEAD + 1) * kStep, D);
-#pragma unroll
-    for (int n = 0; n < AHEAD; ++n)
-        if (from + n < steps) begin(from + n);
-    if (from < steps) end(from);
+    start(from, steps);
 
-    const float factor = a.scale * kLog2E;
+    const float factor = factor_of(a.scale);
+    const Places places = places_of<S>();
     u32x4 q[S::kFrags], g[S::kFrags];
     load_row<S, DIRECT>(grad, there, D, g);
     load_row<S, DIRECT>(a.out.data + row * a.out.ld + col, there, D, q);
-    const float lse = there ? stored_lse(a.lse[at.head * a.Tq + row]) : __builtin_inff();
+    const float lse = there ? a.lse[at.head * a.Tq + row] : -__builtin_inff();
     const float delta = rows_dot<S>(g, q);
-    if (there && half == 0 && split == 0) {
-        a.stats[at.head * a.Tq + row] = lse;
-        a.stats[(a.heads + at.head) * a.Tq + row] = delta;
-    }
     load_row<S, DIRECT>(query, there, D, q);
+
+    Base base = {0.f, stored_lse(lse)};
+    const bool own_far = fabsf(base.power) > kFarLse && lse > -__builtin_inff();
+    const uint64_t wave_far = __ballot(own_far);
+    if (lane == 0) far[wave] = wave_far != 0;
+    if (from < steps) arrive(from, steps);
+    else meet();
+    bool any_far = false;
+#pragma unroll
+    for (int w = 0; w < W; ++w) any_far |= uniform(static_cast<int32_t>(far[w])) != 0;
+    if (any_far) {
+        if constexpr (DIRECT) arrived<0>();
+        meet();
+        float top = -__builtin_inff(), sum = 0.f;
+        start(0, all_steps);
+        for (int step = 0; step < all_steps; ++step) {
+            arrive(step, all_steps);
+            if (step * BN < wave_upto) {
+                const int left = own - step * BN - half * 4;
+#pragma unroll 1
+                for (int b = 0; b < BN / kSide; ++b) {
+                    f32x16 x = block_product<S>(buffer(step) + b * kSide * S::kRow, places, q);
+                    float most = -__builtin_inff();
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) {
+                        if (b * kSide + (r / 4) * 8 + r % 4 >= left) x[r] = -__builtin_inff();
+                        most = fmaxf(most, x[r]);
+                    }
+                    most = halves_max(most);
+                    if (most > top) {
+                        sum *= power2((top - most) * factor);
+                        top = most;
+                    }
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) sum += top > -__builtin_inff() ? power2((x[r] - top) * factor) : 0.f;
+                }
+            }
+            leave(step, all_steps);
+        }
+        sum = halves_sum(sum);
+        if (own_far) base = {top, __builtin_amdgcn_logf(sum)};
+        meet();
+        start(from, steps);
+        if (from < steps) arrive(from, steps);
+    }
+    if (there && half == 0 && split == 0) {
+        float* const stats = a.stats + at.head * a.Tq + row;
+        const int64_t plane = a.heads * a.Tq;
+        stats[0] = base.power;
+        stats[plane] = delta;
+        stats[2 * plane] = base.score;
+    }
     f32x16 dq[S::kBlocks] = {}, mean[MEAN ? S::kBlocks : 1] = {};
     float rest = 0.f;
 
-    const Places places = places_of<S>();
-    const auto compute = [&](int step, auto masked, auto clean) __attribute__((always_inline)) {
-        constexpr bool MASKED = masked.value != 0;
+    const auto compute = [&](int step, auto masked, auto slow) __attribute__((always_inline)) {
+        constexpr bool MASKED = masked.value != 0, SLOW = slow.value != 0;
         const char* const from = buffer(step);
         const int left = own - step * BN - half * 4;
 #pragma unroll
@@ -143,44 +209,44 @@ __global__ __launch_bounds__(W * kLanes) __attribute__((amdgpu_waves_per_eu(kRes
 #pragma unroll
             for (int r = 0; r < 16; ++r) {
                 const bool shown = b * kSide + (r / 4) * 8 + r % 4 < left;
-                p[r] = power2(fmaf(p[r], factor, -lse));
+                p[r] = power2(SLOW ? base.above(p[r], factor) : fmaf(p[r], factor, -base.power));
                 if (MASKED) p[r] = shown ? p[r] : 0.f;
                 ds[r] = p[r] * (ds[r] - delta);
                 if (MASKED) ds[r] = shown ? ds[r] : 0.f;
                 if (S::DT != DETO_F32 || MEAN) rest += ds[r];
             }
-            columns_products<S, TWICE, MEAN, clean.value != 0>(rows_k, places, ds, p, dq, mean);
+            columns_products<S, TWICE, MEAN, SLOW>(rows_k, places, ds, p, dq, mean);
         }
     };
 
-    const auto arrive = [&](int step) __attribute__((always_inline)) {
-        if constexpr (DIRECT) arrived_but<2 * Rows<S, BN, W, DIRECT>::kCalls>(min(AHEAD - 1, steps - 1 - step));
-        meet();
-        if (step + AHEAD < steps) begin(step + AHEAD);
-    };
-    // (loops of their own: a branch between the forms in one would keep a second set of sums)
+    // (loops of their own: a branch between the forms in one would keep a second set of sums.  The first step is there.)
     int step = from;
-    for (; step < whole_steps; ++step) {
-        arrive(step);
-        if (step * BN < wave_upto) compute(step, Type<0>{}, Type<0>{});
-        if (step + AHEAD < steps) end(step + AHEAD);
-    }
-    for (; step < steps; ++step) {
-        arrive(step);
-        find_odd<S, BN, W>(buffer(step), &odd);
-        meet();
-        if (uniform(static_cast<int32_t>(odd))) break;
-        if (step * BN < wave_upto) compute(step, Type<1>{}, Type<0>{});
-        if (step + AHEAD < steps) end(step + AHEAD);
+    if (!any_far) {
+        for (; step < whole_steps; ++step) {
+            if (step > from) arrive(step, steps);
+            if (step * BN < wave_upto) compute(step, Type<0>{}, Type<0>{});
+            leave(step, steps);
+        }
+        for (; step < steps; ++step) {
+            if (step > from) arrive(step, steps);
+            find_odd<S, BN, W>(buffer(step), &odd);
+            meet();
+            if (uniform(static_cast<int32_t>(odd))) break;
+            if (step * BN < wave_upto) compute(step, Type<1>{}, Type<0>{});
+            leave(step, steps);
+        }
     }
     // From the first step on that has infinities or NaNs among the keys, the second product goes without them: its other
     // operand has zeros for what is masked, which they would pass by.  (The scores keep them: one that is -infinity is no
-    // weight.)  What they give to the queries that see them is added behind the stores.
-    for (const int first = step; step < steps; ++step) {
-        if (step > first) arrive(step);
+    // weight.)  What they give to the queries that see them is added behind the stores.  The same loop takes far queries.
+    const int slow_from = step;
+    for (; step < steps; ++step) {
+        if (step > slow_from) arrive(step, steps);
+        if (any_far) find_odd<S, BN, W>(buffer(step), &odd);
         if (step * BN < wave_upto) compute(step, Type<1>{}, Type<1>{});
-        if (step + AHEAD < steps) end(step + AHEAD);
+        leave(step, steps);
     }
+    if (any_far) meet();
 
     float* const part = a.parts + ((int64_t{split} * a.heads + at.head) * a.Tq + row) * part_row(D);
     rest = halves_sum(rest);
@@ -202,12 +268,12 @@ __global__ __launch_bounds__(W * kLanes) __attribute__((amdgpu_waves_per_eu(kRes
         if constexpr (MEAN) store_part<S>(mean, part + splits * a.heads * a.Tq * part_row(D), there, D);
         if (there && half == 0) a.parts[(2 * splits * part_row(D) + split) * a.heads * a.Tq + at.head * a.Tq + row] = rest;
     }
-    if (steps > whole_steps && odd) {
+    if (steps > slow_from && odd) {
         stored();
-        for (int j = whole_steps * BN; j < min(wave_upto, steps * BN); ++j) {
+        for (int j = slow_from * BN; j < min(wave_upto, steps * BN); ++j) {
             const char* const key = keys + j * a.k.ld;
             if (!row_is_odd<S>(key, D)) continue;
-            const float p = power2(fmaf(slow_dot<S>(query, key, D), factor, -lse));
+            const float p = power2(base.above(slow_dot<S>(query, key, D), factor));
             const float ds = p * (slow_dot<S>(grad, values + j * a.v.ld, D) - delta);
             if (!there || j >= own) continue;
             if (splits == 1) add_odd<S>(a.dq.data + row * a.dq.ld + col, key, D, ds * a.scale);
@@ -326,6 +392,7 @@ __global__ __launch_bounds__(W * kLanes) __attribute__((amdgpu_waves_per_eu(kRes
     extern __shared__ __align__(16) char lds[];          // AHEAD + 1 steps of queries and gradients of outputs; values
     __shared__ __align__(16) float stats[AHEAD + 1][HEADS][2 * BQ];      // lse and delta
     __shared__ uint32_t odd;                             // infinities or NaNs among rows that do not see all keys
+    __shared__ uint32_t far[W];                          // a far base among those that a wavefront has looked at
     Place at;
     if (!place_of(a, a.k_starts, a.Tk, BN, a.kv_heads, false, at)) return;
     const Sequence seq = sequence_of(a, at.s);
@@ -397,6 +464,18 @@ __global__ __launch_bounds__(W * kLanes) __attribute__((amdgpu_waves_per_eu(kRes
             for (int c = 0; c < 2 * BQ / kLanes; ++c) stats[s.buffer][0][c * kLanes + lane] = stat[0][c];
         }
     };
+    // Is any of the queries far?  The first ones are on their way together.
+    constexpr int kLooks = 4, kThreads = W * kLanes;
+    const int queries = seq.Lq - first_step * BQ, looks = queries * a.group;
+    const auto look = [&](int n) __attribute__((always_inline)) {
+        const int h = a.group == 1 ? 0 : n / queries;
+        return a.stats[(2 * a.heads + at.head * a.group + h) * a.Tq + seq.q0 + first_step * BQ + n - h * queries];
+    };
+    float looked[kLooks] = {};
+    if (looks > 0) {
+#pragma unroll
+        for (int n = 0; n < kLooks; ++n) looked[n] = look(min(static_cast<int>(threadIdx.x) + n * kThreads, looks - 1));
+    }
     if (threadIdx.x == 0) odd = 0;
     if constexpr (DIRECT) clear<S, W>(lds, (AHEAD + 1) * kStep + (STAY ? BN * S::kRow : 0), D);
     if constexpr (STAY) {
@@ -419,13 +498,14 @@ __global__ __launch_bounds__(W * kLanes) __attribute__((amdgpu_waves_per_eu(kRes
     u32x4 k[S::kFrags], v[S::kFrags];
     load_row<S, DIRECT>(key, there, D, k);
     if constexpr (!STAY) load_row<S, DIRECT>(value, there, D, v);
-    const float factor = a.scale * kLog2E;
+    const float factor = factor_of(a.scale);
     f32x16 dk[S::kBlocks] = {}, dv[S::kBlocks] = {};
 
     const Places places = places_of<S>();
     const char* const own_values = lds + (AHEAD + 1) * kStep + own_block * kSide * S::kRow;
-    const auto compute = [&](Step s, auto masked) __attribute__((always_inline)) {
-        constexpr bool MASKED = masked.value != 0;
+    const auto compute = [&](Step s, auto masked, auto slow) __attribute__((always_inline)) {
+        constexpr bool MASKED = masked.value != 0, SLOW = slow.value != 0;
+        const float* const scores = a.stats + (2 * a.heads + s.head + own_head) * a.Tq + seq.q0 + s.query;
         const char* const from = lds + s.buffer * kStep + 2 * own_head * kMatrix;
 #pragma unroll
         for (int b = 0; b < BQ / kSide; ++b) {
@@ -436,6 +516,7 @@ __global__ __launch_bounds__(W * kLanes) __attribute__((amdgpu_waves_per_eu(kRes
 #pragma unroll
             for (int r = 0; r < 16; ++r) {
                 const int t = (r / 4) * 8 + r % 4;
+                if constexpr (SLOW) p[r] -= scores[min(b * kSide + half * 4 + t, seq.Lq - s.query - 1)];
                 p[r] = power2(fmaf(p[r], factor, -stat[t]));
                 if (MASKED) p[r] = t >= own_from && t < upto ? p[r] : 0.f;
             }
@@ -453,19 +534,21 @@ __global__ __launch_bounds__(W * kLanes) __attribute__((amdgpu_waves_per_eu(kRes
     };
 
     // steps of one form, as long as they are (loops of their own: a branch between the two in one would keep a second set
-    // of sums)
-    const auto walk = [&](int& n, int upto, auto masked) __attribute__((always_inline)) {
-        constexpr bool MASKED = masked.value != 0;
-        while (n < upto && (now.query >= all_from && now.query + BQ <= seq.Lq) != MASKED) {
+    // of sums; one for all steps where a query is far)
+    const auto walk = [&](int& n, int upto, auto masked, auto slow) __attribute__((always_inline)) {
+        constexpr bool MASKED = masked.value != 0, SLOW = slow.value != 0;
+        while (n < upto) {
+            const bool whole = now.query >= all_from && now.query + BQ <= seq.Lq;
+            if (!SLOW && whole == MASKED) break;
             if constexpr (DIRECT) arrived_but<HEADS * (2 * Rows<S, BQ, W, DIRECT>::kCalls + 2 * BQ / kLanes)>(min(AHEAD - 1, total - 1 - n));
             meet();
             const bool more = n + AHEAD < total;
             if (more) begin(ahead);
-            if constexpr (MASKED) {
+            if (SLOW ? !whole : MASKED) {
                 take_out_odd<S, 2 * HEADS * BQ, W>(lds + now.buffer * kStep, &odd);
                 meet();
             }
-            if (now.query + BQ > wave_from) compute(now, masked);
+            if (now.query + BQ > wave_from) compute(now, masked, slow);
             if (more) {
                 end(ahead);
                 ahead = next(ahead);
@@ -474,11 +557,23 @@ __global__ __launch_bounds__(W * kLanes) __attribute__((amdgpu_waves_per_eu(kRes
             ++n;
         }
     };
+    bool own_far = false;
+#pragma unroll
+    for (int n = 0; n < kLooks; ++n) own_far |= looked[n] != 0.f;
+    for (int n = threadIdx.x + kLooks * kThreads; n < looks; n += kThreads) own_far |= look(n) != 0.f;
+    const uint64_t wave_far = __ballot(own_far);
+    if (lane == 0) far[wave] = wave_far != 0;
+    meet();
+    bool any_far = false;
+#pragma unroll
+    for (int w = 0; w < W; ++w) any_far |= uniform(static_cast<int32_t>(far[w])) != 0;
+
     char *const to_k = a.dk.data + row * a.dk.ld + kv, *const to_v = a.dv.data + row * a.dv.ld + kv;
     const auto all = [&](int& n, int upto) __attribute__((always_inline)) {
+        if (any_far) walk(n, upto, Type<1>{}, Type<1>{});
         while (n < upto) {
-            walk(n, upto, Type<0>{});
-            walk(n, upto, Type<1>{});
+            walk(n, upto, Type<0>{}, Type<0>{});
+            walk(n, upto, Type<1>{}, Type<0>{});
         }
     };
     int n = 0;
@@ -520,7 +615,8 @@ __global__ __launch_bounds__(W * kLanes) __attribute__((amdgpu_waves_per_eu(kRes
                 const char *const query = a.q.data + at_t * a.q.ld + col, *const grad = a.dout.data + at_t * a.dout.ld + col;
                 const bool odd_q = row_is_odd<S>(query, D), odd_g = row_is_odd<S>(grad, D);
                 if (!odd_q && !odd_g) continue;
-                const float p = power2(fmaf(slow_dot<S>(query, key, D), factor, -a.stats[h * a.Tq + at_t]));
+                const Base base = {a.stats[(2 * a.heads + h) * a.Tq + at_t], a.stats[h * a.Tq + at_t]};
+                const float p = power2(base.above(slow_dot<S>(query, key, D), factor));
                 const float ds = p * (slow_dot<S>(grad, value, D) - a.stats[(a.heads + h) * a.Tq + at_t]);
                 if (t < own || !there) continue;
                 add_odd<S>(a.dv.data + row * a.dv.ld + kv, grad, D, p);

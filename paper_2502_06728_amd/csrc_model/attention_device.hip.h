@@ -50,7 +50,7 @@ struct Matrix {
 struct Args {
     Matrix q, k, v, out, dout, dq, dk, dv;
     float* lse;
-    float* stats;                        // [2, heads, Tq]: lse in powers of two, and dout . out
+    float* stats;                        // [3, heads, Tq]: lse in powers of two (or a far base's power), dout . out, a far base's score
     const int32_t *q_starts, *k_starts;
     int64_t Tq, Tk, sequences;
     int32_t heads, kv_heads, group, head_dim, causal;
@@ -476,9 +476,11 @@ __device__ __forceinline__ u32x4 operand(const f32x16& w, int run) {
     }
     return r;
 }
-// ... and what the rounding took away, rounded in its turn
+// ... and what the rounding took away, rounded in its turn (of the number that was rounded: fused with the product that it
+// may be, the difference would have bits that depend on the loop it stands in)
 template <int DT>
 __device__ __forceinline__ u32x4 operand_rest(const f32x16& w, int run, const u32x4& rounded) {
+#pragma clang fp contract(off)
     u32x4 r;
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
@@ -682,7 +684,7 @@ inline int splits_of(const deto_attention* cfg, int64_t Tq, int64_t Tk, bool f32
     return static_cast<int>(n < 32 ? n : 32);
 }
 inline int64_t stats_floats(const deto_attention* cfg, int64_t Tq) {        // of the backward pass, to whole pieces
-    return (2 * cfg->heads * Tq + 3) / 4 * 4;
+    return (3 * cfg->heads * Tq + 3) / 4 * 4;
 }
 inline int64_t part_floats(const deto_attention* cfg, int64_t Tq, int splits) {
     return splits > 1 ? splits * cfg->heads * Tq * (2 * part_row(cfg->head_dim) + 2) : 0;

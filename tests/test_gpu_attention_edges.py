@@ -14,7 +14,7 @@ pytestmark = pytest.mark.gpu
 
 def defined(c):
     """out, lse, dq, dk and dv of a case of one sequence, all heads at once in 64 bits; infinite keys count as zeros in the
-    product that gives dq.  And the size of what is added up in dq."""
+    product that gives dq.  And the size of what is added up in dq: of its terms, and of those of their differences."""
     H, K, n, m = c.cfg.heads, c.cfg.kv_heads, len(c.q), len(c.k)
 
     def apart(t, heads):
@@ -31,11 +31,12 @@ def defined(c):
     p = torch.softmax(s, 2)
     out = p @ v
     ds = p * (g @ v.transpose(1, 2).contiguous() - (g * out).sum(2, keepdim=True))
+    terms = p * (g.abs() @ v.abs().transpose(1, 2).contiguous())
     k = torch.where(torch.isfinite(k), k, 0.0)
     dk, dv = (x.transpose(1, 2).contiguous() @ y for x, y in ((ds * c.cfg.scale, q), (p, g)))
     dk, dv = (t.unflatten(0, (K, H // K)).sum(1) for t in (dk, dv))
     return ({"out": together(out), "lse": torch.logsumexp(s, 2), "dq": together(ds @ k * c.cfg.scale), "dk": together(dk),
-             "dv": together(dv)}, together(ds.abs() @ k.abs() * c.cfg.scale))
+             "dv": together(dv)}, together((8 * ds.abs() + 2 * terms) @ k.abs() * c.cfg.scale))
 
 
 def unit(dtype):
@@ -44,14 +45,16 @@ def unit(dtype):
     return 64 * ref.FINE if dtype == F32 else ref.UNIT[dtype]
 
 
-def assert_rows(got, want, u, what):
-    """As a whole to u, each row to 4 u of its size or of the rows' mean size."""
+def assert_rows(got, want, u, what, low=0.0):
+    """As a whole to u, each row to 4 u of its size or of the rows' mean size, and `low` more."""
+    if got.dtype == F16:                                    # half of 2^-24 each is what a result below the normal range loses
+        low += 2.0 ** -25 * got.shape[1] ** 0.5
     got = got.double()
     assert bool(torch.isfinite(got).all()), what
     off, size = (got - want).norm(dim=1), want.norm(dim=1)
     say(what, float(off.norm() / size.norm()) / u)
-    assert float(off.norm()) <= u * float(size.norm()), what
-    assert bool((off <= 4 * u * torch.maximum(size, size.norm() / len(size) ** 0.5)).all()), what
+    assert float(off.norm()) <= u * float(size.norm()) + low * len(size) ** 0.5, what
+    assert bool((off <= 4 * (u * torch.maximum(size, size.norm() / len(size) ** 0.5) + low)).all()), what
 
 
 # ------------------------------------------------------------------ sequences without queries
@@ -184,3 +187,89 @@ def test_scores_above_fp32(gpu, dtype, n, m, causal, heads, kv_heads, head_dim):
     c.forward()
     assert_rows(c.out, defined(c)[0]["out"], unit(dtype), "out")
     assert bool((c.lse == INF).all())
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("name", SCORES)
+@pytest.mark.parametrize("n,m,causal,heads,kv_heads,head_dim", [x for x in LENGTHS if x[0] != 600])
+def test_gradients_of_far_scores(gpu, dtype, name, n, m, causal, heads, kv_heads, head_dim):
+    """The same of the gradients: lse, which they take, is known to a rounding of its size alone."""
+    if dtype == F16 and name == "2^116":
+        pytest.skip("above fp16's largest value")
+    c = far_case(dtype, n, m, causal, heads, kv_heads, head_dim, *SCORES[name])
+    c.forward()
+    c.backward()
+    want, size = defined(c)
+    u = unit(dtype)
+    # what fp16 does not hold is infinite; below its normal range p and ds are off by half of 2^-24 each, at random, and their
+    # sums by the root of as many times the other operand's size
+    low = 2.0 ** -25 if dtype == F16 else 0.0
+    group = heads // kv_heads
+    gradient = low * c.cfg.scale * (group * n) ** 0.5 * float(c.q.abs().max()) * 2 ** 0.5
+    fits = want["dk"].abs().amax(1) < 0.99 * torch.finfo(dtype).max
+    assert_rows(c.dv, want["dv"], u, "dv", low * (group * n * head_dim) ** 0.5 * 4 * 2.0 ** -6)
+    assert_rows(c.dk[fits], want["dk"][fits], u, "dk", gradient)
+    # where all keys are alike, a query's gradients cancel out, to what the terms of dout . v and dout . out are off by (those
+    # of a definition in 64 bits to 2^-44)
+    first = torch.arange(heads * head_dim, device=DEV) % head_dim == 0
+    cancel = low * c.cfg.scale * m ** 0.5 * float(c.k.abs().max())
+    assert bool(((c.dq.double() - want["dq"]).abs() <= u * size + 2.0 ** -44 * size.max() + 4 * cancel)[:, first].all())
+    few = c.k.clone()
+    few[:, 0::head_dim] = 0.0
+    assert_rows(c.dq[:, ~first], want["dq"][:, ~first], u, "dq", low * c.cfg.scale * float(few.double().norm()))
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("n,m,causal,heads,kv_heads,head_dim", LENGTHS)
+def test_gradient_of_values_where_scores_are_above_fp32(gpu, dtype, n, m, causal, heads, kv_heads, head_dim):
+    c = far_case(dtype, n, m, causal, heads, kv_heads, head_dim, *SCORES["2,000 million"][:3], 2.0 ** 110)
+    c.forward()
+    c.backward()
+    assert_rows(c.dv, defined(c)[0]["dv"], unit(dtype), "dv")
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_far_queries_among_others(gpu, dtype):
+    """One query of a block has scores of a million: the others' gradients keep their bits."""
+    n, at = 200, 77
+    c, other = (Case(dtype, [0, n], [0, n], 4, 2, 128, True, packed=False) for _ in range(2))
+    other.dout[at] = 0.0
+    other.q[at] *= 2.0 ** (10 if dtype == F16 else 17)
+    c.dout[at] = 0.0
+    for x in (c, other):
+        x.forward()
+        x.backward()
+    assert float(other.lse[:, at].abs().min()) > 1000
+    same = torch.arange(n, device=DEV) != at
+    for name in ("out", "dq"):
+        assert torch.equal(getattr(c, name)[same], getattr(other, name)[same]), name
+    # (weights of the query that is different times nothing)
+    assert torch.equal(c.dk, other.dk) and torch.equal(c.dv, other.dv)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("n,causal,heads,kv_heads,head_dim", [(150, True, 2, 1, 64), (150, False, 4, 1, 128), (70, True, 4, 2, 128)])
+def test_far_scores_and_infinities(gpu, dtype, n, causal, heads, kv_heads, head_dim):
+    """Both at once: a key without weight, and a row of gradients that is no number."""
+    at = 66
+    c = far_case(dtype, n, n, causal, heads, kv_heads, head_dim, *SCORES["a million"])
+    c.k[at, 0::head_dim] = -INF
+    c.forward()
+    c.backward()
+    want, _ = defined(c)
+    u = unit(dtype)
+    later = torch.arange(head_dim * heads, device=DEV) % head_dim >= 2
+    low = 2.0 ** -25 * n ** 0.5 * 4 if dtype == F16 else 0.0
+    assert_rows(c.out, want["out"], u, "out")
+    assert_rows(c.dv, want["dv"], u, "dv", low)
+    assert_rows(c.dk, want["dk"], u, "dk", low * float(c.q.abs().max()))
+    assert_rows(c.dq[:, later], want["dq"][:, later], u, "dq", low * head_dim ** 0.5)
+    assert not bool(c.dk[at].any()) and not bool(c.dv[at].any())
+    dk, dv, dq = c.dk.clone(), c.dv.clone(), c.dq.clone()
+    c.dout[at, 7::9] = NAN
+    c.backward()
+    same = torch.arange(n, device=DEV) != at
+    assert torch.equal(torch.nan_to_num(c.dq[same], 7.0), torch.nan_to_num(dq[same], 7.0))
+    if causal:
+        assert torch.equal(c.dk[at + 1:], dk[at + 1:]) and torch.equal(c.dv[at + 1:], dv[at + 1:])
+    assert bool(torch.isnan(c.dv[:at + 1, 7:head_dim:9]).all()) and bool(torch.isnan(c.dq[at]).all())
