@@ -213,7 +213,7 @@ __global__ __launch_bounds__(W * kLanes) __attribute__((amdgpu_waves_per_eu(kRes
                 if (MASKED) p[r] = shown ? p[r] : 0.f;
                 ds[r] = p[r] * (ds[r] - delta);
                 if (MASKED) ds[r] = shown ? ds[r] : 0.f;
-                if (S::DT != DETO_F32 || MEAN) rest += ds[r];
+                rest += ds[r];
             }
             columns_products<S, TWICE, MEAN, SLOW>(rows_k, places, ds, p, dq, mean);
         }

@@ -273,3 +273,30 @@ def test_far_scores_and_infinities(gpu, dtype, n, causal, heads, kv_heads, head_
     if causal:
         assert torch.equal(c.dk[at + 1:], dk[at + 1:]) and torch.equal(c.dv[at + 1:], dv[at + 1:])
     assert bool(torch.isnan(c.dv[:at + 1, 7:head_dim:9]).all()) and bool(torch.isnan(c.dq[at]).all())
+
+
+# ------------------------------------------------------------------ few keys
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("head_dim", [64, 128])
+@pytest.mark.parametrize("n", [3, 600])
+def test_an_only_key_gets_no_gradient(gpu, dtype, head_dim, n):
+    """The first query sees one key, whose weight is 1 whatever its score: alone it brings no gradient to any key."""
+    c = Case(dtype, [0, n], [0, n], 2, 1, head_dim, True, packed=False)
+    c.dout[1:] = 0.0
+    c.forward()
+    c.backward()
+    assert not bool(c.dk.any()) and not bool(c.dq.any())
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("head_dim", [64, 128])
+@pytest.mark.parametrize("n", [3, 600])
+@pytest.mark.parametrize("bad", [INF, NAN])
+def test_an_only_key_and_a_nan(gpu, dtype, head_dim, n, bad):
+    """... but where the gradient of its output is no number, its own is none."""
+    c = Case(dtype, [0, n], [0, n], 2, 1, head_dim, True, packed=False)
+    c.dout[0, ::7] = bad
+    c.forward()
+    c.backward()
+    assert bool(torch.isnan(c.dq[0]).all())
