@@ -287,8 +287,9 @@ int detonation_attention_forward(const deto_attention* cfg, int64_t Tq, int64_t 
  *     dp_j = dout_i . v_j      ds_j = p_j (dp_j - dout_i . out_i)
  *     dq_i = scale * sum_j ds_j k_j      dk_j = scale * sum_i ds_j q_i      dv_j = sum_i p_j dout_i
  * with the sums of dk and dv over all heads that read them.  dq, dk and dv are of q's type and shapes, written, not
- * added to.  Under fp16, ds above 65504 becomes infinite.  dout_i . out_i is taken as if out were not rounded, and ds
- * of a query's only key as 0.
+ * added to.  Under fp16, ds above 65504 becomes infinite, and p and ds below 2^-14 lose bits.  ds of a query's only key
+ * is taken as 0.  dout_i . out_i is taken as if out were not rounded, but for dq of queries that see more than 128 keys, in calls
+ * of 512 keys a sequence or more with head_dim above 96, and in fp32 in those of 128 or more.
  */
 int detonation_attention_backward(const deto_attention* cfg, int64_t Tq, int64_t Tk, const deto_rows* q,
                                   const deto_rows* k, const deto_rows* v, const deto_rows* out,

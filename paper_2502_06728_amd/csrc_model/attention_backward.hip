@@ -29,8 +29,12 @@ namespace {
 // 16-bit types take MEAN but for long walks over 128 features, whose registers it does not leave (4 x 2,048 tokens of 16
 // heads, MEAN 189 us, TWICE 158, neither 120), fp32 where there are few keys; TWICE where there is time for it
 // (8 x 114 queries of 12 heads over 512 keys, fp32: MEAN 46 us, without 36, errors 5.7e-7 both).
-// fewer keys a sequence take MEAN
+// Calls with fewer keys a sequence take MEAN.
 template <int DT> constexpr int64_t kFewKeys = DT == DETO_F32 ? 128 : 512;
+// In the others, queries that see up to this many get the sum of ds from a walk in front, so that short sequences are no
+// less exact beside long ones.  (Errors of a row of dq, weights from scores of a standard deviation of 1 and 2: of 2 keys
+// 4.1e-3 and 5.8e-3 without, of 32 1.9e-3 and 2.7e-3, of 128 1.7e-3 and 2.3e-3, and 1.7e-3 with it for all.)
+constexpr int kFewSeen = 128;
 // rows of all heads, up to which there is time for it in both kernels: a row's error may stand out among few, and the chip
 // is not full.  (16,384 rows of keys, 1 x 2,048 tokens of 32 heads over 8: 277 us without, 316 with it)
 constexpr int64_t kFewRows = 32 * kCUs;
@@ -131,9 +135,12 @@ __global__ __launch_bounds__(W * kLanes) __attribute__((amdgpu_waves_per_eu(kRes
     const auto leave = [&](int step, int to) __attribute__((always_inline)) {
         if (step + AHEAD < to) end(step + AHEAD);
     };
+    // (a walk in front of the others, whatever part of the keys this workgroup takes: see below)
+    const bool ahead = !MEAN && seen(i0) <= kFewSeen;
+    const int ahead_steps = min(all_steps, kFewSeen / BN), first_from = ahead ? 0 : from, first_to = ahead ? ahead_steps : steps;
     if (threadIdx.x == 0) odd = 0;
     if constexpr (DIRECT) clear<S, W>(lds, (AHEAD + 1) * kStep, D);
-    start(from, steps);
+    start(first_from, first_to);
 
     const float factor = factor_of(a.scale);
     const Places places = places_of<S>();
@@ -141,14 +148,14 @@ __global__ __launch_bounds__(W * kLanes) __attribute__((amdgpu_waves_per_eu(kRes
     load_row<S, DIRECT>(grad, there, D, g);
     load_row<S, DIRECT>(a.out.data + row * a.out.ld + col, there, D, q);
     const float lse = there ? a.lse[at.head * a.Tq + row] : -__builtin_inff();
-    const float delta = rows_dot<S>(g, q);
+    float delta = rows_dot<S>(g, q);
     load_row<S, DIRECT>(query, there, D, q);
 
     Base base = {0.f, stored_lse(lse)};
     const bool own_far = fabsf(base.power) > kFarLse && lse > -__builtin_inff();
     const uint64_t wave_far = __ballot(own_far);
     if (lane == 0) far[wave] = wave_far != 0;
-    if (from < steps) arrive(from, steps);
+    if (first_from < first_to) arrive(first_from, first_to);
     else meet();
     bool any_far = false;
 #pragma unroll
@@ -184,6 +191,30 @@ __global__ __launch_bounds__(W * kLanes) __attribute__((amdgpu_waves_per_eu(kRes
         }
         sum = halves_sum(sum);
         if (own_far) base = {top, __builtin_amdgcn_logf(sum)};
+        meet();
+        start(first_from, first_to);
+        if (first_from < first_to) arrive(first_from, first_to);
+    }
+    if (ahead) {
+        // the sum of ds alone, in front of the walk that needs dout . out exact, of queries that see no other keys
+        float rest = 0.f;
+        for (int step = 0; step < ahead_steps; ++step) {
+            if (step > 0) arrive(step, ahead_steps);
+            if (step * BN < wave_upto) {
+                const int left = own - step * BN - half * 4;
+#pragma unroll 1
+                for (int b = 0; b < BN / kSide; ++b) {
+                    const char* const rows_k = buffer(step) + b * kSide * S::kRow;
+                    const f32x16 x = block_product<S>(rows_k, places, q), dp = block_product<S>(rows_k + kMatrix, places, g);
+#pragma unroll
+                    for (int r = 0; r < 16; ++r)
+                        rest += b * kSide + (r / 4) * 8 + r % 4 < left ? power2(base.above(x[r], factor)) * (dp[r] - delta) : 0.f;
+                }
+            }
+            leave(step, ahead_steps);
+        }
+        rest = halves_sum(rest);
+        if (own <= kFewSeen) delta += rest;
         meet();
         start(from, steps);
         if (from < steps) arrive(from, steps);

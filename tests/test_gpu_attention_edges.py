@@ -191,7 +191,7 @@ def test_scores_above_fp32(gpu, dtype, n, m, causal, heads, kv_heads, head_dim):
 
 @pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("name", SCORES)
-@pytest.mark.parametrize("n,m,causal,heads,kv_heads,head_dim", [x for x in LENGTHS if x[0] != 600])
+@pytest.mark.parametrize("n,m,causal,heads,kv_heads,head_dim", LENGTHS)
 def test_gradients_of_far_scores(gpu, dtype, name, n, m, causal, heads, kv_heads, head_dim):
     """The same of the gradients: lse, which they take, is known to a rounding of its size alone."""
     if dtype == F16 and name == "2^116":
@@ -300,3 +300,32 @@ def test_an_only_key_and_a_nan(gpu, dtype, head_dim, n, bad):
     c.forward()
     c.backward()
     assert bool(torch.isnan(c.dq[0]).all())
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("heads,kv_heads,head_dim,causal", [(2, 2, 128, False), (4, 2, 104, False), (2, 1, 64, False), (4, 1, 128, True)])
+def test_short_sequences_beside_long_ones(gpu, dtype, heads, kv_heads, head_dim, causal):
+    """The gradients of a short sequence are as exact as without its neighbours."""
+    short, n = 30, 2
+    starts = [n * i for i in range(short + 1)] + [n * short + 2000 * (i + 1) for i in range(11)]
+    c = Case(dtype, starts, starts, heads, kv_heads, head_dim, causal)
+    c.q.mul_(2.0)                                           # weights that differ
+    c.forward()
+    c.backward()
+    m = n * short
+    want = ref.whole(c.q[:m], c.k[:m], c.v[:m], c.dout[:m], heads, kv_heads, c.cfg.scale, causal, short)
+    for name in ("out", "dq", "dk", "dv"):
+        assert_rows(getattr(c, name)[:m], want[name], unit(dtype), name)
+
+
+@pytest.mark.parametrize("dtype,heads,kv_heads,head_dim,L", [
+    (BF16, 32, 8, 128, 2100), (F16, 16, 16, 128, 1000), (BF16, 64, 16, 104, 700), (BF16, 2, 2, 128, 2000)])
+def test_the_first_queries_of_a_long_sequence(gpu, dtype, heads, kv_heads, head_dim, L):
+    """Those that see a few keys, apart from the others."""
+    c = Case(dtype, [0, L], [0, L], heads, kv_heads, head_dim, True, packed=False)
+    c.q.mul_(2.0)
+    c.forward()
+    c.backward()
+    n = 4
+    w = ref.whole(c.q[:n], c.k[:n], c.v[:n], c.dout[:n], heads, kv_heads, c.cfg.scale, True, 1)
+    assert_rows(c.dq[1:n], w["dq"][1:], unit(dtype), "dq")
