@@ -699,6 +699,7 @@ int detonation_attention_backward(const deto_attention* cfg, int64_t Tq, int64_t
     }
     const hipStream_t on = static_cast<hipStream_t>(stream);
     int planned = DETO_OK;
+    bool launch = false;
     fresh();
     by_type(dtype, [&](auto dt) {
         return by_shape<dt.value>(cfg->head_dim, in_words(a.q) && in_words(a.k) && in_words(a.v) && in_words(a.dout),
@@ -709,7 +710,7 @@ int detonation_attention_backward(const deto_attention* cfg, int64_t Tq, int64_t
                 constexpr int W = waves.value, kStep = 2 * kKeys<S, W> * S::kRow;
                 constexpr bool MEAN = mean.value, TWICE = twice.value;
                 if (!plan(a, cfg->q_starts, Tq, W * kSide, H)) return DETO_ERR_UNSUPPORTED;
-                if (Tq) {
+                if (Tq && launch) {
                     const dim3 grid(a.tiles * H, splits);
                     queries_kernel<S, W, MEAN, TWICE, DIRECT><<<grid, W * kLanes, (kAhead<W, kStep, DIRECT> + 1) * kStep, on>>>(a);
                     if (splits > 1) join_kernel<S, W, MEAN><<<dim3(grid.x, kSide), W * kLanes, 0, on>>>(a, splits);
@@ -720,7 +721,7 @@ int detonation_attention_backward(const deto_attention* cfg, int64_t Tq, int64_t
                 constexpr int W = waves.value, HEADS = heads.value, BN = W / HEADS * kSide, kStep = 2 * HEADS * kQueries * S::kRow;
                 constexpr int kLds = (kAheadOfKeys<S, HEADS, DIRECT> + 1) * kStep + (kValuesStay<S> ? BN * S::kRow : 0);
                 if (!plan(a, cfg->k_starts, Tk, BN, K)) return DETO_ERR_UNSUPPORTED;
-                if (Tk) keys_kernel<S, W, HEADS, twice.value, DIRECT><<<a.tiles * K, W * kLanes, kLds, on>>>(a);
+                if (Tk && launch) keys_kernel<S, W, HEADS, twice.value, DIRECT><<<a.tiles * K, W * kLanes, kLds, on>>>(a);
                 return DETO_OK;
             };
             constexpr bool kWide = S::DP == 128;
@@ -732,34 +733,41 @@ int detonation_attention_backward(const deto_attention* cfg, int64_t Tq, int64_t
                 return queries(Type<4>{}, mean, twice);
             };
             const bool few = Tk / cfg->sequences < kFewKeys<S::DT>, spare = Tq * H <= kFewRows;
-            if constexpr (S::DT == DETO_F32) {
-                planned = few ? queries(Type<4>{}, Type<1>{}, Type<0>{}) : by_waves(Type<0>{}, Type<0>{});
-            } else if constexpr (S::DU == 128) {
-                planned = !few ? by_waves(Type<0>{}, Type<1>{}) : spare ? queries(Type<4>{}, Type<1>{}, Type<1>{})
-                                                                        : queries(Type<4>{}, Type<1>{}, Type<0>{});
-            } else {
-                planned = spare ? queries(Type<4>{}, Type<1>{}, Type<1>{}) : by_waves(Type<1>{}, Type<0>{});
-            }
-            if (planned) return planned;
-            // (groups of four heads of 128, bf16, both passes of gradients, four and two heads at a time: 2 x 2,048 tokens of
-            // 32 heads 375 us and 424, 1 x 4,200 706 and 808, 1 x 6,000 1,338 and 1,315, 1 x 8,100 2,198 and 2,045; 12 packed
-            // sequences of up to 1,500, one at a time 520 us, two 399, four 445, the keys' kernel alone)
-            const auto by_heads = [&](auto twice) {
-                if constexpr (kWide && kResidentKeys<S> == 2) {
-                    if constexpr (DIRECT) {
-                        if (Tk * K < int64_t{160} * kCUs && a.group % 4 == 0) return keys(Type<8>{}, Type<4>{}, twice);
-                        if (Tk * K < int64_t{512} * kCUs && a.group % 2 == 0) return keys(Type<8>{}, Type<2>{}, twice);
-                    }
-                    if constexpr (!twice.value) {
-                        if (Tk * K >= int64_t{256} * kCUs) return keys(Type<8>{}, Type<1>{}, twice);
-                    }
+            const auto choose = [&]() -> int {
+                int rc;
+                if constexpr (S::DT == DETO_F32) {
+                    rc = few ? queries(Type<4>{}, Type<1>{}, Type<0>{}) : by_waves(Type<0>{}, Type<0>{});
+                } else if constexpr (S::DU == 128) {
+                    rc = !few ? by_waves(Type<0>{}, Type<1>{}) : spare ? queries(Type<4>{}, Type<1>{}, Type<1>{})
+                                                                       : queries(Type<4>{}, Type<1>{}, Type<0>{});
+                } else {
+                    rc = spare ? queries(Type<4>{}, Type<1>{}, Type<1>{}) : by_waves(Type<1>{}, Type<0>{});
                 }
-                return keys(Type<4>{}, Type<1>{}, twice);
+                if (rc) return rc;
+                // (groups of four heads of 128, bf16, both passes of gradients, four and two heads at a time: 2 x 2,048 tokens of
+                // 32 heads 375 us and 424, 1 x 4,200 706 and 808, 1 x 6,000 1,338 and 1,315, 1 x 8,100 2,198 and 2,045; 12 packed
+                // sequences of up to 1,500, one at a time 520 us, two 399, four 445, the keys' kernel alone)
+                const auto by_heads = [&](auto twice) {
+                    if constexpr (kWide && kResidentKeys<S> == 2) {
+                        if constexpr (DIRECT) {
+                            if (Tk * K < int64_t{160} * kCUs && a.group % 4 == 0) return keys(Type<8>{}, Type<4>{}, twice);
+                            if (Tk * K < int64_t{512} * kCUs && a.group % 2 == 0) return keys(Type<8>{}, Type<2>{}, twice);
+                        }
+                        if constexpr (!twice.value) {
+                            if (Tk * K >= int64_t{256} * kCUs) return keys(Type<8>{}, Type<1>{}, twice);
+                        }
+                    }
+                    return keys(Type<4>{}, Type<1>{}, twice);
+                };
+                if constexpr (S::DT != DETO_F32) {
+                    if (Tk * K <= kFewRows) return by_heads(Type<1>{});
+                }
+                return by_heads(Type<0>{});
             };
-            if constexpr (S::DT != DETO_F32) {
-                if (Tk * K <= kFewRows) return planned = by_heads(Type<1>{});
-            }
-            return planned = by_heads(Type<0>{});
+            // (all of it is planned before any of it is launched)
+            planned = choose();
+            launch = true;
+            return planned ? planned : choose();
         });
     });
     return planned ? planned : enqueued();

@@ -329,3 +329,22 @@ def test_the_first_queries_of_a_long_sequence(gpu, dtype, heads, kv_heads, head_
     n = 4
     w = ref.whole(c.q[:n], c.k[:n], c.v[:n], c.dout[:n], heads, kv_heads, c.cfg.scale, True, 1)
     assert_rows(c.dq[1:n], w["dq"][1:], unit(dtype), "dq")
+
+
+# ------------------------------------------------------------------ refusals
+
+def test_backward_refuses_before_it_writes(gpu):
+    """Few queries, more tiles of keys than a launch counts: nothing was written."""
+    T, H = 1 << 16, 64
+    q, k = (torch.ones((n, H), dtype=BF16, device=DEV) for n in (1, T))
+    out, dq, dk, dv = (torch.full_like(t, NAN) for t in (q, q, k, k))
+    cfg = ops.Attention(heads=H, head_dim=1, scale=1.0, causal=False, sequences=T)
+    qs = torch.zeros(T + 1, dtype=torch.int32, device=DEV)
+    qs[1:] = 1
+    ks = torch.arange(T + 1, dtype=torch.int32, device=DEV)
+    ws = torch.full((ops.attention_workspace(cfg, 1, T),), 0xFF, dtype=torch.uint8, device=DEV)
+    lse = torch.zeros((H, 1), device=DEV)
+    with pytest.raises(ops.DetonationError):
+        ops.detonation_attention_backward(cfg, q, k, k, q, lse, q, dq, dk, dv, q_starts=qs, k_starts=ks, workspace=ws)
+    torch.cuda.synchronize()
+    assert bool(torch.isnan(dq).all()) and bool((ws == 0xFF).all())
