@@ -699,7 +699,8 @@ def detonation_attention_forward(cfg: Attention, q, k, v, out, *, lse=None, q_st
                                  stream=None) -> None:
     """out [Tq, heads * head_dim] from q (the same) and k, v [Tk, kv_heads * head_dim]; lse [heads, Tq], which the
     backward pass takes.  q_starts, k_starts: int32 [sequences + 1], the first rows of packed sequences and the row
-    behind the last one; None: sequences of one length."""
+    behind the last one; None: sequences of one length.  Without a workspace, calls that cut their walks over keys (few
+    queries, many keys) are refused."""
     if _taken((_marshal or _marshalling()).attention_forward(cfg, q, k, v, out, lse, q_starts, k_starts, workspace,
                                                              _handle(stream))):
         return
@@ -711,7 +712,7 @@ def detonation_attention_forward(cfg: Attention, q, k, v, out, *, lse=None, q_st
     qs, ks, vs = c.rows(q, "q", Tq, wide), c.rows(k, "k", Tk, narrow, q.dtype), c.rows(v, "v", Tk, narrow, q.dtype)
     os_, ls = c.rows(out, "out", Tq, wide, q.dtype), c.vector(lse, "lse", cfg.heads * Tq, (torch.float32,))
     need = lib.detonation_attention_workspace(ctypes.byref(s), Tq, Tk)
-    ws = c.scratch(workspace, need)
+    ws = None if workspace is None else c.scratch(workspace, need)       # (the library refuses a call that needs one)
     _disjoint({"out": out, "lse": lse, "workspace": (workspace, need)},
               {"q": q, "k": k, "v": v, "q_starts": q_starts, "k_starts": k_starts})
     _status(lib.detonation_attention_forward(ctypes.byref(s), Tq, Tk, ctypes.byref(qs), ctypes.byref(ks), ctypes.byref(vs),

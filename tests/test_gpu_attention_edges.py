@@ -348,3 +348,21 @@ def test_backward_refuses_before_it_writes(gpu):
         ops.detonation_attention_backward(cfg, q, k, k, q, lse, q, dq, dk, dv, q_starts=qs, k_starts=ks, workspace=ws)
     torch.cuda.synchronize()
     assert bool(torch.isnan(dq).all()) and bool((ws == 0xFF).all())
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_forward_without_a_workspace(gpu, dtype):
+    """A call that does not cut its walks needs none; one that does is refused."""
+    c = Case(dtype, even(3, 40), even(3, 40), 2, 1, 64, True)
+    c.forward()
+    want = c.out.clone()
+    c.clear()
+    c.ws = None
+    c.forward()
+    assert torch.equal(c.out, want)
+    c = Case(dtype, [0, 1], [0, 3000], 2, 1, 64, False)
+    c.ws = None
+    with pytest.raises(ops.DetonationError):
+        c.forward()
+    torch.cuda.synchronize()
+    assert bool(torch.isnan(c.out).all())
