@@ -264,9 +264,10 @@ int detonation_rotary(const deto_rotary* cfg, int64_t T, const deto_rows* x, con
  *              NULL.  Starts that are out of order or out of range leave results undefined, but no access is out of
  *              bounds.
  * head_dim is at most 128 (else DETO_ERR_UNSUPPORTED); kv_heads divides heads, which is at most 65536; scale is above
- * 0 and finite; Tq, Tk and sequences are at most 2^31 - 1, and without starts a multiple of `sequences`.  Tiles of 128
- * rows, with one more for each sequence, times heads are below 2^22 (else DETO_ERR_UNSUPPORTED).  Scores, their
- * statistics and all sums are fp32; p (and ds below) enter the second product rounded to the matrices' type.
+ * 0 and finite; sequences is at most 2^31 - 1; Tq and Tk are at most 2^31 - 512, and without starts a multiple of
+ * `sequences`.  Tiles of 128 rows, with one more for each sequence, times heads are below 2^22 (else
+ * DETO_ERR_UNSUPPORTED).  Scores, their statistics and all sums are fp32; p (and ds below) enter the second product
+ * rounded to the matrices' type.
  */
 typedef struct {
     int32_t heads, kv_heads, head_dim;

@@ -261,8 +261,8 @@ __global__ __launch_bounds__(kJoinWaves * kLanes) void join_kernel(Args a, int s
 
 int check(const deto_attention* cfg, int64_t Tq, int64_t Tk) {
     if (!cfg) return DETO_ERR_NULL;
-    constexpr int64_t kMost = (int64_t{1} << 31) - 1;
-    if (Tq < 0 || Tk < 0 || Tq > kMost || Tk > kMost || cfg->sequences < 1 || cfg->sequences > kMost)
+    constexpr int64_t kMostRows = (int64_t{1} << 31) - 512, kMostSequences = (int64_t{1} << 31) - 1;    // (a tile more is an int)
+    if (Tq < 0 || Tk < 0 || Tq > kMostRows || Tk > kMostRows || cfg->sequences < 1 || cfg->sequences > kMostSequences)
         return DETO_ERR_BAD_CONFIG;
     if (cfg->heads < 1 || cfg->heads > 65536 || cfg->kv_heads < 1 || cfg->heads % cfg->kv_heads || cfg->head_dim < 1)
         return DETO_ERR_BAD_CONFIG;

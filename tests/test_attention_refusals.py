@@ -1,11 +1,11 @@
 """What the operators of an attention block refuse, without a GPU, beside tests/test_attention_abi.py: problems that one of two
-launches cannot count, and outputs that meet an input in part."""
+launches cannot count, lengths at the end of an int, and outputs that meet an input in part."""
 import pytest
 import torch
 
 from paper_2502_06728_amd import model_ops as ops
 from tests.test_attention_abi import attention, m, vp  # noqa: F401
-from tests.test_model_abi import UNSUPPORTED, lib, rows  # noqa: F401
+from tests.test_model_abi import BAD, UNSUPPORTED, lib, rows  # noqa: F401
 from tests.test_model_marshal import OnDevice, mat
 
 
@@ -16,6 +16,16 @@ def test_more_tiles_than_either_launch_counts(lib, Tq, Tk, sequences):  # noqa: 
     cfg = attention(heads=64, kv_heads=64, head_dim=1, sequences=sequences, causal=0, **starts)
     r = rows(ld=64)
     assert lib.detonation_attention_backward(cfg, Tq, Tk, r, r, r, r, vp(4096), r, r, r, r, vp(4096), None) == UNSUPPORTED
+
+
+def test_lengths_that_a_step_would_count_past_an_int(lib):  # noqa: F811
+    """The step behind the last whole one of 2^31 - 1 keys begins in an int and ends outside."""
+    cfg, r, most = attention(heads=1, kv_heads=1, head_dim=1, sequences=1, causal=0), rows(ld=1), (1 << 31) - 512
+    for Tq, Tk in ((1, (1 << 31) - 1), (1, most + 1), ((1 << 31) - 1, 1), (most + 1, 0)):
+        assert lib.detonation_attention_workspace(cfg, Tq, Tk) == -1
+        assert lib.detonation_attention_forward(cfg, Tq, Tk, r, r, r, r, None, vp(4096), None) == BAD
+        assert lib.detonation_attention_backward(cfg, Tq, Tk, r, r, r, r, vp(4096), r, r, r, r, vp(4096), None) == BAD
+    assert lib.detonation_attention_workspace(cfg, 1, most) > 0
 
 
 def test_dropout_onto_other_columns_of_its_inputs(m):  # noqa: F811
