@@ -635,10 +635,10 @@ __device__ __forceinline__ float power2(float x) { return __builtin_amdgcn_exp2f
 // of scores, to powers of two
 __device__ __forceinline__ float factor_of(float scale) { return fminf(scale * kLog2E, 3.402823466e38f); }
 
-// What weights are relative to: that of score x is 2^((x - score) * factor - power).  One of the two is zero.  Of scores in
-// reach it is `score`: the difference to a rounded power is exact in one operation, and the rounding is the same for all
-// weights.  Out of it a power would be rounded by more than a weight may be off by, up to all of its range, so there the
-// scores are subtracted first.
+// What weights are relative to: that of score x is 2^((x - score) * factor - power).  Of scores in reach it is `power` alone:
+// the difference to a rounded power is exact in one operation, and the rounding is the same for all weights.  Out of it a
+// power would be rounded by more than a weight may be off by, up to all of its range, so there the scores are subtracted
+// first.
 constexpr float kReach = 1 << 20;
 struct Base {
     float score, power;
@@ -649,11 +649,11 @@ struct Base {
         return fmaf(score - other.score, factor, power - other.power);
     }
 };
-// (-infinity stays a power: of nothing)
-__device__ __forceinline__ Base base_of(float score, float factor) {
+// the one under which this score weighs 2^up (-infinity stays a power: of nothing)
+__device__ __forceinline__ Base base_of(float score, float factor, float up) {
     const float power = score * factor;
     const bool far = score > -__builtin_inff() && !(fabsf(power) < kReach);
-    return {far ? score : 0.f, far ? 0.f : power};
+    return {far ? score : 0.f, (far ? 0.f : power) - up};
 }
 __device__ __forceinline__ float log_sum(const Base& base, float total, float scale) {
     return total == 0.f ? -__builtin_inff() : fmaf(base.score, scale, (base.power + __builtin_amdgcn_logf(total)) * kLn2);

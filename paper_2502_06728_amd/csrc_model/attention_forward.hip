@@ -18,8 +18,10 @@ namespace {
 
 // Weights are powers of two of a score less the query's base.  The base is the largest score of the first keys, and it
 // stays until a step's weights, which a lane adds up anyway, pass this: no step needs its scores' maximum, and the sums
-// so far are seldom scaled down.  (Weights this large are numbers in fp16, and have as many bits as others.)
-constexpr float kMost = 8192.f;
+// so far are seldom scaled down.  fp16 has numbers up to 65504, and few below 1: there the largest of the first keys weighs
+// 2^10, so that all of a weight's bits stay down to 2^-24 of that, which thousands of other keys may add up to.
+template <int DT> constexpr float kUp = DT == DETO_F16 ? 10.f : 0.f;
+template <int DT> constexpr float kMost = DT == DETO_F16 ? 61440.f : 8192.f;
 
 template <class S, int W, bool DIRECT>
 __global__ __launch_bounds__(W * kLanes) __attribute__((amdgpu_waves_per_eu(kResident<S>, kResident<S>)))
@@ -76,7 +78,7 @@ void forward_kernel(Args a) {
     u32x4 q[S::kFrags];
     load_row<S, DIRECT>(queries + (i < last ? i : last) * a.q.ld, i <= last, D, q);
     Base base = {0.f, own > 0 ? -__builtin_inff() : 0.f};
-    float l = 0.f, most = kMost;
+    float l = 0.f, most = kMost<S::DT>;
     f32x16 o[S::kBlocks] = {};
     const Places places = places_of<S>();
     f32x16 x[NB];                                        // scores of a step, computed in the one before
@@ -112,7 +114,7 @@ void forward_kernel(Args a) {
     // (a far base's weights are always taken the second way)
     const auto set = [&](Base to) __attribute__((always_inline)) {
         base = to;
-        most = to.far() ? -1.f : kMost;
+        most = to.far() ? -1.f : kMost<S::DT>;
     };
     // weights of a step's scores, their products with its values, and the next step's scores (the last step's again
     // behind it: a branch here would keep the three from sharing the time)
@@ -128,8 +130,8 @@ void forward_kernel(Args a) {
             if (MASKED) hide(step);
             const float top = largest();
             // (a query's two lanes do the same, whatever the others do)
-            if ((high | high << kSide | high >> kSide) >> lane & 1 && base.above(top, factor) > 0.f) {
-                const Base risen = base_of(top, factor);
+            if ((high | high << kSide | high >> kSide) >> lane & 1 && base.above(top, factor) > kUp<S::DT>) {
+                const Base risen = base_of(top, factor, kUp<S::DT>);
                 const float less = power2(base.over(risen, factor));
                 set(risen);
                 l *= less;
@@ -153,7 +155,7 @@ void forward_kernel(Args a) {
         meet();
         rows_product<S, NB>(buffer(from), places, q, x);
         const float top = largest();
-        if (own > 0 && from < whole_steps) set(base_of(top, factor));           // (what is masked makes no base too low)
+        if (own > 0 && from < whole_steps) set(base_of(top, factor, kUp<S::DT>));           // (what is masked makes no base too low)
     }
     // (two loops: a branch between the two forms in one would keep a second set of sums)
     const auto walk = [&](int& step, int to, auto masked) __attribute__((always_inline)) {
@@ -223,7 +225,7 @@ __global__ __launch_bounds__(kJoinWaves * kLanes) void join_kernel(Args a, int s
     const Base base = {own ? bases[lane * rows] : 0.f, own ? bases[(splits + lane) * rows] : -__builtin_inff()};
     const float sum = own ? bases[(2 * splits + lane) * rows] : 0.f, factor = factor_of(a.scale);
     // the highest one: by its power, and the far ones that are rounded to the same by their scores
-    const float power = base.far() ? base.score * factor : base.power;
+    const float power = base.far() ? base.score * factor + base.power : base.power;
     float top = power;
 #pragma unroll
     for (int by = 1; by < kLanes; by *= 2) top = fmaxf(top, __shfl_xor(top, by));
@@ -232,7 +234,7 @@ __global__ __launch_bounds__(kJoinWaves * kLanes) void join_kernel(Args a, int s
         float score = power == top && base.far() ? base.score : -__builtin_inff();
 #pragma unroll
         for (int by = 1; by < kLanes; by *= 2) score = fmaxf(score, __shfl_xor(score, by));
-        if (score > -__builtin_inff()) highest = {score, 0.f};
+        if (score > -__builtin_inff()) highest = {score, -kUp<S::DT>};
     }
     const float less = sum == 0.f ? 0.f : power2(base.over(highest, factor));          // (of a part that the query sees nothing of: 0)
     const float total = wave_sum(sum * less);

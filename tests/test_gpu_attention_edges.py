@@ -1,5 +1,7 @@
 """Attention where few tests go: sequences without queries under grouped heads, infinities that are seen, scores so large that
 fp32 does not hold them to a unit, queries with few keys beside long sequences, calls without a workspace."""
+import math
+
 import pytest
 import torch
 
@@ -366,3 +368,26 @@ def test_forward_without_a_workspace(gpu, dtype):
         c.forward()
     torch.cuda.synchronize()
     assert bool(torch.isnan(c.out).all())
+
+
+# ------------------------------------------------------------------ weights below fp16's range
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("first,n", [(2, 40), (99, 1), (4090, 200)])
+def test_many_light_keys(gpu, dtype, first, n):
+    """One key outweighs each of the others by 2^26, and all of them by 2^9 alone: what they add up to is there."""
+    m, scale = 1 << 17, 1.0
+    c = Case(dtype, [0, n], [0, m], 1, 1, 16, False, packed=False, scale=scale)
+    c.q.zero_()
+    c.q[:, 0] = 1.0
+    c.k.zero_()
+    c.k[first, 0] = 18.0                                    # 2^26 = exp(18.02)
+    c.v.fill_(1.0)
+    c.v[first, ::2] = 0.0                                   # (odd features: the weights' sum)
+    c.forward()
+    rest = (m - 1) * math.exp(-18.0)
+    light = rest / (1 + rest)
+    # rounding of the result, and of weights, all alike: half a step each; sums of 4,096 steps of fp32
+    u = ref.UNIT[dtype] * 2 + (m / 32 + 64) * ref.FINE
+    assert bool(((c.out[:, ::2].double() - light).abs() <= u * light).all()), (float(c.out[0, 0]), light)
+    assert bool(((c.out[:, 1::2].double() - 1).abs() <= u).all())
