@@ -289,8 +289,8 @@ int detonation_attention_forward(const deto_attention* cfg, int64_t Tq, int64_t 
  *     dq_i = scale * sum_j ds_j k_j      dk_j = scale * sum_i ds_j q_i      dv_j = sum_i p_j dout_i
  * with the sums of dk and dv over all heads that read them.  dq, dk and dv are of q's type and shapes, written, not
  * added to.  Under fp16, ds above 65504 becomes infinite, and p and ds below 2^-14 lose bits.  ds of a query's only key
- * is taken as 0.  dout_i . out_i is taken as if out were not rounded, but for dq of queries that see more than 128 keys, in calls
- * of 512 keys a sequence or more with head_dim above 96, and in fp32 in those of 128 or more.
+ * is taken as 0.  dout_i . out_i is taken as if out were not rounded, but for dq in calls of 128 keys a sequence or more
+ * (fp32), or of 512 or more (16 bits, head_dim above 96) and there of queries that see more than 128.
  */
 int detonation_attention_backward(const deto_attention* cfg, int64_t Tq, int64_t Tk, const deto_rows* q,
                                   const deto_rows* k, const deto_rows* v, const deto_rows* out,

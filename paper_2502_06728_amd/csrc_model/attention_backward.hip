@@ -31,9 +31,10 @@ namespace {
 // (8 x 114 queries of 12 heads over 512 keys, fp32: MEAN 46 us, without 36, errors 5.7e-7 both).
 // Calls with fewer keys a sequence take MEAN.
 template <int DT> constexpr int64_t kFewKeys = DT == DETO_F32 ? 128 : 512;
-// In the others, queries that see up to this many get the sum of ds from a walk in front, so that short sequences are no
-// less exact beside long ones.  (Errors of a row of dq, weights from scores of a standard deviation of 1 and 2: of 2 keys
-// 4.1e-3 and 5.8e-3 without, of 32 1.9e-3 and 2.7e-3, of 128 1.7e-3 and 2.3e-3, and 1.7e-3 with it for all.)
+// In the others, queries of 16-bit types that see up to this many get the sum of ds from a walk in front, so that short
+// sequences are no less exact beside long ones.  (Errors of a row of dq in bf16, weights from scores of a standard deviation
+// of 1 and 2: of 2 keys 4.1e-3 and 5.8e-3 without, of 32 1.9e-3 and 2.7e-3, of 128 1.7e-3 and 2.3e-3, and 1.7e-3 with it for
+// all.  In fp32 dout . out is off by its own roundings as much as by that of out.)
 constexpr int kFewSeen = 128;
 // rows of all heads, up to which there is time for it in both kernels: a row's error may stand out among few, and the chip
 // is not full.  (16,384 rows of keys, 1 x 2,048 tokens of 32 heads over 8: 277 us without, 316 with it)
@@ -136,7 +137,7 @@ __global__ __launch_bounds__(W * kLanes) __attribute__((amdgpu_waves_per_eu(kRes
         if (step + AHEAD < to) end(step + AHEAD);
     };
     // (a walk in front of the others, whatever part of the keys this workgroup takes: see below)
-    const bool ahead = !MEAN && seen(i0) <= kFewSeen;
+    const bool ahead = !MEAN && S::DT != DETO_F32 && seen(i0) <= kFewSeen;
     const int ahead_steps = min(all_steps, kFewSeen / BN), first_from = ahead ? 0 : from, first_to = ahead ? ahead_steps : steps;
     if (threadIdx.x == 0) odd = 0;
     if constexpr (DIRECT) clear<S, W>(lds, (AHEAD + 1) * kStep, D);
