@@ -4,11 +4,11 @@
 // but every sum has one owner, who adds in a fixed order.  The first launch leaves dout . out of every query for the
 // second.
 //
-// What bounds them: two wavefronts a SIMD, whose matrix products, exponentials and LDS reads only partly share the time;
-// sums of two gradients, or operands in two terms, fill the registers.  4 x 2,048 tokens of 16 heads of 128 under the mask,
-// bf16: queries 151 us (910 TFLOP/s in four products), keys 182 (755 in four); without what makes dout . out exact,
-// queries 120.  64 x 197 tokens of 12 heads of 64 in fp16: 41 and 48.  fp32, 8 x 114 queries over 512 keys: 35 + 11 (the
-// join) and 43, chains of a few steps each.
+// What bounds them: in 16 bits the wait for a step's own loads in its middle (see kLead of the forward walk), and two
+// wavefronts a SIMD, whose matrix products, exponentials and LDS reads only partly share the time; sums of two gradients, or
+// operands in two terms, fill the registers.  4 x 2,048 tokens of 16 heads of 128 under the mask, bf16: queries 156 us (880
+// TFLOP/s in four products), keys 184 (745 in four); without what makes dout . out exact, queries 120.  64 x 197 tokens of 12
+// heads of 64 in fp16: 40 and 48.  fp32, 8 x 114 queries over 512 keys: 35 + 11 (the join) and 44, chains of a few steps each.
 #include "attention_device.hip.h"
 
 namespace deto {
@@ -73,8 +73,8 @@ __device__ __forceinline__ float rows_dot(const u32x4 (&x)[S::kFrags], const u32
     return halves_sum(sum);
 }
 
-// Steps that are on their way while one is computed: three, where the workgroups that share a CU then have room in its
-// LDS (two of four wavefronts, or one of eight); a step that goes through registers is the only one.
+// Steps that are asked for ahead of the one that is computed: three, where the workgroups that share a CU then have room in
+// its LDS (two of four wavefronts, or one of eight); a step that goes through registers is the only one.
 template <int W, int STEP, bool DIRECT>
 constexpr int kAhead = !DIRECT ? 1 : STEP * 4 * (8 / W) <= 144 * 1024 ? 3 : 1;
 

@@ -131,8 +131,9 @@ __device__ __forceinline__ bool find_tile(const Args& a, const int32_t* starts, 
 
 // A workgroup's tile and head.  Workgroups go to the chip's eight parts in turn; heads are dealt out so that those in a
 // row, which share keys, meet in one part, whose own cache then holds these for all of them.  Under a mask the longest
-// tiles of all heads come first (`last_first`: those are the last ones), so that no long one is left over at the end;
-// without one, a head's tiles follow each other.
+// tiles of all heads and of all sequences of one length come first (`last_first`: those are the last ones), so that no long
+// one is left over at the end; packed sequences follow in their order, each one's longest tiles first.  Without a mask, a
+// head's tiles follow each other.
 struct Place {
     int64_t s;
     int32_t head, tile;
@@ -286,8 +287,10 @@ struct Rows {
     }
 };
 
-// The forward walk has the rows of two steps in LDS, which it computes with, and kLead - 2 steps more on their way; staged
-// through registers, one in these.
+// The forward walk has the rows of two steps in LDS, which it computes with, and asks for kLead - 2 steps more; staged
+// through registers, one is in these.  In 16 bits these do not stay on their way for long: the compiler takes the turned reads
+// of the columns form for reads of what the copies to LDS write, and waits for all of a wavefront's loads before the first of
+// them in each step, here and in the walks of both gradients.  (fp32 has none of these reads, nor that wait.)
 template <bool DIRECT> constexpr int kLead = DIRECT ? 3 : 2;
 template <bool DIRECT> constexpr int kBuffers = kLead<DIRECT> + 1;
 

@@ -5,10 +5,11 @@
 // are the second product's operand.  A step's exponentials and second product share the time with the next step's scores.
 //
 // What bounds it: long sequences the matrix cores, at the chip's power (16,384 tokens of 16 heads of 128 under the mask,
-// bf16: 1,020 us, 1.08 PFLOP/s; the library's products of 8,192^3 run at 1.06); 4 x 2,048 tokens (95 us, 0.72) also the
-// tiles' unequal lengths; 64 features the exponentials (64 x 197 tokens of 12 heads, fp16: 28 us); few queries a chain of
-// loads (one query over 2,048 keys of 16 heads: 7.4 us + 3.8 to join 16 parts, 45 in one part).  64 queries a wavefront
-// (one wavefront a SIMD) took 205 us at 4 x 2,048.
+// bf16: 1,040 us, 1.06 PFLOP/s, as the library's products of 8,192^3); 4 x 2,048 tokens (97 us, 0.71) the wait for loads in
+// each step (see kLead) and the tiles' unequal lengths; 64 x 197 tokens of 12 heads of 64 (fp16, 27 us) that wait in walks of
+// seven steps, the last one of five keys (all exponentials of the chip are some 4 us); few queries a chain of loads (one query
+// over 2,048 keys of 16 heads: 7.6 us + 4.2 to join 16 parts, 45 in one part).  64 queries a wavefront (one wavefront a SIMD)
+// took 205 us at 4 x 2,048.
 #include "attention_device.hip.h"
 
 namespace deto {
@@ -338,7 +339,10 @@ int detonation_attention_forward(const deto_attention* cfg, int64_t Tq, int64_t 
     a.lse = lse;
     a.parts = static_cast<float*>(workspace);
     int planned = DETO_OK;
-    // (4 x 2,048 bf16 rows of 16 heads of 128: eight wavefronts 92 us, four 103; 64 x 197 of 12 heads of 64: 37 and 27)
+    // (bf16, 16 heads of 128 under the mask, eight wavefronts and four: 16 x 512 rows 52 us and 48, 8 x 1,024 65 and 64,
+    // 5 x 1,536 78 and 80, 4 x 2,048 98 and 100, 2 x 4,096 157 and 171, 1 x 8,192 311 and 345; on half of the chip, 1 x 2,048,
+    // 60 and 56.  The gradients of queries meet at the same place: 8 x 1,024 both 196, 2 x 4,096 516 and 529, with those of
+    // keys.  64 features, 64 x 197 of 12 heads: 37 and 27)
     const bool wide = Tq * cfg->heads >= int64_t{256} * kCUs && Tq / cfg->sequences >= 2048;
     fresh();
     by_type(q->dtype, [&](auto dt) {

@@ -646,7 +646,7 @@ def rotary_frequencies(rotary_dim: int, *, base: float = 10000.0, factor: float 
     """Angles of one position for rotary_dim / 2 pairs, base ** (-2 i / rotary_dim), in 64 bits on `device`.  For
     contexts `factor` times as long as the `trained` one, wavelengths that it holds `often` times or more stay, those
     that it holds `once` or less become factor times as long, and those between are blended by how often it holds
-    them; trained = 0 lengthens all of them."""
+    them (Peng, Quesnelle, Fan and Shippole, 2023); trained = 0 lengthens all of them."""
     import math
 
     import torch
