@@ -9,7 +9,7 @@ from paper_2502_06728_amd import model_ops as ops
 from tests import attention_reference as ref
 from tests.model_reference import BF16, F16, F32
 from tests.test_gpu_attention import Case, even
-from tests.test_gpu_model_ops import DEV, INF, NAN, TYPES, say
+from tests.test_gpu_model_ops import DEV, INF, NAN, TYPES, say, untouched
 
 pytestmark = pytest.mark.gpu
 
@@ -140,10 +140,10 @@ def test_hundreds_of_sequences(gpu, dtype):
 
 # ------------------------------------------------------------------ scores of any size
 
-def far_case(dtype, n, m, causal, heads, kv_heads, head_dim, q0, k0, k1, scale):
+def far_case(dtype, n, m, causal, heads, kv_heads, head_dim, q0, k0, k1, scale, **layout):
     """Scores scale * (q0 * k0[j] + k1[j]), whose sums fp32 holds exactly; the other features of the keys do not count, as
     those of the queries are zeros."""
-    c = Case(dtype, [0, n], [0, m], heads, kv_heads, head_dim, causal, packed=False, scale=scale)
+    c = Case(dtype, [0, n], [0, m], heads, kv_heads, head_dim, causal, packed=False, scale=scale, **layout)
     c.q.zero_()
     c.q[:, 0::head_dim] = q0
     c.q[:, 1::head_dim] = 1.0
@@ -191,18 +191,10 @@ def test_scores_above_fp32(gpu, dtype, n, m, causal, heads, kv_heads, head_dim):
     assert bool((c.lse == INF).all())
 
 
-@pytest.mark.parametrize("dtype", TYPES)
-@pytest.mark.parametrize("name", SCORES)
-@pytest.mark.parametrize("n,m,causal,heads,kv_heads,head_dim", LENGTHS)
-def test_gradients_of_far_scores(gpu, dtype, name, n, m, causal, heads, kv_heads, head_dim):
-    """The same of the gradients: lse, which they take, is known to a rounding of its size alone."""
-    if dtype == F16 and name == "2^116":
-        pytest.skip("above fp16's largest value")
-    c = far_case(dtype, n, m, causal, heads, kv_heads, head_dim, *SCORES[name])
-    c.forward()
-    c.backward()
+def check_far_gradients(c):
     want, size = defined(c)
-    u = unit(dtype)
+    dtype, heads, kv_heads, head_dim = c.dtype, c.cfg.heads, c.cfg.kv_heads, c.cfg.head_dim
+    n, m, u = len(c.q), len(c.k), unit(dtype)
     # what fp16 does not hold is infinite; below its normal range p and ds are off by half of 2^-24 each, at random, and their
     # sums by the root of as many times the other operand's size
     low = 2.0 ** -25 if dtype == F16 else 0.0
@@ -219,6 +211,19 @@ def test_gradients_of_far_scores(gpu, dtype, name, n, m, causal, heads, kv_heads
     few = c.k.clone()
     few[:, 0::head_dim] = 0.0
     assert_rows(c.dq[:, ~first], want["dq"][:, ~first], u, "dq", low * c.cfg.scale * float(few.double().norm()))
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("name", SCORES)
+@pytest.mark.parametrize("n,m,causal,heads,kv_heads,head_dim", LENGTHS)
+def test_gradients_of_far_scores(gpu, dtype, name, n, m, causal, heads, kv_heads, head_dim):
+    """The same of the gradients: lse, which they take, is known to a rounding of its size alone."""
+    if dtype == F16 and name == "2^116":
+        pytest.skip("above fp16's largest value")
+    c = far_case(dtype, n, m, causal, heads, kv_heads, head_dim, *SCORES[name])
+    c.forward()
+    c.backward()
+    check_far_gradients(c)
 
 
 @pytest.mark.parametrize("dtype", [F32, BF16])
@@ -277,6 +282,34 @@ def test_far_scores_and_infinities(gpu, dtype, n, causal, heads, kv_heads, head_
     assert bool(torch.isnan(c.dv[:at + 1, 7:head_dim:9]).all()) and bool(torch.isnan(c.dq[at]).all())
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("n,m,causal,heads,kv_heads,head_dim,pad,offset", [
+    (150, 150, True, 2, 1, 33, 0, 0), (300, 300, True, 4, 2, 128, 3, 1), (1, 1111, False, 2, 2, 65, 0, 5), (40, 700, False, 2, 1, 96, 7, 3)])
+def test_far_scores_from_any_address(gpu, dtype, n, m, causal, heads, kv_heads, head_dim, pad, offset):
+    """The same where rows start at odd elements, or heads are no whole pieces: both ways, and a replayed graph of them."""
+    c = far_case(dtype, n, m, causal, heads, kv_heads, head_dim, *SCORES["2,000 million"], pad=pad, offset=offset)
+    c.forward()
+    c.backward()
+    assert_rows(c.out, defined(c)[0]["out"], unit(dtype), "out")
+    check_far_gradients(c)
+    for name in ("out", "dq", "dk", "dv"):
+        untouched(getattr(c, name))
+    want = {name: t.clone() for name, t in c.results().items()}
+    stream, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(stream):
+        graph.capture_begin()
+        c.forward(stream)
+        c.backward(stream)
+        graph.capture_end()
+    for _ in range(3):
+        for t in (*c.results().values(), c.ws):
+            t.fill_(0)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(t, want[name]) for name, t in c.results().items())
+
+
 # ------------------------------------------------------------------ few keys
 
 @pytest.mark.parametrize("dtype", TYPES)
@@ -305,7 +338,8 @@ def test_an_only_key_and_a_nan(gpu, dtype, head_dim, n, bad):
 
 
 @pytest.mark.parametrize("dtype", TYPES)
-@pytest.mark.parametrize("heads,kv_heads,head_dim,causal", [(2, 2, 128, False), (4, 2, 104, False), (2, 1, 64, False), (4, 1, 128, True)])
+@pytest.mark.parametrize("heads,kv_heads,head_dim,causal", [
+    (2, 2, 128, False), (4, 2, 104, False), (2, 1, 64, False), (4, 1, 128, True), (2, 1, 127, False)])
 def test_short_sequences_beside_long_ones(gpu, dtype, heads, kv_heads, head_dim, causal):
     """The gradients of a short sequence are as exact as without its neighbours."""
     short, n = 30, 2
